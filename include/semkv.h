@@ -275,6 +275,143 @@ semkv_status semkv_decode_attention_noalloc(const semkv_quant_desc* desc,
                                             const uint16_t* q, float* out, float softmax_scale,
                                             void* stream);
 
+/* ------------------------------------------------ a paged cache held in 4 bits ----
+ * A cache of its own beside semkv_cache, for serving: sequences of different lengths,
+ * pages that several sequences share, queries of one token or of many.  The paper has no
+ * counterpart (its caches are the pools above; Sec. 4.7 prunes tokens, as
+ * semkv_kv4_compact does here by the flags of semkv_rank_assign).
+ *
+ * Format.  A row of head_dim values is held in blocks of 16 along the head dim: one e4m3
+ * scale s and 16 e2m1 codes (two to a byte, the lower dim in the lower half).  With g the
+ * row's float32 scale (its layer's and KV head's entry of k_scale or v_scale) a value is
+ * code * s * g.  Writing a block x, in binary32:
+ *   a = max |x_j| over the entries that are not NaN
+ *   s = e4m3(min(448, a / (6 * g)))           nearest, ties to even
+ *   code_j = e2m1(x_j / (s * g))              nearest, ties to even, limited to +-6
+ * and all codes 0 where s = 0.  A NaN is stored as 0 and an infinity as the largest value
+ * of its block; either writes 4 into the error word.
+ * Sixteen tokens of one head form a tile of 18 * head_dim bytes:
+ *   [K codes 16][head_dim/2] [V codes 16][head_dim/2] [K scales 16][head_dim/16] [V scales]
+ * and a page of page_tokens tokens holds page_tokens / 16 tiles for every head.
+ *
+ * Error word: 1 a wait that timed out, 2 too few free pages, a table too short or a
+ * destination in use, 3 an index outside its range (a page, a sequence, a row range) or
+ * a sequence listed twice where it may not be, 4 a NaN or an infinity stored.  The first
+ * one written stays.  What an entry does with a wrong index is given with each call; none
+ * reads or writes outside the buffers it was given. */
+enum { SEMKV_F16 = 0, SEMKV_BF16 = 1 };
+enum { SEMKV_KV4_MAX_SEQS = 65535 };  /* sequences of one call */
+
+typedef struct {
+  int32_t layers, kv_heads;
+  int32_t head_dim;            /* 64 or 128                                          */
+  int32_t page_tokens;         /* 16, 32, 64 or 128                                  */
+  int32_t num_pages;           /* pages of the pool                                  */
+  int32_t max_seqs, max_pages; /* sequences, and table entries of each               */
+  uint8_t* pages;       /* device [layers][num_pages][kv_heads][page_tokens/16][tile],
+                           16-byte aligned                                           */
+  const float* k_scale; /* device [layers][kv_heads], each in 2^-40 .. 2^40; NULL = 1 */
+  const float* v_scale; /* the same for V                                            */
+  int32_t* table;       /* device [max_seqs][max_pages]: the page of each page_tokens
+                           tokens.  Entries past a sequence's length mean nothing.   */
+  int32_t* length;      /* device [max_seqs]: tokens that each sequence holds        */
+  int32_t* refs;        /* device [num_pages]: table entries in use that name the page;
+                           0 = free.  All zero, like length, in a new cache.         */
+  int32_t* dev_error;   /* device int32 error word (may be NULL)                     */
+} semkv_kv4_cache;
+
+/* The rows of one step: which sequences take part, and how many rows each has in the
+ * row-major tensors of the step's calls (k, v, q, out: [total][heads][head_dim]). */
+typedef struct {
+  int32_t n;             /* sequences that take part, 1..SEMKV_KV4_MAX_SEQS           */
+  int32_t total;         /* rows of the tensors                                       */
+  int32_t max_count;     /* no sequence has more rows than this                       */
+  const int32_t* seqs;   /* device [n], or NULL for 0 .. n-1                          */
+  const int32_t* cu;     /* device [n+1], ascending: rows cu[i] .. cu[i+1]-1 are the
+                            i-th sequence's; rows from cu[n] on belong to nobody and are
+                            left as they are.  NULL: row i is the i-th sequence's     */
+  int32_t* start;        /* device [n]: token position of the i-th sequence's first row,
+                            written by semkv_kv4_reserve, read by semkv_kv4_write and
+                            semkv_kv4_read; negative: its rows take no part           */
+} semkv_kv4_batch;
+
+/* Bytes of a tile, 18 * head_dim; 0 if the head_dim is not supported. */
+size_t semkv_kv4_tile_bytes(int32_t head_dim);
+
+/* Room for each sequence's rows: start[i] = length, length += count, with count = cu[i+1] -
+ * cu[i].  Pages come from those with refs = 0, lowest first, to the sequences in the order
+ * of the list.  A sequence whose last page is part full and shared (refs > 1) first gets a
+ * copy of that page (every layer) in its place, so its new rows reach nobody else.  If the
+ * pool or a table has too little room for all of them nothing changes, every start[i] is -1
+ * and 2 goes into the error word.  A sequence listed before, out of range, or with a wrong
+ * row range gets start[i] = -1 and is left out (3).
+ * ws: device workspace of semkv_kv4_pages_workspace_bytes(cache, n, 0) bytes, 16-byte aligned.
+ * Errors: SEMKV_EINVAL, SEMKV_EALIGN, SEMKV_EUNSUPPORTED, SEMKV_EWORKSPACE. */
+size_t semkv_kv4_pages_workspace_bytes(const semkv_kv4_cache* cache, int32_t n, int32_t tokens);
+semkv_status semkv_kv4_reserve(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch,
+                               void* ws, size_t ws_bytes, void* stream);
+
+/* Quantizes rows of K and V into one layer's pages: row cu[i] + j goes to position start[i]
+ * + j.  k, v: device [total][kv_heads][head_dim] of type `dtype` with k_stride and v_stride
+ * elements from row to row (a multiple of 8, at least kv_heads * head_dim), 16-byte aligned.
+ * A row whose position lies outside its table, or whose page index lies outside the pool, is
+ * left out (3).  Two rows of a call at one position leave either.
+ * semkv_kv4_read is the way back: k_out, v_out [total][kv_heads][head_dim], contiguous,
+ * of type `dtype`, take the values (product with g in binary32, rounded once to the type). */
+semkv_status semkv_kv4_write(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch,
+                             int32_t layer, int32_t dtype, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, void* stream);
+semkv_status semkv_kv4_read(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch,
+                            int32_t layer, int32_t dtype, void* k_out, void* v_out,
+                            void* stream);
+
+/* Causal attention of a step's rows over one layer of their sequences.  With length L and m
+ * rows, the sequence's j-th row stands at position p = L - m + j and sees the positions
+ * max(0, p - window + 1) .. p (window 0: all up to p); a row at a negative position sees
+ * nothing.  For query head h of row r, over the positions it sees, KV head h / (q_heads /
+ * kv_heads):
+ *   out[r][h] = sum_t softmax_t(softmax_scale * q[r][h] . K_t) V_t,   0 if it sees nothing
+ *   lse[r][h] = ln sum_t exp(softmax_scale * q[r][h] . K_t)            (-inf if nothing)
+ * q: device [total][q_heads][head_dim] of type `dtype`, q_stride elements from row to row (a
+ * multiple of 8), 16-byte aligned; out: the same type, contiguous; lse: device f32
+ * [total][q_heads] or NULL.  `start` is not used.  A sequence out of range or with a wrong row
+ * range (more than max_count rows among them) is left out, its rows untouched (3); a length
+ * past the table counts as the table's end and a page index outside the pool as page 0 (3).
+ * Accuracy: products are exact in binary32; the weights are rounded to fp16 before they meet V
+ * (relative 2^-11 each), as the result is to its type.
+ * ws: device workspace of semkv_kv4_attention_workspace_bytes bytes, 16-byte aligned; calls
+ * that may overlap on the GPU need one each. */
+size_t semkv_kv4_attention_workspace_bytes(const semkv_kv4_cache* cache,
+                                           const semkv_kv4_batch* batch, int32_t q_heads);
+semkv_status semkv_kv4_attention(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch,
+                                 int32_t layer, int32_t dtype, const void* q, int64_t q_stride,
+                                 int32_t q_heads, void* out, float* lse, float softmax_scale,
+                                 int32_t window, void* ws, size_t ws_bytes, void* stream);
+
+/* Branches: dst[i] becomes a sequence with src[i]'s length and pages, which both then share
+ * (refs + 1).  dst[i] has to be empty (length 0; else 2), and no destination may appear twice or
+ * among the sources; an entry that breaks this or is out of range is left out (3).  A source
+ * may appear more than once.  src, dst: device [n]. */
+semkv_status semkv_kv4_fork(const semkv_kv4_cache* cache, int32_t n, const int32_t* src,
+                            const int32_t* dst, void* stream);
+
+/* Empties sequences: their pages' refs fall by one (0: free again), length = 0.  A sequence
+ * listed twice is emptied once; one out of range is left out (3).  seqs: device [n] or NULL for
+ * 0 .. n-1. */
+semkv_status semkv_kv4_free(const semkv_kv4_cache* cache, int32_t n, const int32_t* seqs,
+                            void* stream);
+
+/* Prunes sequences to some of their tokens, in order, in every layer: of the i-th sequence the
+ * tokens t < tokens with keep[i][t] != 0 stay, and all from `tokens` on (they have no flag).
+ * keep: device u8 [n][tokens], as semkv_rank_assign leaves is_high.  The kept rows move to
+ * new pages, found as in semkv_kv4_reserve, and the old ones' refs fall by one: whoever else
+ * shares those keeps its tokens.  If too few pages are free nothing changes (2).  A sequence
+ * listed before or out of range is left out (3).
+ * ws: semkv_kv4_pages_workspace_bytes(cache, n, tokens) bytes, 16-byte aligned. */
+semkv_status semkv_kv4_compact(const semkv_kv4_cache* cache, int32_t n, const int32_t* seqs,
+                               const uint8_t* keep, int32_t tokens, void* ws, size_t ws_bytes,
+                               void* stream);
+
 /* Failure-detection check (not a step of the paper's method).  Every kernel that
  * waits on a bulk copy uses one bounded mbarrier wait: after a fixed number of polls
  * (2^22) it gives up, writes 1 (a wait that timed out) into the device error word and

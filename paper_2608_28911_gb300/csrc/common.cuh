@@ -75,7 +75,13 @@ __device__ __forceinline__ float f16_to_f32(uint16_t h) {
 }
 
 // device error codes written to the cache's error word (first error wins)
-enum DevError : int32_t { kDevOk = 0, kDevWaitTimeout = 1, kDevCapacity = 2 };
+enum DevError : int32_t {
+  kDevOk = 0,
+  kDevWaitTimeout = 1,
+  kDevCapacity = 2,
+  kDevIndex = 3,      // an index read from device memory lies outside its range
+  kDevNonFinite = 4   // a NaN or an infinity was stored
+};
 
 __device__ __forceinline__ void raise_error(int32_t* err, int32_t code) {
   if (err) atomicCAS(err, 0, code);

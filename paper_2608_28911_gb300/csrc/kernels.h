@@ -131,6 +131,26 @@ constexpr int kMaxPartialsPerPair = 65;
 size_t decode_workspace_floats(int B, int H, int Hq);
 cudaError_t launch_decode_attention(const DecodeArgs& a, cudaStream_t stream);
 
+// The paged 4-bit cache (kv4.cuh).
+struct Kv4Cache;
+struct Kv4Batch;
+cudaError_t launch_kv4_rows(const Kv4Cache& c, const Kv4Batch& b, bool write, int layer, int dtype,
+                            void* k, int64_t k_stride, void* v, int64_t v_stride, int sms,
+                            cudaStream_t stream);
+size_t kv4_attention_workspace(const Kv4Cache& c, const Kv4Batch& b, int q_heads, int sms);
+cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer, int dtype,
+                                 const void* q, int64_t q_stride, int q_heads, void* out, float* lse,
+                                 float softmax_scale, int window, void* ws, int sms,
+                                 cudaStream_t stream);
+size_t kv4_pages_workspace(const Kv4Cache& c, int n, int tokens);
+cudaError_t launch_kv4_reserve(const Kv4Cache& c, const Kv4Batch& b, void* ws, int sms,
+                               cudaStream_t stream);
+cudaError_t launch_kv4_fork(const Kv4Cache& c, int n, const int32_t* src, const int32_t* dst,
+                            cudaStream_t stream);
+cudaError_t launch_kv4_free(const Kv4Cache& c, int n, const int32_t* seqs, cudaStream_t stream);
+cudaError_t launch_kv4_compact(const Kv4Cache& c, int n, const int32_t* seqs, const uint8_t* keep,
+                               int tokens, void* ws, int sms, cudaStream_t stream);
+
 int device_sm_count();
 
 }  // namespace semkv

@@ -54,6 +54,21 @@ class CacheStruct(ctypes.Structure):
                 ("dev_error", ctypes.c_void_p)]
 
 
+class KV4CacheStruct(ctypes.Structure):
+    _fields_ = [("layers", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("max_seqs", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("pages", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("length", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p), ("dev_error", ctypes.c_void_p)]
+
+
+class KV4BatchStruct(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("total", ctypes.c_int32), ("max_count", ctypes.c_int32),
+                ("seqs", ctypes.c_void_p), ("cu", ctypes.c_void_p), ("start", ctypes.c_void_p)]
+
+
 def _load():
     path = _build.LIB
     if not os.path.exists(path):
@@ -100,6 +115,23 @@ def _load():
     L.semkv_debug_wait_timeout.restype = ctypes.c_int
     L.semkv_status_string.argtypes = [ctypes.c_int]
     L.semkv_status_string.restype = ctypes.c_char_p
+    L.semkv_kv4_tile_bytes.argtypes = [i32]
+    L.semkv_kv4_pages_workspace_bytes.argtypes = [p, i32, i32]
+    L.semkv_kv4_attention_workspace_bytes.argtypes = [p, p, i32]
+    for f in (L.semkv_kv4_tile_bytes, L.semkv_kv4_pages_workspace_bytes,
+              L.semkv_kv4_attention_workspace_bytes):
+        f.restype = sz
+    L.semkv_kv4_reserve.argtypes = [p, p, p, sz, p]
+    L.semkv_kv4_write.argtypes = [p, p, i32, i32, p, i64, p, i64, p]
+    L.semkv_kv4_read.argtypes = [p, p, i32, i32, p, p, p]
+    L.semkv_kv4_attention.argtypes = [p, p, i32, i32, p, i64, i32, p, p, ctypes.c_float, i32, p,
+                                      sz, p]
+    L.semkv_kv4_fork.argtypes = [p, i32, p, p, p]
+    L.semkv_kv4_free.argtypes = [p, i32, p, p]
+    L.semkv_kv4_compact.argtypes = [p, i32, p, p, i32, p, sz, p]
+    for f in (L.semkv_kv4_reserve, L.semkv_kv4_write, L.semkv_kv4_read, L.semkv_kv4_attention,
+              L.semkv_kv4_fork, L.semkv_kv4_free, L.semkv_kv4_compact):
+        f.restype = ctypes.c_int
     return L
 
 
@@ -108,7 +140,10 @@ EXPORTED = ["semkv_row_bytes", "semkv_record_bytes", "semkv_high_count_floor",
             "semkv_block_high_count", "semkv_lloyd_max_gaussian", "semkv_rank_workspace_bytes",
             "semkv_rank_assign", "semkv_score_kv_norm", "semkv_fake_quant", "semkv_quantize_pack", "semkv_append_block",
             "semkv_decode_workspace_bytes", "semkv_decode_attention",
-            "semkv_decode_attention_noalloc", "semkv_debug_wait_timeout", "semkv_status_string"]
+            "semkv_decode_attention_noalloc", "semkv_debug_wait_timeout", "semkv_status_string",
+            "semkv_kv4_tile_bytes", "semkv_kv4_pages_workspace_bytes", "semkv_kv4_reserve",
+            "semkv_kv4_write", "semkv_kv4_read", "semkv_kv4_attention_workspace_bytes",
+            "semkv_kv4_attention", "semkv_kv4_fork", "semkv_kv4_free", "semkv_kv4_compact"]
 
 
 def _ptr(t):
@@ -242,6 +277,126 @@ def semkv_debug_wait_timeout(dev_error: torch.Tensor, polls: int, stream=None):
            LIB.semkv_debug_wait_timeout(_ptr(dev_error), polls, _stream(stream)))
 
 
+# ------------------------------------------- the paged cache held in 4 bits ----
+
+_KV4_TYPES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _here(*tensors):
+    """The calls run on the current device, so what they take has to be there."""
+    dev = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    for t in tensors:
+        _need(t.get_device() == dev, "tensors have to be on the current CUDA device")
+
+
+def _list(t, n, what):
+    if t is not None:
+        _need(t.dtype == torch.int32 and t.is_contiguous() and t.shape == (n,),
+              f"{what} is a contiguous int32 tensor of {n}")
+        _here(t)
+    return t
+
+
+def _rows(t, what, total, heads, head_dim):
+    """Rows [total][heads][head_dim] of a 16-bit type with any stride between rows; the stride."""
+    _need(t.dtype in _KV4_TYPES, f"{what} is float16 or bfloat16")
+    _need(t.dim() == 3 and t.shape[0] == total and t.shape[2] == head_dim
+          and (heads is None or t.shape[1] == heads), f"{what} has the wrong shape {tuple(t.shape)}")
+    st = t.stride()
+    _need(st[2] == 1 and (st[1] == head_dim or t.shape[1] == 1),
+          f"{what}: the heads of a row lie side by side")
+    return st[0] if total > 1 else t.shape[1] * head_dim
+
+
+def semkv_kv4_tile_bytes(head_dim: int) -> int:
+    return LIB.semkv_kv4_tile_bytes(head_dim)
+
+
+def semkv_kv4_reserve(cache: "KV4Cache", batch: "KV4Batch", ws: torch.Tensor, stream=None):
+    """Room for the batch's rows: pages, lengths, and batch.start."""
+    _here(cache.pages, batch.start, ws)
+    _check("semkv_kv4_reserve",
+           LIB.semkv_kv4_reserve(cache.ref, batch.ref, _ptr(ws), ws.numel() * ws.element_size(),
+                                 _stream(stream)))
+
+
+def semkv_kv4_write(cache: "KV4Cache", batch: "KV4Batch", layer: int, k: torch.Tensor,
+                    v: torch.Tensor, stream=None):
+    """Quantize rows k, v [total][kv_heads][head_dim] (any row stride) into the layer's pages."""
+    s = cache.s
+    _need(k.dtype == v.dtype, "k and v have one type")
+    ks = _rows(k, "k", batch.s.total, s.kv_heads, s.head_dim)
+    vs = _rows(v, "v", batch.s.total, s.kv_heads, s.head_dim)
+    _here(cache.pages, batch.start, k, v)
+    _check("semkv_kv4_write",
+           LIB.semkv_kv4_write(cache.ref, batch.ref, layer, _KV4_TYPES[k.dtype], k.data_ptr(), ks,
+                               v.data_ptr(), vs, _stream(stream)))
+
+
+def semkv_kv4_read(cache: "KV4Cache", batch: "KV4Batch", layer: int, k_out: torch.Tensor,
+                   v_out: torch.Tensor, stream=None):
+    """The values of the batch's rows into k_out, v_out [total][kv_heads][head_dim]."""
+    s = cache.s
+    _need(k_out.dtype == v_out.dtype, "k_out and v_out have one type")
+    _rows(k_out, "k_out", batch.s.total, s.kv_heads, s.head_dim)
+    _rows(v_out, "v_out", batch.s.total, s.kv_heads, s.head_dim)
+    _here(cache.pages, batch.start, k_out, v_out)
+    _check("semkv_kv4_read",
+           LIB.semkv_kv4_read(cache.ref, batch.ref, layer, _KV4_TYPES[k_out.dtype], _ptr(k_out),
+                              _ptr(v_out), _stream(stream)))
+
+
+def semkv_kv4_attention(cache: "KV4Cache", batch: "KV4Batch", layer: int, q: torch.Tensor,
+                        out: torch.Tensor, softmax_scale: float, ws: torch.Tensor, lse=None,
+                        window: int = 0, stream=None):
+    """Causal attention of the batch's rows q [total][q_heads][head_dim] over their sequences."""
+    qs = _rows(q, "q", batch.s.total, None, cache.s.head_dim)
+    _need(out.dtype == q.dtype and out.shape == q.shape, "out is as q")
+    if lse is not None:
+        _need(lse.dtype == torch.float32 and lse.shape == q.shape[:2], "lse is float32 [total][q_heads]")
+        _here(lse)
+    _here(cache.pages, q, out, ws)
+    _check("semkv_kv4_attention",
+           LIB.semkv_kv4_attention(cache.ref, batch.ref, layer, _KV4_TYPES[q.dtype], q.data_ptr(), qs,
+                                   q.shape[1], _ptr(out), _ptr(lse), softmax_scale, window, _ptr(ws),
+                                   ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def semkv_kv4_fork(cache: "KV4Cache", src: torch.Tensor, dst: torch.Tensor, stream=None):
+    """dst[i] becomes a branch of src[i]: its length, and its pages shared."""
+    n = src.numel()
+    _here(cache.pages)
+    _check("semkv_kv4_fork",
+           LIB.semkv_kv4_fork(cache.ref, n, _list(src, n, "src").data_ptr(),
+                              _list(dst, n, "dst").data_ptr(), _stream(stream)))
+
+
+def semkv_kv4_free(cache: "KV4Cache", seqs: torch.Tensor, stream=None):
+    """Empties sequences; pages that nobody else holds are free again."""
+    n = seqs.numel()
+    _here(cache.pages)
+    _check("semkv_kv4_free",
+           LIB.semkv_kv4_free(cache.ref, n, _list(seqs, n, "seqs").data_ptr(), _stream(stream)))
+
+
+def semkv_kv4_compact(cache: "KV4Cache", seqs: torch.Tensor, keep: torch.Tensor, ws: torch.Tensor,
+                      stream=None):
+    """Prunes sequences to the tokens with keep[i][t] != 0 (and all from keep.shape[1] on)."""
+    n = seqs.numel()
+    _need(keep.dtype == torch.uint8 and keep.dim() == 2 and keep.shape[0] == n,
+          "keep is uint8 [sequences][tokens]")
+    _here(cache.pages, keep, ws)
+    _check("semkv_kv4_compact",
+           LIB.semkv_kv4_compact(cache.ref, n, _list(seqs, n, "seqs").data_ptr(), _ptr(keep),
+                                 keep.shape[1], _ptr(ws), ws.numel() * ws.element_size(),
+                                 _stream(stream)))
+
+
 # ------------------------------------------------------- owning wrappers ------
 
 class QuantDesc:
@@ -351,3 +506,77 @@ class KVCache:
     def workspace(self):
         nbytes = semkv_decode_workspace_bytes(self)
         return torch.empty(nbytes // 4, dtype=torch.float32, device=self.hi_pool.device)
+
+
+class KV4Cache:
+    """A paged cache held in 4 bits: its device buffers and the struct the library reads.
+    k_scale, v_scale: float32 [layers][kv_heads] (None: 1)."""
+
+    def __init__(self, layers: int, kv_heads: int, head_dim: int, page_tokens: int, num_pages: int,
+                 max_seqs: int, max_pages: int, k_scale=None, v_scale=None, device="cuda"):
+        i32 = dict(dtype=torch.int32, device=device)
+        tile = semkv_kv4_tile_bytes(head_dim)
+        _need(tile and page_tokens in (16, 32, 64, 128),
+              "head_dim is 64 or 128, page_tokens 16, 32, 64 or 128")
+        self._hold(torch.zeros((layers, num_pages, kv_heads, page_tokens // 16, tile),
+                               dtype=torch.uint8, device=device),
+                   torch.full((max_seqs, max_pages), -1, **i32), torch.zeros(max_seqs, **i32),
+                   torch.zeros(num_pages, **i32), head_dim, k_scale, v_scale)
+
+    @classmethod
+    def over(cls, pages, table, length, refs, head_dim: int, k_scale=None, v_scale=None):
+        """A cache over buffers that are there already."""
+        self = cls.__new__(cls)
+        self._hold(pages, table, length, refs, head_dim, k_scale, v_scale)
+        return self
+
+    def _hold(self, pages, table, length, refs, head_dim, k_scale, v_scale):
+        _need(pages.dtype == torch.uint8 and pages.dim() == 5 and pages.is_contiguous()
+              and pages.shape[4] == semkv_kv4_tile_bytes(head_dim),
+              "pages is uint8 [layers][pages][kv_heads][page_tokens / 16][tile]")
+        layers, num_pages, kv_heads, tiles, _ = pages.shape
+        _need(table.dim() == 2, "table is int32 [sequences][pages of each]")
+        for t, shape in ((table, table.shape), (length, table.shape[:1]), (refs, (num_pages,))):
+            _need(t.dtype == torch.int32 and t.is_contiguous() and t.shape == shape,
+                  "table, length and refs are contiguous int32 tensors that fit each other")
+        for t in (k_scale, v_scale):
+            _need(t is None or (t.dtype == torch.float32 and t.is_contiguous()
+                                and t.shape == (layers, kv_heads)),
+                  "the scales are contiguous float32 [layers][kv_heads]")
+        self.pages, self.table, self.length, self.refs = pages, table, length, refs
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self.dev_error = torch.zeros(1, dtype=torch.int32, device=pages.device)
+        for t in (table, length, refs, k_scale, v_scale):
+            _need(t is None or t.device == pages.device, "a cache lies on one device")
+        self.s = KV4CacheStruct(layers=layers, kv_heads=kv_heads, head_dim=head_dim,
+                                page_tokens=16 * tiles, num_pages=num_pages,
+                                max_seqs=table.shape[0], max_pages=table.shape[1],
+                                pages=_ptr(pages), k_scale=_ptr(k_scale), v_scale=_ptr(v_scale),
+                                table=_ptr(table), length=_ptr(length), refs=_ptr(refs),
+                                dev_error=_ptr(self.dev_error))
+        self.ref = ctypes.byref(self.s)
+
+    def pages_workspace(self, n: int, tokens: int = 0):
+        """For reserve (tokens 0) or compact (tokens: keep's columns) of up to n sequences."""
+        size = LIB.semkv_kv4_pages_workspace_bytes(self.ref, n, tokens)
+        return torch.empty(size, dtype=torch.uint8, device=self.pages.device)
+
+    def attention_workspace(self, batch: "KV4Batch", q_heads: int):
+        size = LIB.semkv_kv4_attention_workspace_bytes(self.ref, batch.ref, q_heads)
+        return torch.empty(size, dtype=torch.uint8, device=self.pages.device)
+
+
+class KV4Batch:
+    """The rows of one step over a KV4Cache (semkv_kv4_batch).  cu: int32 [n + 1], or None
+    for one row to a sequence; seqs: int32 [n], or None for 0 .. n-1; total: rows of the
+    step's tensors; max_count: no sequence has more rows."""
+
+    def __init__(self, n: int, cu=None, seqs=None, start=None, total=None, max_count: int = 1,
+                 device="cuda"):
+        _need(total is not None or cu is None, "total: the rows of the step's tensors")
+        self.cu, self.seqs = _list(cu, n + 1, "cu"), _list(seqs, n, "seqs")
+        self.start = (torch.zeros(n, dtype=torch.int32, device=device) if start is None
+                      else _list(start, n, "start"))
+        self.s = KV4BatchStruct(n=n, total=n if total is None else total, max_count=max_count,
+                                seqs=_ptr(self.seqs), cu=_ptr(self.cu), start=_ptr(self.start))
+        self.ref = ctypes.byref(self.s)
