@@ -15,7 +15,8 @@
 // every eight, which leaves K's loads without bank conflicts and V's two-way.
 // S^T's accumulators become P^T's B fragments by one 8x8 transposition (movmatrix).
 //
-// Each warp streams its own units (32 tokens, two tiles) through a ring of bulk copies.
+// Every warp is a worker of its own (kv4_attend.cuh): it streams its range, 32 tokens at a time,
+// through a ring of bulk copies and meets no other warp.
 #include "kernels.h"
 #include "kv4_attend.cuh"
 
@@ -49,6 +50,14 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   return w;
 }
 
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
+  if (!BF16) return pack_half2(lo, hi);
+  uint32_t w;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+  return w;
+}
+
 // token of the tile at place x of the order: {0, 3, 1, 2} and the same four further, ...
 __device__ __forceinline__ int token_at(int x) {
   const int t = (x & 7) >> 1, base = (x & 8) + t + (t & 2);
@@ -61,28 +70,23 @@ struct Layout {
   static constexpr int kRows = 8 * NT;
   static constexpr int kStage = 2 * kTile;
   static constexpr int kStages = 3;
-  static constexpr int kSums = D + 4;  // padded row of the merge area
   static constexpr int ring_bytes() { return kWarps * kStages * kStage; }
-  static constexpr int merge_bytes() { return kWarps * kRows * (kSums + 2) * 4; }
-  // the merge area lies over the ring, which is empty between items
-  static constexpr int data_bytes() { return ring_bytes() > merge_bytes() ? ring_bytes() : merge_bytes(); }
-  static constexpr int q_bytes() { return NT * (D / 16) * 32 * 8; }
-  static constexpr int bytes() { return data_bytes() + q_bytes() + NT * 8 * 4 + kWarps * kStages * 8 + (kThreads + 1) * 8 + kWarps * 8; }
+  // Q's fragments lie in registers where there are eight rows, else in shared memory
+  static constexpr int q_bytes() { return NT == 1 ? 0 : kWarps * NT * (D / 16) * 32 * 8; }
+  static constexpr int bytes() { return ring_bytes() + q_bytes() + kWarps * kStages * 8 + (kThreads + 1) * 8 + kWarps * 8; }
 };
 
-// Q's fragments of an item into shared memory, [n tile][k step][lane]: rows of the step's q for
-// one KV head; bf16 rows are scaled by a power of two, which leaves their values exact in
-// fp16 but for those 2^-24 and less of the row's largest.  scale[row]: what undoes it.
-template <int D, int NT, bool BF16>
-__device__ __forceinline__ void load_queries(const Kv4Attend& a, const Kv4Seq& s, int head, int tile, uint2* qf,
-                                             float* scale) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__host__ __device__ constexpr Kv4Cut few_cut(int n_tiles) { return Kv4Cut{8 * n_tiles, kUnit, 4, 4}; }
+
+// The fragments of eight query rows (row0 + g) for one KV head, w[2k], w[2k + 1] those of k
+// step k.  bf16 rows are scaled by a power of two, which leaves their values exact in fp16 but
+// for those 2^-24 and less of the row's largest; returns what undoes it.
+template <int D, bool BF16>
+__device__ __forceinline__ float load_queries(const Kv4Attend& a, const Kv4Seq& s, int head, int row0, uint32_t (&w)[D / 8]) {
+  const int lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
-  if (warp >= NT) return;
-  const int row = tile * 8 * NT + warp * 8 + g;
+  const int row = row0 + g;
   const int j = row / a.group, h = head * a.group + row % a.group;
-  uint32_t w[D / 8];
-  float most = 0.f;
   if (j < s.count) {
     const uint4* p = reinterpret_cast<const uint4*>(a.q + (int64_t)(s.begin + j) * a.q_stride + h * D + t * (D / 4));
 #pragma unroll
@@ -96,6 +100,7 @@ __device__ __forceinline__ void load_queries(const Kv4Attend& a, const Kv4Seq& s
   }
   float undo = 1.f;
   if (BF16) {
+    float most = 0.f;
 #pragma unroll
     for (int k = 0; k < D / 8; ++k) {
       most = fmaxf(most, fabsf(__uint_as_float(w[k] << 16)));
@@ -103,38 +108,35 @@ __device__ __forceinline__ void load_queries(const Kv4Attend& a, const Kv4Seq& s
     }
     most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
     most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
-    // the row's largest to [2^0, 2^1); rows of zeros, infinities or NaN as they are
+    // the row's largest to [2^0, 2^1); rows of zeros and rows with an infinity as they are
     int e = (int)(__float_as_uint(most) >> 23) - 127;
     if (most == 0.f || !(most < INFINITY)) e = 0;
     e = e < -126 ? -126 : e;
-    const float by = __uint_as_float((uint32_t)(127 - e) << 23);  // 2^-e (e = 127: 0, below)
+    // 2^-127 and 2^127 for e = 127: its inverse is not a normal number
     undo = e == 127 ? 0x1p127f : __uint_as_float((uint32_t)(127 + e) << 23);
-    const float mul = e == 127 ? 0x1p-127f : by;
+    const float mul = e == 127 ? 0x1p-127f : __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
     for (int k = 0; k < D / 8; ++k)
       w[k] = pack_half2(__uint_as_float(w[k] << 16) * mul, __uint_as_float(w[k] & 0xFFFF0000u) * mul);
   }
-#pragma unroll
-  for (int k = 0; k < D / 16; ++k) qf[(warp * (D / 16) + k) * 32 + lane] = make_uint2(w[2 * k], w[2 * k + 1]);
-  if (t == 0) scale[warp * 8 + g] = undo;
+  return undo;
 }
 
 template <int D, int NT, bool BF16>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(Kv4Attend a) {
   using L = Layout<D, NT>;
+  constexpr Kv4Cut cut = few_cut(NT);
   constexpr int kSteps = D / 16;   // k steps of S
   constexpr int kM = D / 16;       // m tiles of O
   extern __shared__ __align__(128) uint8_t smem[];
-  uint8_t* data = smem;
-  uint2* qf = reinterpret_cast<uint2*>(data + L::data_bytes());
-  int64_t* prefix = reinterpret_cast<int64_t*>(reinterpret_cast<uint8_t*>(qf) + L::q_bytes());
+  int64_t* prefix = reinterpret_cast<int64_t*>(smem + L::ring_bytes() + L::q_bytes());
   int64_t* sums = prefix + kThreads + 1;
   uint64_t* bars = reinterpret_cast<uint64_t*>(sums + kWarps);
-  float* q_scale = reinterpret_cast<float*>(bars + kWarps * L::kStages);
 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
-  uint8_t* ring = data + warp * (L::kStages * L::kStage);
+  uint8_t* ring = smem + warp * (L::kStages * L::kStage);
+  uint2* qf = reinterpret_cast<uint2*>(smem + L::ring_bytes()) + warp * (NT * kSteps * 32);
   uint64_t* bar = bars + warp * L::kStages;
   if (lane == 0) {
     for (int s = 0; s < L::kStages; ++s)
@@ -143,31 +145,94 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
   }
   pdl_wait();
   pdl_trigger();
-  kv4_plan<L::kRows, kUnit, kThreads>(a, prefix, sums, blockIdx.x == 0);
+  kv4_plan<kThreads>(a, cut, prefix, sums, blockIdx.x == 0);
   const int64_t W = prefix[kThreads];
-  const int ctas = kv4_ctas(W, gridDim.x);
-  if (W == 0 || (int)blockIdx.x >= ctas) return;
-  const int64_t begin = kv4_range_begin(W, blockIdx.x, ctas), end = kv4_range_begin(W, blockIdx.x + 1, ctas);
+  const int workers = kv4_workers(W, cut, gridDim.x * kWarps);
+  const int worker = warp * gridDim.x + blockIdx.x;  // few workers: spread over the SMs
+  if (W == 0 || worker >= workers) return;
+  const int64_t end = kv4_range_begin(W, worker + 1, workers);
 
   const int row_a = token_at(g), tok_v = token_at(2 * t);  // K row of lane group g; V's first token
-  const int64_t page_bytes = (int64_t)L::kTile << (a.c.page_shift - 4);
+  const int64_t head_bytes = (int64_t)L::kTile << (a.c.page_shift - 4);
+  const int64_t page_stride = head_bytes * a.c.H;
   uint32_t phase = 0;  // parity of each stage's barrier, a bit each
-  bool lost = false;   // a wait ran out
+  int stage = 0;       // of the next unit
 
-  for (int64_t cur = begin; cur < end;) {
-    // the sequence that holds unit `cur`, the item and the part of it that is this CTA's
+  for (int64_t place = kv4_range_begin(W, worker, workers); place < end;) {
     int64_t before;
-    const Kv4Seq s = kv4_find<L::kRows, kUnit, kThreads>(a, prefix, cur, before);
-    const int64_t in_seq = cur - before;
-    const int item = (int)(in_seq / s.units), u0 = (int)(in_seq - (int64_t)item * s.units);
+    const Kv4Seq s = kv4_find<kThreads>(a, cut, prefix, place, before);
+    const int per = s.units + cut.start;
+    const int64_t in_seq = place - before;
+    const int item = (int)(in_seq / per), off = (int)(in_seq - (int64_t)item * per);
+    const int take = (int)min((int64_t)(per - off), end - place);
+    place += take;
+    const int u0 = max(0, off - cut.start), u1 = off + take - cut.start;
+    if (u1 <= u0) continue;
     const int head = item / s.tiles, tile = item - head * s.tiles;
-    const int64_t left = end - cur;
-    const int u1 = s.units - u0 < left ? s.units : u0 + (int)left;
 
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the merge area becomes a ring again
-    __syncthreads();  // the item before is done with the shared areas
-    load_queries<D, NT, BF16>(a, s, head, tile, qf, q_scale);
-    __syncthreads();
+    // the pages of units u0 + k0 .. u0 + k0 + 31, a lane each (with pages of 16 tokens: of both halves)
+    const int mine = u1 - u0, token0 = (s.u_first + u0) * kUnit;
+    const uint8_t* head_base = a.c.pages + kv4_record(a.c, a.layer, 0, head);
+    const int32_t* table = a.c.table + (int64_t)s.seq * a.c.max_pages;
+    int page_x = 0, page_y = 0, k0 = 0;
+    auto fetch_pages = [&](int k) {
+      k0 = k;
+      const int kk = k + lane;
+      if (kk < mine) {
+        const int token = token0 + kk * kUnit;
+        page_x = table[token >> a.c.page_shift];
+        page_y = a.c.page_shift == 4 && token + 16 < s.length ? table[(token >> 4) + 1] : 0;
+        if ((unsigned)page_x >= (unsigned)a.c.num_pages || (unsigned)page_y >= (unsigned)a.c.num_pages) {
+          raise_error(a.c.err, kDevIndex);
+          if ((unsigned)page_x >= (unsigned)a.c.num_pages) page_x = 0;
+          if ((unsigned)page_y >= (unsigned)a.c.num_pages) page_y = 0;
+        }
+      }
+    };
+    auto issue = [&](int k, int to) {
+      if (k >= k0 + 32) fetch_pages(k);
+      const int px = __shfl_sync(~0u, page_x, k - k0), py = __shfl_sync(~0u, page_y, k - k0);
+      if (lane == 0) {
+        const int token = token0 + k * kUnit;
+        const bool two = token + 16 < s.length;
+        const uint32_t dst = smem_addr(ring + to * L::kStage), b = smem_addr(bar + to);
+        const uint8_t* src = head_base + px * page_stride + (int64_t)((token & (a.c.P - 1)) >> 4) * L::kTile;
+        const uint32_t bytes = two ? 2 * L::kTile : L::kTile;
+        const bool whole = a.c.page_shift > 4;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
+        asm volatile(
+            "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+            "r"(whole ? bytes : (uint32_t)L::kTile), "r"(b)
+            : "memory");
+        if (!whole && two)
+          asm volatile(
+              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + L::kTile),
+              "l"(head_base + py * page_stride), "r"((uint32_t)L::kTile), "r"(b)
+              : "memory");
+      }
+    };
+
+    // ---- queries (on their way before the copies, which they would queue behind)
+    uint32_t q1[D / 8];
+    float undo[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      undo[n] = load_queries<D, BF16>(a, s, head, tile * L::kRows + 8 * n, q1);
+      if (NT > 1) {
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) qf[(n * kSteps + k) * 32 + lane] = make_uint2(q1[2 * k], q1[2 * k + 1]);
+      }
+    }
+    fetch_pages(0);
+    {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (the item before has read its stages)
+      const int ahead = min(mine, L::kStages);
+      int to = stage;
+      for (int k = 0; k < ahead; ++k) {
+        issue(k, to);
+        to = to + 1 == L::kStages ? 0 : to + 1;
+      }
+    }
 
     // what this lane's query rows (columns 2t, 2t+1 of each n tile) see
     int see_lo[2 * NT], see_hi[2 * NT];
@@ -176,10 +241,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
     const float gk = a.c.k_scale ? a.c.k_scale[a.layer * a.c.H + head] : 1.f;
 #pragma unroll
     for (int x = 0; x < 2 * NT; ++x) {
-      const int col = (x >> 1) * 8 + 2 * t + (x & 1);
-      kv4_sight(a, s, tile * L::kRows + col, see_lo[x], see_hi[x]);
-      mul[x] = a.scale_log2 * gk * q_scale[col];
-      if (see_hi[x] >= 0 || (tile * L::kRows + col) / a.group < s.count) {
+      const int row = tile * L::kRows + (x >> 1) * 8 + 2 * t + (x & 1);
+      kv4_sight(a, s, row, see_lo[x], see_hi[x]);
+      mul[x] = a.scale_log2 * gk * __shfl_sync(~0u, undo[x >> 1], 4 * (2 * t + (x & 1)));
+      if (row / a.group < s.count) {
         most_lo = max(most_lo, see_lo[x]);
         least_hi = min(least_hi, see_hi[x]);
       }
@@ -197,72 +262,20 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
         for (int x = 0; x < 4; ++x) O[n][m][x] = 0.f;
 #pragma unroll
     for (int x = 0; x < 2 * NT; ++x) ref[x] = kNone, sum[x] = 0.f;
+    __syncwarp();  // Q's fragments are there
 
-    // this warp's units: u0 + warp, + kWarps, ...
-    const int mine = u1 - u0 > warp ? (u1 - u0 - warp + kWarps - 1) / kWarps : 0;
-    const uint8_t* head_base = a.c.pages + kv4_record(a.c, a.layer, 0, head);
-    const int64_t page_stride = page_bytes * a.c.H;
-    const int32_t* table = a.c.table + (int64_t)s.seq * a.c.max_pages;
-    // lane l keeps the pages of the warp's unit k0 + l (with pages of 16 tokens: of both halves)
-    int page_x = 0, page_y = 0, k0 = 0;
-    auto fetch_pages = [&](int k) {
-      k0 = k;
-      const int kk = k + lane;
-      if (kk < mine) {
-        const int token = (s.u_first + u0 + warp + kk * kWarps) * kUnit;
-        page_x = table[token >> a.c.page_shift];
-        page_y = a.c.page_shift == 4 && token + 16 < s.length ? table[(token >> 4) + 1] : 0;
-        if ((unsigned)page_x >= (unsigned)a.c.num_pages || (unsigned)page_y >= (unsigned)a.c.num_pages) {
-          raise_error(a.c.err, kDevIndex);
-          if ((unsigned)page_x >= (unsigned)a.c.num_pages) page_x = 0;
-          if ((unsigned)page_y >= (unsigned)a.c.num_pages) page_y = 0;
-        }
-      }
-    };
-    auto issue = [&](int k, int stage) {
-      if (k >= k0 + 32) fetch_pages(k);
-      const int px = __shfl_sync(~0u, page_x, k - k0), py = __shfl_sync(~0u, page_y, k - k0);
-      if (lane == 0) {
-        const int token = (s.u_first + u0 + warp + k * kWarps) * kUnit;
-        const bool two = token + 16 < s.length;
-        const uint32_t dst = smem_addr(ring + stage * L::kStage), b = smem_addr(bar + stage);
-        const uint8_t* src = head_base + px * page_stride + (int64_t)((token & (a.c.P - 1)) >> 4) * L::kTile;
-        const uint32_t bytes = two ? 2 * L::kTile : L::kTile;
-        const bool whole = a.c.page_shift > 4;
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
-        asm volatile(
-            "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-            "r"(whole ? bytes : (uint32_t)L::kTile), "r"(b)
-            : "memory");
-        if (!whole && two)
-          asm volatile(
-              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + L::kTile),
-              "l"(head_base + py * page_stride), "r"((uint32_t)L::kTile), "r"(b)
-              : "memory");
-      }
-    };
-    fetch_pages(0);
-    const int ahead = mine < L::kStages ? mine : L::kStages;
-    for (int k = 0; k < ahead; ++k) issue(k, k);
-
-    int stage = 0;
     for (int k = 0; k < mine; ++k) {
-      if (!lost && !mbar_wait_bounded(bar + stage, phase >> stage & 1)) {
-        lost = true;
+      if (!__all_sync(~0u, mbar_wait_bounded(bar + stage, phase >> stage & 1))) {
         if (lane == 0) raise_error(a.c.err, kDevWaitTimeout);
-      }
-      lost = __any_sync(~0u, lost);
-      if (lost) {
         // the copies still in flight are waited for, as long again
-        const int issued = min(mine, k + L::kStages);
-        for (int j = k + 1; j < issued; ++j) {
+        for (int j = k + 1; j < min(mine, k + L::kStages); ++j) {
           stage = stage + 1 == L::kStages ? 0 : stage + 1;
           mbar_wait_bounded(bar + stage, phase >> stage & 1);
         }
-        break;
+        return;
       }
       phase ^= 1u << stage;
-      const int token = (s.u_first + u0 + warp + k * kWarps) * kUnit;
+      const int token = token0 + k * kUnit;
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
         const int t0 = token + 16 * half;
@@ -308,9 +321,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              const uint2 q0 = qf[(n * kSteps + 2 * w) * 32 + lane], q1 = qf[(n * kSteps + 2 * w + 1) * 32 + lane];
-              mma16816(S[n], xa[0], xb[0], xa[1], xb[1], q0.x, q0.y);
-              mma16816(S[n], xa[2], xb[2], xa[3], xb[3], q1.x, q1.y);
+              const uint2 b0 = NT == 1 ? make_uint2(q1[4 * w], q1[4 * w + 1]) : qf[(n * kSteps + 2 * w) * 32 + lane];
+              const uint2 b1 = NT == 1 ? make_uint2(q1[4 * w + 2], q1[4 * w + 3]) : qf[(n * kSteps + 2 * w + 1) * 32 + lane];
+              mma16816(S[n], xa[0], xb[0], xa[1], xb[1], b0.x, b0.y);
+              mma16816(S[n], xa[2], xb[2], xa[3], xb[3], b1.x, b1.y);
             }
           }
         }
@@ -408,126 +422,121 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
       }
       stage = stage + 1 == L::kStages ? 0 : stage + 1;
     }
-    // ---- the warps' sums are put together
+
+    // ---- the item's rows, or this range's part of them: lane g holds dims g D/8 .. of columns 2t, 2t+1
 #pragma unroll
     for (int x = 0; x < 2 * NT; ++x) {
       sum[x] += __shfl_xor_sync(~0u, sum[x], 4);
       sum[x] += __shfl_xor_sync(~0u, sum[x], 8);
       sum[x] += __shfl_xor_sync(~0u, sum[x], 16);
     }
-    const bool broken = __syncthreads_or(lost);  // every warp is done with its ring
-    if (broken) return;
-    float* area = reinterpret_cast<float*>(data);
-    float* heads = area + kWarps * L::kRows * L::kSums;  // [warp][row]: reference, then sum
+    const bool done = u0 == 0 && u1 == s.units;
+    const int rows = min(L::kRows, s.count * a.group - tile * L::kRows);
+    const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int col = n * 8 + 2 * t + x;
-        float* o = area + (warp * L::kRows + col) * L::kSums;
+        if (col >= rows) continue;
+        const float total = sum[2 * n + x];
+        if (done) {
+          const int row = tile * L::kRows + col;
+          const int64_t at = (int64_t)(s.begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
+          const float inv = total == 0.f ? 0.f : gv / total;
+          uint32_t w[kM];
 #pragma unroll
-        for (int m = 0; m < kM; ++m)
-          *reinterpret_cast<float2*>(o + g * (D / 8) + 2 * m) = make_float2(O[n][m][x], O[n][m][2 + x]);
-        if (g == 0) {
-          heads[(warp * L::kRows + col) * 2] = ref[2 * n + x];
-          heads[(warp * L::kRows + col) * 2 + 1] = sum[2 * n + x];
-        }
-      }
-    }
-    __syncthreads();
-    const bool done = u0 == 0 && u1 == s.units;
-    const int slot = 2 * (int)blockIdx.x + (cur == begin ? 0 : 1);
-    const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
-    const int rows = min(L::kRows, s.count * a.group - tile * L::kRows);
-    for (int x = threadIdx.x; x < rows * (D / 4); x += kThreads) {
-      const int col = x / (D / 4), d4 = x % (D / 4) * 4;
-      float top = kNone;
+          for (int m = 0; m < kM; ++m) w[m] = pack_out<BF16>(O[n][m][x] * inv, O[n][m][2 + x] * inv);
+          uint4* to = reinterpret_cast<uint4*>(a.out + at * D + g * (D / 8));
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, heads[(w * L::kRows + col) * 2]);
-      float total = 0.f;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = exp2_approx(heads[(w * L::kRows + col) * 2] - top);
-        total += f * heads[(w * L::kRows + col) * 2 + 1];
-        const float4 y = *reinterpret_cast<const float4*>(area + (w * L::kRows + col) * L::kSums + d4);
-        o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
-      }
-      if (done) {
-        const int row = tile * L::kRows + col;
-        const int64_t at = (int64_t)(s.begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
-        const float inv = total == 0.f ? 0.f : gv / total;
-        uint2 packed;
-        if (BF16) {
-          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed.x) : "f"(o.y * inv), "f"(o.x * inv));
-          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed.y) : "f"(o.w * inv), "f"(o.z * inv));
+          for (int m = 0; m < kM; m += 4) to[m / 4] = make_uint4(w[m], w[m + 1], w[m + 2], w[m + 3]);
+          if (a.lse && g == 0) a.lse[at] = total == 0.f ? -INFINITY : (ref[2 * n + x] + log2f(total)) * 0.6931471805599453f;
         } else {
-          packed = make_uint2(pack_half2(o.x * inv, o.y * inv), pack_half2(o.z * inv, o.w * inv));
+          float* part = a.parts + ((int64_t)(2 * worker + (u0 == 0 ? 1 : 0)) * L::kRows + col) * kv4_part_floats(D);
+          float4* to = reinterpret_cast<float4*>(part + g * (D / 8));
+#pragma unroll
+          for (int m = 0; m < kM; m += 2)
+            to[m / 2] = make_float4(O[n][m][x], O[n][m][2 + x], O[n][m + 1][x], O[n][m + 1][2 + x]);
+          if (g == 0) *reinterpret_cast<float2*>(part + D) = make_float2(ref[2 * n + x], total);
         }
-        *reinterpret_cast<uint2*>(a.out + at * D + d4) = packed;
-        if (a.lse && d4 == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
-      } else {
-        float* part = a.parts + ((int64_t)slot * L::kRows + col) * (D + 2);
-        part[d4] = o.x, part[d4 + 1] = o.y, part[d4 + 2] = o.z, part[d4 + 3] = o.w;
-        if (d4 == 0) part[D] = top, part[D + 1] = total;
       }
-    }
-    cur += u1 - u0;
   }
 }
 
-// Joins the parts of the items that several CTAs share, and fills the rows that see nothing.
-// A CTA per (sequence, head and tile of rows), a thread per dim and several rows.
+// Joins the parts of the items that several workers share, and fills the rows that see nothing: a
+// CTA for each query row, whose warps take the parts in turn.
+constexpr int kJoinWarps = 4;
+
 template <int D, bool BF16>
-__global__ void __launch_bounds__(128) kv4_join_kernel(Kv4Attend a, int rows_tile, int unit, int grid) {
+__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, Kv4Cut cut, int most) {
+  __shared__ float acc[kJoinWarps][D];
+  __shared__ float sums[kJoinWarps];
   pdl_wait();
   pdl_trigger();
-  const int i = blockIdx.x;
-  Kv4Seq s;
-  {
-    s.seq = a.b.seqs ? a.b.seqs[i] : i;
-    if (!kv4_range(a.b, i, s.begin, s.count) || s.seq < 0 || s.seq >= a.c.max_seqs) return;
-    s.tiles = (s.count * a.group + rows_tile - 1) / rows_tile;
-  }
+  const int i = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t W = a.prefix[a.b.n], p0 = a.prefix[i], p1 = a.prefix[i + 1];
-  const int ctas = kv4_ctas(W, grid);
-  constexpr int kGroups = 128 / (D / 2);  // rows at a time, two dims to a thread
-  const int d2 = threadIdx.x % (D / 2) * 2;
-  for (int it = blockIdx.y; it < s.tiles * a.c.H; it += gridDim.y) {
-    const int head = it / s.tiles, tile = it - head * s.tiles;
-    const int64_t units = (p1 - p0) / ((int64_t)s.tiles * a.c.H), u0 = p0 + it * units, u1 = u0 + units;
-    int c0 = 0, c1 = -1;
-    if (units > 0) {
-      c0 = kv4_owner(W, u0, ctas);
-      c1 = kv4_owner(W, u1 - 1, ctas);
-      if (c0 == c1) continue;  // finished where it ran
+  int begin, count;
+  const int seq = a.b.seqs ? a.b.seqs[i] : i;
+  if (!kv4_range(a.b, i, begin, count) || seq < 0 || seq >= a.c.max_seqs) return;
+  const int tiles = (count * a.group + cut.rows - 1) / cut.rows;
+  const int per = tiles ? (int)((p1 - p0) / ((int64_t)tiles * a.c.H)) : 0;  // an item's length, 0: it has no units
+  const int workers = kv4_workers(W, cut, most);
+  constexpr int kDims = D / 32;
+  // y: row of the sequence (token j, query head), head by head of the cache
+  for (int y = blockIdx.y; y < count * a.q_heads; y += gridDim.y) {
+    const int head = y / (count * a.group), row = y - head * count * a.group;
+    const int tile = row / cut.rows, col = row - tile * cut.rows;
+    const int64_t v0 = p0 + ((int64_t)head * tiles + tile) * per;
+    int w0 = 0, parts = 0;
+    if (per > 0) {
+      w0 = kv4_owner(W, v0 + cut.start, workers);  // who has its first unit
+      parts = kv4_owner(W, v0 + per - 1, workers) - w0 + 1;
+      if (parts == 1) continue;  // finished where it ran
     }
-    const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
-    const int rows = min(rows_tile, s.count * a.group - tile * rows_tile);
-    const int first_slot = 2 * c0 + (units > 0 && kv4_range_begin(W, c0, ctas) < u0 ? 1 : 0);
-    for (int col = threadIdx.x / (D / 2); col < rows; col += kGroups) {
-      float top = kNone, total = 0.f, x = 0.f, y = 0.f;
-      for (int c = c0; c <= c1; ++c)
-        top = fmaxf(top, a.parts[((int64_t)(c == c0 ? first_slot : 2 * c) * rows_tile + col) * (D + 2) + D]);
+    const int64_t at = (int64_t)(begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
+    const int64_t size = (int64_t)cut.rows * kv4_part_floats(D);
+    // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
+    const float* base = a.parts + 2 * w0 * size + col * kv4_part_floats(D);
+    float top = kNone;
+    for (int p = lane; p < parts; p += 32) top = fmaxf(top, base[(2 * p + (p == 0)) * size + D]);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    float total = 0.f, o[kDims] = {};
 #pragma unroll 4
-      for (int c = c0; c <= c1; ++c) {
-        const float* part = a.parts + ((int64_t)(c == c0 ? first_slot : 2 * c) * rows_tile + col) * (D + 2);
-        const float f = exp2_approx(part[D] - top);
-        const float2 o = *reinterpret_cast<const float2*>(part + d2);
-        total += f * part[D + 1];
-        x += f * o.x;
-        y += f * o.y;
+    for (int p = warp; p < parts; p += kJoinWarps) {
+      const float* part = base + (2 * p + (p == 0)) * size;
+      const float2 rs = *reinterpret_cast<const float2*>(part + D);
+      float x[kDims];
+      if constexpr (kDims == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(part + 4 * lane);
+        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+      } else {
+        const float2 v = *reinterpret_cast<const float2*>(part + 2 * lane);
+        x[0] = v.x, x[1] = v.y;
       }
-      const int row = tile * rows_tile + col;
-      const int64_t at = (int64_t)(s.begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
+      const float f = exp2_approx(rs.x - top);
+      total += f * rs.y;
+#pragma unroll
+      for (int d = 0; d < kDims; ++d) o[d] += f * x[d];
+    }
+    __syncthreads();  // the row before is done with the shared sums
+#pragma unroll
+    for (int d = 0; d < kDims; ++d) acc[warp][kDims * lane + d] = o[d];
+    if (lane == 0) sums[warp] = total;
+    __syncthreads();
+    if (threadIdx.x < D / 2) {
+      const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
+      float x = 0.f, z = 0.f;
+      total = 0.f;
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) {
+        x += acc[w][2 * threadIdx.x];
+        z += acc[w][2 * threadIdx.x + 1];
+        total += sums[w];
+      }
       const float inv = total == 0.f ? 0.f : gv / total;
-      uint32_t packed;
-      if (BF16)
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed) : "f"(y * inv), "f"(x * inv));
-      else
-        packed = pack_half2(x * inv, y * inv);
-      *reinterpret_cast<uint32_t*>(a.out + at * D + d2) = packed;
-      if (a.lse && d2 == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
+      reinterpret_cast<uint32_t*>(a.out + at * D)[threadIdx.x] = pack_out<BF16>(x * inv, z * inv);
+      if (a.lse && threadIdx.x == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
     }
   }
 }
@@ -559,19 +568,19 @@ int few_ctas(int n_tiles, int sms) { return n_tiles == 1 ? 2 * sms : sms; }
 
 }  // namespace
 
-cudaError_t launch_kv4_join(const Kv4Attend& a, int rows, int unit, int ctas, int dtype, cudaStream_t stream) {
-  const int64_t items = ((int64_t)a.b.max_count * a.group + rows - 1) / rows * a.c.H;
-  const dim3 grid(a.b.n, (unsigned)(items < 1024 ? items : 1024));
+cudaError_t launch_kv4_join(const Kv4Attend& a, Kv4Cut cut, int workers, int dtype, cudaStream_t stream) {
+  const int64_t rows = (int64_t)a.b.max_count * a.q_heads;
+  const dim3 grid(a.b.n, (unsigned)(rows < 4096 ? rows : 4096));
   auto kernel = a.c.D == 128 ? (dtype == SEMKV_BF16 ? kv4_join_kernel<128, true> : kv4_join_kernel<128, false>)
                              : (dtype == SEMKV_BF16 ? kv4_join_kernel<64, true> : kv4_join_kernel<64, false>);
-  return launch_pdl(kernel, grid, dim3(128), 0, stream, a, rows, unit, ctas);
+  return launch_pdl(kernel, grid, dim3(kJoinWarps * 32), 0, stream, a, cut, workers);
 }
 
 static size_t prefix_bytes(int n) { return ((size_t)n + 1) * 8 + 15 & ~(size_t)15; }
 
 size_t kv4_attention_workspace(const Kv4Cache& c, const Kv4Batch& b, int q_heads, int sms) {
   const int n = few_tiles(b, q_heads / c.H);
-  return (size_t)2 * few_ctas(n, sms) * 8 * n * (c.D + 2) * 4 + prefix_bytes(b.n);
+  return (size_t)2 * few_ctas(n, sms) * kWarps * 8 * n * kv4_part_floats(c.D) * 4 + prefix_bytes(b.n);
 }
 
 cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer, int dtype, const void* q, int64_t q_stride,
@@ -597,7 +606,7 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
       c.D == 128 ? (bf ? launch_few_rows<128, true>(a, n, ctas, stream) : launch_few_rows<128, false>(a, n, ctas, stream))
                  : (bf ? launch_few_rows<64, true>(a, n, ctas, stream) : launch_few_rows<64, false>(a, n, ctas, stream));
   if (e != cudaSuccess) return e;
-  return launch_kv4_join(a, 8 * n, kUnit, ctas, dtype, stream);
+  return launch_kv4_join(a, few_cut(n), ctas * kWarps, dtype, stream);
 }
 
 }  // namespace semkv

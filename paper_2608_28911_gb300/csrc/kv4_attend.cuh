@@ -1,13 +1,15 @@
-// kv4_attend.cuh — how a step's attention over the paged 4-bit cache is split over CTAs, shared
+// kv4_attend.cuh — how a step's attention over the paged 4-bit cache is split over workers, shared
 // by the kernels that do it and the one that joins their parts.
 //
-// An item is (sequence, KV head, tile of `rows` query rows); a query row is (token j, head
-// g of the group) with index j * group + g.  An item's units are `unit` consecutive positions
-// each, from the unit of the first position that any row of the sequence sees to its last.  The
-// units of all items, in order, are cut into equal contiguous ranges, one per CTA, so ragged
-// lengths balance by themselves; every CTA finds its range from the lengths on the device.
-// A CTA walks its range item by item.  An item that lies in one CTA is finished there; of
-// the others each CTA writes a part, of which a range has at most two: its first and its last.
+// An item is (sequence, KV head, tile of query rows); a query row is (token j, head g of the
+// group) with index j * group + g.  An item's units are `unit` consecutive positions each, from
+// the unit of the first position that any row of the sequence sees to its last.  Each item also
+// counts as a few units of its own before them, the time that starting one costs.  These
+// lengths, item after item, are cut into equal contiguous ranges, one for each worker (a warp or
+// a CTA), so ragged lengths balance by themselves; every worker finds its range from the lengths
+// on the device.  An item that lies in one worker's range is finished there; of the others each
+// worker writes a part: one that begins its item and does not end it (its range's last) or one that
+// continues an item (its range's first), so two slots for each worker hold them.
 #pragma once
 #include "kv4.cuh"
 
@@ -22,9 +24,17 @@ struct Kv4Attend {
   uint16_t* out;
   float* lse;
   float scale_log2;  // softmax scale * log2(e)
-  float* parts;      // [2 * CTAs][rows][D + 2]: sums, then reference exponent and weight sum
-  int64_t* prefix;   // [b.n + 1]: units before each sequence (written by CTA 0, for the join)
+  float* parts;      // [2 * workers][rows][D + 4]: sums, then reference exponent and weight sum
+  int64_t* prefix;   // [b.n + 1]: length before each sequence (written by CTA 0, for the join)
 };
+
+// How a kernel's items are cut: rows of a tile, positions of a unit, units that an item's start
+// counts for, and the least length of a range.
+struct Kv4Cut {
+  int rows, unit, start, least;
+};
+
+__host__ __device__ constexpr int kv4_part_floats(int D) { return D + 4; }
 
 // One sequence's share of the plan.
 struct Kv4Seq {
@@ -33,8 +43,7 @@ struct Kv4Seq {
   int u_first, units;             // units of each item: u_first .. u_first + units - 1
 };
 
-template <int ROWS, int UNIT>
-__device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend& a, int i, bool report) {
+__device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend& a, Kv4Cut cut, int i, bool report) {
   Kv4Seq s;
   s.seq = a.b.seqs ? a.b.seqs[i] : i;
   s.tiles = s.units = s.u_first = s.length = 0;
@@ -49,28 +58,29 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend& a, int i, bool report
   const int t = a.c.length[s.seq];
   s.length = t < 0 ? 0 : t > cap ? (int)cap : t;
   if (report && t > cap) raise_error(a.c.err, kDevIndex);
-  s.tiles = (s.count * a.group + ROWS - 1) / ROWS;
+  s.tiles = (s.count * a.group + cut.rows - 1) / cut.rows;
   if (s.count > 0 && s.length > 0) {
     // the first row's first position
     const int64_t lo = a.window ? (int64_t)s.length - s.count + 1 - a.window : 0;
-    s.u_first = lo > 0 ? (int)(lo / UNIT) : 0;
-    s.units = (s.length + UNIT - 1) / UNIT - s.u_first;
+    s.u_first = lo > 0 ? (int)(lo / cut.unit) : 0;
+    s.units = (s.length + cut.unit - 1) / cut.unit - s.u_first;
   }
   return s;
 }
+__device__ __forceinline__ int64_t kv4_weight(const Kv4Attend& a, Kv4Cut cut, const Kv4Seq& s) {
+  return s.units ? (int64_t)(s.units + cut.start) * s.tiles * a.c.H : 0;
+}
 
-// The plan: thread x of the block counts the units of sequences x * per .. (x + 1) * per - 1, with
-// per = ceil(n / THREADS); prefix[x] = the units before them, prefix[THREADS] = all.
-template <int ROWS, int UNIT, int THREADS>
-__device__ __forceinline__ void kv4_plan(const Kv4Attend& a, int64_t* prefix, int64_t* sums, bool first_cta) {
+// The plan: thread x of the block adds up sequences x * per .. (x + 1) * per - 1, with
+// per = ceil(n / THREADS); prefix[x] = the length before them, prefix[THREADS] = all.
+template <int THREADS>
+__device__ __forceinline__ void kv4_plan(const Kv4Attend& a, Kv4Cut cut, int64_t* prefix, int64_t* sums,
+                                         bool first_cta) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = (a.b.n + THREADS - 1) / THREADS;
   const int i0 = threadIdx.x * per, i1 = min(a.b.n, i0 + per);
   int64_t sum = 0;
-  for (int i = i0; i < i1; ++i) {
-    const Kv4Seq s = kv4_seq<ROWS, UNIT>(a, i, first_cta);
-    sum += (int64_t)s.units * s.tiles * a.c.H;
-  }
+  for (int i = i0; i < i1; ++i) sum += kv4_weight(a, cut, kv4_seq(a, cut, i, first_cta));
   int64_t y = sum;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -86,41 +96,45 @@ __device__ __forceinline__ void kv4_plan(const Kv4Attend& a, int64_t* prefix, in
   if (first_cta) {
     for (int i = i0; i < i1; ++i) {
       a.prefix[i] = at;
-      const Kv4Seq s = kv4_seq<ROWS, UNIT>(a, i, false);
-      at += (int64_t)s.units * s.tiles * a.c.H;
+      at += per == 1 ? sum : kv4_weight(a, cut, kv4_seq(a, cut, i, false));
     }
     if (threadIdx.x == THREADS - 1) a.prefix[a.b.n] = at;
   }
   __syncthreads();
 }
 
-// The sequence that holds unit `cur` (below prefix[THREADS]); `at`: the units before it.
-template <int ROWS, int UNIT, int THREADS>
-__device__ __forceinline__ Kv4Seq kv4_find(const Kv4Attend& a, const int64_t* prefix, int64_t cur, int64_t& at) {
+// The sequence that place `v` (below prefix[THREADS]) lies in; `at`: the length before it.
+template <int THREADS>
+__device__ __forceinline__ Kv4Seq kv4_find(const Kv4Attend& a, Kv4Cut cut, const int64_t* prefix, int64_t v,
+                                           int64_t& at) {
   int lo = 0, hi = THREADS - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (prefix[mid] <= cur) lo = mid; else hi = mid - 1;
+    if (prefix[mid] <= v) lo = mid; else hi = mid - 1;
   }
   const int per = (a.b.n + THREADS - 1) / THREADS;
   at = prefix[lo];
-  Kv4Seq s = kv4_seq<ROWS, UNIT>(a, lo * per, false);
+  Kv4Seq s = kv4_seq(a, cut, lo * per, false);
   for (int k = 1; k < per; ++k) {
-    const int64_t units = (int64_t)s.units * s.tiles * a.c.H;
-    if (cur < at + units || lo * per + k >= a.b.n) break;
-    at += units;
-    s = kv4_seq<ROWS, UNIT>(a, lo * per + k, false);
+    const int64_t w = kv4_weight(a, cut, s);
+    if (v < at + w || lo * per + k >= a.b.n) break;
+    at += w;
+    s = kv4_seq(a, cut, lo * per + k, false);
   }
   return s;
 }
 
-// CTA c's range of W units on `ctas` CTAs (no more than W) begins at W c / ctas.
-__device__ __forceinline__ int64_t kv4_range_begin(int64_t W, int c, int ctas) { return W * c / ctas; }
-// the CTA whose range holds unit u
-__device__ __forceinline__ int kv4_owner(int64_t W, int64_t u, int ctas) {
-  return (int)(((u + 1) * ctas - 1) / W);
+// Workers that take part: no range shorter than cut.least.  Worker w's range of the length W begins
+// at W w / workers.
+__device__ __forceinline__ int kv4_workers(int64_t W, Kv4Cut cut, int most) {
+  const int64_t w = W / cut.least;
+  return w < 1 ? 1 : w < most ? (int)w : most;
 }
-__device__ __forceinline__ int kv4_ctas(int64_t W, int ctas) { return W < ctas ? (int)W : ctas; }
+__device__ __forceinline__ int64_t kv4_range_begin(int64_t W, int w, int workers) { return W * w / workers; }
+// the worker whose range holds place v
+__device__ __forceinline__ int kv4_owner(int64_t W, int64_t v, int workers) {
+  return (int)(((v + 1) * workers - 1) / W);
+}
 
 // Which positions a query row sees: [lo, hi]; hi < 0 for a row that is not there.
 template <typename S>
@@ -136,6 +150,6 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
-cudaError_t launch_kv4_join(const Kv4Attend& a, int rows, int unit, int ctas, int dtype, cudaStream_t stream);
+cudaError_t launch_kv4_join(const Kv4Attend& a, Kv4Cut cut, int workers, int dtype, cudaStream_t stream);
 
 }  // namespace semkv
