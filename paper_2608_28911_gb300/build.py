@@ -15,7 +15,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OUT = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT, "libsemkv.so")
 SOURCES = ["api.cu", "quantize.cu", "rank.cu", "decode.cu", "noalloc.cu", "score.cu",
-           "failure.cu", "kv4_api.cu", "kv4_rows.cu", "kv4_pages.cu", "kv4_attend.cu"]
+           "failure.cu", "kv4_api.cu", "kv4_rows.cu", "kv4_pages.cu", "kv4_attend.cu",
+           "kv4_chunk.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-ftz=false", "-prec-div=true", "-prec-sqrt=true", "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC",
          "-I", INCLUDE]

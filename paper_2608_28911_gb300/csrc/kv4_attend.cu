@@ -26,9 +26,6 @@ namespace {
 constexpr int kUnit = 32;       // tokens of a unit
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
-constexpr float kNone = -1e30f;  // reference exponent of a row without tokens
-constexpr float kHead = 8.f;     // a moved reference puts the largest weight at 2^8
-constexpr float kMost = 15.f;    // largest exponent of a weight
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -44,20 +41,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-  uint32_t w;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
-  return w;
-}
-
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
-  if (!BF16) return pack_half2(lo, hi);
-  uint32_t w;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
-  return w;
-}
-
 // token of the tile at place x of the order: {0, 3, 1, 2} and the same four further, ...
 __device__ __forceinline__ int token_at(int x) {
   const int t = (x & 7) >> 1, base = (x & 8) + t + (t & 2);
@@ -76,7 +59,7 @@ struct Layout {
   static constexpr int bytes() { return ring_bytes() + q_bytes() + kWarps * kStages * 8 + (kThreads + 1) * 8 + kWarps * 8; }
 };
 
-__host__ __device__ constexpr Kv4Cut few_cut(int n_tiles) { return Kv4Cut{8 * n_tiles, kUnit, 4, 4}; }
+__host__ __device__ constexpr Kv4FewCut few_cut(int n_tiles) { return Kv4FewCut{8 * n_tiles, kUnit, 4, 4}; }
 
 // The fragments of eight query rows (row0 + g) for one KV head, w[2k], w[2k + 1] those of k
 // step k.  bf16 rows are scaled by a power of two, which leaves their values exact in fp16 but
@@ -108,13 +91,7 @@ __device__ __forceinline__ float load_queries(const Kv4Attend& a, const Kv4Seq& 
     }
     most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
     most = fmaxf(most, __shfl_xor_sync(~0u, most, 2));
-    // the row's largest to [2^0, 2^1); rows of zeros and rows with an infinity as they are
-    int e = (int)(__float_as_uint(most) >> 23) - 127;
-    if (most == 0.f || !(most < INFINITY)) e = 0;
-    e = e < -126 ? -126 : e;
-    // 2^-127 and 2^127 for e = 127: its inverse is not a normal number
-    undo = e == 127 ? 0x1p127f : __uint_as_float((uint32_t)(127 + e) << 23);
-    const float mul = e == 127 ? 0x1p-127f : __uint_as_float((uint32_t)(127 - e) << 23);
+    const float mul = query_factor(most, undo);
 #pragma unroll
     for (int k = 0; k < D / 8; ++k)
       w[k] = pack_half2(__uint_as_float(w[k] << 16) * mul, __uint_as_float(w[k] & 0xFFFF0000u) * mul);
@@ -125,7 +102,7 @@ __device__ __forceinline__ float load_queries(const Kv4Attend& a, const Kv4Seq& 
 template <int D, int NT, bool BF16>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(Kv4Attend a) {
   using L = Layout<D, NT>;
-  constexpr Kv4Cut cut = few_cut(NT);
+  constexpr Kv4FewCut cut = few_cut(NT);
   constexpr int kSteps = D / 16;   // k steps of S
   constexpr int kM = D / 16;       // m tiles of O
   extern __shared__ __align__(128) uint8_t smem[];
@@ -147,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
   pdl_trigger();
   kv4_plan<kThreads>(a, cut, prefix, sums, blockIdx.x == 0);
   const int64_t W = prefix[kThreads];
-  const int workers = kv4_workers(W, cut, gridDim.x * kWarps);
+  const int workers = kv4_workers(W, cut.least, gridDim.x * kWarps);
   const int worker = warp * gridDim.x + blockIdx.x;  // few workers: spread over the SMs
   if (W == 0 || worker >= workers) return;
   const int64_t end = kv4_range_begin(W, worker + 1, workers);
@@ -467,33 +444,29 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
 // CTA for each query row, whose warps take the parts in turn.
 constexpr int kJoinWarps = 4;
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, Kv4Cut cut, int most) {
+template <int D, bool BF16, class Cut>
+__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, Cut cut, int most) {
   __shared__ float acc[kJoinWarps][D];
   __shared__ float sums[kJoinWarps];
   pdl_wait();
   pdl_trigger();
   const int i = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t W = a.prefix[a.b.n], p0 = a.prefix[i], p1 = a.prefix[i + 1];
-  int begin, count;
-  const int seq = a.b.seqs ? a.b.seqs[i] : i;
-  if (!kv4_range(a.b, i, begin, count) || seq < 0 || seq >= a.c.max_seqs) return;
-  const int tiles = (count * a.group + cut.rows - 1) / cut.rows;
-  const int per = tiles ? (int)((p1 - p0) / ((int64_t)tiles * a.c.H)) : 0;  // an item's length, 0: it has no units
-  const int workers = kv4_workers(W, cut, most);
+  const int64_t W = a.prefix[a.b.n], p0 = a.prefix[i];
+  const Kv4Seq s = cut.seq(a, i, false);
+  const int workers = kv4_workers(W, cut.least, most);
   constexpr int kDims = D / 32;
   // y: row of the sequence (token j, query head), head by head of the cache
-  for (int y = blockIdx.y; y < count * a.q_heads; y += gridDim.y) {
-    const int head = y / (count * a.group), row = y - head * count * a.group;
+  for (int64_t y = blockIdx.y; y < (int64_t)s.count * a.q_heads; y += gridDim.y) {
+    const int head = (int)(y / (s.count * a.group)), row = (int)(y - (int64_t)head * s.count * a.group);
     const int tile = row / cut.rows, col = row - tile * cut.rows;
-    const int64_t v0 = p0 + ((int64_t)head * tiles + tile) * per;
     int w0 = 0, parts = 0;
-    if (per > 0) {
-      w0 = kv4_owner(W, v0 + cut.start, workers);  // who has its first unit
-      parts = kv4_owner(W, v0 + per - 1, workers) - w0 + 1;
+    int64_t first, last;
+    if (cut.ends(a, s, head, tile, first, last)) {
+      w0 = kv4_owner(W, p0 + first, workers);
+      parts = kv4_owner(W, p0 + last, workers) - w0 + 1;
       if (parts == 1) continue;  // finished where it ran
     }
-    const int64_t at = (int64_t)(begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
+    const int64_t at = (int64_t)(s.begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
     const int64_t size = (int64_t)cut.rows * kv4_part_floats(D);
     // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
     const float* base = a.parts + 2 * w0 * size + col * kv4_part_floats(D);
@@ -568,17 +541,26 @@ int few_ctas(int n_tiles, int sms) { return n_tiles == 1 ? 2 * sms : sms; }
 
 }  // namespace
 
-cudaError_t launch_kv4_join(const Kv4Attend& a, Kv4Cut cut, int workers, int dtype, cudaStream_t stream) {
+namespace {
+template <class Cut>
+cudaError_t launch_join(const Kv4Attend& a, Cut cut, int workers, int dtype, cudaStream_t stream) {
   const int64_t rows = (int64_t)a.b.max_count * a.q_heads;
   const dim3 grid(a.b.n, (unsigned)(rows < 4096 ? rows : 4096));
-  auto kernel = a.c.D == 128 ? (dtype == SEMKV_BF16 ? kv4_join_kernel<128, true> : kv4_join_kernel<128, false>)
-                             : (dtype == SEMKV_BF16 ? kv4_join_kernel<64, true> : kv4_join_kernel<64, false>);
+  const bool bf = dtype == SEMKV_BF16;
+  auto kernel = a.c.D == 128 ? (bf ? kv4_join_kernel<128, true, Cut> : kv4_join_kernel<128, false, Cut>)
+                             : (bf ? kv4_join_kernel<64, true, Cut> : kv4_join_kernel<64, false, Cut>);
   return launch_pdl(kernel, grid, dim3(kJoinWarps * 32), 0, stream, a, cut, workers);
+}
+}  // namespace
+
+cudaError_t launch_kv4_join(const Kv4Attend& a, Kv4ManyCut cut, int workers, int dtype, cudaStream_t stream) {
+  return launch_join(a, cut, workers, dtype, stream);
 }
 
 static size_t prefix_bytes(int n) { return ((size_t)n + 1) * 8 + 15 & ~(size_t)15; }
 
 size_t kv4_attention_workspace(const Kv4Cache& c, const Kv4Batch& b, int q_heads, int sms) {
+  if (kv4_many(b, q_heads / c.H)) return kv4_many_part_floats(c.D, sms) * 4 + prefix_bytes(b.n);
   const int n = few_tiles(b, q_heads / c.H);
   return (size_t)2 * few_ctas(n, sms) * kWarps * 8 * n * kv4_part_floats(c.D) * 4 + prefix_bytes(b.n);
 }
@@ -600,13 +582,14 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
   a.scale_log2 = softmax_scale * 1.4426950408889634f;
   a.prefix = static_cast<int64_t*>(ws);
   a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + prefix_bytes(b.n));
+  if (kv4_many(b, a.group)) return launch_kv4_many(a, dtype, sms, stream);
   const int n = few_tiles(b, a.group), ctas = few_ctas(n, sms);
   const bool bf = dtype == SEMKV_BF16;
   const cudaError_t e =
       c.D == 128 ? (bf ? launch_few_rows<128, true>(a, n, ctas, stream) : launch_few_rows<128, false>(a, n, ctas, stream))
                  : (bf ? launch_few_rows<64, true>(a, n, ctas, stream) : launch_few_rows<64, false>(a, n, ctas, stream));
   if (e != cudaSuccess) return e;
-  return launch_kv4_join(a, few_cut(n), ctas * kWarps, dtype, stream);
+  return launch_join(a, few_cut(n), ctas * kWarps, dtype, stream);
 }
 
 }  // namespace semkv

@@ -28,22 +28,16 @@ struct Kv4Attend {
   int64_t* prefix;   // [b.n + 1]: length before each sequence (written by CTA 0, for the join)
 };
 
-// How a kernel's items are cut: rows of a tile, positions of a unit, units that an item's start
-// counts for, and the least length of a range.
-struct Kv4Cut {
-  int rows, unit, start, least;
-};
-
 __host__ __device__ constexpr int kv4_part_floats(int D) { return D + 4; }
 
-// One sequence's share of the plan.
+// One sequence's rows of the step and its tokens.
 struct Kv4Seq {
-  int seq, begin, count, length;  // its rows of the step and its tokens
-  int tiles;                      // tiles of query rows
-  int u_first, units;             // units of each item: u_first .. u_first + units - 1
+  int seq, begin, count, length;
+  int tiles;           // tiles of query rows
+  int u_first, units;  // (Kv4FewCut) units of each item: u_first .. u_first + units - 1
 };
 
-__device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend& a, Kv4Cut cut, int i, bool report) {
+__device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend& a, int rows, int i, bool report) {
   Kv4Seq s;
   s.seq = a.b.seqs ? a.b.seqs[i] : i;
   s.tiles = s.units = s.u_first = s.length = 0;
@@ -58,29 +52,94 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend& a, Kv4Cut cut, int i,
   const int t = a.c.length[s.seq];
   s.length = t < 0 ? 0 : t > cap ? (int)cap : t;
   if (report && t > cap) raise_error(a.c.err, kDevIndex);
-  s.tiles = (s.count * a.group + cut.rows - 1) / cut.rows;
-  if (s.count > 0 && s.length > 0) {
-    // the first row's first position
-    const int64_t lo = a.window ? (int64_t)s.length - s.count + 1 - a.window : 0;
-    s.u_first = lo > 0 ? (int)(lo / cut.unit) : 0;
-    s.units = (s.length + cut.unit - 1) / cut.unit - s.u_first;
-  }
+  s.tiles = (int)(((int64_t)s.count * a.group + rows - 1) / rows);
   return s;
 }
-__device__ __forceinline__ int64_t kv4_weight(const Kv4Attend& a, Kv4Cut cut, const Kv4Seq& s) {
-  return s.units ? (int64_t)(s.units + cut.start) * s.tiles * a.c.H : 0;
-}
+
+// Cut for few rows: lengths in units of `unit` tokens; the items of a sequence are alike, from the
+// unit of the first row's first position to the last.
+struct Kv4FewCut {
+  int rows, unit, start, least;
+  __device__ __forceinline__ Kv4Seq seq(const Kv4Attend& a, int i, bool report) const {
+    Kv4Seq s = kv4_seq(a, rows, i, report);
+    if (s.count > 0 && s.length > 0) {
+      const int64_t lo = a.window ? (int64_t)s.length - s.count + 1 - a.window : 0;
+      s.u_first = lo > 0 ? (int)(lo / unit) : 0;
+      s.units = (s.length + unit - 1) / unit - s.u_first;
+    }
+    return s;
+  }
+  __device__ __forceinline__ int64_t weight(const Kv4Attend& a, const Kv4Seq& s) const {
+    return s.units ? (int64_t)(s.units + start) * s.tiles * a.c.H : 0;
+  }
+  // places, from the sequence's first, of an item's first and last unit; false if it has none
+  __device__ __forceinline__ bool ends(const Kv4Attend& a, const Kv4Seq& s, int head, int tile, int64_t& first,
+                                       int64_t& last) const {
+    if (!s.units) return false;
+    first = ((int64_t)head * s.tiles + tile) * (s.units + start) + start;
+    last = first + s.units - 1;
+    return true;
+  }
+};
+
+// Cut for many rows: lengths in tokens.  A tile holds `tokens` whole tokens of the sequence (its rows are
+// tokens * group); tile x sees the positions below e = p0 + (x + 1) tokens, p0 the first row's, and
+// of them the last `cap` (all, without a window), so lengths add up in closed form.
+struct Kv4ManyCut {
+  int rows, tokens, unit, start, least;
+  __device__ __forceinline__ Kv4Seq seq(const Kv4Attend& a, int i, bool report) const {
+    return kv4_seq(a, rows, i, report);
+  }
+  __device__ __forceinline__ int64_t cap(const Kv4Attend& a) const {
+    return a.window ? (int64_t)a.window + tokens : (int64_t)1 << 40;
+  }
+  // length of one head's tiles before tile k
+  __device__ __forceinline__ int64_t before(const Kv4Attend& a, const Kv4Seq& s, int64_t k) const {
+    if (s.length == 0) return 0;
+    const int64_t p0 = (int64_t)s.length - s.count, most = cap(a);
+    const int64_t k0 = p0 < 0 ? -p0 / tokens : 0;  // tiles that see nothing
+    int64_t kc = (most - p0 + tokens - 1) / tokens - 1;  // the first that sees `most` or more
+    kc = kc < k0 ? k0 : kc;
+    if (k <= k0) return 0;
+    const int64_t x = k < kc ? k : kc;
+    const int64_t ramp = (x - k0) * p0 + tokens * (x * (x + 1) / 2 - k0 * (k0 + 1) / 2);
+    return ramp + (k > kc ? (k - kc) * most : 0) + (k - k0) * start;
+  }
+  __device__ __forceinline__ int64_t weight(const Kv4Attend& a, const Kv4Seq& s) const {
+    return before(a, s, s.tiles) * a.c.H;
+  }
+  // a tile's units [first, last) and the position `from` of its length's first token
+  __device__ __forceinline__ void units(const Kv4Attend& a, const Kv4Seq& s, int tile, int& first, int& last,
+                                        int64_t& from) const {
+    const int64_t e = (int64_t)s.length - s.count + (int64_t)(tile + 1) * tokens, most = cap(a);
+    from = e > most ? e - most : 0;
+    first = (int)(from / unit);
+    const int64_t to = e < s.length ? e : s.length;
+    last = to > 0 ? (int)((to + unit - 1) / unit) : first;
+  }
+  __device__ __forceinline__ bool ends(const Kv4Attend& a, const Kv4Seq& s, int head, int tile, int64_t& first,
+                                       int64_t& last) const {
+    int u0, u1;
+    int64_t from;
+    units(a, s, tile, u0, u1, from);
+    if (s.length == 0 || u1 <= u0) return false;
+    first = head * before(a, s, s.tiles) + before(a, s, tile) + start;
+    const int64_t at = (int64_t)(u1 - 1) * unit - from;
+    last = first + (at > 0 ? at : 0);
+    return true;
+  }
+};
 
 // The plan: thread x of the block adds up sequences x * per .. (x + 1) * per - 1, with
 // per = ceil(n / THREADS); prefix[x] = the length before them, prefix[THREADS] = all.
-template <int THREADS>
-__device__ __forceinline__ void kv4_plan(const Kv4Attend& a, Kv4Cut cut, int64_t* prefix, int64_t* sums,
+template <int THREADS, class Cut>
+__device__ __forceinline__ void kv4_plan(const Kv4Attend& a, Cut cut, int64_t* prefix, int64_t* sums,
                                          bool first_cta) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = (a.b.n + THREADS - 1) / THREADS;
   const int i0 = threadIdx.x * per, i1 = min(a.b.n, i0 + per);
   int64_t sum = 0;
-  for (int i = i0; i < i1; ++i) sum += kv4_weight(a, cut, kv4_seq(a, cut, i, first_cta));
+  for (int i = i0; i < i1; ++i) sum += cut.weight(a, cut.seq(a, i, first_cta));
   int64_t y = sum;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -96,7 +155,7 @@ __device__ __forceinline__ void kv4_plan(const Kv4Attend& a, Kv4Cut cut, int64_t
   if (first_cta) {
     for (int i = i0; i < i1; ++i) {
       a.prefix[i] = at;
-      at += per == 1 ? sum : kv4_weight(a, cut, kv4_seq(a, cut, i, false));
+      at += per == 1 ? sum : cut.weight(a, cut.seq(a, i, false));
     }
     if (threadIdx.x == THREADS - 1) a.prefix[a.b.n] = at;
   }
@@ -104,8 +163,8 @@ __device__ __forceinline__ void kv4_plan(const Kv4Attend& a, Kv4Cut cut, int64_t
 }
 
 // The sequence that place `v` (below prefix[THREADS]) lies in; `at`: the length before it.
-template <int THREADS>
-__device__ __forceinline__ Kv4Seq kv4_find(const Kv4Attend& a, Kv4Cut cut, const int64_t* prefix, int64_t v,
+template <int THREADS, class Cut>
+__device__ __forceinline__ Kv4Seq kv4_find(const Kv4Attend& a, Cut cut, const int64_t* prefix, int64_t v,
                                            int64_t& at) {
   int lo = 0, hi = THREADS - 1;
   while (lo < hi) {
@@ -114,20 +173,20 @@ __device__ __forceinline__ Kv4Seq kv4_find(const Kv4Attend& a, Kv4Cut cut, const
   }
   const int per = (a.b.n + THREADS - 1) / THREADS;
   at = prefix[lo];
-  Kv4Seq s = kv4_seq(a, cut, lo * per, false);
+  Kv4Seq s = cut.seq(a, lo * per, false);
   for (int k = 1; k < per; ++k) {
-    const int64_t w = kv4_weight(a, cut, s);
+    const int64_t w = cut.weight(a, s);
     if (v < at + w || lo * per + k >= a.b.n) break;
     at += w;
-    s = kv4_seq(a, cut, lo * per + k, false);
+    s = cut.seq(a, lo * per + k, false);
   }
   return s;
 }
 
-// Workers that take part: no range shorter than cut.least.  Worker w's range of the length W begins
+// Workers that take part: no range shorter than `least`.  Worker w's range of the length W begins
 // at W w / workers.
-__device__ __forceinline__ int kv4_workers(int64_t W, Kv4Cut cut, int most) {
-  const int64_t w = W / cut.least;
+__device__ __forceinline__ int kv4_workers(int64_t W, int least, int most) {
+  const int64_t w = W / least;
   return w < 1 ? 1 : w < most ? (int)w : most;
 }
 __device__ __forceinline__ int64_t kv4_range_begin(int64_t W, int w, int workers) { return W * w / workers; }
@@ -135,6 +194,35 @@ __device__ __forceinline__ int64_t kv4_range_begin(int64_t W, int w, int workers
 __device__ __forceinline__ int kv4_owner(int64_t W, int64_t v, int workers) {
   return (int)(((v + 1) * workers - 1) / W);
 }
+
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  uint32_t w;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+  return w;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_out(float lo, float hi) {
+  if (!BF16) return pack_half2(lo, hi);
+  uint32_t w;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+  return w;
+}
+
+// bf16 query rows meet the cache as fp16, scaled by a power of two that brings the row's largest
+// value into [1, 2): exact but for values below 2^-14 of it (their last bits, 2^-25 of the largest).
+// The factor from the largest magnitude, and what undoes it.
+__device__ __forceinline__ float query_factor(float most, float& undo) {
+  int e = (int)(__float_as_uint(most) >> 23) - 127;
+  if (most == 0.f || !(most < INFINITY)) e = 0;  // rows of zeros and rows with an infinity as they are
+  e = e < -126 ? -126 : e;
+  // (2^-127, the inverse for e = 127, is not a normal number)
+  undo = e == 127 ? 0x1p127f : __uint_as_float((uint32_t)(127 + e) << 23);
+  return e == 127 ? 0x1p-127f : __uint_as_float((uint32_t)(127 - e) << 23);
+}
+
+constexpr float kNone = -1e30f;  // reference exponent of a row without tokens
+constexpr float kHead = 8.f;     // a moved reference puts the largest weight at 2^8
+constexpr float kMost = 15.f;    // largest exponent of a weight
 
 // Which positions a query row sees: [lo, hi]; hi < 0 for a row that is not there.
 template <typename S>
@@ -150,6 +238,10 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
-cudaError_t launch_kv4_join(const Kv4Attend& a, Kv4Cut cut, int workers, int dtype, cudaStream_t stream);
+// The kernel for many rows (kv4_chunk.cu): whether a step takes it, its parts, its launch.
+bool kv4_many(const Kv4Batch& b, int group);
+size_t kv4_many_part_floats(int D, int sms);
+cudaError_t launch_kv4_many(const Kv4Attend& a, int dtype, int sms, cudaStream_t stream);
+cudaError_t launch_kv4_join(const Kv4Attend& a, Kv4ManyCut cut, int workers, int dtype, cudaStream_t stream);
 
 }  // namespace semkv

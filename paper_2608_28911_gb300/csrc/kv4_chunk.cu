@@ -1,0 +1,623 @@
+// kv4_chunk.cu — attention over the paged 4-bit cache for many query rows (chunks of prompts, whole
+// prompts), bound by the tensor cores.
+//
+// One CTA per SM over its range of the batch's work (kv4_attend.cuh).  A tile is two blocks of 128
+// query rows; for each unit of 128 tokens
+//   S_t = Q_t K^T      tcgen05.mma, 128 x 128 x D, fp16, sums in tensor memory
+//   P_t = 2^(S_t - e)  one thread per row; P_t (fp16) takes S_t's place in tensor memory
+//   O_t += P_t V       tcgen05.mma with P_t read from tensor memory
+// so that 256 rows share the work of turning a unit's codes into fp16, and one block's softmax runs
+// while the other's products do.  Twelve warps and one more:
+//   0-3, 4-7  the softmax of block 0 and 1 (a warp's tensor memory lanes are those of warp % 4)
+//   8-11      the unit's codes to fp16 K and V in shared memory, two buffers each, codes
+//             loaded into registers a unit ahead
+//   12        one thread issues the products
+// The core matrices (8 rows of 16 bytes) of a K or V unit lie 128 bytes apart along the head dim and
+// 16 D bytes apart along the tokens.  That is K-major for S (head dim is its K) and MN-major for
+// O (head dim is its N), so V needs no transposition, and eight lanes storing one 16-byte piece
+// of eight tokens fill 128 bytes: no bank conflicts.
+// The reference exponent e of a row moves only when a weight would pass 2^15; its thread then
+// rescales its row of O, which no product touches at that time: the one before has completed
+// (S_t's barrier, which follows it, tells) and the next waits for P_t.
+// Tensor memory: S_0, S_1, O_0, O_1, 128 columns each.
+#include "kernels.h"
+#include "kv4_attend.cuh"
+
+namespace semkv {
+namespace {
+
+constexpr int kUnit = 128;
+constexpr int kThreads = 13 * 32;
+constexpr int kBlock = 128;     // rows of a block
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// A wait with a limit: false after kWaitPolls polls, or soon after another wait of the CTA ran out.
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* failed) {
+  const uint32_t at = smem_addr(bar);
+  for (uint32_t i = 0; i < kWaitPolls; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(at), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((i & 255) == 255 && *failed) return false;
+  }
+  *failed = 1;
+  return false;
+}
+__device__ __forceinline__ void arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
+// Shared-memory matrix descriptor without swizzle: start, leading and stride offsets in 16 bytes,
+// version 1.  K-major: leading = next core matrix along K, stride = next eight rows; MN-major:
+// leading = next eight along K, stride = next core matrix along the rows.
+__device__ __forceinline__ uint64_t matrix_desc(uint32_t at, uint32_t leading, uint32_t stride) {
+  return (uint64_t)((at >> 4) & 0x3FFFu) | ((uint64_t)((leading >> 4) & 0x3FFFu) << 16) |
+         ((uint64_t)((stride >> 4) & 0x3FFFu) << 32) | ((uint64_t)1 << 46);
+}
+// fp16 operands, fp32 sums, M = 128; bit 16: B is MN-major
+__device__ constexpr uint32_t instr_desc(int n, bool b_mn) {
+  return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kBlock >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
+               : "memory");
+}
+#define SEMKV_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
+#define SEMKV_U8(v, i) "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7])
+#define SEMKV_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+// 32 columns of the warp's lanes, and the wait for them (which takes the registers, so that no use
+// moves above it)
+__device__ __forceinline__ void tmem_load(uint32_t at, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,"
+      "%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : SEMKV_R8(v, 0), SEMKV_R8(v, 8), SEMKV_R8(v, 16), SEMKV_R8(v, 24)
+      : "r"(at));
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : SEMKV_U8(v, 0), SEMKV_U8(v, 8), SEMKV_U8(v, 16), SEMKV_U8(v, 24)
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,"
+      "%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::SEMKV_I8(v, 0),
+      SEMKV_I8(v, 8), SEMKV_I8(v, 16), SEMKV_I8(v, 24), "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::SEMKV_I8(v, 0),
+      SEMKV_I8(v, 8), "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <int D>
+struct Layout {
+  static constexpr int kTile = kBlock * D * 2;        // a block of Q, or a unit of K or V, in fp16
+  static constexpr int kChunk = 128;                  // next core matrix along the head dim
+  static constexpr int kGroup = D / 8 * 128;          // next eight rows
+  static constexpr int v(int b) { return b * kTile; }
+  static constexpr int k(int b) { return (2 + b) * kTile; }
+  static constexpr int q(int t) { return (4 + t) * kTile; }
+  static constexpr int prefix() { return 6 * kTile; }
+  static constexpr int sums() { return prefix() + (kThreads + 1) * 8; }
+  static constexpr int bars() { return sums() + 16 * 8; }
+  static constexpr int bytes() { return bars() + 24 * 8 + 16; }
+};
+
+// The barriers, and the two words behind them.
+struct Bars {
+  uint64_t q_full[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  int failed;
+  uint32_t tmem;
+};
+static_assert(sizeof(Bars) <= 24 * 8 + 16, "room for the barriers");
+
+// An item and this CTA's part of it.
+struct Item {
+  Kv4Seq s;
+  int head, tile, rows;  // rows: of this tile
+  int u0, u1;            // units of this part
+  int first, last;       // units of the item
+};
+
+// The next part of the CTA's range; false where the places taken hold no unit.
+__device__ __forceinline__ bool next_item(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t& place,
+                                          int64_t end, Item& it) {
+  int64_t at;
+  it.s = kv4_find<kThreads>(a, cut, prefix, place, at);
+  const int64_t head_length = cut.before(a, it.s, it.s.tiles);
+  it.head = (int)((place - at) / head_length);
+  const int64_t in_head = place - at - it.head * head_length;
+  int lo = 0, hi = it.s.tiles - 1;  // the last tile that begins at or before the place
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (cut.before(a, it.s, mid) <= in_head) lo = mid; else hi = mid - 1;
+  }
+  it.tile = lo;
+  const int64_t begin = cut.before(a, it.s, lo), length = cut.before(a, it.s, lo + 1) - begin;
+  const int64_t off = in_head - begin, take = min(length - off, end - place);
+  int64_t from;
+  cut.units(a, it.s, lo, it.first, it.last, from);
+  // the unit whose place (that of its first token) is the first at or behind o
+  auto unit_at = [&](int64_t o) {
+    return o <= cut.start ? it.first : (int)min((int64_t)it.last, (from + o - cut.start + kUnit - 1) / kUnit);
+  };
+  it.u0 = unit_at(off);
+  it.u1 = off + take >= length ? it.last : unit_at(off + take);
+  it.rows = min(cut.rows, (it.s.count - lo * cut.tokens) * a.group);
+  place += take;
+  return it.u1 > it.u0;
+}
+
+// ------------------------------------------------------------- softmax ------
+
+template <int D, bool BF16>
+__device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
+                                              int64_t end, uint8_t* smem, Bars* bars, uint32_t tmem) {
+  using L = Layout<D>;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t = warp >> 2, r = (warp & 3) * 32 + lane;
+  const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's tensor memory lanes
+  const uint32_t S = tmem + lanes + 128 * t, O = tmem + lanes + 256 + 128 * t;
+  volatile int* failed = &bars->failed;
+  uint32_t s_phase = 0, o_phase = 0;
+  Item it;
+  while (place < end) {
+    if (!next_item(a, cut, prefix, place, end, it)) continue;
+    if (t * kBlock >= it.rows) continue;  // this block has no rows
+    // ---- this thread's row of Q
+    const int row = it.tile * cut.rows + t * kBlock + r;  // of the sequence
+    const bool there = t * kBlock + r < it.rows;
+    const int j = row / a.group, h = it.head * a.group + row % a.group;
+    const bool flip = a.scale_log2 < 0.f;  // a negative scale goes into Q's signs: the largest logit is S's largest
+    float undo = 1.f;
+    {
+      const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(it.s.begin + j) * a.q_stride + h * D);
+      uint8_t* to = smem + L::q(t) + (r >> 3) * L::kGroup + (r & 7) * 16;
+      float mul = 1.f;
+      if (BF16 && there) {
+        float most = 0.f;
+#pragma unroll 4
+        for (int c = 0; c < D / 8; ++c) {
+          const uint4 x = src[c];
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
+        }
+        mul = query_factor(most, undo);
+      }
+      const uint32_t sign = flip ? 0x80008000u : 0u;
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (there) x = src[c];
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (BF16) w[i] = pack_half2(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xFFFF0000u) * mul);
+          w[i] ^= sign;
+        }
+        *reinterpret_cast<uint4*>(to + c * L::kChunk) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    fence_smem();
+    __syncwarp();
+    if (lane == 0) arrive(&bars->q_full[t]);
+
+    const float gk = a.c.k_scale ? a.c.k_scale[a.layer * a.c.H + it.head] : 1.f;
+    const float mul = fabsf(a.scale_log2) * gk * undo;
+    int lo = 0, hi = 0x7FFFFFFF;  // (a row that is not there sees all: its zeros are nobody's)
+    if (there) kv4_sight(a, it.s, row, lo, hi);
+    const int most_lo = __reduce_max_sync(~0u, lo), least_hi = __reduce_min_sync(~0u, hi);
+    float ref = kNone, sum = 0.f;
+    bool ok = true;
+    for (int u = it.u0; u < it.u1; ++u) {
+      ok = wait(&bars->s_full[t], s_phase, failed);
+      s_phase ^= 1;
+      if (!__all_sync(~0u, ok)) { ok = false; break; }
+      fence_after();
+      const int pos = u * kUnit;
+      const bool open = pos >= most_lo && pos + kUnit - 1 <= least_hi;
+      // ---- the largest logit
+      float top = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < kUnit / 32; ++c) {
+        uint32_t v[32];
+        tmem_load(S + 32 * c, v);
+        tmem_wait(v);
+        if (!open) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int p = pos + 32 * c + i;
+            if (p < lo || p > hi) v[i] = 0xFF800000u;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i += 2)
+          asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(__uint_as_float(v[i])), "f"(__uint_as_float(v[i + 1])));
+      }
+      top = top == -INFINITY ? top : top * mul;  // (a mul of 0 leaves the masked ones out)
+      const bool over = top > ref + kMost;
+      if (__any_sync(~0u, over)) {
+        float f = 1.f;
+        if (over) {
+          f = exp2_approx(ref - (top - kHead));
+          ref = top - kHead;
+          sum *= f;
+        }
+        if (u > it.u0) {
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t v[32];
+            tmem_load(O + 32 * c, v);
+            tmem_wait(v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+            tmem_store32(O + 32 * c, v);
+          }
+        }
+      }
+      // ---- weights, in S's place: column pair 32 c + 2 i to column 16 c + i
+#pragma unroll
+      for (int c = 0; c < kUnit / 32; ++c) {
+        uint32_t v[32], w[16];
+        tmem_load(S + 32 * c, v);
+        tmem_wait(v);
+        float part = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float x = exp2_approx(fmaf(__uint_as_float(v[2 * i]), mul, -ref));
+          float y = exp2_approx(fmaf(__uint_as_float(v[2 * i + 1]), mul, -ref));
+          if (!open) {
+            const int p = pos + 32 * c + 2 * i;
+            if (p < lo || p > hi) x = 0.f;
+            if (p + 1 < lo || p + 1 > hi) y = 0.f;
+          }
+          part += x + y;
+          w[i] = pack_half2(x, y);
+        }
+        sum += part;
+        tmem_store16(S + 16 * c, w);
+      }
+      tmem_stored();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(&bars->p_full[t]);
+    }
+    ok = ok && __all_sync(~0u, wait(&bars->o_full[t], o_phase, failed));
+    o_phase ^= 1;
+    if (!ok) return;
+    fence_after();
+    // ---- the row, or this range's part of it
+    const bool done = it.u0 == it.first && it.u1 == it.last;
+    const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + it.head] : 1.f;
+    const int64_t at = (int64_t)(it.s.begin + j) * a.q_heads + h;
+    const float inv = sum == 0.f ? 0.f : gv / sum;
+    float* part = a.parts + ((int64_t)(2 * blockIdx.x + (it.u0 == it.first ? 1 : 0)) * cut.rows + t * kBlock + r) * kv4_part_floats(D);
+#pragma unroll 1
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t v[32];
+      tmem_load(O + 32 * c, v);
+      tmem_wait(v);
+      if (!there) continue;
+      if (done) {
+        uint4* to = reinterpret_cast<uint4*>(a.out + at * D + 32 * c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t w[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            w[x] = pack_out<BF16>(__uint_as_float(v[8 * i + 2 * x]) * inv, __uint_as_float(v[8 * i + 2 * x + 1]) * inv);
+          to[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      } else {
+        uint4* to = reinterpret_cast<uint4*>(part + 32 * c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) to[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+      }
+    }
+    if (there) {
+      if (done) {
+        if (a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+      } else {
+        *reinterpret_cast<float2*>(part + D) = make_float2(ref, sum);
+      }
+    }
+    fence_before();
+  }
+}
+
+// ------------------------------------------------------- codes to fp16 ------
+
+// Eight tokens' rows of K or V, a lane the quarter q of token l % 8: its codes and its scales.
+template <int D>
+struct Codes {
+  static constexpr int kWords = D / 32;  // 32-bit words of codes in a quarter of a row
+  uint32_t w[kWords];
+  uint32_t scale;                        // D 128: two e4m3 bytes, D 64: one
+};
+
+template <int D>
+__device__ __forceinline__ void load_codes(Codes<D>& x, const uint8_t* codes, const uint8_t* scales, bool there) {
+  if (!there) {
+#pragma unroll
+    for (int i = 0; i < Codes<D>::kWords; ++i) x.w[i] = 0;
+    x.scale = 0;
+    return;
+  }
+  if constexpr (D == 128) {
+    const uint4 v = *reinterpret_cast<const uint4*>(codes);
+    x.w[0] = v.x, x.w[1] = v.y, x.w[2] = v.z, x.w[3] = v.w;
+    x.scale = *reinterpret_cast<const uint16_t*>(scales);
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(codes);
+    x.w[0] = v.x, x.w[1] = v.y;
+    x.scale = *scales;
+  }
+}
+
+// 16-byte pieces of fp16, a core matrix row each
+template <int D>
+__device__ __forceinline__ void store_values(const Codes<D>& x, uint8_t* to) {
+  const uint32_t s2 = e4m3x2_to_half2(x.scale);
+#pragma unroll
+  for (int i = 0; i < Codes<D>::kWords; ++i) {
+    const uint32_t s = __byte_perm(s2, 0, D == 128 && i >= 2 ? 0x3232 : 0x1010);
+    uint32_t h[4];
+    e2m1x8_to_half2(x.w[i], h);
+    *reinterpret_cast<uint4*>(to + i * Layout<D>::kChunk) =
+        make_uint4(hmul2_bits(h[0], s), hmul2_bits(h[1], s), hmul2_bits(h[2], s), hmul2_bits(h[3], s));
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
+                                           int64_t end, uint8_t* smem, Bars* bars) {
+  using L = Layout<D>;
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 8;
+  const int r8 = lane & 7, q = lane >> 3;
+  const int row = warp * 32 + r8;  // of the unit; the lane's further rows are 8, 16, 24 behind
+  volatile int* failed = &bars->failed;
+  const int64_t head_bytes = (int64_t)kv4_tile_bytes(D) << (a.c.page_shift - 4);
+  const int at_codes = q * (D / 8), at_scale = 16 * D + q * (D / 64);
+  uint8_t* to = smem + (row >> 3) * L::kGroup + r8 * 16 + q * (D / 32) * L::kChunk;
+  uint32_t n = 0;  // units so far
+  Item it;
+  while (place < end) {
+    if (!next_item(a, cut, prefix, place, end, it)) continue;
+    const uint8_t* base = a.c.pages + kv4_record(a.c, a.layer, 0, it.head);
+    const int64_t page_stride = head_bytes * a.c.H;
+    const int32_t* table = a.c.table + (int64_t)it.s.seq * a.c.max_pages;
+    // the pages of the warp's two tiles of a unit
+    int page[2];
+    auto find_pages = [&](int u) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int token = u * kUnit + warp * 32 + 16 * x;
+        page[x] = 0;
+        if (u < it.u1 && token < it.s.length) {
+          page[x] = table[token >> a.c.page_shift];
+          if ((unsigned)page[x] >= (unsigned)a.c.num_pages) {
+            raise_error(a.c.err, kDevIndex);
+            page[x] = 0;
+          }
+        }
+      }
+    };
+    Codes<D> k[4], v[4];
+    auto tile_at = [&](int u, int i) {  // the tile of the lane's i-th row
+      const int token = u * kUnit + warp * 32 + 8 * i;
+      return base + page[i >> 1] * page_stride + (int64_t)((token & (a.c.P - 1)) >> 4) * kv4_tile_bytes(D);
+    };
+    auto load = [&](int u, Codes<D>(&x)[4], bool is_v) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int token = u * kUnit + row + 8 * i, in_tile = token & 15;
+        const uint8_t* tile = tile_at(u, i);
+        load_codes<D>(x[i], tile + (is_v ? 8 * D : 0) + in_tile * (D / 2) + at_codes,
+                      tile + (is_v ? D : 0) + at_scale + in_tile * (D / 16), token < it.s.length);
+      }
+    };
+    find_pages(it.u0);
+    load(it.u0, k, false);
+    load(it.u0, v, true);
+    find_pages(it.u0 + 1);
+    for (int u = it.u0; u < it.u1; ++u, ++n) {
+      const int b = n & 1;
+      const uint32_t free_phase = (n >> 1 & 1) ^ 1;
+      if (!__all_sync(~0u, wait(&bars->k_empty[b], free_phase, failed))) return;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) store_values<D>(k[i], to + L::k(b) + i * L::kGroup);
+      fence_smem();
+      __syncwarp();
+      if (lane == 0) arrive(&bars->k_full[b]);
+      if (u + 1 < it.u1) load(u + 1, k, false);
+      if (!__all_sync(~0u, wait(&bars->v_empty[b], free_phase, failed))) return;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) store_values<D>(v[i], to + L::v(b) + i * L::kGroup);
+      fence_smem();
+      __syncwarp();
+      if (lane == 0) arrive(&bars->v_full[b]);
+      if (u + 1 < it.u1) {
+        load(u + 1, v, true);
+        find_pages(u + 2);
+      }
+    }
+  }
+  // the products have read the last buffers (their barriers outlive the arrivals)
+  for (uint32_t m = n < 2 ? 0 : n - 2; m < n; ++m)
+    if (!wait(&bars->k_empty[m & 1], m >> 1 & 1, failed) || !wait(&bars->v_empty[m & 1], m >> 1 & 1, failed)) return;
+}
+
+// ------------------------------------------------------------ products ------
+
+template <int D>
+__device__ __forceinline__ void product_thread(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
+                                               int64_t end, uint8_t* smem, Bars* bars, uint32_t tmem) {
+  using L = Layout<D>;
+  volatile int* failed = &bars->failed;
+  const uint32_t at = smem_addr(smem);
+  uint32_t n = 0, q_phase = 0, p_phase = 0;  // units so far; a bit for each block
+  Item it;
+  auto scores = [&](int t, int b) {  // S_t = Q_t K^T
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+      mma_ss(tmem + 128 * t, matrix_desc(at + L::q(t) + 2 * k * L::kChunk, L::kChunk, L::kGroup),
+             matrix_desc(at + L::k(b) + 2 * k * L::kChunk, L::kChunk, L::kGroup), instr_desc(kUnit, false), k > 0);
+    commit(&bars->s_full[t]);
+  };
+  while (place < end) {
+    if (!next_item(a, cut, prefix, place, end, it)) continue;
+    const int blocks = it.rows > kBlock ? 2 : 1;
+    for (int t = 0; t < blocks; ++t) {
+      if (!wait(&bars->q_full[t], q_phase >> t & 1, failed)) return;
+      q_phase ^= 1u << t;
+    }
+    if (!wait(&bars->k_full[n & 1], n >> 1 & 1, failed)) return;
+    fence_after();
+    for (int t = 0; t < blocks; ++t) scores(t, n & 1);
+    commit(&bars->k_empty[n & 1]);
+    for (int u = it.u0; u < it.u1; ++u, ++n) {
+      const int b = n & 1;
+      if (!wait(&bars->v_full[b], n >> 1 & 1, failed)) return;
+      for (int t = 0; t < blocks; ++t) {
+        if (!wait(&bars->p_full[t], p_phase >> t & 1, failed)) return;
+        p_phase ^= 1u << t;
+        fence_after();
+#pragma unroll
+        for (int k = 0; k < kUnit / 16; ++k)
+          mma_ts(tmem + 256 + 128 * t, tmem + 128 * t + 8 * k,
+                 matrix_desc(at + L::v(b) + 2 * k * L::kGroup, L::kGroup, L::kChunk), instr_desc(D, true), u > it.u0 || k > 0);
+        if (t == blocks - 1) commit(&bars->v_empty[b]);
+        if (u + 1 < it.u1) {
+          if (t == 0 && !wait(&bars->k_full[b ^ 1], (n + 1) >> 1 & 1, failed)) return;
+          if (t == 0) fence_after();
+          scores(t, b ^ 1);
+          if (t == blocks - 1) commit(&bars->k_empty[b ^ 1]);
+        } else {
+          commit(&bars->o_full[t]);
+        }
+      }
+    }
+  }
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4ManyCut cut) {
+  using L = Layout<D>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  int64_t* prefix = reinterpret_cast<int64_t*>(smem + L::prefix());
+  int64_t* sums = reinterpret_cast<int64_t*>(smem + L::sums());
+  Bars* bars = reinterpret_cast<Bars*>(smem + L::bars());
+  const int warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    auto init = [](uint64_t* bar, int count) {
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory");
+    };
+    for (int x = 0; x < 2; ++x) {
+      init(&bars->q_full[x], 4);
+      init(&bars->k_full[x], 4);
+      init(&bars->v_full[x], 4);
+      init(&bars->k_empty[x], 1);
+      init(&bars->v_empty[x], 1);
+      init(&bars->s_full[x], 1);
+      init(&bars->p_full[x], 4);
+      init(&bars->o_full[x], 1);
+    }
+    bars->failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&bars->tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = bars->tmem;
+  pdl_wait();
+  pdl_trigger();
+  kv4_plan<kThreads>(a, cut, prefix, sums, blockIdx.x == 0);
+  const int64_t W = prefix[kThreads];
+  const int workers = kv4_workers(W, cut.least, gridDim.x);
+  if (W > 0 && (int)blockIdx.x < workers) {
+    const int64_t place = kv4_range_begin(W, blockIdx.x, workers), end = kv4_range_begin(W, blockIdx.x + 1, workers);
+    if (warp < 8)
+      softmax_warps<D, BF16>(a, cut, prefix, place, end, smem, bars, tmem);
+    else if (warp < 12)
+      code_warps<D>(a, cut, prefix, place, end, smem, bars);
+    else if ((threadIdx.x & 31) == 0)
+      product_thread<D>(a, cut, prefix, place, end, smem, bars, tmem);
+  }
+  fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && bars->failed) raise_error(a.c.err, kDevWaitTimeout);
+  if (warp == 12) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// Tiles of whole tokens, as many as two blocks hold.
+Kv4ManyCut many_cut(int group) {
+  const int tokens = 2 * kBlock / group;
+  return Kv4ManyCut{tokens * group, tokens, kUnit, 2 * kUnit, 2 * kUnit};
+}
+
+template <int D, bool BF16>
+cudaError_t launch_chunk(const Kv4Attend& a, const Kv4ManyCut& cut, int sms, cudaStream_t stream) {
+  using L = Layout<D>;
+  auto kernel = kv4_chunk_kernel<D, BF16>;
+  static bool done[kAttrDevices];
+  const cudaError_t e = once_per_device(done, [&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::bytes());
+  });
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(sms), dim3(kThreads), L::bytes(), stream, a, cut);
+}
+
+}  // namespace
+
+bool kv4_many(const Kv4Batch& b, int group) {
+  return (int64_t)b.max_count * group > 32 && group <= 2 * kBlock;
+}
+
+size_t kv4_many_part_floats(int D, int sms) { return (size_t)2 * sms * 2 * kBlock * kv4_part_floats(D); }
+
+cudaError_t launch_kv4_many(const Kv4Attend& a, int dtype, int sms, cudaStream_t stream) {
+  const Kv4ManyCut cut = many_cut(a.group);
+  const bool bf = dtype == SEMKV_BF16;
+  const cudaError_t e =
+      a.c.D == 128 ? (bf ? launch_chunk<128, true>(a, cut, sms, stream) : launch_chunk<128, false>(a, cut, sms, stream))
+                   : (bf ? launch_chunk<64, true>(a, cut, sms, stream) : launch_chunk<64, false>(a, cut, sms, stream));
+  if (e != cudaSuccess) return e;
+  return launch_kv4_join(a, cut, sms, dtype, stream);
+}
+
+}  // namespace semkv

@@ -234,6 +234,28 @@ def test_long_and_short_sequences_share_the_work(window):
     attend(c, plain, [5, 1, 0, 1, 2, 7], 2, torch.bfloat16, window)
 
 
+@pytest.mark.parametrize("dtype,D,P,group", [("bfloat16", 128, 64, 4), ("float16", 64, 16, 2), ("float16", 128, 32, 3),
+                                             ("bfloat16", 64, 128, 1)])
+@pytest.mark.parametrize("window", [0, 200])
+def test_prompts_and_chunks(dtype, D, P, group, window):
+    """Many rows: tiles of 256 rows that several CTAs share, prompts, chunks behind a past, rows
+    before the first token, and single tokens in the same call."""
+    import torch
+    lens = [640, 1, 900, 130, 257, 3000]
+    c = make(lens, 1, D, P, seed=12)
+    plain = fill(c)
+    attend(c, plain, [640, 1, 300, 131, 0, 129], group, getattr(torch, dtype), window)
+
+
+@pytest.mark.parametrize("group", [48, 256, 257, 300])
+def test_large_groups(group):
+    """A tile holds whole tokens: groups that leave rows of it empty, fill it, or do not fit one."""
+    import torch
+    c = make([200, 3, 70], 1, 64, 32, seed=3)
+    plain = fill(c)
+    attend(c, plain, [1, 3, 2], group, torch.float16)
+
+
 def test_many_sequences():
     import torch
     rng = np.random.default_rng(0)
