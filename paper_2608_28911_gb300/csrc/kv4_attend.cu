@@ -444,8 +444,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
 // CTA for each query row, whose warps take the parts in turn.
 constexpr int kJoinWarps = 4;
 
-template <int D, bool BF16, class Cut>
-__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, Cut cut, int most) {
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, Kv4FewCut cut, int most) {
   __shared__ float acc[kJoinWarps][D];
   __shared__ float sums[kJoinWarps];
   pdl_wait();
@@ -541,22 +541,6 @@ int few_ctas(int n_tiles, int sms) { return n_tiles == 1 ? 2 * sms : sms; }
 
 }  // namespace
 
-namespace {
-template <class Cut>
-cudaError_t launch_join(const Kv4Attend& a, Cut cut, int workers, int dtype, cudaStream_t stream) {
-  const int64_t rows = (int64_t)a.b.max_count * a.q_heads;
-  const dim3 grid(a.b.n, (unsigned)(rows < 4096 ? rows : 4096));
-  const bool bf = dtype == SEMKV_BF16;
-  auto kernel = a.c.D == 128 ? (bf ? kv4_join_kernel<128, true, Cut> : kv4_join_kernel<128, false, Cut>)
-                             : (bf ? kv4_join_kernel<64, true, Cut> : kv4_join_kernel<64, false, Cut>);
-  return launch_pdl(kernel, grid, dim3(kJoinWarps * 32), 0, stream, a, cut, workers);
-}
-}  // namespace
-
-cudaError_t launch_kv4_join(const Kv4Attend& a, Kv4ManyCut cut, int workers, int dtype, cudaStream_t stream) {
-  return launch_join(a, cut, workers, dtype, stream);
-}
-
 static size_t prefix_bytes(int n) { return ((size_t)n + 1) * 8 + 15 & ~(size_t)15; }
 
 size_t kv4_attention_workspace(const Kv4Cache& c, const Kv4Batch& b, int q_heads, int sms) {
@@ -589,7 +573,11 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
       c.D == 128 ? (bf ? launch_few_rows<128, true>(a, n, ctas, stream) : launch_few_rows<128, false>(a, n, ctas, stream))
                  : (bf ? launch_few_rows<64, true>(a, n, ctas, stream) : launch_few_rows<64, false>(a, n, ctas, stream));
   if (e != cudaSuccess) return e;
-  return launch_join(a, few_cut(n), ctas * kWarps, dtype, stream);
+  const int64_t rows = (int64_t)b.max_count * q_heads;
+  auto join = c.D == 128 ? (bf ? kv4_join_kernel<128, true> : kv4_join_kernel<128, false>)
+                         : (bf ? kv4_join_kernel<64, true> : kv4_join_kernel<64, false>);
+  return launch_pdl(join, dim3(b.n, (unsigned)(rows < 4096 ? rows : 4096)), dim3(kJoinWarps * 32), 0, stream, a, few_cut(n),
+                    ctas * kWarps);
 }
 
 }  // namespace semkv

@@ -242,6 +242,5 @@ __device__ __forceinline__ float exp2_approx(float x) {
 bool kv4_many(const Kv4Batch& b, int group);
 size_t kv4_many_part_floats(int D, int sms);
 cudaError_t launch_kv4_many(const Kv4Attend& a, int dtype, int sms, cudaStream_t stream);
-cudaError_t launch_kv4_join(const Kv4Attend& a, Kv4ManyCut cut, int workers, int dtype, cudaStream_t stream);
 
 }  // namespace semkv

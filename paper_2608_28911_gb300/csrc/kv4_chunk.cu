@@ -11,7 +11,9 @@
 //   0-3, 4-7  the softmax of block 0 and 1 (a warp's tensor memory lanes are those of warp % 4)
 //   8-11      the unit's codes to fp16 K and V in shared memory, two buffers each, codes
 //             loaded into registers a unit ahead
-//   12        one thread issues the products
+//   12        one thread issues the products (13-15 only fill the warpgroup)
+// A softmax thread holds its row's 128 logits of a unit in registers, so tensor memory is read once
+// for them: the warpgroups share the launch's 4 x 128 registers a thread as 184, 184, 88, 56.
 // The core matrices (8 rows of 16 bytes) of a K or V unit lie 128 bytes apart along the head dim and
 // 16 D bytes apart along the tokens.  That is K-major for S (head dim is its K) and MN-major for
 // O (head dim is its N), so V needs no transposition, and eight lanes storing one 16-byte piece
@@ -27,7 +29,7 @@ namespace semkv {
 namespace {
 
 constexpr int kUnit = 128;
-constexpr int kThreads = 13 * 32;
+constexpr int kThreads = 16 * 32;  // (whole warpgroups, for setmaxnreg)
 constexpr int kBlock = 128;     // rows of a block
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -97,11 +99,13 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&v)[32]) {
                :
                : "memory");
 }
-__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t (&v)[32]) {
+// 16 columns, waited for
+__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t (&v)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,"
-      "%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::SEMKV_I8(v, 0),
-      SEMKV_I8(v, 8), SEMKV_I8(v, 16), SEMKV_I8(v, 24), "r"(at)
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : SEMKV_R8(v, 0), SEMKV_R8(v, 8)
+      : "r"(at)
       : "memory");
 }
 __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&v)[16]) {
@@ -114,6 +118,26 @@ __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.s
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// two binary32 values in a register pair
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+  uint64_t p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
+  return p;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& x, float& y) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p));
+}
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 
 template <int D>
 struct Layout {
@@ -199,13 +223,15 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     {
       const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(it.s.begin + j) * a.q_stride + h * D);
       uint8_t* to = smem + L::q(t) + (r >> 3) * L::kGroup + (r & 7) * 16;
+      uint4 x[D / 8];
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) x[c] = there ? src[c] : make_uint4(0, 0, 0, 0);
       float mul = 1.f;
-      if (BF16 && there) {
+      if (BF16) {
         float most = 0.f;
-#pragma unroll 4
+#pragma unroll
         for (int c = 0; c < D / 8; ++c) {
-          const uint4 x = src[c];
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
@@ -213,11 +239,9 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
         mul = query_factor(most, undo);
       }
       const uint32_t sign = flip ? 0x80008000u : 0u;
-#pragma unroll 4
+#pragma unroll
       for (int c = 0; c < D / 8; ++c) {
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (there) x = src[c];
-        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (BF16) w[i] = pack_half2(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xFFFF0000u) * mul);
@@ -231,7 +255,8 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     if (lane == 0) arrive(&bars->q_full[t]);
 
     const float gk = a.c.k_scale ? a.c.k_scale[a.layer * a.c.H + it.head] : 1.f;
-    const float mul = fabsf(a.scale_log2) * gk * undo;
+    // (never 0: a masked logit stays -infinity)
+    const float mul = fmaxf(fabsf(a.scale_log2) * gk * undo, 0x1p-126f);
     int lo = 0, hi = 0x7FFFFFFF;  // (a row that is not there sees all: its zeros are nobody's)
     if (there) kv4_sight(a, it.s, row, lo, hi);
     const int most_lo = __reduce_max_sync(~0u, lo), least_hi = __reduce_min_sync(~0u, hi);
@@ -245,24 +270,29 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       const int pos = u * kUnit;
       const bool open = pos >= most_lo && pos + kUnit - 1 <= least_hi;
       // ---- the largest logit
-      float top = -INFINITY;
+      uint32_t v[kUnit / 32][32];
 #pragma unroll
-      for (int c = 0; c < kUnit / 32; ++c) {
-        uint32_t v[32];
-        tmem_load(S + 32 * c, v);
-        tmem_wait(v);
-        if (!open) {
+      for (int c = 0; c < kUnit / 32; ++c) tmem_load(S + 32 * c, v[c]);
+#pragma unroll
+      for (int c = 0; c < kUnit / 32; ++c) tmem_wait(v[c]);
+      if (!open) {
+#pragma unroll
+        for (int c = 0; c < kUnit / 32; ++c)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const int p = pos + 32 * c + i;
-            if (p < lo || p > hi) v[i] = 0xFF800000u;
+            if (p < lo || p > hi) v[c][i] = 0xFF800000u;
           }
-        }
+      }
+      float most[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        most[c] = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 32; i += 2)
-          asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(__uint_as_float(v[i])), "f"(__uint_as_float(v[i + 1])));
+          asm("max.f32 %0, %0, %1, %2;" : "+f"(most[c]) : "f"(__uint_as_float(v[c][i])), "f"(__uint_as_float(v[c][i + 1])));
       }
-      top = top == -INFINITY ? top : top * mul;  // (a mul of 0 leaves the masked ones out)
+      const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * mul;
       const bool over = top > ref + kMost;
       if (__any_sync(~0u, over)) {
         float f = 1.f;
@@ -273,37 +303,37 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
         }
         if (u > it.u0) {
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t v[32];
-            tmem_load(O + 32 * c, v);
-            tmem_wait(v);
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t o[16];
+            tmem_load16(O + 16 * c, o);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-            tmem_store32(O + 32 * c, v);
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_store16(O + 16 * c, o);
           }
         }
       }
       // ---- weights, in S's place: column pair 32 c + 2 i to column 16 c + i
+      const uint64_t mul2 = pair(mul, mul), ref2 = pair(-ref, -ref);
+      uint64_t sums[2] = {0, 0};
 #pragma unroll
       for (int c = 0; c < kUnit / 32; ++c) {
-        uint32_t v[32], w[16];
-        tmem_load(S + 32 * c, v);
-        tmem_wait(v);
-        float part = 0.f;
+        uint32_t w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          float x = exp2_approx(fmaf(__uint_as_float(v[2 * i]), mul, -ref));
-          float y = exp2_approx(fmaf(__uint_as_float(v[2 * i + 1]), mul, -ref));
-          if (!open) {
-            const int p = pos + 32 * c + 2 * i;
-            if (p < lo || p > hi) x = 0.f;
-            if (p + 1 < lo || p + 1 > hi) y = 0.f;
-          }
-          part += x + y;
-          w[i] = pack_half2(x, y);
+          uint64_t x = pair_fma(pair(__uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1])), mul2, ref2);
+          float lo_x, hi_x;
+          unpair(x, lo_x, hi_x);
+          lo_x = exp2_approx(lo_x);
+          hi_x = exp2_approx(hi_x);
+          sums[i & 1] = pair_add(sums[i & 1], pair(lo_x, hi_x));
+          w[i] = pack_half2(lo_x, hi_x);
         }
-        sum += part;
         tmem_store16(S + 16 * c, w);
+      }
+      {
+        float x, y;
+        unpair(pair_add(sums[0], sums[1]), x, y);
+        sum += x + y;
       }
       tmem_stored();
       fence_before();
@@ -568,12 +598,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   const int workers = kv4_workers(W, cut.least, gridDim.x);
   if (W > 0 && (int)blockIdx.x < workers) {
     const int64_t place = kv4_range_begin(W, blockIdx.x, workers), end = kv4_range_begin(W, blockIdx.x + 1, workers);
-    if (warp < 8)
+    // 184 + 184 + 88 + 56 = 4 * 128, the registers of the launch
+    if (warp < 8) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
       softmax_warps<D, BF16>(a, cut, prefix, place, end, smem, bars, tmem);
-    else if (warp < 12)
+    } else if (warp < 12) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
       code_warps<D>(a, cut, prefix, place, end, smem, bars);
-    else if ((threadIdx.x & 31) == 0)
-      product_thread<D>(a, cut, prefix, place, end, smem, bars, tmem);
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+      if (threadIdx.x == 12 * 32) product_thread<D>(a, cut, prefix, place, end, smem, bars, tmem);
+      __syncwarp();
+    }
   }
   fence_before();
   __syncthreads();
@@ -581,6 +617,54 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   if (warp == 12) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// Joins the parts of the tiles that several CTAs share (a warp for a row; a tile has two or three
+// parts) and fills the rows that see nothing.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinSplit = 4;  // CTAs of a tile
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kJoinThreads) kv4_chunk_join_kernel(Kv4Attend a, Kv4ManyCut cut, int most) {
+  pdl_wait();
+  pdl_trigger();
+  const int i = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t W = a.prefix[a.b.n], p0 = a.prefix[i];
+  const Kv4Seq s = cut.seq(a, i, false);
+  const int workers = kv4_workers(W, cut.least, most);
+  constexpr int kDims = D / 32, kStep = kJoinSplit * kJoinThreads / 32;
+  for (int y = blockIdx.y; y < s.tiles * a.c.H; y += gridDim.y) {
+    const int head = y / s.tiles, tile = y - head * s.tiles;
+    int w0 = 0, parts = 0;
+    int64_t first, last;
+    if (cut.ends(a, s, head, tile, first, last)) {
+      w0 = kv4_owner(W, p0 + first, workers);
+      parts = kv4_owner(W, p0 + last, workers) - w0 + 1;
+      if (parts == 1) continue;  // finished where it ran
+    }
+    const int rows = min(cut.rows, (s.count - tile * cut.tokens) * a.group);
+    const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
+    for (int col = blockIdx.z * (kJoinThreads / 32) + warp; col < rows; col += kStep) {
+      const int row = tile * cut.rows + col;
+      const int64_t at = (int64_t)(s.begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
+      float ref = kNone, total = 0.f, o[kDims] = {};
+      for (int p = 0; p < parts; ++p) {
+        // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
+        const float* part = a.parts + ((int64_t)(2 * (w0 + p) + (p == 0)) * cut.rows + col) * kv4_part_floats(D);
+        const float2 rs = *reinterpret_cast<const float2*>(part + D);
+        const float to = fmaxf(ref, rs.x), f = exp2_approx(ref - to), g = exp2_approx(rs.x - to);
+        ref = to;
+        total = total * f + rs.y * g;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[d] = o[d] * f + part[kDims * lane + d] * g;
+      }
+      const float inv = total == 0.f ? 0.f : gv / total;
+#pragma unroll
+      for (int d = 0; d < kDims; d += 2)
+        *reinterpret_cast<uint32_t*>(a.out + at * D + kDims * lane + d) = pack_out<BF16>(o[d] * inv, o[d + 1] * inv);
+      if (a.lse && lane == 0) a.lse[at] = total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
+    }
   }
 }
 
@@ -617,7 +701,11 @@ cudaError_t launch_kv4_many(const Kv4Attend& a, int dtype, int sms, cudaStream_t
       a.c.D == 128 ? (bf ? launch_chunk<128, true>(a, cut, sms, stream) : launch_chunk<128, false>(a, cut, sms, stream))
                    : (bf ? launch_chunk<64, true>(a, cut, sms, stream) : launch_chunk<64, false>(a, cut, sms, stream));
   if (e != cudaSuccess) return e;
-  return launch_kv4_join(a, cut, sms, dtype, stream);
+  const int64_t items = ((int64_t)a.b.max_count + cut.tokens - 1) / cut.tokens * a.c.H;
+  auto join = a.c.D == 128 ? (bf ? kv4_chunk_join_kernel<128, true> : kv4_chunk_join_kernel<128, false>)
+                           : (bf ? kv4_chunk_join_kernel<64, true> : kv4_chunk_join_kernel<64, false>);
+  return launch_pdl(join, dim3(a.b.n, (unsigned)(items < 1024 ? items : 1024), kJoinSplit), dim3(kJoinThreads), 0, stream, a, cut,
+                    sms);
 }
 
 }  // namespace semkv
