@@ -11,7 +11,7 @@
 //   0-3, 4-7  the softmax of block 0 and 1 (a warp's tensor memory lanes are those of warp % 4)
 //   8-11      the unit's codes to fp16 K and V in shared memory, two buffers each, codes
 //             loaded into registers a unit ahead
-//   12        one thread issues the products (13-15 only fill the warpgroup)
+//   12        issues the products (13-15 only fill the warpgroup)
 // A softmax thread holds its row's 128 logits of a unit in registers, so tensor memory is read once
 // for them: the warpgroups share the launch's 4 x 128 registers a thread as 184, 184, 88, 56.
 // The core matrices (8 rows of 16 bytes) of a K or V unit lie 128 bytes apart along the head dim and
@@ -34,7 +34,8 @@ constexpr int kBlock = 128;     // rows of a block
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// A wait with a limit: false after kWaitPolls polls, or soon after another wait of the CTA ran out.
+// A whole warp's wait with a limit: false after kWaitPolls polls, or soon after another wait of the CTA
+// ran out.
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* failed) {
   const uint32_t at = smem_addr(bar);
   for (uint32_t i = 0; i < kWaitPolls; ++i) {
@@ -44,8 +45,8 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
         : "=r"(ok)
         : "r"(at), "r"(parity)
         : "memory");
-    if (ok) return true;
-    if ((i & 255) == 255 && *failed) return false;
+    if (__all_sync(~0u, ok)) return true;
+    if ((i & 255) == 255 && __any_sync(~0u, *failed)) return false;
   }
   *failed = 1;
   return false;
@@ -54,32 +55,41 @@ __device__ __forceinline__ void arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 
-// Shared-memory matrix descriptor without swizzle: start, leading and stride offsets in 16 bytes,
-// version 1.  K-major: leading = next core matrix along K, stride = next eight rows; MN-major:
-// leading = next eight along K, stride = next core matrix along the rows.
-__device__ __forceinline__ uint64_t matrix_desc(uint32_t at, uint32_t leading, uint32_t stride) {
-  return (uint64_t)((at >> 4) & 0x3FFFu) | ((uint64_t)((leading >> 4) & 0x3FFFu) << 16) |
-         ((uint64_t)((stride >> 4) & 0x3FFFu) << 32) | ((uint64_t)1 << 46);
-}
+// Shared-memory matrix descriptors without swizzle: start (bits 0-13), leading (16-29) and stride
+// (32-45) offsets in 16 bytes, version 1 (46).  K-major: leading = next core matrix along K,
+// stride = next eight rows; MN-major: leading = next eight along K, stride = next core matrix along
+// the rows.  The low word, to which a step along K is added, and the high word.
+__device__ __forceinline__ uint32_t desc_low(uint32_t at, uint32_t leading) { return at >> 4 | leading >> 4 << 16; }
+__device__ constexpr uint32_t desc_high(uint32_t stride) { return stride >> 4 | 1u << 14; }
 // fp16 operands, fp32 sums, M = 128; bit 16: B is MN-major
 __device__ constexpr uint32_t instr_desc(int n, bool b_mn) {
   return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kBlock >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+// The products of one warp, which runs convergent so that their operands stay in uniform registers:
+// `leader` holds in the one lane that issues them.  Issued from a branch of that lane alone,
+// each took 120 cycles, twice what the product takes.
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t idesc,
+                                       uint32_t add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n .reg .pred p, l;\n .reg .b64 x, y;\n setp.ne.u32 l, %0, 0;\n setp.ne.u32 p, %6, 0;\n mov.b64 x, {%2, %4};\n"
+      " mov.b64 y, {%3, %4};\n @l tcgen05.mma.cta_group::1.kind::f16 [%1], x, y, %5, p;\n}" ::"r"(leader),
+      "r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "r"(add)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t idesc,
+                                       uint32_t add) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n .reg .pred p, l;\n .reg .b64 y;\n setp.ne.u32 l, %0, 0;\n setp.ne.u32 p, %6, 0;\n mov.b64 y, {%3, %4};\n"
+      " @l tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], y, %5, p;\n}" ::"r"(leader),
+      "r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "r"(add)
       : "memory");
 }
-__device__ __forceinline__ void commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
-               : "memory");
+__device__ __forceinline__ void commit(uint32_t leader, uint64_t* bar) {
+  asm volatile(
+      "{\n .reg .pred l;\n setp.ne.u32 l, %1, 0;\n"
+      " @l tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(smem_addr(bar)),
+      "r"(leader)
+      : "memory");
 }
 #define SEMKV_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
 #define SEMKV_U8(v, i) "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7])
@@ -265,7 +275,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     for (int u = it.u0; u < it.u1; ++u) {
       ok = wait(&bars->s_full[t], s_phase, failed);
       s_phase ^= 1;
-      if (!__all_sync(~0u, ok)) { ok = false; break; }
+      if (!ok) break;
       fence_after();
       const int pos = u * kUnit;
       const bool open = pos >= most_lo && pos + kUnit - 1 <= least_hi;
@@ -340,7 +350,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       __syncwarp();
       if (lane == 0) arrive(&bars->p_full[t]);
     }
-    ok = ok && __all_sync(~0u, wait(&bars->o_full[t], o_phase, failed));
+    ok = ok && wait(&bars->o_full[t], o_phase, failed);
     o_phase ^= 1;
     if (!ok) return;
     fence_after();
@@ -481,14 +491,14 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
     for (int u = it.u0; u < it.u1; ++u, ++n) {
       const int b = n & 1;
       const uint32_t free_phase = (n >> 1 & 1) ^ 1;
-      if (!__all_sync(~0u, wait(&bars->k_empty[b], free_phase, failed))) return;
+      if (!wait(&bars->k_empty[b], free_phase, failed)) return;
 #pragma unroll
       for (int i = 0; i < 4; ++i) store_values<D>(k[i], to + L::k(b) + i * L::kGroup);
       fence_smem();
       __syncwarp();
       if (lane == 0) arrive(&bars->k_full[b]);
       if (u + 1 < it.u1) load(u + 1, k, false);
-      if (!__all_sync(~0u, wait(&bars->v_empty[b], free_phase, failed))) return;
+      if (!wait(&bars->v_empty[b], free_phase, failed)) return;
 #pragma unroll
       for (int i = 0; i < 4; ++i) store_values<D>(v[i], to + L::v(b) + i * L::kGroup);
       fence_smem();
@@ -508,23 +518,33 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
 // ------------------------------------------------------------ products ------
 
 template <int D>
-__device__ __forceinline__ void product_thread(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
-                                               int64_t end, uint8_t* smem, Bars* bars, uint32_t tmem) {
+__device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
+                                             int64_t end, uint8_t* smem, Bars* bars, uint32_t tmem) {
   using L = Layout<D>;
   volatile int* failed = &bars->failed;
   const uint32_t at = smem_addr(smem);
-  uint32_t n = 0, q_phase = 0, p_phase = 0;  // units so far; a bit for each block
-  Item it;
-  auto scores = [&](int t, int b) {  // S_t = Q_t K^T
+  uint32_t leader;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(leader));
+  constexpr uint32_t kHigh = desc_high(L::kGroup), vHigh = desc_high(L::kChunk);
+  const uint32_t k0 = desc_low(at + L::k(0), L::kChunk), q0 = desc_low(at + L::q(0), L::kChunk);
+  const uint32_t v0 = desc_low(at + L::v(0), L::kGroup);
+  auto scores = [&](int t, uint32_t b) {  // S_t = Q_t K^T
+    const uint32_t q = q0 + t * (L::kTile >> 4), k = k0 + b * (L::kTile >> 4);
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k)
-      mma_ss(tmem + 128 * t, matrix_desc(at + L::q(t) + 2 * k * L::kChunk, L::kChunk, L::kGroup),
-             matrix_desc(at + L::k(b) + 2 * k * L::kChunk, L::kChunk, L::kGroup), instr_desc(kUnit, false), k > 0);
-    commit(&bars->s_full[t]);
+    for (int x = 0; x < D / 16; ++x)
+      mma_ss(leader, tmem + 128 * t, q + x * (2 * L::kChunk >> 4), k + x * (2 * L::kChunk >> 4), kHigh, instr_desc(kUnit, false),
+             x > 0);
+    commit(leader, &bars->s_full[t]);
   };
+  uint32_t n = 0, q_phase = 0, p_phase = 0;  // units so far; a bit for each block
   while (place < end) {
-    if (!next_item(a, cut, prefix, place, end, it)) continue;
-    const int blocks = it.rows > kBlock ? 2 : 1;
+    int blocks, units;
+    {
+      Item it;
+      if (!next_item(a, cut, prefix, place, end, it)) continue;
+      blocks = it.rows > kBlock ? 2 : 1;
+      units = it.u1 - it.u0;
+    }
     for (int t = 0; t < blocks; ++t) {
       if (!wait(&bars->q_full[t], q_phase >> t & 1, failed)) return;
       q_phase ^= 1u << t;
@@ -532,26 +552,29 @@ __device__ __forceinline__ void product_thread(const Kv4Attend& a, const Kv4Many
     if (!wait(&bars->k_full[n & 1], n >> 1 & 1, failed)) return;
     fence_after();
     for (int t = 0; t < blocks; ++t) scores(t, n & 1);
-    commit(&bars->k_empty[n & 1]);
-    for (int u = it.u0; u < it.u1; ++u, ++n) {
-      const int b = n & 1;
+    commit(leader, &bars->k_empty[n & 1]);
+    for (int u = 0; u < units; ++u, ++n) {
+      const uint32_t b = n & 1;
       if (!wait(&bars->v_full[b], n >> 1 & 1, failed)) return;
       for (int t = 0; t < blocks; ++t) {
         if (!wait(&bars->p_full[t], p_phase >> t & 1, failed)) return;
         p_phase ^= 1u << t;
         fence_after();
+        const uint32_t v = v0 + b * (L::kTile >> 4);
 #pragma unroll
-        for (int k = 0; k < kUnit / 16; ++k)
-          mma_ts(tmem + 256 + 128 * t, tmem + 128 * t + 8 * k,
-                 matrix_desc(at + L::v(b) + 2 * k * L::kGroup, L::kGroup, L::kChunk), instr_desc(D, true), u > it.u0 || k > 0);
-        if (t == blocks - 1) commit(&bars->v_empty[b]);
-        if (u + 1 < it.u1) {
-          if (t == 0 && !wait(&bars->k_full[b ^ 1], (n + 1) >> 1 & 1, failed)) return;
-          if (t == 0) fence_after();
+        for (int x = 0; x < kUnit / 16; ++x)  // O_t += P_t V
+          mma_ts(leader, tmem + 256 + 128 * t, tmem + 128 * t + 8 * x, v + x * (2 * L::kGroup >> 4), vHigh, instr_desc(D, true),
+                 (uint32_t)(u > 0 || x > 0));
+        if (t == blocks - 1) commit(leader, &bars->v_empty[b]);
+        if (u + 1 < units) {
+          if (t == 0) {
+            if (!wait(&bars->k_full[b ^ 1], (n + 1) >> 1 & 1, failed)) return;
+            fence_after();
+          }
           scores(t, b ^ 1);
-          if (t == blocks - 1) commit(&bars->k_empty[b ^ 1]);
+          if (t == blocks - 1) commit(leader, &bars->k_empty[b ^ 1]);
         } else {
-          commit(&bars->o_full[t]);
+          commit(leader, &bars->o_full[t]);
         }
       }
     }
@@ -607,8 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
       code_warps<D>(a, cut, prefix, place, end, smem, bars);
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-      if (threadIdx.x == 12 * 32) product_thread<D>(a, cut, prefix, place, end, smem, bars, tmem);
-      __syncwarp();
+      if (warp == 12) product_warp<D>(a, cut, prefix, place, end, smem, bars, tmem);
     }
   }
   fence_before();
