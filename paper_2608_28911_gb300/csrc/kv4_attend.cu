@@ -137,7 +137,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
 
   for (int64_t place = kv4_range_begin(W, worker, workers); place < end;) {
     int64_t before;
-    const Kv4Seq s = kv4_find<kThreads>(a, cut, prefix, place, before);
+    int which;
+    const Kv4Seq s = kv4_find<kThreads>(a, cut, prefix, place, before, which);
     const int per = s.units + cut.start;
     const int64_t in_seq = place - before;
     const int item = (int)(in_seq / per), off = (int)(in_seq - (int64_t)item * per);

@@ -105,6 +105,11 @@ struct Kv4ManyCut {
     const int64_t ramp = (x - k0) * p0 + tokens * (x * (x + 1) / 2 - k0 * (k0 + 1) / 2);
     return ramp + (k > kc ? (k - kc) * most : 0) + (k - k0) * start;
   }
+  // a tile's own length
+  __device__ __forceinline__ int64_t length(const Kv4Attend& a, const Kv4Seq& s, int tile) const {
+    const int64_t e = (int64_t)s.length - s.count + (int64_t)(tile + 1) * tokens;
+    return s.length == 0 || e <= 0 ? 0 : min(e, cap(a)) + start;
+  }
   __device__ __forceinline__ int64_t weight(const Kv4Attend& a, const Kv4Seq& s) const {
     return before(a, s, s.tiles) * a.c.H;
   }
@@ -162,10 +167,10 @@ __device__ __forceinline__ void kv4_plan(const Kv4Attend& a, Cut cut, int64_t* p
   __syncthreads();
 }
 
-// The sequence that place `v` (below prefix[THREADS]) lies in; `at`: the length before it.
+// The sequence that place `v` (below prefix[THREADS]) lies in; `at`: the length before it, `i`: which.
 template <int THREADS, class Cut>
 __device__ __forceinline__ Kv4Seq kv4_find(const Kv4Attend& a, Cut cut, const int64_t* prefix, int64_t v,
-                                           int64_t& at) {
+                                           int64_t& at, int& i) {
   int lo = 0, hi = THREADS - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -173,12 +178,13 @@ __device__ __forceinline__ Kv4Seq kv4_find(const Kv4Attend& a, Cut cut, const in
   }
   const int per = (a.b.n + THREADS - 1) / THREADS;
   at = prefix[lo];
-  Kv4Seq s = cut.seq(a, lo * per, false);
+  i = lo * per;
+  Kv4Seq s = cut.seq(a, i, false);
   for (int k = 1; k < per; ++k) {
     const int64_t w = cut.weight(a, s);
-    if (v < at + w || lo * per + k >= a.b.n) break;
+    if (v < at + w || i + 1 >= a.b.n) break;
     at += w;
-    s = cut.seq(a, lo * per + k, false);
+    s = cut.seq(a, ++i, false);
   }
   return s;
 }

@@ -7,13 +7,14 @@
 //   P_t = 2^(S_t - e)  one thread per row; P_t (fp16) takes S_t's place in tensor memory
 //   O_t += P_t V       tcgen05.mma with P_t read from tensor memory
 // so that 256 rows share the work of turning a unit's codes into fp16, and one block's softmax runs
-// while the other's products do.  Twelve warps and one more:
+// while the other's products do.  Sixteen warps:
 //   0-3, 4-7  the softmax of block 0 and 1 (a warp's tensor memory lanes are those of warp % 4)
 //   8-11      the unit's codes to fp16 K and V in shared memory, two buffers each, codes
 //             loaded into registers a unit ahead
-//   12        issues the products (13-15 only fill the warpgroup)
+//   12        issues the products
+//   13-15     the query rows, those of the next item while the last unit of this one is at work
 // A softmax thread holds its row's 128 logits of a unit in registers, so tensor memory is read once
-// for them: the warpgroups share the launch's 4 x 128 registers a thread as 184, 184, 88, 56.
+// for them: the warpgroups share the launch's 4 x 128 registers a thread as 176, 176, 88, 72.
 // The core matrices (8 rows of 16 bytes) of a K or V unit lie 128 bytes apart along the head dim and
 // 16 D bytes apart along the tokens.  That is K-major for S (head dim is its K) and MN-major for
 // O (head dim is its N), so V needs no transposition, and eight lanes storing one 16-byte piece
@@ -29,7 +30,7 @@ namespace semkv {
 namespace {
 
 constexpr int kUnit = 128;
-constexpr int kThreads = 16 * 32;  // (whole warpgroups, for setmaxnreg)
+constexpr int kThreads = 16 * 32;
 constexpr int kBlock = 128;     // rows of a block
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -158,14 +159,15 @@ struct Layout {
   static constexpr int k(int b) { return (2 + b) * kTile; }
   static constexpr int q(int t) { return (4 + t) * kTile; }
   static constexpr int prefix() { return 6 * kTile; }
-  static constexpr int sums() { return prefix() + (kThreads + 1) * 8; }
+  static constexpr int undo() { return prefix() + (kThreads + 2) * 8; }
+  static constexpr int sums() { return undo() + 4 * kBlock * 4; }
   static constexpr int bars() { return sums() + 16 * 8; }
   static constexpr int bytes() { return bars() + 24 * 8 + 16; }
 };
 
 // The barriers, and the two words behind them.
 struct Bars {
-  uint64_t q_full[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t q_full[2], q_empty[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2];
   int failed;
   uint32_t tmem;
 };
@@ -173,102 +175,159 @@ static_assert(sizeof(Bars) <= 24 * 8 + 16, "room for the barriers");
 
 // An item and this CTA's part of it.
 struct Item {
-  Kv4Seq s;
   int head, tile, rows;  // rows: of this tile
   int u0, u1;            // units of this part
   int first, last;       // units of the item
 };
 
-// The next part of the CTA's range; false where the places taken hold no unit.
-__device__ __forceinline__ bool next_item(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t& place,
-                                          int64_t end, Item& it) {
-  int64_t at;
-  it.s = kv4_find<kThreads>(a, cut, prefix, place, at);
-  const int64_t head_length = cut.before(a, it.s, it.s.tiles);
-  it.head = (int)((place - at) / head_length);
-  const int64_t in_head = place - at - it.head * head_length;
-  int lo = 0, hi = it.s.tiles - 1;  // the last tile that begins at or before the place
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (cut.before(a, it.s, mid) <= in_head) lo = mid; else hi = mid - 1;
+// A walk over the CTA's range: found once, then from item to item.
+struct Walk {
+  Kv4Seq s;
+  int i, head, tile;
+  int64_t off, left;  // places of the item that are behind the walk, places of the range before it
+
+  __device__ __forceinline__ Walk(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place, int64_t end) {
+    int64_t at;
+    s = kv4_find<kThreads>(a, cut, prefix, place, at, i);
+    const int64_t head_length = cut.before(a, s, s.tiles);
+    head = (int)((place - at) / head_length);
+    const int64_t in_head = place - at - head * head_length;
+    int lo = 0, hi = s.tiles - 1;  // the last tile that begins at or before the place
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (cut.before(a, s, mid) <= in_head) lo = mid; else hi = mid - 1;
+    }
+    tile = lo;
+    off = in_head - cut.before(a, s, lo);
+    left = end - place;
   }
-  it.tile = lo;
-  const int64_t begin = cut.before(a, it.s, lo), length = cut.before(a, it.s, lo + 1) - begin;
-  const int64_t off = in_head - begin, take = min(length - off, end - place);
-  int64_t from;
-  cut.units(a, it.s, lo, it.first, it.last, from);
-  // the unit whose place (that of its first token) is the first at or behind o
-  auto unit_at = [&](int64_t o) {
-    return o <= cut.start ? it.first : (int)min((int64_t)it.last, (from + o - cut.start + kUnit - 1) / kUnit);
-  };
-  it.u0 = unit_at(off);
-  it.u1 = off + take >= length ? it.last : unit_at(off + take);
-  it.rows = min(cut.rows, (it.s.count - lo * cut.tokens) * a.group);
-  place += take;
-  return it.u1 > it.u0;
+
+  // The next item with units in the range; false at its end.  `s` stays the item's until the next call.
+  __device__ __forceinline__ bool next(const Kv4Attend& a, const Kv4ManyCut& cut, Item& it) {
+    while (left > 0) {
+      if (tile == s.tiles) {
+        tile = 0;
+        if (++head == a.c.H) {
+          head = 0;
+          do {
+            if (++i >= a.b.n) return false;
+            s = cut.seq(a, i, false);
+          } while (s.tiles == 0);
+        }
+      }
+      const int64_t length = cut.length(a, s, tile), take = min(length - off, left);
+      int64_t from;
+      cut.units(a, s, tile, it.first, it.last, from);
+      // the unit whose place (that of its first token) is the first at or behind o
+      auto unit_at = [&](int64_t o) {
+        return o <= cut.start ? it.first : (int)min((int64_t)it.last, (from + o - cut.start + kUnit - 1) / kUnit);
+      };
+      it.u0 = unit_at(off);
+      it.u1 = off + take >= length ? it.last : unit_at(off + take);
+      it.head = head;
+      it.tile = tile;
+      it.rows = min(cut.rows, (s.count - tile * cut.tokens) * a.group);
+      ++tile;
+      off = 0;
+      left -= take;
+      if (take > 0 && it.u1 > it.u0) return true;
+    }
+    return false;
+  }
+};
+
+// ------------------------------------------------------------- queries ------
+
+// Q's rows into shared memory as the first operand of S: eight rows at a time, a lane a quarter of
+// row l % 8.  Two sets of factors, by the item's parity: the softmax of one item may still want
+// its own while the next one's rows are put in place.
+template <int D, bool BF16>
+__device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
+                                            int64_t end, uint8_t* smem, Bars* bars, float* undo) {
+  using L = Layout<D>;
+  constexpr int kPieces = D / 32;  // 16-byte pieces of a quarter
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 13;
+  const int r8 = lane & 7, q = lane >> 3;
+  const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // a negative scale goes into Q's signs: the largest
+  volatile int* failed = &bars->failed;                            // logit is S's largest
+  uint32_t n[2] = {0, 0}, items = 0;
+  Walk walk(a, cut, prefix, place, end);
+  Item it;
+  for (; walk.next(a, cut, it); ++items) {
+    for (int t = 0; t < 2 && t * kBlock < it.rows; ++t) {
+      if (!wait(&bars->q_empty[t], (n[t] & 1) ^ 1, failed)) return;
+      ++n[t];
+      for (int group = warp; group < kBlock / 8; group += 3) {
+        const int in_tile = t * kBlock + group * 8 + r8, row = it.tile * cut.rows + in_tile;
+        uint4 x[kPieces];
+#pragma unroll
+        for (int c = 0; c < kPieces; ++c) x[c] = make_uint4(0, 0, 0, 0);
+        if (in_tile < it.rows) {
+          const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(walk.s.begin + row / a.group) * a.q_stride +
+                                                            (it.head * a.group + row % a.group) * D + q * (D / 4));
+#pragma unroll
+          for (int c = 0; c < kPieces; ++c) x[c] = src[c];
+        }
+        float by = 1.f, back = 1.f;
+        if (BF16) {
+          float most = 0.f;
+#pragma unroll
+          for (int c = 0; c < kPieces; ++c) {
+            const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
+          }
+          most = fmaxf(most, __shfl_xor_sync(~0u, most, 8));
+          most = fmaxf(most, __shfl_xor_sync(~0u, most, 16));
+          by = query_factor(most, back);
+        }
+        uint8_t* to = smem + L::q(t) + group * L::kGroup + r8 * 16 + q * kPieces * L::kChunk;
+#pragma unroll
+        for (int c = 0; c < kPieces; ++c) {
+          uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (BF16) w[i] = pack_half2(__uint_as_float(w[i] << 16) * by, __uint_as_float(w[i] & 0xFFFF0000u) * by);
+            w[i] ^= sign;
+          }
+          *reinterpret_cast<uint4*>(to + c * L::kChunk) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        if (q == 0) undo[(items & 1) * 2 * kBlock + in_tile] = back;
+      }
+      fence_smem();
+      __syncwarp();
+      if (lane == 0) arrive(&bars->q_full[t]);
+    }
+  }
+  // the products have read the last rows (their barriers outlive the arrivals)
+  for (int t = 0; t < 2; ++t)
+    if (n[t] && !wait(&bars->q_empty[t], (n[t] & 1) ^ 1, failed)) return;
 }
 
 // ------------------------------------------------------------- softmax ------
 
 template <int D, bool BF16>
 __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
-                                              int64_t end, uint8_t* smem, Bars* bars, uint32_t tmem) {
-  using L = Layout<D>;
+                                              int64_t end, const float* undo, Bars* bars, uint32_t tmem) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = warp >> 2, r = (warp & 3) * 32 + lane;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's tensor memory lanes
   const uint32_t S = tmem + lanes + 128 * t, O = tmem + lanes + 256 + 128 * t;
   volatile int* failed = &bars->failed;
-  uint32_t s_phase = 0, o_phase = 0;
+  uint32_t s_phase = 0, o_phase = 0, items = 0;
+  Walk walk(a, cut, prefix, place, end);
   Item it;
-  while (place < end) {
-    if (!next_item(a, cut, prefix, place, end, it)) continue;
+  for (; walk.next(a, cut, it); ++items) {
     if (t * kBlock >= it.rows) continue;  // this block has no rows
-    // ---- this thread's row of Q
     const int row = it.tile * cut.rows + t * kBlock + r;  // of the sequence
     const bool there = t * kBlock + r < it.rows;
     const int j = row / a.group, h = it.head * a.group + row % a.group;
-    const bool flip = a.scale_log2 < 0.f;  // a negative scale goes into Q's signs: the largest logit is S's largest
-    float undo = 1.f;
-    {
-      const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(it.s.begin + j) * a.q_stride + h * D);
-      uint8_t* to = smem + L::q(t) + (r >> 3) * L::kGroup + (r & 7) * 16;
-      uint4 x[D / 8];
-#pragma unroll
-      for (int c = 0; c < D / 8; ++c) x[c] = there ? src[c] : make_uint4(0, 0, 0, 0);
-      float mul = 1.f;
-      if (BF16) {
-        float most = 0.f;
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
-        }
-        mul = query_factor(most, undo);
-      }
-      const uint32_t sign = flip ? 0x80008000u : 0u;
-#pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (BF16) w[i] = pack_half2(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xFFFF0000u) * mul);
-          w[i] ^= sign;
-        }
-        *reinterpret_cast<uint4*>(to + c * L::kChunk) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
-    fence_smem();
-    __syncwarp();
-    if (lane == 0) arrive(&bars->q_full[t]);
-
     const float gk = a.c.k_scale ? a.c.k_scale[a.layer * a.c.H + it.head] : 1.f;
-    // (never 0: a masked logit stays -infinity)
-    const float mul = fmaxf(fabsf(a.scale_log2) * gk * undo, 0x1p-126f);
+    const float scale = fabsf(a.scale_log2) * gk;
+    float mul = 0.f;
     int lo = 0, hi = 0x7FFFFFFF;  // (a row that is not there sees all: its zeros are nobody's)
-    if (there) kv4_sight(a, it.s, row, lo, hi);
+    if (there) kv4_sight(a, walk.s, row, lo, hi);
     const int most_lo = __reduce_max_sync(~0u, lo), least_hi = __reduce_min_sync(~0u, hi);
     float ref = kNone, sum = 0.f;
     bool ok = true;
@@ -277,6 +336,8 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       s_phase ^= 1;
       if (!ok) break;
       fence_after();
+      // (S is there, so Q was; never 0: a masked logit stays -infinity)
+      if (u == it.u0) mul = fmaxf(scale * undo[(items & 1) * 2 * kBlock + t * kBlock + r], 0x1p-126f);
       const int pos = u * kUnit;
       const bool open = pos >= most_lo && pos + kUnit - 1 <= least_hi;
       // ---- the largest logit
@@ -357,7 +418,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     // ---- the row, or this range's part of it
     const bool done = it.u0 == it.first && it.u1 == it.last;
     const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + it.head] : 1.f;
-    const int64_t at = (int64_t)(it.s.begin + j) * a.q_heads + h;
+    const int64_t at = (int64_t)(walk.s.begin + j) * a.q_heads + h;
     const float inv = sum == 0.f ? 0.f : gv / sum;
     float* part = a.parts + ((int64_t)(2 * blockIdx.x + (it.u0 == it.first ? 1 : 0)) * cut.rows + t * kBlock + r) * kv4_part_floats(D);
 #pragma unroll 1
@@ -448,12 +509,12 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
   const int at_codes = q * (D / 8), at_scale = 16 * D + q * (D / 64);
   uint8_t* to = smem + (row >> 3) * L::kGroup + r8 * 16 + q * (D / 32) * L::kChunk;
   uint32_t n = 0;  // units so far
+  Walk walk(a, cut, prefix, place, end);
   Item it;
-  while (place < end) {
-    if (!next_item(a, cut, prefix, place, end, it)) continue;
+  while (walk.next(a, cut, it)) {
     const uint8_t* base = a.c.pages + kv4_record(a.c, a.layer, 0, it.head);
     const int64_t page_stride = head_bytes * a.c.H;
-    const int32_t* table = a.c.table + (int64_t)it.s.seq * a.c.max_pages;
+    const int32_t* table = a.c.table + (int64_t)walk.s.seq * a.c.max_pages;
     // the pages of the warp's two tiles of a unit
     int page[2];
     auto find_pages = [&](int u) {
@@ -461,7 +522,7 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
       for (int x = 0; x < 2; ++x) {
         const int token = u * kUnit + warp * 32 + 16 * x;
         page[x] = 0;
-        if (u < it.u1 && token < it.s.length) {
+        if (u < it.u1 && token < walk.s.length) {
           page[x] = table[token >> a.c.page_shift];
           if ((unsigned)page[x] >= (unsigned)a.c.num_pages) {
             raise_error(a.c.err, kDevIndex);
@@ -481,7 +542,7 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
         const int token = u * kUnit + row + 8 * i, in_tile = token & 15;
         const uint8_t* tile = tile_at(u, i);
         load_codes<D>(x[i], tile + (is_v ? 8 * D : 0) + in_tile * (D / 2) + at_codes,
-                      tile + (is_v ? D : 0) + at_scale + in_tile * (D / 16), token < it.s.length);
+                      tile + (is_v ? D : 0) + at_scale + in_tile * (D / 16), token < walk.s.length);
       }
     };
     find_pages(it.u0);
@@ -537,21 +598,20 @@ __device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCu
     commit(leader, &bars->s_full[t]);
   };
   uint32_t n = 0, q_phase = 0, p_phase = 0;  // units so far; a bit for each block
-  while (place < end) {
-    int blocks, units;
-    {
-      Item it;
-      if (!next_item(a, cut, prefix, place, end, it)) continue;
-      blocks = it.rows > kBlock ? 2 : 1;
-      units = it.u1 - it.u0;
-    }
+  Walk walk(a, cut, prefix, place, end);
+  Item it;
+  while (walk.next(a, cut, it)) {
+    const int blocks = it.rows > kBlock ? 2 : 1, units = it.u1 - it.u0;
     for (int t = 0; t < blocks; ++t) {
       if (!wait(&bars->q_full[t], q_phase >> t & 1, failed)) return;
       q_phase ^= 1u << t;
     }
     if (!wait(&bars->k_full[n & 1], n >> 1 & 1, failed)) return;
     fence_after();
-    for (int t = 0; t < blocks; ++t) scores(t, n & 1);
+    for (int t = 0; t < blocks; ++t) {
+      scores(t, n & 1);
+      if (units == 1) commit(leader, &bars->q_empty[t]);
+    }
     commit(leader, &bars->k_empty[n & 1]);
     for (int u = 0; u < units; ++u, ++n) {
       const uint32_t b = n & 1;
@@ -572,6 +632,7 @@ __device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCu
             fence_after();
           }
           scores(t, b ^ 1);
+          if (u + 2 == units) commit(leader, &bars->q_empty[t]);
           if (t == blocks - 1) commit(leader, &bars->k_empty[b ^ 1]);
         } else {
           commit(leader, &bars->o_full[t]);
@@ -587,6 +648,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   extern __shared__ __align__(128) uint8_t smem[];
   int64_t* prefix = reinterpret_cast<int64_t*>(smem + L::prefix());
   int64_t* sums = reinterpret_cast<int64_t*>(smem + L::sums());
+  float* undo = reinterpret_cast<float*>(smem + L::undo());
   Bars* bars = reinterpret_cast<Bars*>(smem + L::bars());
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
@@ -594,7 +656,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory");
     };
     for (int x = 0; x < 2; ++x) {
-      init(&bars->q_full[x], 4);
+      init(&bars->q_full[x], 3);
+      init(&bars->q_empty[x], 1);
       init(&bars->k_full[x], 4);
       init(&bars->v_full[x], 4);
       init(&bars->k_empty[x], 1);
@@ -621,16 +684,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   const int workers = kv4_workers(W, cut.least, gridDim.x);
   if (W > 0 && (int)blockIdx.x < workers) {
     const int64_t place = kv4_range_begin(W, blockIdx.x, workers), end = kv4_range_begin(W, blockIdx.x + 1, workers);
-    // 184 + 184 + 88 + 56 = 4 * 128, the registers of the launch
+    // 176 + 176 + 88 + 72 = 4 * 128, the registers of the launch
     if (warp < 8) {
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-      softmax_warps<D, BF16>(a, cut, prefix, place, end, smem, bars, tmem);
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+      softmax_warps<D, BF16>(a, cut, prefix, place, end, undo, bars, tmem);
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
       code_warps<D>(a, cut, prefix, place, end, smem, bars);
     } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-      if (warp == 12) product_warp<D>(a, cut, prefix, place, end, smem, bars, tmem);
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+      if (warp == 12)
+        product_warp<D>(a, cut, prefix, place, end, smem, bars, tmem);
+      else
+        query_warps<D, BF16>(a, cut, prefix, place, end, smem, bars, undo);
     }
   }
   fence_before();
