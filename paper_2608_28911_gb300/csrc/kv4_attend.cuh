@@ -35,6 +35,7 @@ struct Kv4Seq {
   int seq, begin, count, length;
   int tiles;           // tiles of query rows
   int u_first, units;  // (Kv4FewCut) units of each item: u_first .. u_first + units - 1
+  int hidden, level;   // (Kv4ManyCut) tiles at the front that see nothing; the first that sees `cap`
 };
 
 __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attend& a, int rows, int i, bool report) {
@@ -87,49 +88,65 @@ struct Kv4FewCut {
 // of them the last `cap` (all, without a window), so lengths add up in closed form.
 struct Kv4ManyCut {
   int rows, tokens, unit, start, least;
+  uint64_t magic;  // 2^32 / group, rounded up: x / group = x * magic >> 32 for the rows x of a tile
+  __device__ __forceinline__ int token_of(int x) const { return (int)((uint64_t)x * magic >> 32); }
   __device__ __forceinline__ Kv4Seq seq(const Kv4Attend& a, int i, bool report) const {
-    return kv4_seq(a, rows, i, report);
+    Kv4Seq s = kv4_seq(a, rows, i, report);
+    const int p0 = s.length - s.count;
+    s.hidden = p0 < 0 ? -p0 / tokens : 0;
+    s.level = 0x7FFFFFFF;
+    if (a.window) {
+      const int64_t x = (cap(a) - p0 + tokens - 1) / tokens - 1;  // (rare, so 64 bits)
+      s.level = x < s.hidden ? s.hidden : x < s.level ? (int)x : s.level;
+    }
+    return s;
   }
   __device__ __forceinline__ int64_t cap(const Kv4Attend& a) const {
     return a.window ? (int64_t)a.window + tokens : (int64_t)1 << 40;
   }
+  // the tile that a place of one head lies in
+  __device__ __forceinline__ int find(const Kv4Attend& a, const Kv4Seq& s, int64_t place) const {
+    int lo = 0, hi = s.tiles - 1;  // the last that begins at or before it
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (before(a, s, mid) <= place) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+  }
   // length of one head's tiles before tile k
   __device__ __forceinline__ int64_t before(const Kv4Attend& a, const Kv4Seq& s, int64_t k) const {
     if (s.length == 0) return 0;
-    const int64_t p0 = (int64_t)s.length - s.count, most = cap(a);
-    const int64_t k0 = p0 < 0 ? -p0 / tokens : 0;  // tiles that see nothing
-    int64_t kc = (most - p0 + tokens - 1) / tokens - 1;  // the first that sees `most` or more
-    kc = kc < k0 ? k0 : kc;
-    if (k <= k0) return 0;
-    const int64_t x = k < kc ? k : kc;
-    const int64_t ramp = (x - k0) * p0 + tokens * (x * (x + 1) / 2 - k0 * (k0 + 1) / 2);
-    return ramp + (k > kc ? (k - kc) * most : 0) + (k - k0) * start;
+    if (k <= s.hidden) return 0;
+    const int64_t p0 = (int64_t)s.length - s.count, k0 = s.hidden;
+    const int64_t x = k < s.level ? k : s.level;
+    const int64_t ramp = (x - k0) * p0 + tokens * ((x * (x + 1) - k0 * (k0 + 1)) >> 1);
+    return ramp + (k > x ? (k - x) * cap(a) : 0) + (k - k0) * start;
   }
-  // a tile's own length
-  __device__ __forceinline__ int64_t length(const Kv4Attend& a, const Kv4Seq& s, int tile) const {
-    const int64_t e = (int64_t)s.length - s.count + (int64_t)(tile + 1) * tokens;
-    return s.length == 0 || e <= 0 ? 0 : min(e, cap(a)) + start;
+  // a tile's own length (positions end at 2^30, a tile at 256 more)
+  __device__ __forceinline__ int length(const Kv4Attend& a, const Kv4Seq& s, int tile) const {
+    const int e = s.length - s.count + (tile + 1) * tokens;
+    if (s.length == 0 || e <= 0) return 0;
+    return (a.window && e - tokens > a.window ? a.window + tokens : e) + start;
   }
   __device__ __forceinline__ int64_t weight(const Kv4Attend& a, const Kv4Seq& s) const {
     return before(a, s, s.tiles) * a.c.H;
   }
   // a tile's units [first, last) and the position `from` of its length's first token
   __device__ __forceinline__ void units(const Kv4Attend& a, const Kv4Seq& s, int tile, int& first, int& last,
-                                        int64_t& from) const {
-    const int64_t e = (int64_t)s.length - s.count + (int64_t)(tile + 1) * tokens, most = cap(a);
-    from = e > most ? e - most : 0;
-    first = (int)(from / unit);
-    const int64_t to = e < s.length ? e : s.length;
-    last = to > 0 ? (int)((to + unit - 1) / unit) : first;
+                                        int& from) const {
+    const int e = s.length - s.count + (tile + 1) * tokens;
+    from = a.window && e - tokens > a.window ? e - tokens - a.window : 0;
+    first = from / unit;
+    const int to = e < s.length ? e : s.length;
+    last = to > 0 ? (to + unit - 1) / unit : first;
   }
   __device__ __forceinline__ bool ends(const Kv4Attend& a, const Kv4Seq& s, int head, int tile, int64_t& first,
                                        int64_t& last) const {
-    int u0, u1;
-    int64_t from;
+    int u0, u1, from;
     units(a, s, tile, u0, u1, from);
     if (s.length == 0 || u1 <= u0) return false;
     first = head * before(a, s, s.tiles) + before(a, s, tile) + start;
-    const int64_t at = (int64_t)(u1 - 1) * unit - from;
+    const int at = (u1 - 1) * unit - from;
     last = first + (at > 0 ? at : 0);
     return true;
   }

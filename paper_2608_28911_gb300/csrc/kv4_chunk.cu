@@ -144,11 +144,18 @@ __device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c)
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
   return d;
 }
+__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 __device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+
+constexpr int kStagePitch = 80, kStageBytes = 32 * kStagePitch;  // a softmax warp's stage of results
 
 template <int D>
 struct Layout {
@@ -158,7 +165,8 @@ struct Layout {
   static constexpr int v(int b) { return b * kTile; }
   static constexpr int k(int b) { return (2 + b) * kTile; }
   static constexpr int q(int t) { return (4 + t) * kTile; }
-  static constexpr int prefix() { return 6 * kTile; }
+  static constexpr int stage() { return 6 * kTile; }
+  static constexpr int prefix() { return stage() + 8 * kStageBytes; }
   static constexpr int undo() { return prefix() + (kThreads + 2) * 8; }
   static constexpr int sums() { return undo() + 4 * kBlock * 4; }
   static constexpr int bars() { return sums() + 16 * 8; }
@@ -184,7 +192,8 @@ struct Item {
 struct Walk {
   Kv4Seq s;
   int i, head, tile;
-  int64_t off, left;  // places of the item that are behind the walk, places of the range before it
+  int off;       // places of the item that are behind the walk
+  int64_t left;  // places of the range before it
 
   __device__ __forceinline__ Walk(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place, int64_t end) {
     int64_t at;
@@ -192,13 +201,8 @@ struct Walk {
     const int64_t head_length = cut.before(a, s, s.tiles);
     head = (int)((place - at) / head_length);
     const int64_t in_head = place - at - head * head_length;
-    int lo = 0, hi = s.tiles - 1;  // the last tile that begins at or before the place
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (cut.before(a, s, mid) <= in_head) lo = mid; else hi = mid - 1;
-    }
-    tile = lo;
-    off = in_head - cut.before(a, s, lo);
+    tile = cut.find(a, s, in_head);
+    off = (int)(in_head - cut.before(a, s, tile));
     left = end - place;
   }
 
@@ -215,12 +219,12 @@ struct Walk {
           } while (s.tiles == 0);
         }
       }
-      const int64_t length = cut.length(a, s, tile), take = min(length - off, left);
-      int64_t from;
+      const int length = cut.length(a, s, tile), take = left < length - off ? (int)left : length - off;
+      int from;
       cut.units(a, s, tile, it.first, it.last, from);
       // the unit whose place (that of its first token) is the first at or behind o
-      auto unit_at = [&](int64_t o) {
-        return o <= cut.start ? it.first : (int)min((int64_t)it.last, (from + o - cut.start + kUnit - 1) / kUnit);
+      auto unit_at = [&](int o) {
+        return o <= cut.start ? it.first : min(it.last, (from + o - cut.start + kUnit - 1) / kUnit);
       };
       it.u0 = unit_at(off);
       it.u1 = off + take >= length ? it.last : unit_at(off + take);
@@ -254,46 +258,63 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
   Walk walk(a, cut, prefix, place, end);
   Item it;
   for (; walk.next(a, cut, it); ++items) {
+    const uint16_t* base = a.q + (int64_t)(walk.s.begin + it.tile * cut.tokens) * a.q_stride + it.head * a.group * D;
+    // the rows come nearer while those before them are still wanted
+    for (int x = warp * 32 + lane; x < it.rows * (D / 64); x += 96) {
+      const int in_tile = x / (D / 64), j = cut.token_of(in_tile);
+      const uint16_t* at = base + (int64_t)j * a.q_stride + (in_tile - j * a.group) * D + x % (D / 64) * 64;
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+    }
     for (int t = 0; t < 2 && t * kBlock < it.rows; ++t) {
       if (!wait(&bars->q_empty[t], (n[t] & 1) ^ 1, failed)) return;
       ++n[t];
-      for (int group = warp; group < kBlock / 8; group += 3) {
-        const int in_tile = t * kBlock + group * 8 + r8, row = it.tile * cut.rows + in_tile;
-        uint4 x[kPieces];
+      // two groups of eight rows on their way at a time
+      for (int two = warp; two < kBlock / 16; two += 3) {
+        uint4 x[2][kPieces];
 #pragma unroll
-        for (int c = 0; c < kPieces; ++c) x[c] = make_uint4(0, 0, 0, 0);
-        if (in_tile < it.rows) {
-          const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(walk.s.begin + row / a.group) * a.q_stride +
-                                                            (it.head * a.group + row % a.group) * D + q * (D / 4));
+        for (int g = 0; g < 2; ++g) {
+          const int in_tile = t * kBlock + two * 16 + g * 8 + r8, j = cut.token_of(in_tile);
+          const bool there = in_tile < it.rows;
+          const uint4* src = reinterpret_cast<const uint4*>(base + (int64_t)j * a.q_stride + (in_tile - j * a.group) * D + q * (D / 4));
 #pragma unroll
-          for (int c = 0; c < kPieces; ++c) x[c] = src[c];
+          for (int c = 0; c < kPieces; ++c) x[g][c] = there ? src[c] : make_uint4(0, 0, 0, 0);
         }
-        float by = 1.f, back = 1.f;
-        if (BF16) {
-          float most = 0.f;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          uint64_t by2 = 0;
+          float back = 1.f;
+          if (BF16) {
+            uint32_t m = 0;  // largest magnitudes, pairwise
+#pragma unroll
+            for (int c = 0; c < kPieces; ++c) {
+              const uint32_t w[4] = {x[g][c].x, x[g][c].y, x[g][c].z, x[g][c].w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i] & 0x7FFF7FFFu));
+            }
+            float most = fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+            most = fmaxf(most, __shfl_xor_sync(~0u, most, 8));
+            most = fmaxf(most, __shfl_xor_sync(~0u, most, 16));
+            const float by = query_factor(most, back);
+            by2 = sign ? pair(-by, -by) : pair(by, by);
+          }
+          uint8_t* to = smem + L::q(t) + (2 * two + g) * L::kGroup + r8 * 16 + q * kPieces * L::kChunk;
 #pragma unroll
           for (int c = 0; c < kPieces; ++c) {
-            const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+            uint32_t w[4] = {x[g][c].x, x[g][c].y, x[g][c].z, x[g][c].w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
+            for (int i = 0; i < 4; ++i) {
+              if (BF16) {
+                float lo, hi;
+                unpair(pair_mul(pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u)), by2), lo, hi);
+                w[i] = pack_half2(lo, hi);
+              } else {
+                w[i] ^= sign;
+              }
+            }
+            *reinterpret_cast<uint4*>(to + c * L::kChunk) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-          most = fmaxf(most, __shfl_xor_sync(~0u, most, 8));
-          most = fmaxf(most, __shfl_xor_sync(~0u, most, 16));
-          by = query_factor(most, back);
+          if (q == 0) undo[(items & 1) * 2 * kBlock + t * kBlock + two * 16 + g * 8 + r8] = back;
         }
-        uint8_t* to = smem + L::q(t) + group * L::kGroup + r8 * 16 + q * kPieces * L::kChunk;
-#pragma unroll
-        for (int c = 0; c < kPieces; ++c) {
-          uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (BF16) w[i] = pack_half2(__uint_as_float(w[i] << 16) * by, __uint_as_float(w[i] & 0xFFFF0000u) * by);
-            w[i] ^= sign;
-          }
-          *reinterpret_cast<uint4*>(to + c * L::kChunk) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        if (q == 0) undo[(items & 1) * 2 * kBlock + in_tile] = back;
       }
       fence_smem();
       __syncwarp();
@@ -309,25 +330,36 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
 
 template <int D, bool BF16>
 __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
-                                              int64_t end, const float* undo, Bars* bars, uint32_t tmem) {
+                                              int64_t end, const float* undo, uint8_t* stage, Bars* bars, uint32_t tmem) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = warp >> 2, r = (warp & 3) * 32 + lane;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's tensor memory lanes
   const uint32_t S = tmem + lanes + 128 * t, O = tmem + lanes + 256 + 128 * t;
   volatile int* failed = &bars->failed;
   uint32_t s_phase = 0, o_phase = 0, items = 0;
+  // places, from a tile's first row, of this thread's row of the results and of the rows it stores
+  const int token = cut.token_of(t * kBlock + r);
+  const int own = token * a.q_heads + (t * kBlock + r - token * a.group);
+  int place_of[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int x = t * kBlock + (warp & 3) * 32 + 8 * i + (lane >> 2), j = cut.token_of(x);
+    place_of[i] = j * a.q_heads + (x - j * a.group);
+  }
   Walk walk(a, cut, prefix, place, end);
   Item it;
   for (; walk.next(a, cut, it); ++items) {
     if (t * kBlock >= it.rows) continue;  // this block has no rows
-    const int row = it.tile * cut.rows + t * kBlock + r;  // of the sequence
     const bool there = t * kBlock + r < it.rows;
-    const int j = row / a.group, h = it.head * a.group + row % a.group;
+    const int64_t first_row = (int64_t)(walk.s.begin + it.tile * cut.tokens) * a.q_heads + it.head * a.group;
     const float gk = a.c.k_scale ? a.c.k_scale[a.layer * a.c.H + it.head] : 1.f;
     const float scale = fabsf(a.scale_log2) * gk;
     float mul = 0.f;
     int lo = 0, hi = 0x7FFFFFFF;  // (a row that is not there sees all: its zeros are nobody's)
-    if (there) kv4_sight(a, walk.s, row, lo, hi);
+    if (there) {
+      hi = walk.s.length - walk.s.count + it.tile * cut.tokens + token;
+      lo = a.window && hi >= a.window ? hi - a.window + 1 : 0;
+    }
     const int most_lo = __reduce_max_sync(~0u, lo), least_hi = __reduce_min_sync(~0u, hi);
     float ref = kNone, sum = 0.f;
     bool ok = true;
@@ -415,39 +447,62 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     o_phase ^= 1;
     if (!ok) return;
     fence_after();
-    // ---- the row, or this range's part of it
+    // ---- the rows, or this range's part of them: 64 bytes of each at a time through the warp's stage, so
+    // that a store writes eight rows' 64 bytes and not 32 rows' 16 (which took 6000 cycles an item)
     const bool done = it.u0 == it.first && it.u1 == it.last;
     const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + it.head] : 1.f;
-    const int64_t at = (int64_t)(walk.s.begin + j) * a.q_heads + h;
     const float inv = sum == 0.f ? 0.f : gv / sum;
-    float* part = a.parts + ((int64_t)(2 * blockIdx.x + (it.u0 == it.first ? 1 : 0)) * cut.rows + t * kBlock + r) * kv4_part_floats(D);
+    uint8_t* mine = stage + warp * kStageBytes;
+    uint4* put = reinterpret_cast<uint4*>(mine + lane * kStagePitch);
+    const uint4* get = reinterpret_cast<const uint4*>(mine + (lane >> 2) * kStagePitch + (lane & 3) * 16);
+    float* parts = a.parts + (int64_t)(2 * blockIdx.x + (it.u0 == it.first ? 1 : 0)) * cut.rows * kv4_part_floats(D);
+    uint8_t* to[4];  // row 8 i + lane / 4 of the warp's
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = t * kBlock + (warp & 3) * 32 + 8 * i + (lane >> 2);
+      to[i] = done ? reinterpret_cast<uint8_t*>(a.out + (first_row + place_of[i]) * D) : reinterpret_cast<uint8_t*>(parts + x * kv4_part_floats(D));
+      to[i] = x < it.rows ? to[i] + (lane & 3) * 16 : nullptr;
+    }
+    auto flush = [&](int piece) {  // the stage's rows to byte `piece` of theirs
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4 w = get[i * (8 * kStagePitch / 16)];
+        if (to[i]) *reinterpret_cast<uint4*>(to[i] + piece) = w;
+      }
+      __syncwarp();
+    };
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
       uint32_t v[32];
       tmem_load(O + 32 * c, v);
       tmem_wait(v);
-      if (!there) continue;
       if (done) {
-        uint4* to = reinterpret_cast<uint4*>(a.out + at * D + 32 * c);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t w[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x)
             w[x] = pack_out<BF16>(__uint_as_float(v[8 * i + 2 * x]) * inv, __uint_as_float(v[8 * i + 2 * x + 1]) * inv);
-          to[i] = make_uint4(w[0], w[1], w[2], w[3]);
+          put[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
+        flush(64 * c);
       } else {
-        uint4* to = reinterpret_cast<uint4*>(part + 32 * c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) to[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            put[i] = make_uint4(v[16 * half + 4 * i], v[16 * half + 4 * i + 1], v[16 * half + 4 * i + 2], v[16 * half + 4 * i + 3]);
+          flush(128 * c + 64 * half);
+        }
       }
     }
     if (there) {
       if (done) {
-        if (a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+        if (a.lse)
+          a.lse[first_row + own] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
       } else {
-        *reinterpret_cast<float2*>(part + D) = make_float2(ref, sum);
+        *reinterpret_cast<float2*>(parts + (t * kBlock + r) * kv4_part_floats(D) + D) = make_float2(ref, sum);
       }
     }
     fence_before();
@@ -687,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
     // 176 + 176 + 88 + 72 = 4 * 128, the registers of the launch
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-      softmax_warps<D, BF16>(a, cut, prefix, place, end, undo, bars, tmem);
+      softmax_warps<D, BF16>(a, cut, prefix, place, end, undo, smem + L::stage(), bars, tmem);
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
       code_warps<D>(a, cut, prefix, place, end, smem, bars);
@@ -708,58 +763,74 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   }
 }
 
-// Joins the parts of the tiles that several CTAs share (a warp for a row; a tile has two or three
-// parts) and fills the rows that see nothing.
+// Joins the parts of the tiles that several CTAs share: CTA x takes the tile that range x begins and
+// does not end, a warp for a row.  CTAs behind those fill the rows that see nothing, one for each
+// sequence.
 constexpr int kJoinThreads = 256;
-constexpr int kJoinSplit = 4;  // CTAs of a tile
+constexpr int kJoinSplit = 8;  // CTAs of a tile
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kJoinThreads) kv4_chunk_join_kernel(Kv4Attend a, Kv4ManyCut cut, int most) {
   pdl_wait();
   pdl_trigger();
-  const int i = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t W = a.prefix[a.b.n], p0 = a.prefix[i];
-  const Kv4Seq s = cut.seq(a, i, false);
-  const int workers = kv4_workers(W, cut.least, most);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, x = blockIdx.x;
   constexpr int kDims = D / 32, kStep = kJoinSplit * kJoinThreads / 32;
-  for (int y = blockIdx.y; y < s.tiles * a.c.H; y += gridDim.y) {
-    const int head = y / s.tiles, tile = y - head * s.tiles;
-    int w0 = 0, parts = 0;
-    int64_t first, last;
-    if (cut.ends(a, s, head, tile, first, last)) {
-      w0 = kv4_owner(W, p0 + first, workers);
-      parts = kv4_owner(W, p0 + last, workers) - w0 + 1;
-      if (parts == 1) continue;  // finished where it ran
-    }
-    const int rows = min(cut.rows, (s.count - tile * cut.tokens) * a.group);
-    const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
-    for (int col = blockIdx.z * (kJoinThreads / 32) + warp; col < rows; col += kStep) {
-      const int row = tile * cut.rows + col;
-      const int64_t at = (int64_t)(s.begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
-      float ref = kNone, total = 0.f, o[kDims] = {};
-      for (int p = 0; p < parts; ++p) {
-        // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
-        const float* part = a.parts + ((int64_t)(2 * (w0 + p) + (p == 0)) * cut.rows + col) * kv4_part_floats(D);
-        const float2 rs = *reinterpret_cast<const float2*>(part + D);
-        const float to = fmaxf(ref, rs.x), f = exp2_approx(ref - to), g = exp2_approx(rs.x - to);
-        ref = to;
-        total = total * f + rs.y * g;
+  const int row0 = blockIdx.y * (kJoinThreads / 32) + warp;
+  if (x >= most) {
+    const Kv4Seq s = cut.seq(a, x - most, false);
+    const int64_t hidden = s.length == 0 ? s.count : min((int64_t)s.count, (int64_t)s.hidden * cut.tokens);
+    for (int64_t y = row0; y < hidden * a.q_heads; y += kStep) {
+      const int64_t at = (int64_t)s.begin * a.q_heads + y;
 #pragma unroll
-        for (int d = 0; d < kDims; ++d) o[d] = o[d] * f + part[kDims * lane + d] * g;
-      }
-      const float inv = total == 0.f ? 0.f : gv / total;
-#pragma unroll
-      for (int d = 0; d < kDims; d += 2)
-        *reinterpret_cast<uint32_t*>(a.out + at * D + kDims * lane + d) = pack_out<BF16>(o[d] * inv, o[d + 1] * inv);
-      if (a.lse && lane == 0) a.lse[at] = total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
+      for (int d = 0; d < kDims; d += 2) *reinterpret_cast<uint32_t*>(a.out + at * D + kDims * lane + d) = 0;
+      if (a.lse && lane == 0) a.lse[at] = -INFINITY;
     }
+    return;
+  }
+  const int64_t W = a.prefix[a.b.n];
+  const int workers = kv4_workers(W, cut.least, most);
+  if (W == 0 || x + 1 >= workers) return;
+  const int64_t place = kv4_range_begin(W, x + 1, workers);
+  int lo = 0, hi = a.b.n - 1;  // the sequence that the next range begins in
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.prefix[mid] <= place) lo = mid; else hi = mid - 1;
+  }
+  const Kv4Seq s = cut.seq(a, lo, false);
+  const int64_t p0 = a.prefix[lo], head_length = cut.before(a, s, s.tiles);
+  const int head = (int)((place - p0) / head_length), tile = cut.find(a, s, place - p0 - head * head_length);
+  int64_t first, last;
+  if (!cut.ends(a, s, head, tile, first, last)) return;
+  const int parts = kv4_owner(W, p0 + last, workers) - x + 1;
+  if (kv4_owner(W, p0 + first, workers) != x || parts < 2) return;
+  const int rows = min(cut.rows, (s.count - tile * cut.tokens) * a.group);
+  const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
+  for (int col = row0; col < rows; col += kStep) {
+    const int row = tile * cut.rows + col;
+    const int64_t at = (int64_t)(s.begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
+    float ref = kNone, total = 0.f, o[kDims] = {};
+    for (int p = 0; p < parts; ++p) {
+      // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
+      const float* part = a.parts + ((int64_t)(2 * (x + p) + (p == 0)) * cut.rows + col) * kv4_part_floats(D);
+      const float2 rs = *reinterpret_cast<const float2*>(part + D);
+      const float to = fmaxf(ref, rs.x), f = exp2_approx(ref - to), g = exp2_approx(rs.x - to);
+      ref = to;
+      total = total * f + rs.y * g;
+#pragma unroll
+      for (int d = 0; d < kDims; ++d) o[d] = o[d] * f + part[kDims * lane + d] * g;
+    }
+    const float inv = total == 0.f ? 0.f : gv / total;
+#pragma unroll
+    for (int d = 0; d < kDims; d += 2)
+      *reinterpret_cast<uint32_t*>(a.out + at * D + kDims * lane + d) = pack_out<BF16>(o[d] * inv, o[d + 1] * inv);
+    if (a.lse && lane == 0) a.lse[at] = total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
   }
 }
 
 // Tiles of whole tokens, as many as two blocks hold.
 Kv4ManyCut many_cut(int group) {
   const int tokens = 2 * kBlock / group;
-  return Kv4ManyCut{tokens * group, tokens, kUnit, 2 * kUnit, 2 * kUnit};
+  return Kv4ManyCut{tokens * group, tokens, kUnit, 2 * kUnit, 2 * kUnit, ((1ull << 32) + group - 1) / group};
 }
 
 template <int D, bool BF16>
@@ -789,11 +860,9 @@ cudaError_t launch_kv4_many(const Kv4Attend& a, int dtype, int sms, cudaStream_t
       a.c.D == 128 ? (bf ? launch_chunk<128, true>(a, cut, sms, stream) : launch_chunk<128, false>(a, cut, sms, stream))
                    : (bf ? launch_chunk<64, true>(a, cut, sms, stream) : launch_chunk<64, false>(a, cut, sms, stream));
   if (e != cudaSuccess) return e;
-  const int64_t items = ((int64_t)a.b.max_count + cut.tokens - 1) / cut.tokens * a.c.H;
   auto join = a.c.D == 128 ? (bf ? kv4_chunk_join_kernel<128, true> : kv4_chunk_join_kernel<128, false>)
                            : (bf ? kv4_chunk_join_kernel<64, true> : kv4_chunk_join_kernel<64, false>);
-  return launch_pdl(join, dim3(a.b.n, (unsigned)(items < 1024 ? items : 1024), kJoinSplit), dim3(kJoinThreads), 0, stream, a, cut,
-                    sms);
+  return launch_pdl(join, dim3(sms + a.b.n, kJoinSplit), dim3(kJoinThreads), 0, stream, a, cut, sms);
 }
 
 }  // namespace semkv
