@@ -155,6 +155,7 @@ __device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
   return d;
 }
 
+constexpr int kWalkBytes = 128;
 constexpr int kStagePitch = 80, kStageBytes = 32 * kStagePitch;  // a softmax warp's stage of results
 
 template <int D>
@@ -170,7 +171,8 @@ struct Layout {
   static constexpr int undo() { return prefix() + (kThreads + 2) * 8; }
   static constexpr int sums() { return undo() + 4 * kBlock * 4; }
   static constexpr int bars() { return sums() + 16 * 8; }
-  static constexpr int bytes() { return bars() + 24 * 8 + 16; }
+  static constexpr int walks() { return bars() + 24 * 8 + 16; }
+  static constexpr int bytes() { return walks() + kThreads / 32 * kWalkBytes; }
 };
 
 // The barriers, and the two words behind them.
@@ -183,62 +185,91 @@ static_assert(sizeof(Bars) <= 24 * 8 + 16, "room for the barriers");
 
 // An item and this CTA's part of it.
 struct Item {
-  int head, tile, rows;  // rows: of this tile
-  int u0, u1;            // units of this part
-  int first, last;       // units of the item
+  int seq, begin, count, length;  // its sequence (Kv4Seq)
+  int head, tile, rows;           // rows: of this tile
+  int u0, u1;                     // units of this part
+  int first, last;                // units of the item
 };
 
-// A walk over the CTA's range: found once, then from item to item.
+// A walk over the CTA's range: found once, then from item to item.  Each warp has its own, in shared
+// memory: its fields are wanted between items only, and the softmax warps have no registers to spare.
 struct Walk {
   Kv4Seq s;
   int i, head, tile;
   int off;       // places of the item that are behind the walk
   int64_t left;  // places of the range before it
+  Item it;
 
-  __device__ __forceinline__ Walk(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place, int64_t end) {
+  __device__ __forceinline__ void start(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
+                                        int64_t end) {
     int64_t at;
-    s = kv4_find<kThreads>(a, cut, prefix, place, at, i);
-    const int64_t head_length = cut.before(a, s, s.tiles);
-    head = (int)((place - at) / head_length);
-    const int64_t in_head = place - at - head * head_length;
-    tile = cut.find(a, s, in_head);
-    off = (int)(in_head - cut.before(a, s, tile));
-    left = end - place;
+    int which;
+    const Kv4Seq q = kv4_find<kThreads>(a, cut, prefix, place, at, which);
+    const int64_t head_length = cut.before(a, q, q.tiles);
+    const int h = (int)((place - at) / head_length);
+    const int64_t in_head = place - at - h * head_length;
+    const int t = cut.find(a, q, in_head);
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) {
+      s = q;
+      i = which;
+      head = h;
+      tile = t;
+      off = (int)(in_head - cut.before(a, q, t));
+      left = end - place;
+    }
+    __syncwarp();
   }
 
-  // The next item with units in the range; false at its end.  `s` stays the item's until the next call.
-  __device__ __forceinline__ bool next(const Kv4Attend& a, const Kv4ManyCut& cut, Item& it) {
-    while (left > 0) {
-      if (tile == s.tiles) {
-        tile = 0;
-        if (++head == a.c.H) {
-          head = 0;
+  // The next item with units in the range, into `it`; false at the range's end.
+  __device__ __forceinline__ bool next(const Kv4Attend& a, const Kv4ManyCut& cut) {
+    Kv4Seq q = s;
+    int which = i, h = head, t = tile, o = off;
+    int64_t more = left;
+    Item x;
+    bool found = false;
+    while (more > 0 && !found) {
+      if (t == q.tiles) {
+        t = 0;
+        if (++h == a.c.H) {
+          h = 0;
           do {
-            if (++i >= a.b.n) return false;
-            s = cut.seq(a, i, false);
-          } while (s.tiles == 0);
+            if (++which >= a.b.n) return false;
+            q = cut.seq(a, which, false);
+          } while (q.tiles == 0);
         }
       }
-      const int length = cut.length(a, s, tile), take = left < length - off ? (int)left : length - off;
+      const int length = cut.length(a, q, t), take = more < length - o ? (int)more : length - o;
       int from;
-      cut.units(a, s, tile, it.first, it.last, from);
-      // the unit whose place (that of its first token) is the first at or behind o
-      auto unit_at = [&](int o) {
-        return o <= cut.start ? it.first : min(it.last, (from + o - cut.start + kUnit - 1) / kUnit);
+      cut.units(a, q, t, x.first, x.last, from);
+      // the unit whose place (that of its first token) is the first at or behind p
+      auto unit_at = [&](int p) {
+        return p <= cut.start ? x.first : min(x.last, (from + p - cut.start + kUnit - 1) / kUnit);
       };
-      it.u0 = unit_at(off);
-      it.u1 = off + take >= length ? it.last : unit_at(off + take);
-      it.head = head;
-      it.tile = tile;
-      it.rows = min(cut.rows, (s.count - tile * cut.tokens) * a.group);
-      ++tile;
-      off = 0;
-      left -= take;
-      if (take > 0 && it.u1 > it.u0) return true;
+      x.u0 = unit_at(o);
+      x.u1 = o + take >= length ? x.last : unit_at(o + take);
+      x.head = h;
+      x.tile = t;
+      x.rows = min(cut.rows, (q.count - t * cut.tokens) * a.group);
+      ++t;
+      o = 0;
+      more -= take;
+      found = take > 0 && x.u1 > x.u0;
     }
-    return false;
+    x.seq = q.seq, x.begin = q.begin, x.count = q.count, x.length = q.length;
+    __syncwarp();  // the lanes have read the fields
+    if ((threadIdx.x & 31) == 0) {
+      s = q;
+      i = which, head = h, tile = t, off = o;
+      left = more;
+      it = x;
+    }
+    __syncwarp();
+    return found;
   }
 };
+
+static_assert(sizeof(Walk) <= kWalkBytes, "room for the walks");
 
 // ------------------------------------------------------------- queries ------
 
@@ -246,8 +277,7 @@ struct Walk {
 // row l % 8.  Two sets of factors, by the item's parity: the softmax of one item may still want
 // its own while the next one's rows are put in place.
 template <int D, bool BF16>
-__device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
-                                            int64_t end, uint8_t* smem, Bars* bars, float* undo) {
+__device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, uint8_t* smem, Bars* bars, float* undo) {
   using L = Layout<D>;
   constexpr int kPieces = D / 32;  // 16-byte pieces of a quarter
   const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 13;
@@ -255,10 +285,9 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
   const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // a negative scale goes into Q's signs: the largest
   volatile int* failed = &bars->failed;                            // logit is S's largest
   uint32_t n[2] = {0, 0}, items = 0;
-  Walk walk(a, cut, prefix, place, end);
-  Item it;
-  for (; walk.next(a, cut, it); ++items) {
-    const uint16_t* base = a.q + (int64_t)(walk.s.begin + it.tile * cut.tokens) * a.q_stride + it.head * a.group * D;
+  const Item& it = walk.it;
+  for (; walk.next(a, cut); ++items) {
+    const uint16_t* base = a.q + (int64_t)(it.begin + it.tile * cut.tokens) * a.q_stride + it.head * a.group * D;
     // the rows come nearer while those before them are still wanted
     for (int x = warp * 32 + lane; x < it.rows * (D / 64); x += 96) {
       const int in_tile = x / (D / 64), j = cut.token_of(in_tile);
@@ -329,71 +358,58 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
 // ------------------------------------------------------------- softmax ------
 
 template <int D, bool BF16>
-__device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
-                                              int64_t end, const float* undo, uint8_t* stage, Bars* bars, uint32_t tmem) {
+__device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, const float* undo, uint8_t* stage, Bars* bars, uint32_t tmem) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = warp >> 2, r = (warp & 3) * 32 + lane;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's tensor memory lanes
   const uint32_t S = tmem + lanes + 128 * t, O = tmem + lanes + 256 + 128 * t;
   volatile int* failed = &bars->failed;
   uint32_t s_phase = 0, o_phase = 0, items = 0;
-  // places, from a tile's first row, of this thread's row of the results and of the rows it stores
-  const int token = cut.token_of(t * kBlock + r);
-  const int own = token * a.q_heads + (t * kBlock + r - token * a.group);
-  int place_of[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int x = t * kBlock + (warp & 3) * 32 + 8 * i + (lane >> 2), j = cut.token_of(x);
-    place_of[i] = j * a.q_heads + (x - j * a.group);
-  }
-  Walk walk(a, cut, prefix, place, end);
-  Item it;
-  for (; walk.next(a, cut, it); ++items) {
+  const Item& it = walk.it;
+  for (; walk.next(a, cut); ++items) {
     if (t * kBlock >= it.rows) continue;  // this block has no rows
     const bool there = t * kBlock + r < it.rows;
-    const int64_t first_row = (int64_t)(walk.s.begin + it.tile * cut.tokens) * a.q_heads + it.head * a.group;
     const float gk = a.c.k_scale ? a.c.k_scale[a.layer * a.c.H + it.head] : 1.f;
     const float scale = fabsf(a.scale_log2) * gk;
     float mul = 0.f;
     int lo = 0, hi = 0x7FFFFFFF;  // (a row that is not there sees all: its zeros are nobody's)
     if (there) {
-      hi = walk.s.length - walk.s.count + it.tile * cut.tokens + token;
+      hi = it.length - it.count + it.tile * cut.tokens + cut.token_of(t * kBlock + r);
       lo = a.window && hi >= a.window ? hi - a.window + 1 : 0;
     }
     const int most_lo = __reduce_max_sync(~0u, lo), least_hi = __reduce_min_sync(~0u, hi);
     float ref = kNone, sum = 0.f;
     bool ok = true;
-    for (int u = it.u0; u < it.u1; ++u) {
+    const int u0 = it.u0, u1 = it.u1;
+    for (int u = u0; u < u1; ++u) {
       ok = wait(&bars->s_full[t], s_phase, failed);
       s_phase ^= 1;
       if (!ok) break;
       fence_after();
       // (S is there, so Q was; never 0: a masked logit stays -infinity)
-      if (u == it.u0) mul = fmaxf(scale * undo[(items & 1) * 2 * kBlock + t * kBlock + r], 0x1p-126f);
+      if (u == u0) mul = fmaxf(scale * undo[(items & 1) * 2 * kBlock + t * kBlock + r], 0x1p-126f);
       const int pos = u * kUnit;
       const bool open = pos >= most_lo && pos + kUnit - 1 <= least_hi;
       // ---- the largest logit
       uint32_t v[kUnit / 32][32];
+      float most[kUnit / 32];
+      tmem_load(S, v[0]);
 #pragma unroll
-      for (int c = 0; c < kUnit / 32; ++c) tmem_load(S + 32 * c, v[c]);
-#pragma unroll
-      for (int c = 0; c < kUnit / 32; ++c) tmem_wait(v[c]);
-      if (!open) {
-#pragma unroll
-        for (int c = 0; c < kUnit / 32; ++c)
+      for (int c = 0; c < kUnit / 32; ++c) {
+        tmem_wait(v[c]);
+        if (c + 1 < kUnit / 32) tmem_load(S + 32 * (c + 1), v[c + 1]);  // on its way behind this one's maximum
+        if (!open) {
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const int p = pos + 32 * c + i;
             if (p < lo || p > hi) v[c][i] = 0xFF800000u;
           }
-      }
-      float most[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        most[c] = -INFINITY;
+        }
+        float m[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int i = 0; i < 32; i += 2)
-          asm("max.f32 %0, %0, %1, %2;" : "+f"(most[c]) : "f"(__uint_as_float(v[c][i])), "f"(__uint_as_float(v[c][i + 1])));
+          asm("max.f32 %0, %0, %1, %2;" : "+f"(m[i >> 1 & 1]) : "f"(__uint_as_float(v[c][i])), "f"(__uint_as_float(v[c][i + 1])));
+        most[c] = fmaxf(m[0], m[1]);
       }
       const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * mul;
       const bool over = top > ref + kMost;
@@ -404,7 +420,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
           ref = top - kHead;
           sum *= f;
         }
-        if (u > it.u0) {
+        if (u > u0) {
 #pragma unroll 1
           for (int c = 0; c < D / 16; ++c) {
             uint32_t o[16];
@@ -456,11 +472,13 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     uint4* put = reinterpret_cast<uint4*>(mine + lane * kStagePitch);
     const uint4* get = reinterpret_cast<const uint4*>(mine + (lane >> 2) * kStagePitch + (lane & 3) * 16);
     float* parts = a.parts + (int64_t)(2 * blockIdx.x + (it.u0 == it.first ? 1 : 0)) * cut.rows * kv4_part_floats(D);
+    const int64_t first_row = (int64_t)(it.begin + it.tile * cut.tokens) * a.q_heads + it.head * a.group;
     uint8_t* to[4];  // row 8 i + lane / 4 of the warp's
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int x = t * kBlock + (warp & 3) * 32 + 8 * i + (lane >> 2);
-      to[i] = done ? reinterpret_cast<uint8_t*>(a.out + (first_row + place_of[i]) * D) : reinterpret_cast<uint8_t*>(parts + x * kv4_part_floats(D));
+      const int x = t * kBlock + (warp & 3) * 32 + 8 * i + (lane >> 2), j = cut.token_of(x);
+      to[i] = done ? reinterpret_cast<uint8_t*>(a.out + (first_row + j * a.q_heads + (x - j * a.group)) * D)
+                   : reinterpret_cast<uint8_t*>(parts + x * kv4_part_floats(D));
       to[i] = x < it.rows ? to[i] + (lane & 3) * 16 : nullptr;
     }
     auto flush = [&](int piece) {  // the stage's rows to byte `piece` of theirs
@@ -472,18 +490,20 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       }
       __syncwarp();
     };
-#pragma unroll 1
+    uint32_t v[D / 32][32];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) tmem_load(O + 32 * c, v[c]);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) tmem_wait(v[c]);
+#pragma unroll
     for (int c = 0; c < D / 32; ++c) {
-      uint32_t v[32];
-      tmem_load(O + 32 * c, v);
-      tmem_wait(v);
       if (done) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t w[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            w[x] = pack_out<BF16>(__uint_as_float(v[8 * i + 2 * x]) * inv, __uint_as_float(v[8 * i + 2 * x + 1]) * inv);
+            w[x] = pack_out<BF16>(__uint_as_float(v[c][8 * i + 2 * x]) * inv, __uint_as_float(v[c][8 * i + 2 * x + 1]) * inv);
           put[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
         flush(64 * c);
@@ -492,7 +512,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
         for (int half = 0; half < 2; ++half) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            put[i] = make_uint4(v[16 * half + 4 * i], v[16 * half + 4 * i + 1], v[16 * half + 4 * i + 2], v[16 * half + 4 * i + 3]);
+            put[i] = make_uint4(v[c][16 * half + 4 * i], v[c][16 * half + 4 * i + 1], v[c][16 * half + 4 * i + 2], v[c][16 * half + 4 * i + 3]);
           flush(128 * c + 64 * half);
         }
       }
@@ -500,7 +520,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     if (there) {
       if (done) {
         if (a.lse)
-          a.lse[first_row + own] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+          a.lse[first_row + cut.token_of(t * kBlock + r) * (a.q_heads - a.group) + t * kBlock + r] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
       } else {
         *reinterpret_cast<float2*>(parts + (t * kBlock + r) * kv4_part_floats(D) + D) = make_float2(ref, sum);
       }
@@ -553,8 +573,7 @@ __device__ __forceinline__ void store_values(const Codes<D>& x, uint8_t* to) {
 }
 
 template <int D>
-__device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
-                                           int64_t end, uint8_t* smem, Bars* bars) {
+__device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, uint8_t* smem, Bars* bars) {
   using L = Layout<D>;
   const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 8;
   const int r8 = lane & 7, q = lane >> 3;
@@ -564,12 +583,11 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
   const int at_codes = q * (D / 8), at_scale = 16 * D + q * (D / 64);
   uint8_t* to = smem + (row >> 3) * L::kGroup + r8 * 16 + q * (D / 32) * L::kChunk;
   uint32_t n = 0;  // units so far
-  Walk walk(a, cut, prefix, place, end);
-  Item it;
-  while (walk.next(a, cut, it)) {
+  const Item& it = walk.it;
+  while (walk.next(a, cut)) {
     const uint8_t* base = a.c.pages + kv4_record(a.c, a.layer, 0, it.head);
     const int64_t page_stride = head_bytes * a.c.H;
-    const int32_t* table = a.c.table + (int64_t)walk.s.seq * a.c.max_pages;
+    const int32_t* table = a.c.table + (int64_t)it.seq * a.c.max_pages;
     // the pages of the warp's two tiles of a unit
     int page[2];
     auto find_pages = [&](int u) {
@@ -577,7 +595,7 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
       for (int x = 0; x < 2; ++x) {
         const int token = u * kUnit + warp * 32 + 16 * x;
         page[x] = 0;
-        if (u < it.u1 && token < walk.s.length) {
+        if (u < it.u1 && token < it.length) {
           page[x] = table[token >> a.c.page_shift];
           if ((unsigned)page[x] >= (unsigned)a.c.num_pages) {
             raise_error(a.c.err, kDevIndex);
@@ -597,7 +615,7 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
         const int token = u * kUnit + row + 8 * i, in_tile = token & 15;
         const uint8_t* tile = tile_at(u, i);
         load_codes<D>(x[i], tile + (is_v ? 8 * D : 0) + in_tile * (D / 2) + at_codes,
-                      tile + (is_v ? D : 0) + at_scale + in_tile * (D / 16), token < walk.s.length);
+                      tile + (is_v ? D : 0) + at_scale + in_tile * (D / 16), token < it.length);
       }
     };
     find_pages(it.u0);
@@ -634,8 +652,7 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
 // ------------------------------------------------------------ products ------
 
 template <int D>
-__device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
-                                             int64_t end, uint8_t* smem, Bars* bars, uint32_t tmem) {
+__device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, uint8_t* smem, Bars* bars, uint32_t tmem) {
   using L = Layout<D>;
   volatile int* failed = &bars->failed;
   const uint32_t at = smem_addr(smem);
@@ -653,9 +670,8 @@ __device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCu
     commit(leader, &bars->s_full[t]);
   };
   uint32_t n = 0, q_phase = 0, p_phase = 0;  // units so far; a bit for each block
-  Walk walk(a, cut, prefix, place, end);
-  Item it;
-  while (walk.next(a, cut, it)) {
+  const Item& it = walk.it;
+  while (walk.next(a, cut)) {
     const int blocks = it.rows > kBlock ? 2 : 1, units = it.u1 - it.u0;
     for (int t = 0; t < blocks; ++t) {
       if (!wait(&bars->q_full[t], q_phase >> t & 1, failed)) return;
@@ -738,20 +754,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   const int64_t W = prefix[kThreads];
   const int workers = kv4_workers(W, cut.least, gridDim.x);
   if (W > 0 && (int)blockIdx.x < workers) {
-    const int64_t place = kv4_range_begin(W, blockIdx.x, workers), end = kv4_range_begin(W, blockIdx.x + 1, workers);
+    Walk& walk = reinterpret_cast<Walk*>(smem + L::walks())[warp];
+    walk.start(a, cut, prefix, kv4_range_begin(W, blockIdx.x, workers), kv4_range_begin(W, blockIdx.x + 1, workers));
     // 176 + 176 + 88 + 72 = 4 * 128, the registers of the launch
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-      softmax_warps<D, BF16>(a, cut, prefix, place, end, undo, smem + L::stage(), bars, tmem);
+      softmax_warps<D, BF16>(a, cut, walk, undo, smem + L::stage(), bars, tmem);
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-      code_warps<D>(a, cut, prefix, place, end, smem, bars);
+      code_warps<D>(a, cut, walk, smem, bars);
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
       if (warp == 12)
-        product_warp<D>(a, cut, prefix, place, end, smem, bars, tmem);
+        product_warp<D>(a, cut, walk, smem, bars, tmem);
       else
-        query_warps<D, BF16>(a, cut, prefix, place, end, smem, bars, undo);
+        query_warps<D, BF16>(a, cut, walk, smem, bars, undo);
     }
   }
   fence_before();
