@@ -87,7 +87,8 @@ struct Kv4FewCut {
 // tokens * group); tile x sees the positions below e = p0 + (x + 1) tokens, p0 the first row's, and
 // of them the last `cap` (all, without a window), so lengths add up in closed form.
 struct Kv4ManyCut {
-  int rows, tokens, unit, start, least;
+  static constexpr int unit = 128, start = 448, least = 256;
+  int rows, tokens;
   uint64_t magic;  // 2^32 / group, rounded up: x / group = x * magic >> 32 for the rows x of a tile
   __device__ __forceinline__ int token_of(int x) const { return (int)((uint64_t)x * magic >> 32); }
   __device__ __forceinline__ Kv4Seq seq(const Kv4Attend& a, int i, bool report) const {

@@ -29,7 +29,7 @@
 namespace semkv {
 namespace {
 
-constexpr int kUnit = 128;
+constexpr int kUnit = Kv4ManyCut::unit;
 constexpr int kThreads = 16 * 32;
 constexpr int kBlock = 128;     // rows of a block
 
@@ -155,7 +155,7 @@ __device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
   return d;
 }
 
-constexpr int kWalkBytes = 128;
+constexpr int kWalkBytes = 384, kBarBytes = 32 * 8;
 constexpr int kStagePitch = 80, kStageBytes = 32 * kStagePitch;  // a softmax warp's stage of results
 
 template <int D>
@@ -171,17 +171,19 @@ struct Layout {
   static constexpr int undo() { return prefix() + (kThreads + 2) * 8; }
   static constexpr int sums() { return undo() + 4 * kBlock * 4; }
   static constexpr int bars() { return sums() + 16 * 8; }
-  static constexpr int walks() { return bars() + 24 * 8 + 16; }
-  static constexpr int bytes() { return walks() + kThreads / 32 * kWalkBytes; }
+  static constexpr int walk() { return bars() + kBarBytes; }
+  static constexpr int bytes() { return walk() + kWalkBytes; }
 };
+
+constexpr int kItems = 4;  // of the ring that hands items from warp to warp
 
 // The barriers, and the two words behind them.
 struct Bars {
-  uint64_t q_full[2], q_empty[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t i_full[kItems], i_empty[kItems], q_full[2], q_empty[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2];
   int failed;
   uint32_t tmem;
 };
-static_assert(sizeof(Bars) <= 24 * 8 + 16, "room for the barriers");
+static_assert(sizeof(Bars) <= kBarBytes, "room for the barriers");
 
 // An item and this CTA's part of it.
 struct Item {
@@ -191,14 +193,14 @@ struct Item {
   int first, last;                // units of the item
 };
 
-// A walk over the CTA's range: found once, then from item to item.  Each warp has its own, in shared
-// memory: its fields are wanted between items only, and the softmax warps have no registers to spare.
+// A walk over the CTA's range: found once, then from item to item.  One warp walks and hands the items
+// to the others through a ring in shared memory; an item without rows ends it.
 struct Walk {
   Kv4Seq s;
   int i, head, tile;
   int off;       // places of the item that are behind the walk
   int64_t left;  // places of the range before it
-  Item it;
+  Item items[kItems];
 
   __device__ __forceinline__ void start(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
                                         int64_t end) {
@@ -209,7 +211,6 @@ struct Walk {
     const int h = (int)((place - at) / head_length);
     const int64_t in_head = place - at - h * head_length;
     const int t = cut.find(a, q, in_head);
-    __syncwarp();
     if ((threadIdx.x & 31) == 0) {
       s = q;
       i = which;
@@ -221,12 +222,11 @@ struct Walk {
     __syncwarp();
   }
 
-  // The next item with units in the range, into `it`; false at the range's end.
-  __device__ __forceinline__ bool next(const Kv4Attend& a, const Kv4ManyCut& cut) {
+  // The next item with units in the range into x; without rows at the range's end.
+  __device__ __forceinline__ void next(const Kv4Attend& a, const Kv4ManyCut& cut, Item& x) {
     Kv4Seq q = s;
     int which = i, h = head, t = tile, o = off;
     int64_t more = left;
-    Item x;
     bool found = false;
     while (more > 0 && !found) {
       if (t == q.tiles) {
@@ -234,9 +234,10 @@ struct Walk {
         if (++h == a.c.H) {
           h = 0;
           do {
-            if (++which >= a.b.n) return false;
+            if (++which >= a.b.n) break;
             q = cut.seq(a, which, false);
           } while (q.tiles == 0);
+          if (which >= a.b.n) break;
         }
       }
       const int length = cut.length(a, q, t), take = more < length - o ? (int)more : length - o;
@@ -256,16 +257,34 @@ struct Walk {
       more -= take;
       found = take > 0 && x.u1 > x.u0;
     }
+    if (!found) x.rows = 0;
     x.seq = q.seq, x.begin = q.begin, x.count = q.count, x.length = q.length;
     __syncwarp();  // the lanes have read the fields
     if ((threadIdx.x & 31) == 0) {
       s = q;
       i = which, head = h, tile = t, off = o;
       left = more;
-      it = x;
     }
     __syncwarp();
-    return found;
+  }
+};
+
+// A warp's place in the ring of items.
+struct Feed {
+  Bars* bars;
+  const Item* items;
+  uint32_t n = 0;
+  // the next item; null at the end, or when a wait ran out
+  __device__ __forceinline__ const Item* next() {
+    const uint32_t slot = n % kItems;
+    if (!wait(&bars->i_full[slot], n / kItems & 1, &bars->failed)) return nullptr;
+    return items[slot].rows ? items + slot : nullptr;
+  }
+  // this warp wants nothing more of it
+  __device__ __forceinline__ void done() {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) arrive(&bars->i_empty[n % kItems]);
+    ++n;
   }
 };
 
@@ -284,9 +303,29 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
   const int r8 = lane & 7, q = lane >> 3;
   const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0u;  // a negative scale goes into Q's signs: the largest
   volatile int* failed = &bars->failed;                            // logit is S's largest
-  uint32_t n[2] = {0, 0}, items = 0;
-  const Item& it = walk.it;
-  for (; walk.next(a, cut); ++items) {
+  uint32_t n[2] = {0, 0}, published = 0;
+  bool ended = false;
+  // warp 2 walks, two items ahead of these warps' own
+  auto publish = [&] {
+    Item x;
+    walk.next(a, cut, x);
+    const uint32_t slot = published % kItems;
+    if (!wait(&bars->i_empty[slot], (published / kItems & 1) ^ 1, failed)) return;
+    if (lane == 0) {
+      walk.items[slot] = x;
+      arrive(&bars->i_full[slot]);
+    }
+    __syncwarp();
+    ++published;
+    ended = x.rows == 0;
+  };
+  if (warp == 2) {
+    publish();
+    if (!ended) publish();
+  }
+  Feed feed{bars, walk.items};
+  while (const Item* item = feed.next()) {
+    const Item& it = *item;
     const uint16_t* base = a.q + (int64_t)(it.begin + it.tile * cut.tokens) * a.q_stride + it.head * a.group * D;
     // the rows come nearer while those before them are still wanted
     for (int x = warp * 32 + lane; x < it.rows * (D / 64); x += 96) {
@@ -297,39 +336,46 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
     for (int t = 0; t < 2 && t * kBlock < it.rows; ++t) {
       if (!wait(&bars->q_empty[t], (n[t] & 1) ^ 1, failed)) return;
       ++n[t];
-      // two groups of eight rows on their way at a time
-      for (int two = warp; two < kBlock / 16; two += 3) {
-        uint4 x[2][kPieces];
+      // all rows on their way at once, straight to their places; a lane turns what it copied itself
+      uint8_t* to = smem + L::q(t) + warp * L::kGroup + r8 * 16 + q * kPieces * L::kChunk;
+#pragma unroll 2
+      for (int group = warp; group < kBlock / 8; group += 3) {
+        const int in_tile = t * kBlock + group * 8 + r8, j = cut.token_of(in_tile);
+        const uint32_t bytes = in_tile < it.rows ? 16 : 0;  // (0: the piece is filled with zeros)
+        const uint16_t* src = bytes ? base + (int64_t)j * a.q_stride + (in_tile - j * a.group) * D + q * (D / 4) : a.q;
+        const uint32_t dst = smem_addr(to + (group - warp) * L::kGroup);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const int in_tile = t * kBlock + two * 16 + g * 8 + r8, j = cut.token_of(in_tile);
-          const bool there = in_tile < it.rows;
-          const uint4* src = reinterpret_cast<const uint4*>(base + (int64_t)j * a.q_stride + (in_tile - j * a.group) * D + q * (D / 4));
+        for (int c = 0; c < kPieces; ++c)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + c * L::kChunk), "l"(src + 8 * c), "r"(bytes)
+                       : "memory");
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      if (BF16 || sign) {
+#pragma unroll 1
+        for (int group = warp; group < kBlock / 8; group += 3) {
+          uint4 x[kPieces];
+          uint4* at = reinterpret_cast<uint4*>(to + (group - warp) * L::kGroup);
 #pragma unroll
-          for (int c = 0; c < kPieces; ++c) x[g][c] = there ? src[c] : make_uint4(0, 0, 0, 0);
-        }
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
+          for (int c = 0; c < kPieces; ++c) x[c] = at[c * (L::kChunk / 16)];
           uint64_t by2 = 0;
-          float back = 1.f;
           if (BF16) {
             uint32_t m = 0;  // largest magnitudes, pairwise
 #pragma unroll
             for (int c = 0; c < kPieces; ++c) {
-              const uint32_t w[4] = {x[g][c].x, x[g][c].y, x[g][c].z, x[g][c].w};
+              const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
               for (int i = 0; i < 4; ++i) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i] & 0x7FFF7FFFu));
             }
-            float most = fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+            float most = fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u)), back;
             most = fmaxf(most, __shfl_xor_sync(~0u, most, 8));
             most = fmaxf(most, __shfl_xor_sync(~0u, most, 16));
             const float by = query_factor(most, back);
             by2 = sign ? pair(-by, -by) : pair(by, by);
+            if (q == 0) undo[(feed.n & 1) * 2 * kBlock + t * kBlock + group * 8 + r8] = back;
           }
-          uint8_t* to = smem + L::q(t) + (2 * two + g) * L::kGroup + r8 * 16 + q * kPieces * L::kChunk;
 #pragma unroll
           for (int c = 0; c < kPieces; ++c) {
-            uint32_t w[4] = {x[g][c].x, x[g][c].y, x[g][c].z, x[g][c].w};
+            uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               if (BF16) {
@@ -340,15 +386,16 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
                 w[i] ^= sign;
               }
             }
-            *reinterpret_cast<uint4*>(to + c * L::kChunk) = make_uint4(w[0], w[1], w[2], w[3]);
+            at[c * (L::kChunk / 16)] = make_uint4(w[0], w[1], w[2], w[3]);
           }
-          if (q == 0) undo[(items & 1) * 2 * kBlock + t * kBlock + two * 16 + g * 8 + r8] = back;
         }
       }
       fence_smem();
       __syncwarp();
       if (lane == 0) arrive(&bars->q_full[t]);
     }
+    if (warp == 2 && !ended) publish();
+    feed.done();
   }
   // the products have read the last rows (their barriers outlive the arrivals)
   for (int t = 0; t < 2; ++t)
@@ -364,12 +411,14 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's tensor memory lanes
   const uint32_t S = tmem + lanes + 128 * t, O = tmem + lanes + 256 + 128 * t;
   volatile int* failed = &bars->failed;
-  uint32_t s_phase = 0, o_phase = 0, items = 0;
-  const Item& it = walk.it;
-  for (; walk.next(a, cut); ++items) {
+  uint32_t s_phase = 0, o_phase = 0;
+  Feed feed{bars, walk.items};
+  for (; const Item* item = feed.next(); feed.done()) {
+    const Item& it = *item;
     if (t * kBlock >= it.rows) continue;  // this block has no rows
     const bool there = t * kBlock + r < it.rows;
     const float gk = a.c.k_scale ? a.c.k_scale[a.layer * a.c.H + it.head] : 1.f;
+    const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + it.head] : 1.f;
     const float scale = fabsf(a.scale_log2) * gk;
     float mul = 0.f;
     int lo = 0, hi = 0x7FFFFFFF;  // (a row that is not there sees all: its zeros are nobody's)
@@ -387,7 +436,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       if (!ok) break;
       fence_after();
       // (S is there, so Q was; never 0: a masked logit stays -infinity)
-      if (u == u0) mul = fmaxf(scale * undo[(items & 1) * 2 * kBlock + t * kBlock + r], 0x1p-126f);
+      if (u == u0) mul = fmaxf(BF16 ? scale * undo[(feed.n & 1) * 2 * kBlock + t * kBlock + r] : scale, 0x1p-126f);
       const int pos = u * kUnit;
       const bool open = pos >= most_lo && pos + kUnit - 1 <= least_hi;
       // ---- the largest logit
@@ -466,7 +515,6 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     // ---- the rows, or this range's part of them: 64 bytes of each at a time through the warp's stage, so
     // that a store writes eight rows' 64 bytes and not 32 rows' 16 (which took 6000 cycles an item)
     const bool done = it.u0 == it.first && it.u1 == it.last;
-    const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + it.head] : 1.f;
     const float inv = sum == 0.f ? 0.f : gv / sum;
     uint8_t* mine = stage + warp * kStageBytes;
     uint4* put = reinterpret_cast<uint4*>(mine + lane * kStagePitch);
@@ -582,67 +630,71 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
   const int64_t head_bytes = (int64_t)kv4_tile_bytes(D) << (a.c.page_shift - 4);
   const int at_codes = q * (D / 8), at_scale = 16 * D + q * (D / 64);
   uint8_t* to = smem + (row >> 3) * L::kGroup + r8 * 16 + q * (D / 32) * L::kChunk;
-  uint32_t n = 0;  // units so far
-  const Item& it = walk.it;
-  while (walk.next(a, cut)) {
-    const uint8_t* base = a.c.pages + kv4_record(a.c, a.layer, 0, it.head);
-    const int64_t page_stride = head_bytes * a.c.H;
-    const int32_t* table = a.c.table + (int64_t)it.seq * a.c.max_pages;
-    // the pages of the warp's two tiles of a unit
-    int page[2];
-    auto find_pages = [&](int u) {
+  const int64_t page_stride = head_bytes * a.c.H;
+  // the unit whose codes are loaded next, of the item [.., u1) with `length` tokens
+  const uint8_t* base = nullptr;
+  const int32_t* table = nullptr;
+  int u = 0, u1 = 0, length = 0;
+  int page[2];  // of the warp's two tiles of it
+  Feed feed{bars, walk.items};
+  // the next unit, this item's or the next one's, and its pages
+  auto step = [&] {
+    if (++u >= u1) {
+      const Item* it = feed.next();
+      if (!it) return false;
+      base = a.c.pages + kv4_record(a.c, a.layer, 0, it->head);
+      table = a.c.table + (int64_t)it->seq * a.c.max_pages;
+      u = it->u0, u1 = it->u1, length = it->length;
+      feed.done();
+    }
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int token = u * kUnit + warp * 32 + 16 * x;
-        page[x] = 0;
-        if (u < it.u1 && token < it.length) {
-          page[x] = table[token >> a.c.page_shift];
-          if ((unsigned)page[x] >= (unsigned)a.c.num_pages) {
-            raise_error(a.c.err, kDevIndex);
-            page[x] = 0;
-          }
+    for (int x = 0; x < 2; ++x) {
+      const int token = u * kUnit + warp * 32 + 16 * x;
+      page[x] = 0;
+      if (token < length) {
+        page[x] = table[token >> a.c.page_shift];
+        if ((unsigned)page[x] >= (unsigned)a.c.num_pages) {
+          raise_error(a.c.err, kDevIndex);
+          page[x] = 0;
         }
       }
-    };
-    Codes<D> k[4], v[4];
-    auto tile_at = [&](int u, int i) {  // the tile of the lane's i-th row
-      const int token = u * kUnit + warp * 32 + 8 * i;
-      return base + page[i >> 1] * page_stride + (int64_t)((token & (a.c.P - 1)) >> 4) * kv4_tile_bytes(D);
-    };
-    auto load = [&](int u, Codes<D>(&x)[4], bool is_v) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int token = u * kUnit + row + 8 * i, in_tile = token & 15;
-        const uint8_t* tile = tile_at(u, i);
-        load_codes<D>(x[i], tile + (is_v ? 8 * D : 0) + in_tile * (D / 2) + at_codes,
-                      tile + (is_v ? D : 0) + at_scale + in_tile * (D / 16), token < it.length);
-      }
-    };
-    find_pages(it.u0);
-    load(it.u0, k, false);
-    load(it.u0, v, true);
-    find_pages(it.u0 + 1);
-    for (int u = it.u0; u < it.u1; ++u, ++n) {
-      const int b = n & 1;
-      const uint32_t free_phase = (n >> 1 & 1) ^ 1;
-      if (!wait(&bars->k_empty[b], free_phase, failed)) return;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) store_values<D>(k[i], to + L::k(b) + i * L::kGroup);
-      fence_smem();
-      __syncwarp();
-      if (lane == 0) arrive(&bars->k_full[b]);
-      if (u + 1 < it.u1) load(u + 1, k, false);
-      if (!wait(&bars->v_empty[b], free_phase, failed)) return;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) store_values<D>(v[i], to + L::v(b) + i * L::kGroup);
-      fence_smem();
-      __syncwarp();
-      if (lane == 0) arrive(&bars->v_full[b]);
-      if (u + 1 < it.u1) {
-        load(u + 1, v, true);
-        find_pages(u + 2);
-      }
     }
+    return true;
+  };
+  auto load = [&](Codes<D>(&x)[4], bool is_v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int token = u * kUnit + row + 8 * i, in_tile = token & 15;
+      const uint8_t* tile = base + page[i >> 1] * page_stride + (int64_t)((token & (a.c.P - 1)) >> 4) * kv4_tile_bytes(D);
+      load_codes<D>(x[i], tile + (is_v ? 8 * D : 0) + in_tile * (D / 2) + at_codes,
+                    tile + (is_v ? D : 0) + at_scale + in_tile * (D / 16), token < length);
+    }
+  };
+  Codes<D> k[4], v[4];
+  uint32_t n = 0;  // units so far
+  bool more = step();
+  if (more) {
+    load(k, false);
+    load(v, true);
+  }
+  for (; more; ++n) {
+    more = step();  // the pages of the next unit are on their way behind this one's stores
+    const int b = n & 1;
+    const uint32_t free_phase = (n >> 1 & 1) ^ 1;
+    if (!wait(&bars->k_empty[b], free_phase, failed)) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) store_values<D>(k[i], to + L::k(b) + i * L::kGroup);
+    fence_smem();
+    __syncwarp();
+    if (lane == 0) arrive(&bars->k_full[b]);
+    if (more) load(k, false);
+    if (!wait(&bars->v_empty[b], free_phase, failed)) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) store_values<D>(v[i], to + L::v(b) + i * L::kGroup);
+    fence_smem();
+    __syncwarp();
+    if (lane == 0) arrive(&bars->v_full[b]);
+    if (more) load(v, true);
   }
   // the products have read the last buffers (their barriers outlive the arrivals)
   for (uint32_t m = n < 2 ? 0 : n - 2; m < n; ++m)
@@ -670,9 +722,10 @@ __device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCu
     commit(leader, &bars->s_full[t]);
   };
   uint32_t n = 0, q_phase = 0, p_phase = 0;  // units so far; a bit for each block
-  const Item& it = walk.it;
-  while (walk.next(a, cut)) {
-    const int blocks = it.rows > kBlock ? 2 : 1, units = it.u1 - it.u0;
+  Feed feed{bars, walk.items};
+  while (const Item* item = feed.next()) {
+    const int blocks = item->rows > kBlock ? 2 : 1, units = item->u1 - item->u0;
+    feed.done();
     for (int t = 0; t < blocks; ++t) {
       if (!wait(&bars->q_full[t], q_phase >> t & 1, failed)) return;
       q_phase ^= 1u << t;
@@ -726,6 +779,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
     auto init = [](uint64_t* bar, int count) {
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory");
     };
+    for (int x = 0; x < kItems; ++x) {
+      init(&bars->i_full[x], 1);
+      init(&bars->i_empty[x], kThreads / 32);
+    }
     for (int x = 0; x < 2; ++x) {
       init(&bars->q_full[x], 3);
       init(&bars->q_empty[x], 1);
@@ -754,8 +811,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   const int64_t W = prefix[kThreads];
   const int workers = kv4_workers(W, cut.least, gridDim.x);
   if (W > 0 && (int)blockIdx.x < workers) {
-    Walk& walk = reinterpret_cast<Walk*>(smem + L::walks())[warp];
-    walk.start(a, cut, prefix, kv4_range_begin(W, blockIdx.x, workers), kv4_range_begin(W, blockIdx.x + 1, workers));
+    Walk& walk = *reinterpret_cast<Walk*>(smem + L::walk());
+    if (warp == kThreads / 32 - 1)
+      walk.start(a, cut, prefix, kv4_range_begin(W, blockIdx.x, workers), kv4_range_begin(W, blockIdx.x + 1, workers));
     // 176 + 176 + 88 + 72 = 4 * 128, the registers of the launch
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
@@ -847,7 +905,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_chunk_join_kernel(Kv4Attend 
 // Tiles of whole tokens, as many as two blocks hold.
 Kv4ManyCut many_cut(int group) {
   const int tokens = 2 * kBlock / group;
-  return Kv4ManyCut{tokens * group, tokens, kUnit, 2 * kUnit, 2 * kUnit, ((1ull << 32) + group - 1) / group};
+  return Kv4ManyCut{tokens * group, tokens, ((1ull << 32) + group - 1) / group};
 }
 
 template <int D, bool BF16>
