@@ -291,7 +291,8 @@ def _here(*tensors):
     """The calls run on the current device, so what they take has to be there."""
     dev = torch.cuda.current_device() if _raw_device is None else _raw_device()
     for t in tensors:
-        _need(t.get_device() == dev, "tensors have to be on the current CUDA device")
+        if t.get_device() != dev:
+            raise ValueError("tensors have to be on the current CUDA device")
 
 
 def _list(t, n, what):
@@ -303,14 +304,20 @@ def _list(t, n, what):
 
 
 def _rows(t, what, total, heads, head_dim):
-    """Rows [total][heads][head_dim] of a 16-bit type with any stride between rows; the stride."""
-    _need(t.dtype in _KV4_TYPES, f"{what} is float16 or bfloat16")
-    _need(t.dim() == 3 and t.shape[0] == total and t.shape[2] == head_dim
-          and (heads is None or t.shape[1] == heads), f"{what} has the wrong shape {tuple(t.shape)}")
+    """Rows [total][heads][head_dim] with any stride between rows: the stride."""
     st = t.stride()
-    _need(st[2] == 1 and (st[1] == head_dim or t.shape[1] == 1),
-          f"{what}: the heads of a row lie side by side")
-    return st[0] if total > 1 else t.shape[1] * head_dim
+    if t.shape != (total, heads, head_dim) or st[2] != 1 or (st[1] != head_dim and heads > 1):
+        raise ValueError(f"{what} is [{total}][{heads}][{head_dim}] with the heads of a row side by "
+                         f"side: got {tuple(t.shape)}, strides {st}")
+    return st[0] if total > 1 else heads * head_dim
+
+
+def _type16(t, other, what):
+    dtype = t.dtype
+    kind = _KV4_TYPES.get(dtype)
+    if kind is None or other.dtype != dtype:
+        raise ValueError(f"{what} have one type, float16 or bfloat16")
+    return kind
 
 
 def semkv_kv4_tile_bytes(head_dim: int) -> int:
@@ -321,50 +328,52 @@ def semkv_kv4_reserve(cache: "KV4Cache", batch: "KV4Batch", ws: torch.Tensor, st
     """Room for the batch's rows: pages, lengths, and batch.start."""
     _here(cache.pages, batch.start, ws)
     _check("semkv_kv4_reserve",
-           LIB.semkv_kv4_reserve(cache.ref, batch.ref, _ptr(ws), ws.numel() * ws.element_size(),
-                                 _stream(stream)))
+           LIB.semkv_kv4_reserve(cache.ref, batch.ref, _ptr(ws), ws.nbytes, _stream(stream)))
 
 
 def semkv_kv4_write(cache: "KV4Cache", batch: "KV4Batch", layer: int, k: torch.Tensor,
                     v: torch.Tensor, stream=None):
     """Quantize rows k, v [total][kv_heads][head_dim] (any row stride) into the layer's pages."""
-    s = cache.s
-    _need(k.dtype == v.dtype, "k and v have one type")
-    ks = _rows(k, "k", batch.s.total, s.kv_heads, s.head_dim)
-    vs = _rows(v, "v", batch.s.total, s.kv_heads, s.head_dim)
+    total, heads, head_dim = batch.total, cache.kv_heads, cache.head_dim
+    kind = _type16(k, v, "k and v")
+    ks = _rows(k, "k", total, heads, head_dim)
+    vs = _rows(v, "v", total, heads, head_dim)
     _here(cache.pages, batch.start, k, v)
     _check("semkv_kv4_write",
-           LIB.semkv_kv4_write(cache.ref, batch.ref, layer, _KV4_TYPES[k.dtype], k.data_ptr(), ks,
-                               v.data_ptr(), vs, _stream(stream)))
+           LIB.semkv_kv4_write(cache.ref, batch.ref, layer, kind, k.data_ptr(), ks, v.data_ptr(), vs,
+                               _stream(stream)))
 
 
 def semkv_kv4_read(cache: "KV4Cache", batch: "KV4Batch", layer: int, k_out: torch.Tensor,
                    v_out: torch.Tensor, stream=None):
     """The values of the batch's rows into k_out, v_out [total][kv_heads][head_dim]."""
-    s = cache.s
-    _need(k_out.dtype == v_out.dtype, "k_out and v_out have one type")
-    _rows(k_out, "k_out", batch.s.total, s.kv_heads, s.head_dim)
-    _rows(v_out, "v_out", batch.s.total, s.kv_heads, s.head_dim)
+    total, heads, head_dim = batch.total, cache.kv_heads, cache.head_dim
+    kind = _type16(k_out, v_out, "k_out and v_out")
+    _rows(k_out, "k_out", total, heads, head_dim)
+    _rows(v_out, "v_out", total, heads, head_dim)
     _here(cache.pages, batch.start, k_out, v_out)
     _check("semkv_kv4_read",
-           LIB.semkv_kv4_read(cache.ref, batch.ref, layer, _KV4_TYPES[k_out.dtype], _ptr(k_out),
-                              _ptr(v_out), _stream(stream)))
+           LIB.semkv_kv4_read(cache.ref, batch.ref, layer, kind, _ptr(k_out), _ptr(v_out),
+                              _stream(stream)))
 
 
 def semkv_kv4_attention(cache: "KV4Cache", batch: "KV4Batch", layer: int, q: torch.Tensor,
                         out: torch.Tensor, softmax_scale: float, ws: torch.Tensor, lse=None,
                         window: int = 0, stream=None):
     """Causal attention of the batch's rows q [total][q_heads][head_dim] over their sequences."""
-    qs = _rows(q, "q", batch.s.total, None, cache.s.head_dim)
-    _need(out.dtype == q.dtype and out.shape == q.shape, "out is as q")
+    kind = _type16(q, out, "q and out")
+    shape = q.shape
+    heads = shape[1]
+    qs = _rows(q, "q", batch.total, heads, cache.head_dim)
+    _need(out.shape == shape, "out is as q")
     if lse is not None:
-        _need(lse.dtype == torch.float32 and lse.shape == q.shape[:2], "lse is float32 [total][q_heads]")
+        _need(lse.dtype == torch.float32 and lse.shape == shape[:2], "lse is float32 [total][q_heads]")
         _here(lse)
     _here(cache.pages, q, out, ws)
     _check("semkv_kv4_attention",
-           LIB.semkv_kv4_attention(cache.ref, batch.ref, layer, _KV4_TYPES[q.dtype], q.data_ptr(), qs,
-                                   q.shape[1], _ptr(out), _ptr(lse), softmax_scale, window, _ptr(ws),
-                                   ws.numel() * ws.element_size(), _stream(stream)))
+           LIB.semkv_kv4_attention(cache.ref, batch.ref, layer, kind, q.data_ptr(), qs, heads,
+                                   _ptr(out), _ptr(lse), softmax_scale, window, _ptr(ws), ws.nbytes,
+                                   _stream(stream)))
 
 
 def semkv_kv4_fork(cache: "KV4Cache", src: torch.Tensor, dst: torch.Tensor, stream=None):
@@ -393,8 +402,7 @@ def semkv_kv4_compact(cache: "KV4Cache", seqs: torch.Tensor, keep: torch.Tensor,
     _here(cache.pages, keep, ws)
     _check("semkv_kv4_compact",
            LIB.semkv_kv4_compact(cache.ref, n, _list(seqs, n, "seqs").data_ptr(), _ptr(keep),
-                                 keep.shape[1], _ptr(ws), ws.numel() * ws.element_size(),
-                                 _stream(stream)))
+                                 keep.shape[1], _ptr(ws), ws.nbytes, _stream(stream)))
 
 
 # ------------------------------------------------------- owning wrappers ------
@@ -544,6 +552,7 @@ class KV4Cache:
                                 and t.shape == (layers, kv_heads)),
                   "the scales are contiguous float32 [layers][kv_heads]")
         self.pages, self.table, self.length, self.refs = pages, table, length, refs
+        self.kv_heads, self.head_dim = kv_heads, head_dim
         self.k_scale, self.v_scale = k_scale, v_scale
         self.dev_error = torch.zeros(1, dtype=torch.int32, device=pages.device)
         for t in (table, length, refs, k_scale, v_scale):
@@ -577,6 +586,7 @@ class KV4Batch:
         self.cu, self.seqs = _list(cu, n + 1, "cu"), _list(seqs, n, "seqs")
         self.start = (torch.zeros(n, dtype=torch.int32, device=device) if start is None
                       else _list(start, n, "start"))
-        self.s = KV4BatchStruct(n=n, total=n if total is None else total, max_count=max_count,
+        self.total = n if total is None else total
+        self.s = KV4BatchStruct(n=n, total=self.total, max_count=max_count,
                                 seqs=_ptr(self.seqs), cu=_ptr(self.cu), start=_ptr(self.start))
         self.ref = ctypes.byref(self.s)

@@ -137,10 +137,14 @@ def test_the_binding_refuses_tensors_that_do_not_fit(sk):
         sk.KV4Cache.over(c.pages, c.table, c.length, c.refs, 64, k_scale=torch.ones(2))
     assert sk.KV4Cache.over(c.pages, c.table, c.length, c.refs, 64, k_scale=torch.ones(1, 2)).s.page_tokens == 16
     x = torch.zeros((3, 2, 64), dtype=torch.float16)
-    for bad in (x.float(), x[:2], x[:, :1], x[..., :32], x.transpose(0, 1).contiguous().transpose(0, 1)):
+    for bad in (x[:2], x[:, :1], x[..., :32], x.transpose(0, 1).contiguous().transpose(0, 1)):
         with pytest.raises(ValueError):
             sk._rows(bad, "k", 3, 2, 64)
     assert sk._rows(x, "k", 3, 2, 64) == 128
+    for a, b in ((x.float(), x.float()), (x, x.bfloat16())):
+        with pytest.raises(ValueError):
+            sk._type16(a, b, "k and v")
+    assert sk._type16(x, x, "k") == 0 and sk._type16(x.bfloat16(), x.bfloat16(), "k") == 1
     wide = torch.zeros((3, 5, 64), dtype=torch.bfloat16)
     assert sk._rows(wide[:, 1:3], "k", 3, 2, 64) == 320
 
