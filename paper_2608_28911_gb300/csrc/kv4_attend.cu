@@ -122,12 +122,12 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
   }
   pdl_wait();
   pdl_trigger();
-  kv4_plan<kThreads>(a, cut, prefix, sums, blockIdx.x == 0);
+  kv4_plan<kThreads, false>(a, cut, prefix, sums, blockIdx.x == 0);
   const int64_t W = prefix[kThreads];
-  const int workers = kv4_workers(W, cut.least, gridDim.x * kWarps);
+  const Kv4Ranges ranges(W, cut.least, gridDim.x * kWarps);
   const int worker = warp * gridDim.x + blockIdx.x;  // few workers: spread over the SMs
-  if (W == 0 || worker >= workers) return;
-  const int64_t end = kv4_range_begin(W, worker + 1, workers);
+  if (W == 0 || worker >= ranges.count) return;
+  const int64_t end = ranges.begin(worker + 1);
 
   const int row_a = token_at(g), tok_v = token_at(2 * t);  // K row of lane group g; V's first token
   const int64_t head_bytes = (int64_t)L::kTile << (a.c.page_shift - 4);
@@ -135,13 +135,13 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
   uint32_t phase = 0;  // parity of each stage's barrier, a bit each
   int stage = 0;       // of the next unit
 
-  for (int64_t place = kv4_range_begin(W, worker, workers); place < end;) {
+  for (int64_t place = ranges.begin(worker); place < end;) {
     int64_t before;
     int which;
     const Kv4Seq s = kv4_find<kThreads>(a, cut, prefix, place, before, which);
     const int per = s.units + cut.start;
     const int64_t in_seq = place - before;
-    const int item = (int)(in_seq / per), off = (int)(in_seq - (int64_t)item * per);
+    const int item = (int)kv4_div(in_seq, per), off = (int)(in_seq - (int64_t)item * per);
     const int take = (int)min((int64_t)(per - off), end - place);
     place += take;
     const int u0 = max(0, off - cut.start), u1 = off + take - cut.start;
@@ -242,6 +242,94 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
     for (int x = 0; x < 2 * NT; ++x) ref[x] = kNone, sum[x] = 0.f;
     __syncwarp();  // Q's fragments are there
 
+    // S^T += K Q^T of a tile
+    auto scores = [&](const uint8_t* tl, float(&S)[NT][4]) {
+      uint32_t ka[D / 32], kb[D / 32];
+      const uint8_t* pa = tl + row_a * (D / 2) + t * (D / 8);
+      if constexpr (D == 128) {
+        const uint4 x = *reinterpret_cast<const uint4*>(pa), y = *reinterpret_cast<const uint4*>(pa + 8 * (D / 2));
+        ka[0] = x.x, ka[1] = x.y, ka[2] = x.z, ka[3] = x.w;
+        kb[0] = y.x, kb[1] = y.y, kb[2] = y.z, kb[3] = y.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(pa), y = *reinterpret_cast<const uint2*>(pa + 8 * (D / 2));
+        ka[0] = x.x, ka[1] = x.y;
+        kb[0] = y.x, kb[1] = y.y;
+      }
+      uint32_t sa[D / 64], sb[D / 64];  // a scale twice, for each 16 dims of the lane
+      const uint8_t* ps = tl + 16 * D + row_a * (D / 16) + t * (D / 64);
+      if constexpr (D == 128) {
+        const uint32_t ha = e4m3x2_to_half2(*reinterpret_cast<const uint16_t*>(ps));
+        const uint32_t hb = e4m3x2_to_half2(*reinterpret_cast<const uint16_t*>(ps + 8 * (D / 16)));
+        sa[0] = __byte_perm(ha, 0, 0x1010), sa[1] = __byte_perm(ha, 0, 0x3232);
+        sb[0] = __byte_perm(hb, 0, 0x1010), sb[1] = __byte_perm(hb, 0, 0x3232);
+      } else {
+        const uint32_t h = e4m3x2_to_half2((uint32_t)ps[0] | (uint32_t)ps[8 * (D / 16)] << 8);
+        sa[0] = __byte_perm(h, 0, 0x1010);
+        sb[0] = __byte_perm(h, 0, 0x3232);
+      }
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w) {
+        uint32_t xa[4], xb[4];
+        e2m1x8_to_half2(ka[w], xa);
+        e2m1x8_to_half2(kb[w], xb);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          xa[i] = hmul2_bits(xa[i], sa[w / 2]);
+          xb[i] = hmul2_bits(xb[i], sb[w / 2]);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint2 b0 = NT == 1 ? make_uint2(q1[4 * w], q1[4 * w + 1]) : qf[(n * kSteps + 2 * w) * 32 + lane];
+          const uint2 b1 = NT == 1 ? make_uint2(q1[4 * w + 2], q1[4 * w + 3]) : qf[(n * kSteps + 2 * w + 1) * 32 + lane];
+          mma16816(S[n], xa[0], xb[0], xa[1], xb[1], b0.x, b0.y);
+          mma16816(S[n], xa[2], xb[2], xa[3], xb[3], b1.x, b1.y);
+        }
+      }
+    };
+    // O^T += V^T P^T of a tile with `left` tokens: a = tok_v and a ^ 3 (places 2t, 2t+1), and both + 8
+    auto values = [&](const uint8_t* tl, int left, const uint32_t(&pb)[NT][2]) {
+      const int ta = tok_v, tb = tok_v ^ 3;
+      const uint8_t* pv = tl + 8 * D + g * (D / 16);
+      const uint8_t* ps = tl + 17 * D + (D == 128 ? g : g >> 1);
+      uint32_t s01 = (uint32_t)ps[ta * (D / 16)] | (uint32_t)ps[tb * (D / 16)] << 8;
+      uint32_t s23 = (uint32_t)ps[(ta + 8) * (D / 16)] | (uint32_t)ps[(tb + 8) * (D / 16)] << 8;
+      if (left < 16) {
+        // rows behind the last token hold anything: their scale is 0
+        if (ta >= left) s01 &= 0xFF00u;
+        if (tb >= left) s01 &= 0x00FFu;
+        if (ta + 8 >= left) s23 &= 0xFF00u;
+        if (tb + 8 >= left) s23 &= 0x00FFu;
+      }
+      const uint32_t h01 = e4m3x2_to_half2(s01), h23 = e4m3x2_to_half2(s23);
+      uint32_t va[D / 64], vb[D / 64], vc[D / 64], vd[D / 64];
+      if constexpr (D == 128) {
+        const uint2 xa = *reinterpret_cast<const uint2*>(pv + ta * (D / 2)), xb = *reinterpret_cast<const uint2*>(pv + tb * (D / 2));
+        const uint2 xc = *reinterpret_cast<const uint2*>(pv + (ta + 8) * (D / 2)), xd = *reinterpret_cast<const uint2*>(pv + (tb + 8) * (D / 2));
+        va[0] = xa.x, va[1] = xa.y, vb[0] = xb.x, vb[1] = xb.y;
+        vc[0] = xc.x, vc[1] = xc.y, vd[0] = xd.x, vd[1] = xd.y;
+      } else {
+        va[0] = *reinterpret_cast<const uint32_t*>(pv + ta * (D / 2));
+        vb[0] = *reinterpret_cast<const uint32_t*>(pv + tb * (D / 2));
+        vc[0] = *reinterpret_cast<const uint32_t*>(pv + (ta + 8) * (D / 2));
+        vd[0] = *reinterpret_cast<const uint32_t*>(pv + (tb + 8) * (D / 2));
+      }
+#pragma unroll
+      for (int w = 0; w < D / 64; ++w) {
+        uint32_t e01[4], o01[4], e23[4], o23[4];  // even and odd dims of the byte, token pairs
+        e2m1x8_to_half2((va[w] & 0x0F0F0F0Fu) | ((vb[w] << 4) & 0xF0F0F0F0u), e01);
+        e2m1x8_to_half2(((va[w] >> 4) & 0x0F0F0F0Fu) | (vb[w] & 0xF0F0F0F0u), o01);
+        e2m1x8_to_half2((vc[w] & 0x0F0F0F0Fu) | ((vd[w] << 4) & 0xF0F0F0F0u), e23);
+        e2m1x8_to_half2(((vc[w] >> 4) & 0x0F0F0F0Fu) | (vd[w] & 0xF0F0F0F0u), o23);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t a0 = hmul2_bits(e01[i], h01), a1 = hmul2_bits(o01[i], h01);
+          const uint32_t a2 = hmul2_bits(e23[i], h23), a3 = hmul2_bits(o23[i], h23);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma16816(O[n][4 * w + i], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+        }
+      }
+    };
+
     for (int k = 0; k < mine; ++k) {
       if (!__all_sync(~0u, mbar_wait_bounded(bar + stage, phase >> stage & 1))) {
         if (lane == 0) raise_error(a.c.err, kDevWaitTimeout);
@@ -254,82 +342,49 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
       }
       phase ^= 1u << stage;
       const int token = token0 + k * kUnit;
+      // a unit's two tiles together (up to 16 rows: registers), so that their products and conversions overlap
+      // and one vote serves both; what lies behind the last token is masked, whatever the stage holds there
+      constexpr int kTogether = NT <= 2 ? 2 : 1;
 #pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
+      for (int half = 0; half < 2; half += kTogether) {
         const int t0 = token + 16 * half;
         if (t0 >= s.length) break;
         const uint8_t* tl = ring + stage * L::kStage + half * L::kTile;
-        // ---- S^T = K Q^T
-        float S[NT][4];
+        float S[kTogether][NT][4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) S[n][0] = S[n][1] = S[n][2] = S[n][3] = 0.f;
-        {
-          uint32_t ka[D / 32], kb[D / 32];
-          const uint8_t* pa = tl + row_a * (D / 2) + t * (D / 8);
-          if constexpr (D == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(pa), y = *reinterpret_cast<const uint4*>(pa + 8 * (D / 2));
-            ka[0] = x.x, ka[1] = x.y, ka[2] = x.z, ka[3] = x.w;
-            kb[0] = y.x, kb[1] = y.y, kb[2] = y.z, kb[3] = y.w;
-          } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(pa), y = *reinterpret_cast<const uint2*>(pa + 8 * (D / 2));
-            ka[0] = x.x, ka[1] = x.y;
-            kb[0] = y.x, kb[1] = y.y;
-          }
-          uint32_t sa[D / 64], sb[D / 64];  // a scale twice, for each 16 dims of the lane
-          const uint8_t* ps = tl + 16 * D + row_a * (D / 16) + t * (D / 64);
-          if constexpr (D == 128) {
-            const uint32_t ha = e4m3x2_to_half2(*reinterpret_cast<const uint16_t*>(ps));
-            const uint32_t hb = e4m3x2_to_half2(*reinterpret_cast<const uint16_t*>(ps + 8 * (D / 16)));
-            sa[0] = __byte_perm(ha, 0, 0x1010), sa[1] = __byte_perm(ha, 0, 0x3232);
-            sb[0] = __byte_perm(hb, 0, 0x1010), sb[1] = __byte_perm(hb, 0, 0x3232);
-          } else {
-            const uint32_t h = e4m3x2_to_half2((uint32_t)ps[0] | (uint32_t)ps[8 * (D / 16)] << 8);
-            sa[0] = __byte_perm(h, 0, 0x1010);
-            sb[0] = __byte_perm(h, 0, 0x3232);
-          }
+        for (int h = 0; h < kTogether; ++h) {
 #pragma unroll
-          for (int w = 0; w < D / 32; ++w) {
-            uint32_t xa[4], xb[4];
-            e2m1x8_to_half2(ka[w], xa);
-            e2m1x8_to_half2(kb[w], xb);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              xa[i] = hmul2_bits(xa[i], sa[w / 2]);
-              xb[i] = hmul2_bits(xb[i], sb[w / 2]);
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const uint2 b0 = NT == 1 ? make_uint2(q1[4 * w], q1[4 * w + 1]) : qf[(n * kSteps + 2 * w) * 32 + lane];
-              const uint2 b1 = NT == 1 ? make_uint2(q1[4 * w + 2], q1[4 * w + 3]) : qf[(n * kSteps + 2 * w + 1) * 32 + lane];
-              mma16816(S[n], xa[0], xb[0], xa[1], xb[1], b0.x, b0.y);
-              mma16816(S[n], xa[2], xb[2], xa[3], xb[3], b1.x, b1.y);
-            }
-          }
+          for (int n = 0; n < NT; ++n) S[h][n][0] = S[h][n][1] = S[h][n][2] = S[h][n][3] = 0.f;
+          scores(tl + h * L::kTile, S[h]);
         }
         // ---- weights
-        const bool open = t0 >= most_lo && t0 + 15 <= least_hi;  // every row sees the whole tile
-        const int pos_a = t0 + row_a, pos_b = pos_a + 8;
+        const bool open = t0 >= most_lo && t0 + 16 * kTogether - 1 <= least_hi;  // every row sees all of it
         bool over = false;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int h = 0; h < kTogether; ++h) {
+          const int pos_a = t0 + 16 * h + row_a, pos_b = pos_a + 8;
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int i = 2 * n + x;
-            S[n][x] *= mul[i];
-            S[n][2 + x] *= mul[i];
-            if (!open) {
-              if (pos_a < see_lo[i] || pos_a > see_hi[i]) S[n][x] = -INFINITY;
-              if (pos_b < see_lo[i] || pos_b > see_hi[i]) S[n][2 + x] = -INFINITY;
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int i = 2 * n + x;
+              S[h][n][x] *= mul[i];
+              S[h][n][2 + x] *= mul[i];
+              if (!open) {
+                if (pos_a < see_lo[i] || pos_a > see_hi[i]) S[h][n][x] = -INFINITY;
+                if (pos_b < see_lo[i] || pos_b > see_hi[i]) S[h][n][2 + x] = -INFINITY;
+              }
+              over = over || fmaxf(S[h][n][x], S[h][n][2 + x]) > ref[i] + kMost;
             }
-            over = over || S[n][x] > ref[i] + kMost || S[n][2 + x] > ref[i] + kMost;
-          }
+        }
         if (__any_sync(~0u, over)) {
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const int i = 2 * n + x;
-              float top = fmaxf(S[n][x], S[n][2 + x]);
+              float top = fmaxf(S[0][n][x], S[0][n][2 + x]);
+              if (kTogether == 2) top = fmaxf(top, fmaxf(S[kTogether - 1][n][x], S[kTogether - 1][n][2 + x]));
               top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
               top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
               top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
@@ -345,52 +400,20 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
               }
             }
         }
-        uint32_t pb[NT][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int h = 0; h < kTogether; ++h) {
+          uint32_t pb[NT][2];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            S[n][x] = exp2_approx(S[n][x] - ref[2 * n + (x & 1)]);
-            sum[2 * n + (x & 1)] += S[n][x];
-          }
-          pb[n][0] = transpose8x8(pack_half2(S[n][0], S[n][1]));
-          pb[n][1] = transpose8x8(pack_half2(S[n][2], S[n][3]));
-        }
-        // ---- O^T += V^T P^T: tokens a = tok_v and a ^ 3 (places 2t, 2t+1), and both + 8
-        {
-          const int ta = tok_v, tb = tok_v ^ 3;
-          const uint8_t* pv = tl + 8 * D + g * (D / 16);
-          const uint8_t* ps = tl + 17 * D + (D == 128 ? g : g >> 1);
-          uint32_t s01 = (uint32_t)ps[ta * (D / 16)] | (uint32_t)ps[tb * (D / 16)] << 8;
-          uint32_t s23 = (uint32_t)ps[(ta + 8) * (D / 16)] | (uint32_t)ps[(tb + 8) * (D / 16)] << 8;
-          if (t0 + 16 > s.length) {
-            // rows behind the last token hold anything: their scale is 0
-            const int over_end = s.length - t0;
-            if (ta >= over_end) s01 &= 0xFF00u;
-            if (tb >= over_end) s01 &= 0x00FFu;
-            if (ta + 8 >= over_end) s23 &= 0xFF00u;
-            if (tb + 8 >= over_end) s23 &= 0x00FFu;
-          }
-          const uint32_t h01 = e4m3x2_to_half2(s01), h23 = e4m3x2_to_half2(s23);
+          for (int n = 0; n < NT; ++n) {
 #pragma unroll
-          for (int w = 0; w < D / 64; ++w) {
-            const uint32_t va = *reinterpret_cast<const uint32_t*>(pv + ta * (D / 2) + 4 * w);
-            const uint32_t vb = *reinterpret_cast<const uint32_t*>(pv + tb * (D / 2) + 4 * w);
-            const uint32_t vc = *reinterpret_cast<const uint32_t*>(pv + (ta + 8) * (D / 2) + 4 * w);
-            const uint32_t vd = *reinterpret_cast<const uint32_t*>(pv + (tb + 8) * (D / 2) + 4 * w);
-            uint32_t e01[4], o01[4], e23[4], o23[4];  // even and odd dims of the byte, token pairs
-            e2m1x8_to_half2((va & 0x0F0F0F0Fu) | ((vb << 4) & 0xF0F0F0F0u), e01);
-            e2m1x8_to_half2(((va >> 4) & 0x0F0F0F0Fu) | (vb & 0xF0F0F0F0u), o01);
-            e2m1x8_to_half2((vc & 0x0F0F0F0Fu) | ((vd << 4) & 0xF0F0F0F0u), e23);
-            e2m1x8_to_half2(((vc >> 4) & 0x0F0F0F0Fu) | (vd & 0xF0F0F0F0u), o23);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t a0 = hmul2_bits(e01[i], h01), a1 = hmul2_bits(o01[i], h01);
-              const uint32_t a2 = hmul2_bits(e23[i], h23), a3 = hmul2_bits(o23[i], h23);
-#pragma unroll
-              for (int n = 0; n < NT; ++n) mma16816(O[n][4 * w + i], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+            for (int x = 0; x < 4; ++x) {
+              S[h][n][x] = exp2_approx(S[h][n][x] - ref[2 * n + (x & 1)]);
+              sum[2 * n + (x & 1)] += S[h][n][x];
             }
+            pb[n][0] = transpose8x8(pack_half2(S[h][n][0], S[h][n][1]));
+            pb[n][1] = transpose8x8(pack_half2(S[h][n][2], S[h][n][3]));
           }
+          values(tl + h * L::kTile, s.length - t0 - 16 * h, pb);
         }
       }
       __syncwarp();
@@ -411,6 +434,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
     const bool done = u0 == 0 && u1 == s.units;
     const int rows = min(L::kRows, s.count * a.group - tile * L::kRows);
     const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
+    if (lane == 0) {
+      int2* span = a.spans + ((int64_t)which * a.c.H + head) * a.tiles + tile;
+      if (u0 == 0) span->x = done ? -1 : worker;
+      else if (u1 == s.units) span->y = worker;
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -446,29 +474,31 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
 constexpr int kJoinWarps = 4;
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, Kv4FewCut cut, int most) {
+__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, int rows_tile) {
   __shared__ float acc[kJoinWarps][D];
   __shared__ float sums[kJoinWarps];
   pdl_wait();
   pdl_trigger();
   const int i = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t W = a.prefix[a.b.n], p0 = a.prefix[i];
-  const Kv4Seq s = cut.seq(a, i, false);
-  const int workers = kv4_workers(W, cut.least, most);
+  int begin, count;
+  const int seq = a.b.seqs ? a.b.seqs[i] : i;
+  if (!kv4_range(a.b, i, begin, count) || seq < 0 || seq >= a.c.max_seqs) return;
+  const bool empty = a.c.length[seq] <= 0;
   constexpr int kDims = D / 32;
   // y: row of the sequence (token j, query head), head by head of the cache
-  for (int64_t y = blockIdx.y; y < (int64_t)s.count * a.q_heads; y += gridDim.y) {
-    const int head = (int)(y / (s.count * a.group)), row = (int)(y - (int64_t)head * s.count * a.group);
-    const int tile = row / cut.rows, col = row - tile * cut.rows;
+  const int group_rows = count * a.group;
+  for (int64_t y = blockIdx.y; y < (int64_t)count * a.q_heads; y += gridDim.y) {
+    const int head = (int)kv4_div(y, group_rows), row = (int)(y - (int64_t)head * group_rows);
+    const int tile = row / rows_tile, col = row - tile * rows_tile;
     int w0 = 0, parts = 0;
-    int64_t first, last;
-    if (cut.ends(a, s, head, tile, first, last)) {
-      w0 = kv4_owner(W, p0 + first, workers);
-      parts = kv4_owner(W, p0 + last, workers) - w0 + 1;
-      if (parts == 1) continue;  // finished where it ran
+    if (!empty) {
+      const int2 span = a.spans[((int64_t)i * a.c.H + head) * a.tiles + tile];
+      if (span.x < 0) continue;  // finished where it ran
+      w0 = span.x;
+      parts = span.y - w0 + 1;
     }
-    const int64_t at = (int64_t)(s.begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
-    const int64_t size = (int64_t)cut.rows * kv4_part_floats(D);
+    const int64_t at = (int64_t)(begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
+    const int64_t size = (int64_t)rows_tile * kv4_part_floats(D);
     // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
     const float* base = a.parts + 2 * w0 * size + col * kv4_part_floats(D);
     float top = kNone;
@@ -542,12 +572,20 @@ int few_ctas(int n_tiles, int sms) { return n_tiles == 1 ? 2 * sms : sms; }
 
 }  // namespace
 
-static size_t prefix_bytes(int n) { return ((size_t)n + 1) * 8 + 15 & ~(size_t)15; }
+// Workspace: the parts, behind the lengths before each sequence (many rows) or the items' spans (few).
+static int few_items(const Kv4Batch& b, int group, int n_tiles) {
+  return (int)(((int64_t)b.max_count * group + 8 * n_tiles - 1) / (8 * n_tiles));
+}
+static size_t front_bytes(const Kv4Cache& c, const Kv4Batch& b, int group) {
+  const size_t words = kv4_many(b, group) ? (size_t)b.n + 1 : (size_t)b.n * c.H * few_items(b, group, few_tiles(b, group));
+  return words * 8 + 15 & ~(size_t)15;
+}
 
 size_t kv4_attention_workspace(const Kv4Cache& c, const Kv4Batch& b, int q_heads, int sms) {
-  if (kv4_many(b, q_heads / c.H)) return kv4_many_part_floats(c.D, sms) * 4 + prefix_bytes(b.n);
-  const int n = few_tiles(b, q_heads / c.H);
-  return (size_t)2 * few_ctas(n, sms) * kWarps * 8 * n * kv4_part_floats(c.D) * 4 + prefix_bytes(b.n);
+  const int group = q_heads / c.H, n = few_tiles(b, group);
+  const size_t floats = kv4_many(b, group) ? kv4_many_part_floats(c.D, sms)
+                                           : (size_t)2 * few_ctas(n, sms) * kWarps * 8 * n * kv4_part_floats(c.D);
+  return floats * 4 + front_bytes(c, b, group);
 }
 
 cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer, int dtype, const void* q, int64_t q_stride,
@@ -566,9 +604,11 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
   a.lse = lse;
   a.scale_log2 = softmax_scale * 1.4426950408889634f;
   a.prefix = static_cast<int64_t*>(ws);
-  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + prefix_bytes(b.n));
+  a.spans = static_cast<int2*>(ws);
+  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + front_bytes(c, b, a.group));
   if (kv4_many(b, a.group)) return launch_kv4_many(a, dtype, sms, stream);
   const int n = few_tiles(b, a.group), ctas = few_ctas(n, sms);
+  a.tiles = few_items(b, a.group, n);
   const bool bf = dtype == SEMKV_BF16;
   const cudaError_t e =
       c.D == 128 ? (bf ? launch_few_rows<128, true>(a, n, ctas, stream) : launch_few_rows<128, false>(a, n, ctas, stream))
@@ -577,8 +617,7 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
   const int64_t rows = (int64_t)b.max_count * q_heads;
   auto join = c.D == 128 ? (bf ? kv4_join_kernel<128, true> : kv4_join_kernel<128, false>)
                          : (bf ? kv4_join_kernel<64, true> : kv4_join_kernel<64, false>);
-  return launch_pdl(join, dim3(b.n, (unsigned)(rows < 4096 ? rows : 4096)), dim3(kJoinWarps * 32), 0, stream, a, few_cut(n),
-                    ctas * kWarps);
+  return launch_pdl(join, dim3(b.n, (unsigned)(rows < 4096 ? rows : 4096)), dim3(kJoinWarps * 32), 0, stream, a, 8 * n);
 }
 
 }  // namespace semkv

@@ -25,7 +25,9 @@ struct Kv4Attend {
   float* lse;
   float scale_log2;  // softmax scale * log2(e)
   float* parts;      // [2 * workers][rows][D + 4]: sums, then reference exponent and weight sum
-  int64_t* prefix;   // [b.n + 1]: length before each sequence (written by CTA 0, for the join)
+  int64_t* prefix;   // (many rows) [b.n + 1]: length before each sequence
+  int2* spans;       // (few rows) [b.n][heads][tiles]: first and last worker of each item; first -1: it was
+  int tiles;         //   finished by one
 };
 
 __host__ __device__ constexpr int kv4_part_floats(int D) { return D + 4; }
@@ -72,14 +74,6 @@ struct Kv4FewCut {
   }
   __device__ __forceinline__ int64_t weight(const Kv4Attend& a, const Kv4Seq& s) const {
     return s.units ? (int64_t)(s.units + start) * s.tiles * a.c.H : 0;
-  }
-  // places, from the sequence's first, of an item's first and last unit; false if it has none
-  __device__ __forceinline__ bool ends(const Kv4Attend& a, const Kv4Seq& s, int head, int tile, int64_t& first,
-                                       int64_t& last) const {
-    if (!s.units) return false;
-    first = ((int64_t)head * s.tiles + tile) * (s.units + start) + start;
-    last = first + s.units - 1;
-    return true;
   }
 };
 
@@ -141,6 +135,7 @@ struct Kv4ManyCut {
     const int to = e < s.length ? e : s.length;
     last = to > 0 ? (to + unit - 1) / unit : first;
   }
+  // places, from the sequence's first, of an item's first and last unit; false if it has none
   __device__ __forceinline__ bool ends(const Kv4Attend& a, const Kv4Seq& s, int head, int tile, int64_t& first,
                                        int64_t& last) const {
     int u0, u1, from;
@@ -155,7 +150,8 @@ struct Kv4ManyCut {
 
 // The plan: thread x of the block adds up sequences x * per .. (x + 1) * per - 1, with
 // per = ceil(n / THREADS); prefix[x] = the length before them, prefix[THREADS] = all.
-template <int THREADS, class Cut>
+// KEEP: CTA 0 leaves each sequence's in a.prefix.
+template <int THREADS, bool KEEP, class Cut>
 __device__ __forceinline__ void kv4_plan(const Kv4Attend& a, Cut cut, int64_t* prefix, int64_t* sums,
                                          bool first_cta) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -175,7 +171,7 @@ __device__ __forceinline__ void kv4_plan(const Kv4Attend& a, Cut cut, int64_t* p
   for (int w = 0; w < warp; ++w) at += sums[w];
   prefix[threadIdx.x] = at;
   if (threadIdx.x == THREADS - 1) prefix[THREADS] = at + sum;
-  if (first_cta) {
+  if (KEEP && first_cta) {
     for (int i = i0; i < i1; ++i) {
       a.prefix[i] = at;
       at += per == 1 ? sum : cut.weight(a, cut.seq(a, i, false));
@@ -207,17 +203,30 @@ __device__ __forceinline__ Kv4Seq kv4_find(const Kv4Attend& a, Cut cut, const in
   return s;
 }
 
-// Workers that take part: no range shorter than `least`.  Worker w's range of the length W begins
-// at W w / workers.
-__device__ __forceinline__ int kv4_workers(int64_t W, int least, int most) {
-  const int64_t w = W / least;
-  return w < 1 ? 1 : w < most ? (int)w : most;
+// a / b; most dividends fit 32 bits, and a 64-bit division is a few hundred cycles of code that a
+// short kernel first has to fetch
+__device__ __forceinline__ int64_t kv4_div(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
-__device__ __forceinline__ int64_t kv4_range_begin(int64_t W, int w, int workers) { return W * w / workers; }
-// the worker whose range holds place v
-__device__ __forceinline__ int kv4_owner(int64_t W, int64_t v, int workers) {
-  return (int)(((v + 1) * workers - 1) / W);
-}
+
+// The length W cut into ranges: as many as there are workers, but none shorter than `least`; the first
+// W % count are one longer.
+struct Kv4Ranges {
+  int count, longer;
+  int64_t each;
+  __device__ __forceinline__ Kv4Ranges(int64_t W, int least, int most) {
+    const int64_t w = W / least;
+    count = w < 1 ? 1 : w < most ? (int)w : most;
+    each = kv4_div(W, count);
+    longer = (int)(W - each * count);
+  }
+  __device__ __forceinline__ int64_t begin(int w) const { return w * each + min(w, longer); }
+  // the range that holds place v
+  __device__ __forceinline__ int owner(int64_t v) const {
+    const int64_t front = longer * (each + 1);
+    return v < front ? (int)kv4_div(v, each + 1) : longer + (int)kv4_div(v - front, each);
+  }
+};
 
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   uint32_t w;

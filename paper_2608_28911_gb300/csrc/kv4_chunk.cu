@@ -208,7 +208,7 @@ struct Walk {
     int which;
     const Kv4Seq q = kv4_find<kThreads>(a, cut, prefix, place, at, which);
     const int64_t head_length = cut.before(a, q, q.tiles);
-    const int h = (int)((place - at) / head_length);
+    const int h = (int)kv4_div(place - at, head_length);
     const int64_t in_head = place - at - h * head_length;
     const int t = cut.find(a, q, in_head);
     if ((threadIdx.x & 31) == 0) {
@@ -807,13 +807,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   const uint32_t tmem = bars->tmem;
   pdl_wait();
   pdl_trigger();
-  kv4_plan<kThreads>(a, cut, prefix, sums, blockIdx.x == 0);
+  kv4_plan<kThreads, true>(a, cut, prefix, sums, blockIdx.x == 0);
   const int64_t W = prefix[kThreads];
-  const int workers = kv4_workers(W, cut.least, gridDim.x);
-  if (W > 0 && (int)blockIdx.x < workers) {
+  const Kv4Ranges ranges(W, cut.least, gridDim.x);
+  if (W > 0 && (int)blockIdx.x < ranges.count) {
     Walk& walk = *reinterpret_cast<Walk*>(smem + L::walk());
     if (warp == kThreads / 32 - 1)
-      walk.start(a, cut, prefix, kv4_range_begin(W, blockIdx.x, workers), kv4_range_begin(W, blockIdx.x + 1, workers));
+      walk.start(a, cut, prefix, ranges.begin(blockIdx.x), ranges.begin(blockIdx.x + 1));
     // 176 + 176 + 88 + 72 = 4 * 128, the registers of the launch
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
@@ -863,9 +863,9 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_chunk_join_kernel(Kv4Attend 
     return;
   }
   const int64_t W = a.prefix[a.b.n];
-  const int workers = kv4_workers(W, cut.least, most);
-  if (W == 0 || x + 1 >= workers) return;
-  const int64_t place = kv4_range_begin(W, x + 1, workers);
+  const Kv4Ranges ranges(W, cut.least, most);
+  if (W == 0 || x + 1 >= ranges.count) return;
+  const int64_t place = ranges.begin(x + 1);
   int lo = 0, hi = a.b.n - 1;  // the sequence that the next range begins in
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -873,11 +873,11 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_chunk_join_kernel(Kv4Attend 
   }
   const Kv4Seq s = cut.seq(a, lo, false);
   const int64_t p0 = a.prefix[lo], head_length = cut.before(a, s, s.tiles);
-  const int head = (int)((place - p0) / head_length), tile = cut.find(a, s, place - p0 - head * head_length);
+  const int head = (int)kv4_div(place - p0, head_length), tile = cut.find(a, s, place - p0 - head * head_length);
   int64_t first, last;
   if (!cut.ends(a, s, head, tile, first, last)) return;
-  const int parts = kv4_owner(W, p0 + last, workers) - x + 1;
-  if (kv4_owner(W, p0 + first, workers) != x || parts < 2) return;
+  const int parts = ranges.owner(p0 + last) - x + 1;
+  if (ranges.owner(p0 + first) != x || parts < 2) return;
   const int rows = min(cut.rows, (s.count - tile * cut.tokens) * a.group);
   const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
   for (int col = row0; col < rows; col += kStep) {
