@@ -923,7 +923,7 @@ cudaError_t launch_chunk(const Kv4Attend& a, const Kv4ManyCut& cut, int sms, cud
 }  // namespace
 
 bool kv4_many(const Kv4Batch& b, int group) {
-  return (int64_t)b.max_count * group > 32 && group <= 2 * kBlock;
+  return (int64_t)b.max_count * group > 64 && group <= 2 * kBlock;
 }
 
 size_t kv4_many_part_floats(int D, int sms) { return (size_t)2 * sms * 2 * kBlock * kv4_part_floats(D); }
