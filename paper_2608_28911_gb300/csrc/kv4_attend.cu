@@ -59,13 +59,14 @@ struct Layout {
   static constexpr int bytes() { return ring_bytes() + q_bytes() + kWarps * kStages * 8 + (kThreads + 1) * 8 + kWarps * 8; }
 };
 
-__host__ __device__ constexpr Kv4FewCut few_cut(int n_tiles) { return Kv4FewCut{8 * n_tiles, kUnit, 4, 4}; }
+// An item's start counts for two units (with one, ragged batches end 15% later; with four it is the same);
+// a range has four at least (fewer cost the join more than they save: one session at 4K 13.6, 16.3, 21.9 us
+// with ranges of 4, 2, 1).
+__host__ __device__ constexpr Kv4FewCut few_cut(int n_tiles) { return Kv4FewCut{8 * n_tiles, kUnit, 2, 4}; }
 
-// The fragments of eight query rows (row0 + g) for one KV head, w[2k], w[2k + 1] those of k
-// step k.  bf16 rows are scaled by a power of two, which leaves their values exact in fp16 but
-// for those 2^-24 and less of the row's largest; returns what undoes it.
-template <int D, bool BF16>
-__device__ __forceinline__ float load_queries(const Kv4Attend& a, const Kv4Seq& s, int head, int row0, uint32_t (&w)[D / 8]) {
+// The fragments of eight query rows (row0 + g) for one KV head, w[2k], w[2k + 1] those of k step k.
+template <int D>
+__device__ __forceinline__ void load_queries(const Kv4Attend& a, const Kv4Seq& s, int head, int row0, uint32_t (&w)[D / 8]) {
   const int lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
   const int row = row0 + g;
@@ -81,6 +82,10 @@ __device__ __forceinline__ float load_queries(const Kv4Attend& a, const Kv4Seq& 
 #pragma unroll
     for (int k = 0; k < D / 8; ++k) w[k] = 0;
   }
+}
+// bf16 rows as fp16, times their factor; returns what undoes it.
+template <int D, bool BF16>
+__device__ __forceinline__ float turn_queries(uint32_t (&w)[D / 8]) {
   float undo = 1.f;
   if (BF16) {
     float most = 0.f;
@@ -97,6 +102,25 @@ __device__ __forceinline__ float load_queries(const Kv4Attend& a, const Kv4Seq& 
       w[k] = pack_half2(__uint_as_float(w[k] << 16) * mul, __uint_as_float(w[k] & 0xFFFF0000u) * mul);
   }
   return undo;
+}
+
+// Rows of sequences without tokens, and their items' spans.
+template <int D>
+__device__ __forceinline__ void fill_empty(const Kv4Attend& a, Kv4FewCut cut) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int i0 = warp * 32; i0 < a.b.n; i0 += kThreads) {
+    const Kv4Seq mine = i0 + lane < a.b.n ? cut.seq(a, i0 + lane, false) : Kv4Seq{};
+    // (a sequence that is left out has count 0)
+    for (uint32_t m = __ballot_sync(~0u, mine.count > 0 && mine.units == 0); m; m &= m - 1) {
+      const int x = __ffs(m) - 1, count = __shfl_sync(~0u, mine.count, x), tiles = __shfl_sync(~0u, mine.tiles, x);
+      const int64_t row0 = (int64_t)__shfl_sync(~0u, mine.begin, x) * a.q_heads;
+      for (int64_t y = lane; y < (int64_t)count * a.q_heads * (D / 8); y += 32)
+        reinterpret_cast<uint4*>(a.out + row0 * D)[y] = make_uint4(0, 0, 0, 0);
+      for (int64_t y = lane; a.lse && y < (int64_t)count * a.q_heads; y += 32) a.lse[row0 + y] = -INFINITY;
+      for (int y = lane; y < a.c.H * tiles; y += 32)
+        a.spans[((int64_t)(i0 + x) * a.c.H + y / tiles) * a.tiles + y % tiles].x = -1;
+    }
+  }
 }
 
 template <int D, int NT, bool BF16>
@@ -123,6 +147,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
   pdl_wait();
   pdl_trigger();
   kv4_plan<kThreads, false>(a, cut, prefix, sums, blockIdx.x == 0);
+  if (blockIdx.x == 0) fill_empty<D>(a, cut);
   const int64_t W = prefix[kThreads];
   const Kv4Ranges ranges(W, cut.least, gridDim.x * kWarps);
   const int worker = warp * gridDim.x + blockIdx.x;  // few workers: spread over the SMs
@@ -146,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
     place += take;
     const int u0 = max(0, off - cut.start), u1 = off + take - cut.start;
     if (u1 <= u0) continue;
-    const int head = item / s.tiles, tile = item - head * s.tiles;
+    const int head = s.tiles == 1 ? item : item / s.tiles, tile = item - head * s.tiles;
 
     // the pages of units u0 + k0 .. u0 + k0 + 31, a lane each (with pages of 16 tokens: of both halves)
     const int mine = u1 - u0, token0 = (s.u_first + u0) * kUnit;
@@ -190,17 +215,9 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
       }
     };
 
-    // ---- queries (on their way before the copies, which they would queue behind)
+    // ---- the (first) queries on their way before the copies, which they would queue behind
     uint32_t q1[D / 8];
-    float undo[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      undo[n] = load_queries<D, BF16>(a, s, head, tile * L::kRows + 8 * n, q1);
-      if (NT > 1) {
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) qf[(n * kSteps + k) * 32 + lane] = make_uint2(q1[2 * k], q1[2 * k + 1]);
-      }
-    }
+    load_queries<D>(a, s, head, tile * L::kRows, q1);
     fetch_pages(0);
     {
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (the item before has read its stages)
@@ -209,6 +226,17 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
       for (int k = 0; k < ahead; ++k) {
         issue(k, to);
         to = to + 1 == L::kStages ? 0 : to + 1;
+      }
+    }
+
+    float undo[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (n > 0) load_queries<D>(a, s, head, tile * L::kRows + 8 * n, q1);
+      undo[n] = turn_queries<D, BF16>(q1);
+      if (NT > 1) {
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) qf[(n * kSteps + k) * 32 + lane] = make_uint2(q1[2 * k], q1[2 * k + 1]);
       }
     }
 
@@ -469,79 +497,75 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
   }
 }
 
-// Joins the parts of the items that several workers share, and fills the rows that see nothing: a
-// CTA for each query row, whose warps take the parts in turn.
+// Joins the parts of the items that several workers share: a CTA for each query row, whose warps take
+// the parts in turn.  (A warp for each row is slower even where most items have few parts: the long
+// sequences of a ragged batch have fifty.)
 constexpr int kJoinWarps = 4;
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, int rows_tile) {
   __shared__ float acc[kJoinWarps][D];
-  __shared__ float sums[kJoinWarps];
+  __shared__ float2 sums[kJoinWarps];  // reference exponent, weight sum
   pdl_wait();
   pdl_trigger();
   const int i = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int begin, count;
-  const int seq = a.b.seqs ? a.b.seqs[i] : i;
-  if (!kv4_range(a.b, i, begin, count) || seq < 0 || seq >= a.c.max_seqs) return;
-  const bool empty = a.c.length[seq] <= 0;
   constexpr int kDims = D / 32;
-  // y: row of the sequence (token j, query head), head by head of the cache
-  const int group_rows = count * a.group;
-  for (int64_t y = blockIdx.y; y < (int64_t)count * a.q_heads; y += gridDim.y) {
-    const int head = (int)kv4_div(y, group_rows), row = (int)(y - (int64_t)head * group_rows);
+  // y: row of the sequence (token j, query head), head by head of the cache, as if it had the most tokens,
+  // so that the loads below do not wait for one another
+  const int most_rows = a.b.max_count * a.group;
+  for (int64_t y = blockIdx.y; y < (int64_t)most_rows * a.c.H; y += gridDim.y) {
+    const int head = (int)kv4_div(y, most_rows), row = (int)(y - (int64_t)head * most_rows);
     const int tile = row / rows_tile, col = row - tile * rows_tile;
-    int w0 = 0, parts = 0;
-    if (!empty) {
-      const int2 span = a.spans[((int64_t)i * a.c.H + head) * a.tiles + tile];
-      if (span.x < 0) continue;  // finished where it ran
-      w0 = span.x;
-      parts = span.y - w0 + 1;
-    }
-    const int64_t at = (int64_t)(begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
+    const int2 span = a.spans[((int64_t)i * a.c.H + head) * a.tiles + tile];
+    const int seq = a.b.seqs ? a.b.seqs[i] : i;
+    const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
+    int begin, count;
+    const bool ok = kv4_range(a.b, i, begin, count) && seq >= 0 && seq < a.c.max_seqs;
+    // (a row that is not there, or that was finished where it ran)
+    if (!ok || row >= count * a.group || span.x < 0) continue;
+    const int parts = span.y - span.x + 1;
     const int64_t size = (int64_t)rows_tile * kv4_part_floats(D);
     // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
-    const float* base = a.parts + 2 * w0 * size + col * kv4_part_floats(D);
-    float top = kNone;
-    for (int p = lane; p < parts; p += 32) top = fmaxf(top, base[(2 * p + (p == 0)) * size + D]);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-    float total = 0.f, o[kDims] = {};
+    const float* base = a.parts + 2 * span.x * size + col * kv4_part_floats(D) + kDims * lane;
+    float ref = kNone, total = 0.f, o[kDims] = {};
 #pragma unroll 4
     for (int p = warp; p < parts; p += kJoinWarps) {
       const float* part = base + (2 * p + (p == 0)) * size;
-      const float2 rs = *reinterpret_cast<const float2*>(part + D);
+      const float2 rs = *reinterpret_cast<const float2*>(part + D - kDims * lane);
       float x[kDims];
       if constexpr (kDims == 4) {
-        const float4 v = *reinterpret_cast<const float4*>(part + 4 * lane);
+        const float4 v = *reinterpret_cast<const float4*>(part);
         x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
       } else {
-        const float2 v = *reinterpret_cast<const float2*>(part + 2 * lane);
+        const float2 v = *reinterpret_cast<const float2*>(part);
         x[0] = v.x, x[1] = v.y;
       }
-      const float f = exp2_approx(rs.x - top);
-      total += f * rs.y;
+      const float to = fmaxf(ref, rs.x), f = exp2_approx(ref - to), g = exp2_approx(rs.x - to);
+      ref = to;
+      total = total * f + rs.y * g;
 #pragma unroll
-      for (int d = 0; d < kDims; ++d) o[d] += f * x[d];
+      for (int d = 0; d < kDims; ++d) o[d] = o[d] * f + x[d] * g;
     }
     __syncthreads();  // the row before is done with the shared sums
 #pragma unroll
     for (int d = 0; d < kDims; ++d) acc[warp][kDims * lane + d] = o[d];
-    if (lane == 0) sums[warp] = total;
+    if (lane == 0) sums[warp] = make_float2(ref, total);
     __syncthreads();
-    if (threadIdx.x < D / 2) {
-      const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
-      float x = 0.f, z = 0.f;
-      total = 0.f;
+    if (warp > 0) continue;
 #pragma unroll
-      for (int w = 0; w < kJoinWarps; ++w) {
-        x += acc[w][2 * threadIdx.x];
-        z += acc[w][2 * threadIdx.x + 1];
-        total += sums[w];
-      }
-      const float inv = total == 0.f ? 0.f : gv / total;
-      reinterpret_cast<uint32_t*>(a.out + at * D)[threadIdx.x] = pack_out<BF16>(x * inv, z * inv);
-      if (a.lse && threadIdx.x == 0) a.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
+    for (int w = 1; w < kJoinWarps; ++w) {
+      const float to = fmaxf(ref, sums[w].x), f = exp2_approx(ref - to), g = exp2_approx(sums[w].x - to);
+      ref = to;
+      total = total * f + sums[w].y * g;
+#pragma unroll
+      for (int d = 0; d < kDims; ++d) o[d] = o[d] * f + acc[w][kDims * lane + d] * g;
     }
+    const int64_t at = (int64_t)(begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
+    const float inv = total == 0.f ? 0.f : gv / total;
+    uint32_t* to = reinterpret_cast<uint32_t*>(a.out + at * D) + kDims / 2 * lane;
+#pragma unroll
+    for (int d = 0; d < kDims / 2; ++d) to[d] = pack_out<BF16>(o[2 * d] * inv, o[2 * d + 1] * inv);
+    if (a.lse && lane == 0) a.lse[at] = total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
   }
 }
 
@@ -622,9 +646,9 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
       c.D == 128 ? (bf ? launch_few_rows<128, true>(a, n, ctas, stream) : launch_few_rows<128, false>(a, n, ctas, stream))
                  : (bf ? launch_few_rows<64, true>(a, n, ctas, stream) : launch_few_rows<64, false>(a, n, ctas, stream));
   if (e != cudaSuccess) return e;
-  const int64_t rows = (int64_t)b.max_count * q_heads;
   auto join = c.D == 128 ? (bf ? kv4_join_kernel<128, true> : kv4_join_kernel<128, false>)
                          : (bf ? kv4_join_kernel<64, true> : kv4_join_kernel<64, false>);
+  const int64_t rows = (int64_t)b.max_count * q_heads;
   return launch_pdl(join, dim3(b.n, (unsigned)(rows < 4096 ? rows : 4096)), dim3(kJoinWarps * 32), 0, stream, a, 8 * n);
 }
 

@@ -185,11 +185,13 @@ __device__ __forceinline__ void kv4_plan(const Kv4Attend& a, Cut cut, int64_t* p
 template <int THREADS, class Cut>
 __device__ __forceinline__ Kv4Seq kv4_find(const Kv4Attend& a, Cut cut, const int64_t* prefix, int64_t v,
                                            int64_t& at, int& i) {
-  int lo = 0, hi = THREADS - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (prefix[mid] <= v) lo = mid; else hi = mid - 1;
-  }
+  // the last entry at or below v: of every THREADS / 32-th by one vote, of those behind it by another (the
+  // whole warp asks for one place)
+  constexpr int kStep = THREADS / 32;
+  static_assert(kStep <= 32 && THREADS % 32 == 0, "two votes find an entry");
+  const int lane = threadIdx.x & 31;
+  int lo = (31 - __clz(__ballot_sync(~0u, prefix[lane * kStep] <= v))) * kStep;
+  lo += 31 - __clz(__ballot_sync(~0u, lane < kStep && prefix[lo + (lane < kStep ? lane : 0)] <= v));
   const int per = (a.b.n + THREADS - 1) / THREADS;
   at = prefix[lo];
   i = lo * per;
