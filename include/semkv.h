@@ -345,7 +345,7 @@ size_t semkv_kv4_tile_bytes(int32_t head_dim);
  * pool or a table has too little room for all of them nothing changes, every start[i] is -1
  * and 2 goes into the error word.  A sequence listed before, out of range, or with a wrong
  * row range gets start[i] = -1 and is left out (3).
- * ws: device workspace of semkv_kv4_pages_workspace_bytes(cache, n, 0) bytes, 16-byte aligned.
+ * ws: device workspace of semkv_kv4_pages_workspace_bytes(cache, n, -1) bytes, 16-byte aligned.
  * Errors: SEMKV_EINVAL, SEMKV_EALIGN, SEMKV_EUNSUPPORTED, SEMKV_EWORKSPACE. */
 size_t semkv_kv4_pages_workspace_bytes(const semkv_kv4_cache* cache, int32_t n, int32_t tokens);
 semkv_status semkv_kv4_reserve(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch,

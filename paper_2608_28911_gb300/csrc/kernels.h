@@ -142,7 +142,7 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
                                  const void* q, int64_t q_stride, int q_heads, void* out, float* lse,
                                  float softmax_scale, int window, void* ws, int sms,
                                  cudaStream_t stream);
-size_t kv4_pages_workspace(const Kv4Cache& c, int n, int tokens);
+size_t kv4_pages_workspace(const Kv4Cache& c, int n, int tokens, bool compact);
 cudaError_t launch_kv4_reserve(const Kv4Cache& c, const Kv4Batch& b, void* ws, int sms,
                                cudaStream_t stream);
 cudaError_t launch_kv4_fork(const Kv4Cache& c, int n, const int32_t* src, const int32_t* dst,

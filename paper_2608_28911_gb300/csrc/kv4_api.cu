@@ -93,8 +93,8 @@ size_t semkv_kv4_tile_bytes(int32_t head_dim) {
 
 size_t semkv_kv4_pages_workspace_bytes(const semkv_kv4_cache* cache, int32_t n, int32_t tokens) {
   Kv4Cache c;
-  if (check_kv4(cache, c) != SEMKV_OK || check_list(n, nullptr) != SEMKV_OK || tokens < 0) return 0;
-  return kv4_pages_workspace(c, n, tokens);
+  if (check_kv4(cache, c) != SEMKV_OK || check_list(n, nullptr) != SEMKV_OK ) return 0;
+  return kv4_pages_workspace(c, n, tokens, tokens >= 0);
 }
 
 semkv_status semkv_kv4_reserve(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch, void* ws, size_t ws_bytes,
@@ -107,7 +107,7 @@ semkv_status semkv_kv4_reserve(const semkv_kv4_cache* cache, const semkv_kv4_bat
   s = check_kv4_batch(batch, true, b);
   if (s != SEMKV_OK) return s;
   if (b.n == 0) return SEMKV_OK;
-  s = check_ws(ws, ws_bytes, kv4_pages_workspace(c, b.n, 0));
+  s = check_ws(ws, ws_bytes, kv4_pages_workspace(c, b.n, 0, false));
   if (s != SEMKV_OK) return s;
   const int sms = device_sm_count();
   if (sms <= 0) return SEMKV_ECUDA;
@@ -195,7 +195,7 @@ semkv_status semkv_kv4_compact(const semkv_kv4_cache* cache, int32_t n, const in
   if (s != SEMKV_OK) return s;
   if (tokens < 0 || (n > 0 && tokens > 0 && !keep)) return SEMKV_EINVAL;
   if (n == 0) return SEMKV_OK;
-  s = check_ws(ws, ws_bytes, kv4_pages_workspace(c, n, tokens));
+  s = check_ws(ws, ws_bytes, kv4_pages_workspace(c, n, tokens, true));
   if (s != SEMKV_OK) return s;
   const int sms = device_sm_count();
   if (sms <= 0) return SEMKV_ECUDA;

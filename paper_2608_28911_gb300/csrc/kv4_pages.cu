@@ -15,22 +15,25 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kMoveThreads = 256;
 
-// Workspace: [claim: max_seqs][offset: n + 1][kept: n][pairs: 2 n][counters: 4][list: num_pages]
-// [source: n * tokens], 32-bit words.
+// Workspace: [claim: max_seqs][offset: n + 1][kept: n][held: n][pairs: 2 n][counters: 4][list: num_pages]
+// and for compact [old: n * max_pages][source: n * tokens], 32-bit words.
 struct PagesWs {
   int32_t* claim;   // lowest list index that names the sequence
   int32_t* offset;  // first of the i-th sequence's new pages in the list; bit 31: copy its last page
-  int32_t* kept;    // (compact) flagged tokens that stay
+  int32_t* kept;    // (compact) flagged tokens that stay, and all tokens that there were
+  int32_t* held;
   int2* pairs;      // (reserve) pages to copy: from, to
   int32_t* counters;  // [0] pages to copy, [1] new pages (-1: refused)
   int32_t* list;    // new pages, ascending
-  int32_t* source;  // (compact) [n][tokens] position of each token that stays
+  int32_t* old;     // (compact) [n][max_pages] the sequences' pages before the call
+  int32_t* source;  // (compact) [n][tokens] position of each flagged token that stays
 };
 
 __host__ __device__ inline int64_t pad4(int64_t words) { return (words + 3) & ~(int64_t)3; }
 
-int64_t ws_words(int64_t max_seqs, int64_t n, int64_t num_pages, int64_t tokens) {
-  return pad4(max_seqs) + pad4(n + 1) + pad4(n) + pad4(2 * n) + 4 + pad4(num_pages) + pad4(n * tokens);
+int64_t ws_words(const Kv4Cache& c, int64_t n, int64_t tokens, bool compact) {
+  return pad4(c.max_seqs) + pad4(n + 1) + 2 * pad4(n) + pad4(2 * n) + 4 + pad4(c.num_pages) +
+         (compact ? pad4(n * c.max_pages) + pad4(n * tokens) : 0);
 }
 
 PagesWs carve(const Kv4Cache& c, int n, void* ws) {
@@ -42,12 +45,16 @@ PagesWs carve(const Kv4Cache& c, int n, void* ws) {
   p += pad4((int64_t)n + 1);
   w.kept = p;
   p += pad4(n);
+  w.held = p;
+  p += pad4(n);
   w.pairs = reinterpret_cast<int2*>(p);
   p += pad4(2 * (int64_t)n);
   w.counters = p;
   p += 4;
   w.list = p;
   p += pad4(c.num_pages);
+  w.old = p;
+  p += pad4((int64_t)n * c.max_pages);
   w.source = p;
   return w;
 }
@@ -346,7 +353,8 @@ __global__ void __launch_bounds__(128) kv4_free_kernel(Kv4Cache c, int n, const 
 
 // ------------------------------------------------------------- compact ------
 
-// Positions of the flagged tokens of one sequence, in order.
+// Positions of the flagged tokens of one sequence, in order, and its pages as they were: the kernels
+// behind read these, so that the table may change while the rows are still on their way.
 __global__ void __launch_bounds__(kPlanThreads) kv4_keep_kernel(Kv4Cache c, const int32_t* seqs, const uint8_t* keep,
                                                                 int tokens, PagesWs w) {
   __shared__ int64_t sums[32];
@@ -355,6 +363,8 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_keep_kernel(Kv4Cache c, cons
   const int i = blockIdx.x, s = seqs ? seqs[i] : i;
   if (s < 0 || s >= c.max_seqs) return;
   const int held = tokens_of(c, s), flagged = held < tokens ? held : tokens;
+  for (int k = threadIdx.x; k < pages_for(c, held); k += kPlanThreads)
+    w.old[(int64_t)i * c.max_pages + k] = c.table[(int64_t)s * c.max_pages + k];
   const uint8_t* flags = keep + (int64_t)i * tokens;
   int32_t* source = w.source + (int64_t)i * tokens;
   const bool wide = ((uintptr_t)flags & 15) == 0;
@@ -378,12 +388,15 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_keep_kernel(Kv4Cache c, cons
     for (; bits; bits &= bits - 1) source[at++] = t + __ffs(bits) - 1;
     carry += total;
   }
-  if (threadIdx.x == 0) w.kept[i] = (int)carry;
+  if (threadIdx.x == 0) {
+    w.kept[i] = (int)carry;
+    w.held[i] = held;
+  }
 }
 
 // tokens that stay: the flagged ones, then all behind the flags
-__device__ __forceinline__ int left_of(const Kv4Cache& c, const PagesWs& w, int i, int s, int tokens) {
-  const int held = tokens_of(c, s);
+__device__ __forceinline__ int left_of(const PagesWs& w, int i, int tokens) {
+  const int held = w.held[i];
   return w.kept[i] + (held > tokens ? held - tokens : 0);
 }
 
@@ -399,7 +412,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_compact_plan_kernel(Kv4Cache
     int64_t need = 0;
     if (i < n) {
       const int s = claimed_seq(c, i, seqs, w.claim);
-      if (s >= 0) need = pages_for(c, left_of(c, w, i, s, tokens));
+      if (s >= 0) need = pages_for(c, left_of(w, i, tokens));
       else raise_error(c.err, kDevIndex);
     }
     int64_t total;
@@ -416,105 +429,104 @@ __global__ void __launch_bounds__(kPlanThreads) kv4_compact_plan_kernel(Kv4Cache
   }
 }
 
-// Rows of one new page of one layer: a CTA looks the rows' old places up once, then
-// moves them head by head, 16 bytes at a time.
+// One piece of heads h0, h0 + step, ...: N loads on their way before the first store.
+template <typename T, int N>
+__device__ __forceinline__ void copy_heads(uint8_t* dst, const uint8_t* src, int64_t stride, int h0, int step, int H) {
+  for (int h = h0; h < H; h += N * step) {
+    T x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (h + i * step < H) x[i] = *reinterpret_cast<const T*>(src + (h + i * step) * stride);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (h + i * step < H) *reinterpret_cast<T*>(dst + (h + i * step) * stride) = x[i];
+  }
+}
+
+// The first n CTAs put a sequence's new pages in the old ones' place; the others move rows, a unit of
+// one new page of one layer at a time.  A thread has a row, K or V, and a 16-byte piece of its codes for
+// all heads, so that its addresses are worked out once and the heads' loads follow one another.
 template <int D>
-__global__ void __launch_bounds__(kMoveThreads) kv4_move_kernel(Kv4Cache c, int n, const int32_t* seqs,
-                                                                int tokens, PagesWs w) {
-  __shared__ int64_t from[128];  // byte offset of the row's tile in (layer 0, its page, head 0), + row
-  __shared__ int rows_s, seq_s, first_s, i_s;
-  constexpr int kCodes = D / 2 / 16;  // 16-byte pieces of a row's codes
+__global__ void __launch_bounds__(kMoveThreads) kv4_move_kernel(Kv4Cache c, int n, const int32_t* seqs, int tokens, PagesWs w) {
   pdl_wait();
   pdl_trigger();
   const int pages = w.counters[1];
-  const int64_t head_bytes = (int64_t)kv4_tile_bytes(D) << (c.page_shift - 4);
-  for (int64_t u = blockIdx.x; u < (int64_t)pages * c.layers; u += gridDim.x) {
-    const int k = (int)(u / c.layers), layer = (int)(u % c.layers);
-    __syncthreads();  // the unit before is done with the shared words
-    if (threadIdx.x == 0) {
-      // the sequence whose new pages k is among: the last i with offset[i] <= k
-      int lo = 0, hi = n - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (w.offset[mid] <= k) lo = mid; else hi = mid - 1;
+  if (pages < 0) return;
+  if ((int)blockIdx.x < n) {
+    const int i = blockIdx.x, s = claimed_seq(c, i, seqs, w.claim);
+    if (s < 0) return;
+    const int left = left_of(w, i, tokens), used = pages_for(c, w.held[i]), need = pages_for(c, left), at = w.offset[i];
+    int32_t* row = c.table + (int64_t)s * c.max_pages;
+    for (int k = threadIdx.x; k < used; k += kMoveThreads) {  // (need <= used)
+      const int old = w.old[(int64_t)i * c.max_pages + k];
+      if (page_ok(c, old)) atomicSub(c.refs + old, 1);
+      else raise_error(c.err, kDevIndex);
+      if (k < need) {
+        const int page = w.list[at + k];
+        row[k] = page;
+        c.refs[page] = 1;
       }
-      const int s = seqs ? seqs[lo] : lo;
-      i_s = lo;
-      seq_s = s;
-      first_s = (k - w.offset[lo]) << c.page_shift;
-      const int left = left_of(c, w, lo, s, tokens) - first_s;
-      rows_s = left < c.P ? left : c.P;
     }
-    __syncthreads();
-    const int rows = rows_s;
-    if ((int)threadIdx.x < rows) {
-      const int j = first_s + threadIdx.x, kept = w.kept[i_s];
-      const int old = j < kept ? w.source[(int64_t)i_s * tokens + j] : tokens + (j - kept);
-      int page = c.table[(int64_t)seq_s * c.max_pages + (old >> c.page_shift)];
+    if (threadIdx.x == 0) c.length[s] = left;
+    return;
+  }
+  constexpr int kTile = kv4_tile_bytes(D);
+  constexpr int kCodes = D / 2 / 16;  // 16-byte pieces of a row's codes
+  using Scales = typename std::conditional<D == 128, uint2, uint32_t>::type;
+  const int64_t head_bytes = (int64_t)kTile << (c.page_shift - 4);
+  for (int64_t u = blockIdx.x - n; u < (int64_t)pages * c.layers; u += gridDim.x - n) {
+    const int k = (int)(u / c.layers), layer = (int)(u - (int64_t)k * c.layers);
+    int lo = 0, hi = n - 1;  // the sequence whose new pages k is among: the last with offset <= k
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (w.offset[mid] <= k) lo = mid; else hi = mid - 1;
+    }
+    const int first = (k - w.offset[lo]) << c.page_shift, kept = w.kept[lo];
+    const int rows = min(c.P, left_of(w, lo, tokens) - first);
+    uint8_t* to = c.pages + kv4_record(c, layer, w.list[k], 0);
+    // where row r of the page was, in its head 0 record
+    auto from = [&](int r, int& in_tile) {
+      const int j = first + r;
+      const int old = j < kept ? w.source[(int64_t)lo * tokens + j] : tokens + (j - kept);
+      int page = w.old[(int64_t)lo * c.max_pages + (old >> c.page_shift)];
       if (!page_ok(c, page)) {
         raise_error(c.err, kDevIndex);
         page = 0;
       }
       const int in_page = old & (c.P - 1);
-      from[threadIdx.x] = (kv4_record(c, layer, page, 0) + (int64_t)(in_page >> 4) * kv4_tile_bytes(D)) * 16 + (in_page & 15);
-    }
-    __syncthreads();
-    uint8_t* to = c.pages + kv4_record(c, layer, w.list[k], 0);
-    // codes: (head, K or V, row, piece), pieces of neighbouring rows to neighbouring threads
-    const int total = c.H * 2 * rows * kCodes;
-#pragma unroll 4
-    for (int x = threadIdx.x; x < total; x += kMoveThreads) {
-      const int piece = x % kCodes, y = x / kCodes;
-      const int row = y % rows, z = y / rows;
-      const int v = z & 1, h = z >> 1;
-      const int64_t f = from[row];
-      const uint4 data = __ldcs(reinterpret_cast<const uint4*>(c.pages + (f >> 4) + h * head_bytes + v * 8 * D +
-                                                               (int)(f & 15) * (D / 2) + piece * 16));
-      *reinterpret_cast<uint4*>(to + h * head_bytes + (row >> 4) * kv4_tile_bytes(D) + v * 8 * D + (row & 15) * (D / 2) + piece * 16) = data;
-    }
-    // scales, D / 16 bytes a row
-    using Piece = typename std::conditional<D == 128, uint2, uint32_t>::type;
-    const int total2 = c.H * 2 * rows;
-#pragma unroll 2
-    for (int x = threadIdx.x; x < total2; x += kMoveThreads) {
-      const int row = x % rows, z = x / rows;
-      const int v = z & 1, h = z >> 1;
-      const int64_t f = from[row];
-      const Piece data = *reinterpret_cast<const Piece*>(c.pages + (f >> 4) + h * head_bytes + 16 * D + v * D + (int)(f & 15) * (D / 16));
-      *reinterpret_cast<Piece*>(to + h * head_bytes + (row >> 4) * kv4_tile_bytes(D) + 16 * D + v * D + (row & 15) * (D / 16)) = data;
-    }
+      in_tile = in_page & 15;
+      return c.pages + kv4_record(c, layer, page, 0) + (in_page >> 4) * kTile;
+    };
+    // pieces of codes, then of scales; with fewer of them than threads the heads are shared out
+    auto pieces = [&](int total, auto body) {
+      const int share = total >= kMoveThreads ? 1 : kMoveThreads / total;
+      if ((int)threadIdx.x >= total * share && share > 1) return;
+      const int h0 = share > 1 ? threadIdx.x / total : 0;
+      for (int x = share > 1 ? threadIdx.x - h0 * total : threadIdx.x; x < total; x += kMoveThreads) body(x, h0, share);
+    };
+    pieces(rows * 2 * kCodes, [&](int x, int h0, int step) {
+      const int piece = x % kCodes, v = x / kCodes & 1, r = x / (2 * kCodes);
+      int in_tile;
+      const uint8_t* src = from(r, in_tile);
+      src += v * 8 * D + in_tile * (D / 2) + piece * 16;
+      uint8_t* dst = to + (r >> 4) * kTile + v * 8 * D + (r & 15) * (D / 2) + piece * 16;
+      copy_heads<uint4, 8>(dst, src, head_bytes, h0, step, c.H);
+    });
+    pieces(rows * 2, [&](int x, int h0, int step) {
+      const int v = x & 1, r = x >> 1;
+      int in_tile;
+      const uint8_t* src = from(r, in_tile);
+      src += 16 * D + v * D + in_tile * (D / 16);
+      uint8_t* dst = to + (r >> 4) * kTile + 16 * D + v * D + (r & 15) * (D / 16);
+      copy_heads<Scales, 8>(dst, src, head_bytes, h0, step, c.H);
+    });
   }
-}
-
-// The new pages take the old ones' place.
-__global__ void __launch_bounds__(128) kv4_compact_finish_kernel(Kv4Cache c, const int32_t* seqs, int tokens,
-                                                                 PagesWs w) {
-  pdl_wait();
-  pdl_trigger();
-  if (w.counters[1] < 0) return;
-  const int i = blockIdx.x, s = claimed_seq(c, i, seqs, w.claim);
-  if (s < 0) return;
-  const int left = left_of(c, w, i, s, tokens), used = pages_for(c, tokens_of(c, s)), need = pages_for(c, left);
-  __syncthreads();  // every thread has read the length
-  const int at = w.offset[i];
-  int32_t* row = c.table + (int64_t)s * c.max_pages;
-  for (int k = threadIdx.x; k < used; k += blockDim.x) {  // (need <= used)
-    const int old = row[k];
-    if (page_ok(c, old)) atomicSub(c.refs + old, 1);
-    else raise_error(c.err, kDevIndex);
-    if (k < need) {
-      const int page = w.list[at + k];
-      row[k] = page;
-      c.refs[page] = 1;
-    }
-  }
-  if (threadIdx.x == 0) c.length[s] = left;
 }
 
 }  // namespace
 
-size_t kv4_pages_workspace(const Kv4Cache& c, int n, int tokens) {
-  return (size_t)ws_words(c.max_seqs, n, c.num_pages, tokens) * 4;
+size_t kv4_pages_workspace(const Kv4Cache& c, int n, int tokens, bool compact) {
+  return (size_t)ws_words(c, n, tokens, compact) * 4;
 }
 
 cudaError_t launch_kv4_reserve(const Kv4Cache& c, const Kv4Batch& b, void* ws, int sms, cudaStream_t stream) {
@@ -542,9 +554,7 @@ cudaError_t launch_kv4_compact(const Kv4Cache& c, int n, const int32_t* seqs, co
   e = launch_pdl(kv4_compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, c, n, seqs, tokens, w);
   if (e != cudaSuccess) return e;
   auto move = c.D == 128 ? kv4_move_kernel<128> : kv4_move_kernel<64>;
-  e = launch_pdl(move, dim3(6 * sms), dim3(kMoveThreads), 0, stream, c, n, seqs, tokens, w);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(kv4_compact_finish_kernel, dim3(n), dim3(128), 0, stream, c, seqs, tokens, w);
+  return launch_pdl(move, dim3(n + 6 * sms), dim3(kMoveThreads), 0, stream, c, n, seqs, tokens, w);
 }
 
 }  // namespace semkv

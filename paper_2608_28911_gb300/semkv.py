@@ -565,8 +565,8 @@ class KV4Cache:
                                 dev_error=_ptr(self.dev_error))
         self.ref = ctypes.byref(self.s)
 
-    def pages_workspace(self, n: int, tokens: int = 0):
-        """For reserve (tokens 0) or compact (tokens: keep's columns) of up to n sequences."""
+    def pages_workspace(self, n: int, tokens: int = -1):
+        """For reserve, or with keep's columns `tokens` for compact, of up to n sequences."""
         size = LIB.semkv_kv4_pages_workspace_bytes(self.ref, n, tokens)
         return torch.empty(size, dtype=torch.uint8, device=self.pages.device)
 

@@ -349,7 +349,7 @@ def test_cache_past_32_bit_offsets():
 
 # ------------------------------------------------------------ pages ------
 
-def pages_ws(c, n, tokens=0):
+def pages_ws(c, n, tokens=-1):
     ws = c.pages_workspace(n, tokens)
     ws.fill_(255)
     return ws

@@ -57,6 +57,7 @@ def test_tile_and_workspace_sizes(sk):
     assert sk.LIB.semkv_kv4_pages_workspace_bytes(ctypes.byref(c), 2, 1000) >= size + 8000
     assert sk.LIB.semkv_kv4_pages_workspace_bytes(ctypes.byref(cache(sk, head_dim=100)), 2, 0) == 0
     assert sk.LIB.semkv_kv4_pages_workspace_bytes(ctypes.byref(c), -1, 0) == 0
+    assert 4 * (4 + 3 + 2 + 4 + 10) <= sk.LIB.semkv_kv4_pages_workspace_bytes(ctypes.byref(c), 2, -1) < size
 
 
 @pytest.mark.parametrize("field,bad,status", [
@@ -107,7 +108,7 @@ def test_arguments_that_are_refused(sk):
     # workspaces: none, too small, misaligned
     got = calls(sk, c, b, ws=None)
     assert got["reserve"] == EWORKSPACE and got["compact"] == EWORKSPACE
-    size = sk.LIB.semkv_kv4_pages_workspace_bytes(ctypes.byref(c), 2, 0)
+    size = sk.LIB.semkv_kv4_pages_workspace_bytes(ctypes.byref(c), 2, -1)
     assert sk.LIB.semkv_kv4_reserve(ctypes.byref(c), ctypes.byref(b), FAKE, size - 1, None) == EWORKSPACE
     assert sk.LIB.semkv_kv4_reserve(ctypes.byref(c), ctypes.byref(b), FAKE + 8, size, None) == EWORKSPACE
     assert sk.LIB.semkv_kv4_compact(ctypes.byref(c), 2, None, None, 5, FAKE, 1 << 30, None) == EINVAL
