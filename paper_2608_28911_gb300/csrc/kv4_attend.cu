@@ -385,39 +385,52 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
           for (int n = 0; n < NT; ++n) S[h][n][0] = S[h][n][1] = S[h][n][2] = S[h][n][3] = 0.f;
           scores(tl + h * L::kTile, S[h]);
         }
-        // ---- weights
+        // ---- weights: exponents S mul - ref, two rows of a lane at a time
         const bool open = t0 >= most_lo && t0 + 16 * kTogether - 1 <= least_hi;  // every row sees all of it
-        bool over = false;
+        float E[kTogether][NT][4];
+        float top = -INFINITY;
+        auto exponents = [&] {
 #pragma unroll
-        for (int h = 0; h < kTogether; ++h) {
-          const int pos_a = t0 + 16 * h + row_a, pos_b = pos_a + 8;
+          for (int h = 0; h < kTogether; ++h) {
+            const int pos_a = t0 + 16 * h + row_a, pos_b = pos_a + 8;
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int i = 2 * n + x;
-              S[h][n][x] *= mul[i];
-              S[h][n][2 + x] *= mul[i];
+            for (int n = 0; n < NT; ++n) {
+              const uint64_t m2 = pair(mul[2 * n], mul[2 * n + 1]), r2 = pair(-ref[2 * n], -ref[2 * n + 1]);
+              float(&e)[4] = E[h][n];
+              unpair(pair_fma(pair(S[h][n][0], S[h][n][1]), m2, r2), e[0], e[1]);
+              unpair(pair_fma(pair(S[h][n][2], S[h][n][3]), m2, r2), e[2], e[3]);
               if (!open) {
-                if (pos_a < see_lo[i] || pos_a > see_hi[i]) S[h][n][x] = -INFINITY;
-                if (pos_b < see_lo[i] || pos_b > see_hi[i]) S[h][n][2 + x] = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                  if (pos_a < see_lo[2 * n + x] || pos_a > see_hi[2 * n + x]) e[x] = -INFINITY;
+                  if (pos_b < see_lo[2 * n + x] || pos_b > see_hi[2 * n + x]) e[2 + x] = -INFINITY;
+                }
               }
-              over = over || fmaxf(S[h][n][x], S[h][n][2 + x]) > ref[i] + kMost;
+              asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(e[0]), "f"(e[1]));
+              asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(e[2]), "f"(e[3]));
             }
-        }
-        if (__any_sync(~0u, over)) {
+          }
+        };
+        exponents();
+        if (__any_sync(~0u, top > kMost)) {
+          // references move to 2^8 below their rows' largest, and the sums with them
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const int i = 2 * n + x;
-              float top = fmaxf(S[0][n][x], S[0][n][2 + x]);
-              if (kTogether == 2) top = fmaxf(top, fmaxf(S[kTogether - 1][n][x], S[kTogether - 1][n][2 + x]));
-              top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
-              top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
-              top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
-              if (top > ref[i] + kMost) {
-                const float to = top - kHead, f = exp2_approx(ref[i] - to);
+              // (a first reference is so far from the logits that E says nothing of them)
+              float l = -INFINITY;
+#pragma unroll
+              for (int h = 0; h < kTogether; ++h) {
+                if (E[h][n][x] > -INFINITY) l = fmaxf(l, S[h][n][x] * mul[i]);
+                if (E[h][n][2 + x] > -INFINITY) l = fmaxf(l, S[h][n][2 + x] * mul[i]);
+              }
+              l = fmaxf(l, __shfl_xor_sync(~0u, l, 4));
+              l = fmaxf(l, __shfl_xor_sync(~0u, l, 8));
+              l = fmaxf(l, __shfl_xor_sync(~0u, l, 16));
+              if (l > ref[i] + kMost) {
+                const float to = l - kHead, f = exp2_approx(ref[i] - to);
                 ref[i] = to;
                 sum[i] *= f;
 #pragma unroll
@@ -427,19 +440,19 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
                 }
               }
             }
+          exponents();
         }
 #pragma unroll
         for (int h = 0; h < kTogether; ++h) {
           uint32_t pb[NT][2];
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
+            float(&e)[4] = E[h][n];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              S[h][n][x] = exp2_approx(S[h][n][x] - ref[2 * n + (x & 1)]);
-              sum[2 * n + (x & 1)] += S[h][n][x];
-            }
-            pb[n][0] = transpose8x8(pack_half2(S[h][n][0], S[h][n][1]));
-            pb[n][1] = transpose8x8(pack_half2(S[h][n][2], S[h][n][3]));
+            for (int x = 0; x < 4; ++x) e[x] = exp2_approx(e[x]);
+            unpair(pair_add(pair(sum[2 * n], sum[2 * n + 1]), pair_add(pair(e[0], e[1]), pair(e[2], e[3]))), sum[2 * n], sum[2 * n + 1]);
+            pb[n][0] = transpose8x8(pack_half2(e[0], e[1]));
+            pb[n][1] = transpose8x8(pack_half2(e[2], e[3]));
           }
           values(tl + h * L::kTile, s.length - t0 - 16 * h, pb);
         }
