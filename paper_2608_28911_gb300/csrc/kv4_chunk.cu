@@ -22,6 +22,8 @@
 // The reference exponent e of a row moves only when a weight would pass 2^15; its thread then
 // rescales its row of O, which no product touches at that time: the one before has completed
 // (S_t's barrier, which follows it, tells) and the next waits for P_t.
+// A tile of one block only (a few tokens of a large group, the end of a chunk) has both halves work on it:
+// they take its units in turn, and the first puts the two sums together, which halves its time.
 // Tensor memory: S_0, S_1, O_0, O_1, 128 columns each.
 #include "kernels.h"
 #include "kv4_attend.cuh"
@@ -144,7 +146,8 @@ struct Layout {
   static constexpr int stage() { return 6 * kTile; }
   static constexpr int prefix() { return stage() + 8 * kStageBytes; }
   static constexpr int undo() { return prefix() + (kThreads + 2) * 8; }
-  static constexpr int sums() { return undo() + 4 * kBlock * 4; }
+  static constexpr int other() { return undo() + 4 * kBlock * 4; }
+  static constexpr int sums() { return other() + kBlock * 8; }
   static constexpr int bars() { return sums() + 16 * 8; }
   static constexpr int walk() { return bars() + kBarBytes; }
   static constexpr int bytes() { return walk() + kWalkBytes; }
@@ -154,7 +157,7 @@ constexpr int kItems = 4;  // of the ring that hands items from warp to warp
 
 // The barriers, and the two words behind them.
 struct Bars {
-  uint64_t i_full[kItems], i_empty[kItems], q_full[2], q_empty[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t i_full[kItems], i_empty[kItems], q_full[2], q_empty[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2], x_full, x_empty;
   int failed;
   uint32_t tmem;
 };
@@ -380,38 +383,42 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
 // ------------------------------------------------------------- softmax ------
 
 template <int D, bool BF16>
-__device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, const float* undo, uint8_t* stage, Bars* bars, uint32_t tmem) {
+__device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, const float* undo, float2* other, uint8_t* stage, Bars* bars, uint32_t tmem) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = warp >> 2, r = (warp & 3) * 32 + lane;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's tensor memory lanes
   const uint32_t S = tmem + lanes + 128 * t, O = tmem + lanes + 256 + 128 * t;
   volatile int* failed = &bars->failed;
-  uint32_t s_phase = 0, o_phase = 0;
+  uint32_t s_phase = 0, o_phase = 0, x_phase = 0;
   Feed feed{bars, walk.items};
   for (; const Item* item = feed.next(); feed.done()) {
     const Item& it = *item;
-    if (t * kBlock >= it.rows) continue;  // this block has no rows
-    const bool there = t * kBlock + r < it.rows;
+    // with one block of rows both halves work on it, in turn unit by unit, and the first puts the two
+    // results together
+    const bool split = it.rows <= kBlock;
+    const int u0 = it.u0 + (split ? t : 0), u1 = it.u1, step = split ? 2 : 1;
+    if (u0 >= u1) continue;
+    const int rr = split ? r : t * kBlock + r;  // this thread's row of the tile
+    const bool there = rr < it.rows;
     const float gk = a.c.k_scale ? a.c.k_scale[a.layer * a.c.H + it.head] : 1.f;
     const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + it.head] : 1.f;
     const float scale = fabsf(a.scale_log2) * gk;
     float mul = 0.f;
     int lo = 0, hi = 0x7FFFFFFF;  // (a row that is not there sees all: its zeros are nobody's)
     if (there) {
-      hi = it.length - it.count + it.tile * cut.tokens + cut.token_of(t * kBlock + r);
+      hi = it.length - it.count + it.tile * cut.tokens + cut.token_of(rr);
       lo = a.window && hi >= a.window ? hi - a.window + 1 : 0;
     }
     const int most_lo = __reduce_max_sync(~0u, lo), least_hi = __reduce_min_sync(~0u, hi);
     float ref = kNone, sum = 0.f;
     bool ok = true;
-    const int u0 = it.u0, u1 = it.u1;
-    for (int u = u0; u < u1; ++u) {
+    for (int u = u0; u < u1; u += step) {
       ok = wait(&bars->s_full[t], s_phase, failed);
       s_phase ^= 1;
       if (!ok) break;
       fence_after();
       // (S is there, so Q was; never 0: a masked logit stays -infinity)
-      if (u == u0) mul = fmaxf(BF16 ? scale * undo[(feed.n & 1) * 2 * kBlock + t * kBlock + r] : scale, 0x1p-126f);
+      if (u == u0) mul = fmaxf(BF16 ? scale * undo[(feed.n & 1) * 2 * kBlock + rr] : scale, 0x1p-126f);
       const int pos = u * kUnit;
       const bool open = pos >= most_lo && pos + kUnit - 1 <= least_hi;
       // ---- the largest logit
@@ -487,6 +494,29 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     o_phase ^= 1;
     if (!ok) return;
     fence_after();
+    const bool both = split && it.u1 - it.u0 > 1;
+    if (both && t == 1) {
+      other[r] = make_float2(ref, sum);
+      fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(&bars->x_full);
+      // (its half of O is read before the next item may touch it)
+      if (!wait(&bars->x_empty, x_phase, failed)) return;
+      x_phase ^= 1;
+      continue;
+    }
+    float f = 1.f, g = 0.f;  // factors of the halves' sums
+    if (both) {
+      if (!wait(&bars->x_full, x_phase, failed)) return;
+      x_phase ^= 1;
+      fence_after();
+      const float2 o = other[r];
+      const float top = fmaxf(ref, o.x);
+      f = exp2_approx(ref - top);
+      g = exp2_approx(o.x - top);
+      ref = top;
+      sum = sum * f + o.y * g;
+    }
     // ---- the rows, or this range's part of them: 64 bytes of each at a time through the warp's stage, so
     // that a store writes eight rows' 64 bytes and not 32 rows' 16 (which took 6000 cycles an item)
     const bool done = it.u0 == it.first && it.u1 == it.last;
@@ -499,7 +529,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     uint8_t* to[4];  // row 8 i + lane / 4 of the warp's
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int x = t * kBlock + (warp & 3) * 32 + 8 * i + (lane >> 2), j = cut.token_of(x);
+      const int x = rr - lane + 8 * i + (lane >> 2), j = cut.token_of(x);
       to[i] = done ? reinterpret_cast<uint8_t*>(a.out + (first_row + j * a.q_heads + (x - j * a.group)) * D)
                    : reinterpret_cast<uint8_t*>(parts + x * kv4_part_floats(D));
       to[i] = x < it.rows ? to[i] + (lane & 3) * 16 : nullptr;
@@ -513,20 +543,32 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       }
       __syncwarp();
     };
-    uint32_t v[D / 32][32];
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) tmem_load(O + 32 * c, v[c]);
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) tmem_wait(v[c]);
-#pragma unroll
+#pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
+      uint32_t v[32];
+      tmem_load(O + 32 * c, v);
+      if (both) {
+        uint32_t y[32];
+        tmem_load(O + 128 + 32 * c, y);
+        tmem_wait(v);
+        tmem_wait(y);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f + __uint_as_float(y[i]) * g);
+        if (c + 1 == D / 32) {
+          fence_before();
+          __syncwarp();
+          if (lane == 0) arrive(&bars->x_empty);
+        }
+      } else {
+        tmem_wait(v);
+      }
       if (done) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t w[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            w[x] = pack_out<BF16>(__uint_as_float(v[c][8 * i + 2 * x]) * inv, __uint_as_float(v[c][8 * i + 2 * x + 1]) * inv);
+            w[x] = pack_out<BF16>(__uint_as_float(v[8 * i + 2 * x]) * inv, __uint_as_float(v[8 * i + 2 * x + 1]) * inv);
           put[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
         flush(64 * c);
@@ -535,7 +577,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
         for (int half = 0; half < 2; ++half) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            put[i] = make_uint4(v[c][16 * half + 4 * i], v[c][16 * half + 4 * i + 1], v[c][16 * half + 4 * i + 2], v[c][16 * half + 4 * i + 3]);
+            put[i] = make_uint4(v[16 * half + 4 * i], v[16 * half + 4 * i + 1], v[16 * half + 4 * i + 2], v[16 * half + 4 * i + 3]);
           flush(128 * c + 64 * half);
         }
       }
@@ -543,9 +585,9 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     if (there) {
       if (done) {
         if (a.lse)
-          a.lse[first_row + cut.token_of(t * kBlock + r) * (a.q_heads - a.group) + t * kBlock + r] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+          a.lse[first_row + cut.token_of(rr) * (a.q_heads - a.group) + rr] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
       } else {
-        *reinterpret_cast<float2*>(parts + (t * kBlock + r) * kv4_part_floats(D) + D) = make_float2(ref, sum);
+        *reinterpret_cast<float2*>(parts + rr * kv4_part_floats(D) + D) = make_float2(ref, sum);
       }
     }
     fence_before();
@@ -563,13 +605,7 @@ struct Codes {
 };
 
 template <int D>
-__device__ __forceinline__ void load_codes(Codes<D>& x, const uint8_t* codes, const uint8_t* scales, bool there) {
-  if (!there) {
-#pragma unroll
-    for (int i = 0; i < Codes<D>::kWords; ++i) x.w[i] = 0;
-    x.scale = 0;
-    return;
-  }
+__device__ __forceinline__ void load_codes(Codes<D>& x, const uint8_t* codes, const uint8_t* scales) {
   if constexpr (D == 128) {
     const uint4 v = *reinterpret_cast<const uint4*>(codes);
     x.w[0] = v.x, x.w[1] = v.y, x.w[2] = v.z, x.w[3] = v.w;
@@ -603,7 +639,7 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
   const int row = warp * 32 + r8;  // of the unit; the lane's further rows are 8, 16, 24 behind
   volatile int* failed = &bars->failed;
   const int64_t head_bytes = (int64_t)kv4_tile_bytes(D) << (a.c.page_shift - 4);
-  const int at_codes = q * (D / 8), at_scale = 16 * D + q * (D / 64);
+  const int at_codes = r8 * (D / 2) + q * (D / 8), at_scale = 16 * D + r8 * (D / 16) + q * (D / 64);
   uint8_t* to = smem + (row >> 3) * L::kGroup + r8 * 16 + q * (D / 32) * L::kChunk;
   const int64_t page_stride = head_bytes * a.c.H;
   // the unit whose codes are loaded next, of the item [.., u1) with `length` tokens
@@ -638,11 +674,20 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
   };
   auto load = [&](Codes<D>(&x)[4], bool is_v) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int token = u * kUnit + row + 8 * i, in_tile = token & 15;
-      const uint8_t* tile = base + page[i >> 1] * page_stride + (int64_t)((token & (a.c.P - 1)) >> 4) * kv4_tile_bytes(D);
-      load_codes<D>(x[i], tile + (is_v ? 8 * D : 0) + in_tile * (D / 2) + at_codes,
-                    tile + (is_v ? D : 0) + at_scale + in_tile * (D / 16), token < length);
+    for (int half = 0; half < 2; ++half) {  // a tile: rows r8 and r8 + 8 of it
+      const int token = u * kUnit + warp * 32 + 16 * half;
+      const uint8_t* tile = base + page[half] * page_stride + ((token & (a.c.P - 1)) >> 4) * kv4_tile_bytes(D);
+      const uint8_t* codes = tile + at_codes + (is_v ? 8 * D : 0);
+      const uint8_t* scales = tile + at_scale + (is_v ? D : 0);
+      // (rows behind the last token may be anything, a tile without tokens is not there at all)
+      if (token < length) {
+        load_codes<D>(x[2 * half], codes, scales);
+        load_codes<D>(x[2 * half + 1], codes + 8 * (D / 2), scales + 8 * (D / 16));
+      }
+      if (token + 16 > length) {
+        if (token + r8 >= length) x[2 * half] = Codes<D>{};
+        if (token + r8 + 8 >= length) x[2 * half + 1] = Codes<D>{};
+      }
     }
   };
   Codes<D> k[4], v[4];
@@ -688,8 +733,8 @@ __device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCu
   constexpr uint32_t kHigh = desc_high(L::kGroup), vHigh = desc_high(L::kChunk);
   const uint32_t k0 = desc_low(at + L::k(0), L::kChunk), q0 = desc_low(at + L::q(0), L::kChunk);
   const uint32_t v0 = desc_low(at + L::v(0), L::kGroup);
-  auto scores = [&](int t, uint32_t b) {  // S_t = Q_t K^T
-    const uint32_t q = q0 + t * (L::kTile >> 4), k = k0 + b * (L::kTile >> 4);
+  auto scores = [&](int block, int t, uint32_t b) {  // S_t = Q_block K^T
+    const uint32_t q = q0 + block * (L::kTile >> 4), k = k0 + b * (L::kTile >> 4);
 #pragma unroll
     for (int x = 0; x < D / 16; ++x)
       mma_ss(leader, tmem + 128 * t, q + x * (2 * L::kChunk >> 4), k + x * (2 * L::kChunk >> 4), kHigh, instr_desc(kUnit, false),
@@ -698,41 +743,79 @@ __device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCu
   };
   uint32_t n = 0, q_phase = 0, p_phase = 0;  // units so far; a bit for each block
   Feed feed{bars, walk.items};
+  auto values = [&](int t, uint32_t b, bool add) {  // O_t += P_t V
+    const uint32_t v = v0 + b * (L::kTile >> 4);
+#pragma unroll
+    for (int x = 0; x < kUnit / 16; ++x)
+      mma_ts(leader, tmem + 256 + 128 * t, tmem + 128 * t + 8 * x, v + x * (2 * L::kGroup >> 4), vHigh, instr_desc(D, true),
+             (uint32_t)(add || x > 0));
+  };
+  auto queries = [&](int t) {
+    const bool ok = wait(&bars->q_full[t], q_phase >> t & 1, failed);
+    q_phase ^= 1u << t;
+    return ok;
+  };
+  auto weights = [&](int t) {
+    const bool ok = wait(&bars->p_full[t], p_phase >> t & 1, failed);
+    p_phase ^= 1u << t;
+    fence_after();
+    return ok;
+  };
   while (const Item* item = feed.next()) {
-    const int blocks = item->rows > kBlock ? 2 : 1, units = item->u1 - item->u0;
+    const bool split = item->rows <= kBlock;
+    const int units = item->u1 - item->u0;
     feed.done();
-    for (int t = 0; t < blocks; ++t) {
-      if (!wait(&bars->q_full[t], q_phase >> t & 1, failed)) return;
-      q_phase ^= 1u << t;
+    if (!queries(0) || (!split && !queries(1))) return;
+    if (split) {
+      // the halves take units in turn: S_0 and S_1 are of neighbouring units
+      for (int u = 0; u < units && u < 2; ++u) {
+        const uint32_t m = n + u;
+        if (!wait(&bars->k_full[m & 1], m >> 1 & 1, failed)) return;
+        fence_after();
+        scores(0, u, m & 1);
+        commit(leader, &bars->k_empty[m & 1]);
+        if (u + 1 == units) commit(leader, &bars->q_empty[0]);
+      }
+      for (int u = 0; u < units; ++u, ++n) {
+        const uint32_t b = n & 1;
+        const int t = u & 1;
+        if (!wait(&bars->v_full[b], n >> 1 & 1, failed) || !weights(t)) return;
+        values(t, b, u > 1);
+        commit(leader, &bars->v_empty[b]);
+        if (u + 2 < units) {
+          if (!wait(&bars->k_full[b], (n + 2) >> 1 & 1, failed)) return;
+          fence_after();
+          scores(0, t, b);
+          commit(leader, &bars->k_empty[b]);
+          if (u + 3 == units) commit(leader, &bars->q_empty[0]);
+        } else {
+          commit(leader, &bars->o_full[t]);
+        }
+      }
+      continue;
     }
     if (!wait(&bars->k_full[n & 1], n >> 1 & 1, failed)) return;
     fence_after();
-    for (int t = 0; t < blocks; ++t) {
-      scores(t, n & 1);
+    for (int t = 0; t < 2; ++t) {
+      scores(t, t, n & 1);
       if (units == 1) commit(leader, &bars->q_empty[t]);
     }
     commit(leader, &bars->k_empty[n & 1]);
     for (int u = 0; u < units; ++u, ++n) {
       const uint32_t b = n & 1;
       if (!wait(&bars->v_full[b], n >> 1 & 1, failed)) return;
-      for (int t = 0; t < blocks; ++t) {
-        if (!wait(&bars->p_full[t], p_phase >> t & 1, failed)) return;
-        p_phase ^= 1u << t;
-        fence_after();
-        const uint32_t v = v0 + b * (L::kTile >> 4);
-#pragma unroll
-        for (int x = 0; x < kUnit / 16; ++x)  // O_t += P_t V
-          mma_ts(leader, tmem + 256 + 128 * t, tmem + 128 * t + 8 * x, v + x * (2 * L::kGroup >> 4), vHigh, instr_desc(D, true),
-                 (uint32_t)(u > 0 || x > 0));
-        if (t == blocks - 1) commit(leader, &bars->v_empty[b]);
+      for (int t = 0; t < 2; ++t) {
+        if (!weights(t)) return;
+        values(t, b, u > 0);
+        if (t == 1) commit(leader, &bars->v_empty[b]);
         if (u + 1 < units) {
           if (t == 0) {
             if (!wait(&bars->k_full[b ^ 1], (n + 1) >> 1 & 1, failed)) return;
             fence_after();
           }
-          scores(t, b ^ 1);
+          scores(t, t, b ^ 1);
           if (u + 2 == units) commit(leader, &bars->q_empty[t]);
-          if (t == blocks - 1) commit(leader, &bars->k_empty[b ^ 1]);
+          if (t == 1) commit(leader, &bars->k_empty[b ^ 1]);
         } else {
           commit(leader, &bars->o_full[t]);
         }
@@ -769,6 +852,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
       init(&bars->p_full[x], 4);
       init(&bars->o_full[x], 1);
     }
+    init(&bars->x_full, 4);
+    init(&bars->x_empty, 4);
     bars->failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -792,7 +877,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
     // 176 + 176 + 88 + 72 = 4 * 128, the registers of the launch
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-      softmax_warps<D, BF16>(a, cut, walk, undo, smem + L::stage(), bars, tmem);
+      softmax_warps<D, BF16>(a, cut, walk, undo, reinterpret_cast<float2*>(smem + L::other()), smem + L::stage(), bars, tmem);
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
       code_warps<D>(a, cut, walk, smem, bars);
