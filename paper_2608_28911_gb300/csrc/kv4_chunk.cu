@@ -642,13 +642,18 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
   const int at_codes = r8 * (D / 2) + q * (D / 8), at_scale = 16 * D + r8 * (D / 16) + q * (D / 64);
   uint8_t* to = smem + (row >> 3) * L::kGroup + r8 * 16 + q * (D / 32) * L::kChunk;
   const int64_t page_stride = head_bytes * a.c.H;
-  // the unit whose codes are loaded next, of the item [.., u1) with `length` tokens
+  // Two units ahead of the one in hand: of `next` the pages' numbers are on their way, of the one before it
+  // the warp's two tiles are known and their codes are loaded.
   const uint8_t* base = nullptr;
   const int32_t* table = nullptr;
   int u = 0, u1 = 0, length = 0;
-  int page[2];  // of the warp's two tiles of it
+  int page[2], next_left = 0;           // left: tokens from the warp's first on
+  const uint8_t* next_base = nullptr;
+  int next_in_page = 0;
+  const uint8_t* tile[2];
+  int left = 0;
   Feed feed{bars, walk.items};
-  // the next unit, this item's or the next one's, and its pages
+  // the next unit, this item's or the next one's: its pages' numbers are asked for
   auto step = [&] {
     if (++u >= u1) {
       const Item* it = feed.next();
@@ -658,47 +663,59 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
       u = it->u0, u1 = it->u1, length = it->length;
       feed.done();
     }
+    const int token = u * kUnit + warp * 32;
+    next_base = base;
+    next_left = length - token;
+    next_in_page = token & (a.c.P - 1);
+    page[0] = next_left > 0 ? table[token >> a.c.page_shift] : 0;
+    page[1] = next_left > 16 ? table[(token + 16) >> a.c.page_shift] : 0;
+    return true;
+  };
+  // the numbers are there: its tiles
+  auto find_tiles = [&] {
+    left = next_left;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int token = u * kUnit + warp * 32 + 16 * x;
-      page[x] = 0;
-      if (token < length) {
-        page[x] = table[token >> a.c.page_shift];
-        if ((unsigned)page[x] >= (unsigned)a.c.num_pages) {
-          raise_error(a.c.err, kDevIndex);
-          page[x] = 0;
-        }
+      if ((unsigned)page[x] >= (unsigned)a.c.num_pages) {
+        raise_error(a.c.err, kDevIndex);
+        page[x] = 0;
       }
+      const int in_page = (next_in_page + 16 * x) & (a.c.P - 1);
+      tile[x] = next_base + page[x] * page_stride + (in_page >> 4) * kv4_tile_bytes(D) + at_codes;
     }
-    return true;
   };
   auto load = [&](Codes<D>(&x)[4], bool is_v) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {  // a tile: rows r8 and r8 + 8 of it
-      const int token = u * kUnit + warp * 32 + 16 * half;
-      const uint8_t* tile = base + page[half] * page_stride + ((token & (a.c.P - 1)) >> 4) * kv4_tile_bytes(D);
-      const uint8_t* codes = tile + at_codes + (is_v ? 8 * D : 0);
-      const uint8_t* scales = tile + at_scale + (is_v ? D : 0);
+      const uint8_t* codes = tile[half] + (is_v ? 8 * D : 0);
+      const uint8_t* scales = tile[half] + (is_v ? D : 0) + (at_scale - at_codes);
+      const int here = left - 16 * half;
       // (rows behind the last token may be anything, a tile without tokens is not there at all)
-      if (token < length) {
+      if (here > 0) {
         load_codes<D>(x[2 * half], codes, scales);
         load_codes<D>(x[2 * half + 1], codes + 8 * (D / 2), scales + 8 * (D / 16));
       }
-      if (token + 16 > length) {
-        if (token + r8 >= length) x[2 * half] = Codes<D>{};
-        if (token + r8 + 8 >= length) x[2 * half + 1] = Codes<D>{};
+      if (here < 16) {
+        if (r8 >= here) x[2 * half] = Codes<D>{};
+        if (r8 + 8 >= here) x[2 * half + 1] = Codes<D>{};
       }
     }
   };
   Codes<D> k[4], v[4];
   uint32_t n = 0;  // units so far
-  bool more = step();
+  bool more = step(), ahead = false;
   if (more) {
+    find_tiles();
     load(k, false);
     load(v, true);
+    ahead = step();
   }
   for (; more; ++n) {
-    more = step();  // the pages of the next unit are on their way behind this one's stores
+    more = ahead;
+    if (more) {
+      find_tiles();
+      ahead = step();
+    }
     const int b = n & 1;
     const uint32_t free_phase = (n >> 1 & 1) ^ 1;
     if (!wait(&bars->k_empty[b], free_phase, failed)) return;
@@ -982,8 +999,10 @@ cudaError_t launch_chunk(const Kv4Attend& a, const Kv4ManyCut& cut, int sms, cud
 
 }  // namespace
 
-bool kv4_many(const Kv4Batch& b, int group) {
-  return (int64_t)b.max_count * group > 64 && group <= 2 * kBlock;
+bool kv4_many(const Kv4Batch& b, int group, int D) {
+  // one tile of the small kernel holds up to 32 rows, 48 at head dim 64; more would read the cache again.
+  // 8 sequences of 32K, head dim 128: 20 rows 117 us there and 190 here, 36 rows 261 and 190.
+  return (int64_t)b.max_count * group > (D == 128 ? 32 : 48) && group <= 2 * kBlock;
 }
 
 size_t kv4_many_part_floats(int D, int sms) { return (size_t)2 * sms * 2 * kBlock * kv4_part_floats(D); }
