@@ -256,6 +256,15 @@ def test_large_groups(group):
     attend(c, plain, [1, 3, 2], group, torch.float16)
 
 
+@pytest.mark.parametrize("H,count", [(1, 8), (2, 12), (3, 40)])
+def test_few_tiles_with_many_parts(H, count):
+    """One long sequence whose few tiles are spread over all CTAs, the first rows of one without a past."""
+    import torch
+    c = make([9001, 5], H, 128, 32, seed=21)
+    plain = fill(c)
+    attend(c, plain, [count, 8], 8, torch.float16)
+
+
 def test_many_sequences():
     import torch
     rng = np.random.default_rng(0)
