@@ -9,10 +9,11 @@
 // so that 256 rows share the work of turning a unit's codes into fp16, and one block's softmax runs
 // while the other's products do.  Sixteen warps:
 //   0-3, 4-7  the softmax of block 0 and 1 (a warp's tensor memory lanes are those of warp % 4)
-//   8-11      the unit's codes to fp16 K and V in shared memory, two buffers each, codes
-//             loaded into registers a unit ahead
+//   8-11      the unit's codes to fp16 K and V in shared memory, two buffers each, the codes
+//             loaded into registers a unit ahead and the page numbers two
 //   12        issues the products
 //   13-15     the query rows, those of the next item while the last unit of this one is at work
+// One of the last walks the range and hands its items to all through a ring in shared memory.
 // A softmax thread holds its row's 128 logits of a unit in registers, so tensor memory is read once
 // for them: the warpgroups share the launch's 4 x 128 registers a thread as 176, 176, 88, 72.
 // The core matrices (8 rows of 16 bytes) of a K or V unit lie 128 bytes apart along the head dim and
@@ -87,6 +88,11 @@ __device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, 
       "r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "r"(add)
       : "memory");
 }
+__device__ __forceinline__ uint32_t elect() {
+  uint32_t leader;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(leader));
+  return leader;
+}
 __device__ __forceinline__ void commit(uint32_t leader, uint64_t* bar) {
   asm volatile(
       "{\n .reg .pred l;\n setp.ne.u32 l, %1, 0;\n"
@@ -157,7 +163,7 @@ constexpr int kItems = 4;  // of the ring that hands items from warp to warp
 
 // The barriers, and the two words behind them.
 struct Bars {
-  uint64_t i_full[kItems], i_empty[kItems], q_full[2], q_empty[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2], x_full, x_empty;
+  uint64_t i_full[kItems], i_empty[kItems], q_full[2], q_empty[2], k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2], x_full, x_empty, drain;
   int failed;
   uint32_t tmem;
 };
@@ -741,12 +747,11 @@ __device__ __forceinline__ void code_warps(const Kv4Attend& a, const Kv4ManyCut&
 // ------------------------------------------------------------ products ------
 
 template <int D>
-__device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, uint8_t* smem, Bars* bars, uint32_t tmem) {
+__device__ __forceinline__ void product_warp(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, uint8_t* smem, Bars* bars, uint32_t tmem,
+                                             uint32_t leader) {
   using L = Layout<D>;
   volatile int* failed = &bars->failed;
   const uint32_t at = smem_addr(smem);
-  uint32_t leader;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(leader));
   constexpr uint32_t kHigh = desc_high(L::kGroup), vHigh = desc_high(L::kChunk);
   const uint32_t k0 = desc_low(at + L::k(0), L::kChunk), q0 = desc_low(at + L::q(0), L::kChunk);
   const uint32_t v0 = desc_low(at + L::v(0), L::kGroup);
@@ -871,6 +876,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
     }
     init(&bars->x_full, 4);
     init(&bars->x_empty, 4);
+    init(&bars->drain, 1);
     bars->failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -900,9 +906,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
       code_warps<D>(a, cut, walk, smem, bars);
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-      if (warp == 12)
-        product_warp<D>(a, cut, walk, smem, bars, tmem);
-      else
+      if (warp == 12) {
+        const uint32_t leader = elect();
+        product_warp<D>(a, cut, walk, smem, bars, tmem, leader);
+        if (__any_sync(~0u, *(volatile int*)&bars->failed)) {
+          // products still at work are waited for, as long again
+          commit(leader, &bars->drain);
+          mbar_wait_bounded(&bars->drain, 0);
+        }
+      } else
         query_warps<D, BF16>(a, cut, walk, smem, bars, undo);
     }
   }

@@ -274,6 +274,61 @@ def test_many_sequences():
     attend(c, plain, [int(x) for x in rng.integers(0, 3, 700)], 2, torch.float16)
 
 
+@pytest.mark.parametrize("group,counts", [(2, 1), (4, 20)])
+def test_many_ragged_prompts_and_a_sequence_listed_twice(group, counts):
+    """More sequences than a CTA has threads, in both kernels; some sequences are asked twice, and
+    lse is left away."""
+    import torch
+    rng = np.random.default_rng(1)
+    lens = [int(x) for x in rng.integers(0, 60, 1200)]
+    c = make(lens, 1, 64, 16, seed=16)
+    plain = fill(c)
+    seqs = [int(x) for x in rng.integers(0, 1200, 1300)]
+    attend(c, plain, [int(x) for x in rng.integers(0, counts + 1, 1300)], group, torch.bfloat16, seqs=seqs, lse=False)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 30, 128, 129])
+def test_windows_at_the_ends_of_their_range(window):
+    import torch
+    c = make([700, 129, 1], 1, 64, 32, seed=17)
+    plain = fill(c)
+    attend(c, plain, [1, 2, 1], 3, torch.float16, window)
+    attend(c, plain, [300, 129, 1], 3, torch.float16, window)
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each, both kernels at work on one cache."""
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    lens = [4000, 900, 2500]
+    c = make(lens, 2, 128, 64, seed=18)
+    fill(c)
+    calls = []
+    for k, counts in enumerate(([1, 1, 1], [200, 64, 1], [3, 1, 2], [500, 1, 130])):
+        rng = np.random.default_rng(k)
+        q = rows_like(rng, (sum(counts), 8, 128), torch.float16)
+        b = semkv.KV4Batch(3, cu=cu_of(counts), total=sum(counts), max_count=max(counts))
+        calls.append((b, q, c.attention_workspace(b, 8)))
+    def run(call, out):
+        b, q, ws = call
+        semkv.semkv_kv4_attention(c, b, 0, q, out, 128 ** -0.5, ws)
+    alone = [torch.empty_like(q) for _, q, _ in calls]
+    for call, out in zip(calls, alone):
+        run(call, out)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    outs = [[torch.empty_like(q) for _, q, _ in calls] for _ in range(5)]
+    for row in outs:
+        for s, call, out in zip(streams, calls, row):
+            with torch.cuda.stream(s):
+                run(call, out)
+    torch.cuda.synchronize()
+    for row in outs:
+        for a, b in zip(alone, row):
+            assert torch.equal(a, b)               # (the same split, the same order of sums)
+    assert int(c.dev_error.item()) == 0
+
+
 def test_large_and_small_logits():
     """Weights far apart, all equal, and logits whose size makes the reference exponent move often."""
     import torch
