@@ -59,9 +59,8 @@ struct Layout {
   static constexpr int bytes() { return ring_bytes() + q_bytes() + kWarps * kStages * 8 + (kThreads + 1) * 8 + kWarps * 8; }
 };
 
-// An item's start counts for two units (with one, ragged batches end 15% later; with four it is the same);
-// a range has four at least (fewer cost the join more than they save: one session at 4K 13.6, 16.3, 21.9 us
-// with ranges of 4, 2, 1).
+// An item's start counts for two units (with one, ragged batches end 15% later; with three or four it is the
+// same); a range has four at least (fewer cost the join what they save).
 __host__ __device__ constexpr Kv4FewCut few_cut(int n_tiles) { return Kv4FewCut{8 * n_tiles, kUnit, 2, 4}; }
 
 // The fragments of eight query rows (row0 + g) for one KV head, w[2k], w[2k + 1] those of k step k.
@@ -511,11 +510,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
 }
 
 // Joins the parts of the items that several workers share: a CTA for each query row, whose warps take
-// the parts in turn.  (A warp for each row is slower even where most items have few parts: the long
-// sequences of a ragged batch have fifty.)
-constexpr int kJoinWarps = 4;
-
-template <int D, bool BF16>
+// the parts in turn: eight where the CTAs of all rows are then resident at once, else four (the long
+// sequences of a ragged batch have fifty parts).  One session at 4K takes 16.1, 13.6, 11.8 us in all with
+// 2, 4, 8 warps, 61 ragged sequences 42.0, 39.8, 41.0.
+template <int D, bool BF16, int kJoinWarps>
 __global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, int rows_tile) {
   __shared__ float acc[kJoinWarps][D];
   __shared__ float2 sums[kJoinWarps];  // reference exponent, weight sum
@@ -580,6 +578,17 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, 
     for (int d = 0; d < kDims / 2; ++d) to[d] = pack_out<BF16>(o[2 * d] * inv, o[2 * d + 1] * inv);
     if (a.lse && lane == 0) a.lse[at] = total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
   }
+}
+
+template <bool BF16, int WARPS>
+cudaError_t launch_join_of(const Kv4Attend& a, int rows_tile, cudaStream_t stream) {
+  const int64_t rows = (int64_t)a.b.max_count * a.q_heads;
+  auto kernel = a.c.D == 128 ? kv4_join_kernel<128, BF16, WARPS> : kv4_join_kernel<64, BF16, WARPS>;
+  return launch_pdl(kernel, dim3(a.b.n, (unsigned)(rows < 4096 ? rows : 4096)), dim3(WARPS * 32), 0, stream, a, rows_tile);
+}
+template <bool BF16>
+cudaError_t launch_join(const Kv4Attend& a, int rows_tile, int64_t warps, cudaStream_t stream) {
+  return warps >= 8 ? launch_join_of<BF16, 8>(a, rows_tile, stream) : launch_join_of<BF16, 4>(a, rows_tile, stream);
 }
 
 template <int D, int NT, bool BF16>
@@ -659,10 +668,8 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
       c.D == 128 ? (bf ? launch_few_rows<128, true>(a, n, ctas, stream) : launch_few_rows<128, false>(a, n, ctas, stream))
                  : (bf ? launch_few_rows<64, true>(a, n, ctas, stream) : launch_few_rows<64, false>(a, n, ctas, stream));
   if (e != cudaSuccess) return e;
-  auto join = c.D == 128 ? (bf ? kv4_join_kernel<128, true> : kv4_join_kernel<128, false>)
-                         : (bf ? kv4_join_kernel<64, true> : kv4_join_kernel<64, false>);
-  const int64_t rows = (int64_t)b.max_count * q_heads;
-  return launch_pdl(join, dim3(b.n, (unsigned)(rows < 4096 ? rows : 4096)), dim3(kJoinWarps * 32), 0, stream, a, 8 * n);
+  const int64_t rows = (int64_t)b.max_count * q_heads, warps = (int64_t)80 * sms / (rows * b.n);
+  return bf ? launch_join<true>(a, 8 * n, warps, stream) : launch_join<false>(a, 8 * n, warps, stream);
 }
 
 }  // namespace semkv
