@@ -496,6 +496,23 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       __syncwarp();
       if (lane == 0) arrive(&bars->p_full[t]);
     }
+    // ---- while the last products run: where the rows go, or this range's part of them.  They go 64 bytes of
+    // each at a time through the warp's stage, so that a store writes eight rows' 64 bytes and not 32 rows'
+    // 16 (which took 6000 cycles an item).
+    const bool done = it.u0 == it.first && it.u1 == it.last;
+    uint8_t* mine = stage + warp * kStageBytes;
+    uint4* put = reinterpret_cast<uint4*>(mine + lane * kStagePitch);
+    const uint4* get = reinterpret_cast<const uint4*>(mine + (lane >> 2) * kStagePitch + (lane & 3) * 16);
+    float* parts = a.parts + (int64_t)(2 * blockIdx.x + (it.u0 == it.first ? 1 : 0)) * cut.rows * kv4_part_floats(D);
+    const int64_t first_row = (int64_t)(it.begin + it.tile * cut.tokens) * a.q_heads + it.head * a.group;
+    uint8_t* to[4];  // row 8 i + lane / 4 of the warp's
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = rr - lane + 8 * i + (lane >> 2), j = cut.token_of(x);
+      to[i] = done ? reinterpret_cast<uint8_t*>(a.out + (first_row + j * a.q_heads + (x - j * a.group)) * D)
+                   : reinterpret_cast<uint8_t*>(parts + x * kv4_part_floats(D));
+      to[i] = x < it.rows ? to[i] + (lane & 3) * 16 : nullptr;
+    }
     ok = ok && wait(&bars->o_full[t], o_phase, failed);
     o_phase ^= 1;
     if (!ok) return;
@@ -523,23 +540,7 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       ref = top;
       sum = sum * f + o.y * g;
     }
-    // ---- the rows, or this range's part of them: 64 bytes of each at a time through the warp's stage, so
-    // that a store writes eight rows' 64 bytes and not 32 rows' 16 (which took 6000 cycles an item)
-    const bool done = it.u0 == it.first && it.u1 == it.last;
     const float inv = sum == 0.f ? 0.f : gv / sum;
-    uint8_t* mine = stage + warp * kStageBytes;
-    uint4* put = reinterpret_cast<uint4*>(mine + lane * kStagePitch);
-    const uint4* get = reinterpret_cast<const uint4*>(mine + (lane >> 2) * kStagePitch + (lane & 3) * 16);
-    float* parts = a.parts + (int64_t)(2 * blockIdx.x + (it.u0 == it.first ? 1 : 0)) * cut.rows * kv4_part_floats(D);
-    const int64_t first_row = (int64_t)(it.begin + it.tile * cut.tokens) * a.q_heads + it.head * a.group;
-    uint8_t* to[4];  // row 8 i + lane / 4 of the warp's
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int x = rr - lane + 8 * i + (lane >> 2), j = cut.token_of(x);
-      to[i] = done ? reinterpret_cast<uint8_t*>(a.out + (first_row + j * a.q_heads + (x - j * a.group)) * D)
-                   : reinterpret_cast<uint8_t*>(parts + x * kv4_part_floats(D));
-      to[i] = x < it.rows ? to[i] + (lane & 3) * 16 : nullptr;
-    }
     auto flush = [&](int piece) {  // the stage's rows to byte `piece` of theirs
       __syncwarp();
 #pragma unroll
@@ -549,24 +550,26 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       }
       __syncwarp();
     };
+    // (a loop: code that runs once an item is fetched anew each time, and unrolled it was 4% of a prompt slower)
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
       uint32_t v[32];
       tmem_load(O + 32 * c, v);
+      tmem_wait(v);
       if (both) {
-        uint32_t y[32];
-        tmem_load(O + 128 + 32 * c, y);
-        tmem_wait(v);
-        tmem_wait(y);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f + __uint_as_float(y[i]) * g);
+        for (int half = 0; half < 2; ++half) {
+          uint32_t y[16];
+          tmem_load16(O + 128 + 32 * c + 16 * half, y);
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            v[16 * half + i] = __float_as_uint(__uint_as_float(v[16 * half + i]) * f + __uint_as_float(y[i]) * g);
+        }
         if (c + 1 == D / 32) {
           fence_before();
           __syncwarp();
           if (lane == 0) arrive(&bars->x_empty);
         }
-      } else {
-        tmem_wait(v);
       }
       if (done) {
 #pragma unroll
