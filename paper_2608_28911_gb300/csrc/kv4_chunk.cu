@@ -427,64 +427,94 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       if (u == u0) mul = fmaxf(BF16 ? scale * undo[(feed.n & 1) * 2 * kBlock + rr] : scale, 0x1p-126f);
       const int pos = u * kUnit;
       const bool open = pos >= most_lo && pos + kUnit - 1 <= least_hi;
-      // ---- the largest logit
-      uint32_t v[kUnit / 32][32];
-      float most[kUnit / 32];
-      tmem_load(S, v[0]);
-#pragma unroll
-      for (int c = 0; c < kUnit / 32; ++c) {
-        tmem_wait(v[c]);
-        if (c + 1 < kUnit / 32) tmem_load(S + 32 * (c + 1), v[c + 1]);  // on its way behind this one's maximum
-        if (!open) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const int p = pos + 32 * c + i;
-            if (p < lo || p > hi) v[c][i] = 0xFF800000u;
-          }
-        }
-        float m[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-        for (int i = 0; i < 32; i += 2)
-          asm("max.f32 %0, %0, %1, %2;" : "+f"(m[i >> 1 & 1]) : "f"(__uint_as_float(v[c][i])), "f"(__uint_as_float(v[c][i + 1])));
-        most[c] = fmaxf(m[0], m[1]);
-      }
-      const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * mul;
-      const bool over = top > ref + kMost;
-      if (__any_sync(~0u, over)) {
+      // the reference exponent for a unit whose largest logit is `top`, and the sums with it
+      auto settle = [&](float top) {
+        const bool over = top > ref + kMost;
+        if (!__any_sync(~0u, over)) return;
         float f = 1.f;
         if (over) {
           f = exp2_approx(ref - (top - kHead));
           ref = top - kHead;
           sum *= f;
         }
-        if (u > u0) {
+        if (u == u0) return;
 #pragma unroll 1
-          for (int c = 0; c < D / 16; ++c) {
-            uint32_t o[16];
-            tmem_load16(O + 16 * c, o);
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t o[16];
+          tmem_load16(O + 16 * c, o);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_store16(O + 16 * c, o);
-          }
+          for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+          tmem_store16(O + 16 * c, o);
         }
-      }
-      // ---- weights, in S's place: column pair 32 c + 2 i to column 16 c + i
-      const uint64_t mul2 = pair(mul, mul), ref2 = pair(-ref, -ref);
+      };
+      // the weights of 32 logits: those of columns 2 i, 2 i + 1 into w[i]
       uint64_t sums[2] = {0, 0};
-#pragma unroll
-      for (int c = 0; c < kUnit / 32; ++c) {
-        uint32_t w[16];
+      auto turn = [&](const uint32_t(&v)[32], uint64_t mul2, uint64_t ref2, uint32_t(&w)[16]) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          uint64_t x = pair_fma(pair(__uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1])), mul2, ref2);
-          float lo_x, hi_x;
-          unpair(x, lo_x, hi_x);
-          lo_x = exp2_approx(lo_x);
-          hi_x = exp2_approx(hi_x);
-          sums[i & 1] = pair_add(sums[i & 1], pair(lo_x, hi_x));
-          w[i] = pack_half2(lo_x, hi_x);
+          float x, y;
+          unpair(pair_fma(pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), mul2, ref2), x, y);
+          x = exp2_approx(x);
+          y = exp2_approx(y);
+          sums[i & 1] = pair_add(sums[i & 1], pair(x, y));
+          w[i] = pack_half2(x, y);
         }
-        tmem_store16(S + 16 * c, w);
+      };
+      auto largest = [](const uint32_t(&v)[32]) {
+        float m[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 32; i += 2)
+          asm("max.f32 %0, %0, %1, %2;" : "+f"(m[i >> 1 & 1]) : "f"(__uint_as_float(v[i])), "f"(__uint_as_float(v[i + 1])));
+        return fmaxf(m[0], m[1]);
+      };
+      if (open) {
+        uint32_t v[kUnit / 32][32];
+        float top = -INFINITY;
+        tmem_load(S, v[0]);
+#pragma unroll
+        for (int c = 0; c < kUnit / 32; ++c) {
+          tmem_wait(v[c]);
+          if (c + 1 < kUnit / 32) tmem_load(S + 32 * (c + 1), v[c + 1]);  // on its way behind this one's maximum
+          top = fmaxf(top, largest(v[c]));
+        }
+        settle(top * mul);
+        const uint64_t mul2 = pair(mul, mul), ref2 = pair(-ref, -ref);
+#pragma unroll
+        for (int c = 0; c < kUnit / 32; ++c) {
+          uint32_t w[16];
+          turn(v[c], mul2, ref2, w);
+          tmem_store16(S + 16 * c, w);  // in S's place
+        }
+      } else {
+        // a unit that some row sees a part of: in short loops, since what runs seldom has to be fetched first
+        // (with everything unrolled six ragged prompts took 268 us, so 236)
+        float top = -INFINITY;
+        uint32_t v[32];
+        auto hide = [&](int c) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int p = pos + c + i;
+            if (p < lo || p > hi) v[i] = 0xFF800000u;
+          }
+        };
+#pragma unroll 1
+        for (int c = 0; c < kUnit; c += 32) {
+          tmem_load(S + c, v);
+          tmem_wait(v);
+          hide(c);
+          top = fmaxf(top, largest(v));
+        }
+        settle(top * mul);
+        const uint64_t mul2 = pair(mul, mul), ref2 = pair(-ref, -ref);
+#pragma unroll 1
+        for (int c = 0; c < kUnit; c += 32) {
+          uint32_t w[16];
+          tmem_load(S + c, v);
+          tmem_wait(v);
+          hide(c);
+          turn(v, mul2, ref2, w);
+          tmem_store16(S + c / 2, w);
+        }
       }
       {
         float x, y;
