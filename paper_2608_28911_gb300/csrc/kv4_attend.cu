@@ -514,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
 // sequences of a ragged batch have fifty parts).  One session at 4K takes 16.1, 13.6, 11.8 us in all with
 // 2, 4, 8 warps, 61 ragged sequences 42.0, 39.8, 41.0.
 template <int D, bool BF16, int kJoinWarps>
-__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, int rows_tile) {
+__global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, int rows_tile, int workers) {
   __shared__ float acc[kJoinWarps][D];
   __shared__ float2 sums[kJoinWarps];  // reference exponent, weight sum
   pdl_wait();
@@ -532,8 +532,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, 
     const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
     int begin, count;
     const bool ok = kv4_range(a.b, i, begin, count) && seq >= 0 && seq < a.c.max_seqs;
-    // (a row that is not there, or that was finished where it ran)
-    if (!ok || row >= count * a.group || span.x < 0) continue;
+    // (a row that is not there, or that was finished where it ran; a worker whose wait ran out left no span)
+    if (!ok || row >= count * a.group || span.x < 0 || span.x > span.y || span.y >= workers) continue;
     const int parts = span.y - span.x + 1;
     const int64_t size = (int64_t)rows_tile * kv4_part_floats(D);
     // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
@@ -581,14 +581,16 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv4_join_kernel(Kv4Attend a, 
 }
 
 template <bool BF16, int WARPS>
-cudaError_t launch_join_of(const Kv4Attend& a, int rows_tile, cudaStream_t stream) {
+cudaError_t launch_join_of(const Kv4Attend& a, int rows_tile, int workers, cudaStream_t stream) {
   const int64_t rows = (int64_t)a.b.max_count * a.q_heads;
   auto kernel = a.c.D == 128 ? kv4_join_kernel<128, BF16, WARPS> : kv4_join_kernel<64, BF16, WARPS>;
-  return launch_pdl(kernel, dim3(a.b.n, (unsigned)(rows < 4096 ? rows : 4096)), dim3(WARPS * 32), 0, stream, a, rows_tile);
+  return launch_pdl(kernel, dim3(a.b.n, (unsigned)(rows < 4096 ? rows : 4096)), dim3(WARPS * 32), 0, stream, a, rows_tile,
+                    workers);
 }
 template <bool BF16>
-cudaError_t launch_join(const Kv4Attend& a, int rows_tile, int64_t warps, cudaStream_t stream) {
-  return warps >= 8 ? launch_join_of<BF16, 8>(a, rows_tile, stream) : launch_join_of<BF16, 4>(a, rows_tile, stream);
+cudaError_t launch_join(const Kv4Attend& a, int rows_tile, int workers, int64_t warps, cudaStream_t stream) {
+  return warps >= 8 ? launch_join_of<BF16, 8>(a, rows_tile, workers, stream)
+                    : launch_join_of<BF16, 4>(a, rows_tile, workers, stream);
 }
 
 template <int D, int NT, bool BF16>
@@ -669,7 +671,8 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
                  : (bf ? launch_few_rows<64, true>(a, n, ctas, stream) : launch_few_rows<64, false>(a, n, ctas, stream));
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)b.max_count * q_heads, warps = (int64_t)80 * sms / (rows * b.n);
-  return bf ? launch_join<true>(a, 8 * n, warps, stream) : launch_join<false>(a, 8 * n, warps, stream);
+  return bf ? launch_join<true>(a, 8 * n, ctas * kWarps, warps, stream)
+            : launch_join<false>(a, 8 * n, ctas * kWarps, warps, stream);
 }
 
 }  // namespace semkv
