@@ -323,8 +323,8 @@ typedef struct {
 /* The rows of one step: which sequences take part, and how many rows each has in the
  * row-major tensors of the step's calls (k, v, q, out: [total][heads][head_dim]). */
 typedef struct {
-  int32_t n;             /* sequences that take part, 1..SEMKV_KV4_MAX_SEQS           */
-  int32_t total;         /* rows of the tensors                                       */
+  int32_t n;             /* sequences that take part, 0..SEMKV_KV4_MAX_SEQS           */
+  int32_t total;         /* rows of the tensors, 0..2^30; with 0 they may be NULL     */
   int32_t max_count;     /* no sequence has more rows than this                       */
   const int32_t* seqs;   /* device [n], or NULL for 0 .. n-1                          */
   const int32_t* cu;     /* device [n+1], ascending: rows cu[i] .. cu[i+1]-1 are the
@@ -355,7 +355,7 @@ semkv_status semkv_kv4_reserve(const semkv_kv4_cache* cache, const semkv_kv4_bat
  * + j.  k, v: device [total][kv_heads][head_dim] of type `dtype` with k_stride and v_stride
  * elements from row to row (a multiple of 8, at least kv_heads * head_dim), 16-byte aligned.
  * A row whose position lies outside its table, or whose page index lies outside the pool, is
- * left out (3).  Two rows of a call at one position leave either.
+ * left out (3).  Two rows of a call at one position leave parts of both.
  * semkv_kv4_read is the way back: k_out, v_out [total][kv_heads][head_dim], contiguous,
  * of type `dtype`, take the values (product with g in binary32, rounded once to the type). */
 semkv_status semkv_kv4_write(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch,
@@ -373,8 +373,8 @@ semkv_status semkv_kv4_read(const semkv_kv4_cache* cache, const semkv_kv4_batch*
  *   out[r][h] = sum_t softmax_t(softmax_scale * q[r][h] . K_t) V_t,   0 if it sees nothing
  *   lse[r][h] = ln sum_t exp(softmax_scale * q[r][h] . K_t)            (-inf if nothing)
  * q: device [total][q_heads][head_dim] of type `dtype`, q_stride elements from row to row (a
- * multiple of 8), 16-byte aligned; out: the same type, contiguous; lse: device f32
- * [total][q_heads] or NULL.  `start` is not used.  A sequence out of range or with a wrong row
+ * multiple of 8), 16-byte aligned; out: the same type, contiguous, apart from q; lse: device
+ * f32 [total][q_heads] or NULL.  `start` is not used.  A sequence out of range or with a wrong row
  * range (more than max_count rows among them) is left out, its rows untouched (3); a length
  * past the table counts as the table's end and a page index outside the pool as page 0 (3).
  * Accuracy: products are exact in binary32; the weights are rounded to fp16 before they meet V

@@ -47,10 +47,12 @@ semkv_status check_list(int32_t n, const int32_t* seqs) {
 }
 
 semkv_status check_kv4_batch(const semkv_kv4_batch* b, bool start, Kv4Batch& to) {
-  if (!b || b->total < 0 || b->max_count < 1) return SEMKV_EINVAL;
+  if (!b || b->total < 0 || b->max_count < (b->total > 0)) return SEMKV_EINVAL;
   const semkv_status s = check_list(b->n, b->seqs);
   if (s != SEMKV_OK) return s;
-  if ((!b->cu && b->total < b->n) || (start && !b->start)) return SEMKV_EINVAL;
+  if ((!b->cu && b->total < b->n) || (start && !b->start && b->n > 0)) return SEMKV_EINVAL;
+  // row indices are 32-bit inside the kernels
+  if (b->total > 1 << 30) return SEMKV_EUNSUPPORTED;
   if (!aligned(b->cu, 4) || !aligned(b->start, 4)) return SEMKV_EALIGN;
   to.n = b->n;
   to.total = b->total;
@@ -73,7 +75,7 @@ semkv_status rows(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch, bo
   if (s != SEMKV_OK) return s;
   s = check_kv4_batch(batch, true, b);
   if (s != SEMKV_OK) return s;
-  if (!k || !v || layer < 0 || layer >= c.layers) return SEMKV_EINVAL;
+  if ((b.total > 0 && (!k || !v)) || layer < 0 || layer >= c.layers) return SEMKV_EINVAL;
   if (dtype != SEMKV_F16 && dtype != SEMKV_BF16) return SEMKV_EUNSUPPORTED;
   if (k_stride < (int64_t)c.H * c.D || v_stride < (int64_t)c.H * c.D) return SEMKV_EINVAL;
   if (!aligned(k, 16) || !aligned(v, 16) || k_stride % 8 || v_stride % 8) return SEMKV_EALIGN;
@@ -93,7 +95,7 @@ size_t semkv_kv4_tile_bytes(int32_t head_dim) {
 
 size_t semkv_kv4_pages_workspace_bytes(const semkv_kv4_cache* cache, int32_t n, int32_t tokens) {
   Kv4Cache c;
-  if (check_kv4(cache, c) != SEMKV_OK || check_list(n, nullptr) != SEMKV_OK ) return 0;
+  if (check_kv4(cache, c) != SEMKV_OK || check_list(n, nullptr) != SEMKV_OK) return 0;
   return kv4_pages_workspace(c, n, tokens, tokens >= 0);
 }
 
@@ -146,7 +148,7 @@ semkv_status semkv_kv4_attention(const semkv_kv4_cache* cache, const semkv_kv4_b
   if (s != SEMKV_OK) return s;
   s = check_kv4_batch(batch, false, b);
   if (s != SEMKV_OK) return s;
-  if (!q || !out || layer < 0 || layer >= c.layers || window < 0) return SEMKV_EINVAL;
+  if ((b.total > 0 && (!q || !out)) || layer < 0 || layer >= c.layers || window < 0) return SEMKV_EINVAL;
   if (q_heads < 1 || q_heads % c.H) return SEMKV_EINVAL;
   if (dtype != SEMKV_F16 && dtype != SEMKV_BF16) return SEMKV_EUNSUPPORTED;
   // row indices of a sequence are 32-bit inside the kernels

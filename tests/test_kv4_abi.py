@@ -123,6 +123,21 @@ def test_empty_calls_are_nothing(sk):
     assert sk.LIB.semkv_kv4_write(ctypes.byref(c), ctypes.byref(batch(sk, cu=FAKE, total=0)), 0, 0, FAKE, 256, FAKE, 256, None) == 0
 
 
+def test_empty_tensors_have_no_address(sk):
+    c = cache(sk)
+    for b in (batch(sk, n=0, total=0, max_count=0, start=None), batch(sk, cu=FAKE, total=0, max_count=0),
+              batch(sk, n=0, total=0, cu=FAKE, start=None)):
+        got = calls(sk, c, b, x=None)
+        assert [got[k] for k in ("write", "read", "attention")] == [0] * 3, got
+        assert b.n > 0 or got["reserve"] == 0
+    assert calls(sk, c, batch(sk, n=0, total=0), layer=2)["write"] == EINVAL
+
+
+def test_steps_of_too_many_rows_are_refused(sk):
+    got = calls(sk, cache(sk), batch(sk, cu=FAKE, total=(1 << 30) + 1))
+    assert [got[k] for k in ("reserve", "write", "read", "attention")] == [EUNSUPPORTED] * 4, got
+
+
 def test_the_binding_refuses_tensors_that_do_not_fit(sk):
     cpu = dict(device="cpu")
     with pytest.raises(ValueError):
