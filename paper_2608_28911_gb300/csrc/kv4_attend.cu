@@ -628,20 +628,21 @@ int few_ctas(int n_tiles, int sms) { return n_tiles == 1 ? 2 * sms : sms; }
 
 }  // namespace
 
-// Workspace: the parts, behind the lengths before each sequence (many rows) or the items' spans (few).
+// Workspace: the parts, behind the lengths before each sequence and the joins (many rows) or the items' spans (few).
 static int few_items(const Kv4Batch& b, int group, int n_tiles) {
   return (int)(((int64_t)b.max_count * group + 8 * n_tiles - 1) / (8 * n_tiles));
 }
-static size_t front_bytes(const Kv4Cache& c, const Kv4Batch& b, int group) {
-  const size_t words = kv4_many(b, group, c.D) ? (size_t)b.n + 1 : (size_t)b.n * c.H * few_items(b, group, few_tiles(b, group, c.D));
-  return words * 8 + 15 & ~(size_t)15;
+static size_t front_bytes(const Kv4Cache& c, const Kv4Batch& b, int group, int sms) {
+  if (kv4_many(b, group, c.D)) return kv4_many_front_bytes(b, sms);
+  const size_t spans = (size_t)b.n * c.H * few_items(b, group, few_tiles(b, group, c.D));
+  return (spans * 8 + 15) & ~(size_t)15;
 }
 
 size_t kv4_attention_workspace(const Kv4Cache& c, const Kv4Batch& b, int q_heads, int sms) {
   const int group = q_heads / c.H, n = few_tiles(b, group, c.D);
   const size_t floats = kv4_many(b, group, c.D) ? kv4_many_part_floats(c.D, sms)
                                            : (size_t)2 * few_ctas(n, sms) * kWarps * 8 * n * kv4_part_floats(c.D);
-  return floats * 4 + front_bytes(c, b, group);
+  return floats * 4 + front_bytes(c, b, group, sms);
 }
 
 cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer, int dtype, const void* q, int64_t q_stride,
@@ -661,7 +662,8 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
   a.scale_log2 = softmax_scale * 1.4426950408889634f;
   a.prefix = static_cast<int64_t*>(ws);
   a.spans = static_cast<int2*>(ws);
-  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + front_bytes(c, b, a.group));
+  a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + front_bytes(c, b, a.group, sms));
+  a.joins = reinterpret_cast<int4*>(a.parts) - sms;
   if (kv4_many(b, a.group, c.D)) return launch_kv4_many(a, dtype, sms, stream);
   const int n = few_tiles(b, a.group, c.D), ctas = few_ctas(n, sms);
   a.tiles = few_items(b, a.group, n);

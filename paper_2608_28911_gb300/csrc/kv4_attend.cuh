@@ -26,6 +26,7 @@ struct Kv4Attend {
   float scale_log2;  // softmax scale * log2(e)
   float* parts;      // [2 * workers][rows][D + 4]: sums, then reference exponent and weight sum
   int64_t* prefix;   // (many rows) [b.n + 1]: length before each sequence
+  int4* joins;       // (many rows) [workers]: the item that each begins and does not end (Kv4Join)
   int2* spans;       // (few rows) [b.n][heads][tiles]: first and last worker of each item; first -1: it was
   int tiles;         //   finished by one
 };
@@ -301,6 +302,7 @@ __device__ __forceinline__ float exp2_approx(float x) {
 // The kernel for many rows (kv4_chunk.cu): whether a step takes it, its parts, its launch.
 bool kv4_many(const Kv4Batch& b, int group, int D);
 size_t kv4_many_part_floats(int D, int sms);
+size_t kv4_many_front_bytes(const Kv4Batch& b, int sms);  // prefix, then joins
 cudaError_t launch_kv4_many(const Kv4Attend& a, int dtype, int sms, cudaStream_t stream);
 
 }  // namespace semkv

@@ -175,7 +175,16 @@ struct Item {
   int head, tile, rows;           // rows: of this tile
   int u0, u1;                     // units of this part
   int first, last;                // units of the item
+  int parts;                      // workers that share it, where it begins and does not end here; else 0
 };
+// What the join has to know of an item that a worker begins and does not end: its first row (of those of all
+// query heads), rows | parts << 16, V's scale.  Left here rather than looked for in the join, it takes 4 of 236 us off six ragged prompts.
+struct Kv4Join {
+  int64_t first_row;
+  uint32_t rows_parts;
+  float gv;
+};
+static_assert(sizeof(Kv4Join) == sizeof(int4), "stored as one");
 
 // A walk over the CTA's range: found once, then from item to item.  One warp walks and hands the items
 // to the others through a ring in shared memory; an item without rows ends it.
@@ -184,10 +193,11 @@ struct Walk {
   int i, head, tile;
   int off;       // places of the item that are behind the walk
   int64_t left;  // places of the range before it
+  Kv4Ranges ranges;
   Item items[kItems];
 
-  __device__ __forceinline__ void start(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, int64_t place,
-                                        int64_t end) {
+  __device__ __forceinline__ void start(const Kv4Attend& a, const Kv4ManyCut& cut, const int64_t* prefix, const Kv4Ranges& all) {
+    const int64_t place = all.begin(blockIdx.x), end = all.begin(blockIdx.x + 1);
     int64_t at;
     int which;
     const Kv4Seq q = kv4_find<kThreads>(a, cut, prefix, place, at, which);
@@ -202,6 +212,7 @@ struct Walk {
       tile = t;
       off = (int)(in_head - cut.before(a, q, t));
       left = end - place;
+      ranges = all;
     }
     __syncwarp();
   }
@@ -236,6 +247,12 @@ struct Walk {
       x.head = h;
       x.tile = t;
       x.rows = min(cut.rows, (q.count - t * cut.tokens) * a.group);
+      x.parts = 0;
+      if (x.u0 == x.first && x.u1 < x.last && x.u1 > x.u0) {
+        // (the range ends in it) the range of its last unit's place
+        const int last = cut.start + max(0, (x.last - 1) * kUnit - from);
+        x.parts = ranges.owner(ranges.begin(blockIdx.x + 1) + (last - (o + take))) - (int)blockIdx.x + 1;
+      }
       ++t;
       o = 0;
       more -= take;
@@ -296,6 +313,12 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
     const uint32_t slot = published % kItems;
     if (!wait(&bars->i_empty[slot], (published / kItems & 1) ^ 1, failed)) return;
     if (lane == 0) {
+      if (x.rows && x.parts) {
+        const Kv4Join join{(int64_t)(x.begin + x.tile * cut.tokens) * a.q_heads + x.head * a.group,
+                           (uint32_t)x.rows | (uint32_t)x.parts << 16,
+                           a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + x.head] : 1.f};
+        a.joins[blockIdx.x] = *reinterpret_cast<const int4*>(&join);
+      }
       walk.items[slot] = x;
       arrive(&bars->i_full[slot]);
     }
@@ -926,10 +949,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   kv4_plan<kThreads, true>(a, cut, prefix, sums, blockIdx.x == 0);
   const int64_t W = prefix[kThreads];
   const Kv4Ranges ranges(W, cut.least, gridDim.x);
+  if (threadIdx.x == kThreads - 32) a.joins[blockIdx.x] = make_int4(0, 0, 0, 0);  // (the thread that may replace it)
   if (W > 0 && (int)blockIdx.x < ranges.count) {
     Walk& walk = *reinterpret_cast<Walk*>(smem + L::walk());
-    if (warp == kThreads / 32 - 1)
-      walk.start(a, cut, prefix, ranges.begin(blockIdx.x), ranges.begin(blockIdx.x + 1));
+    if (warp == kThreads / 32 - 1) walk.start(a, cut, prefix, ranges);
     // 176 + 176 + 88 + 72 = 4 * 128, the registers of the launch
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
@@ -961,7 +984,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
 }
 
 // Joins the parts of the tiles that several CTAs share: CTA x takes the tile that range x begins and
-// does not end, a warp for a row.  CTAs behind those fill the rows that see nothing, one for each
+// does not end, a warp for four rows.  CTAs behind those fill the rows that see nothing, one for each
 // sequence.
 constexpr int kJoinThreads = 256;
 constexpr int kJoinSplit = 8;  // CTAs of a tile
@@ -984,43 +1007,55 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_chunk_join_kernel(Kv4Attend 
     }
     return;
   }
-  const int64_t W = a.prefix[a.b.n];
-  const Kv4Ranges ranges(W, cut.least, most);
-  if (W == 0 || x + 1 >= ranges.count) return;
-  const int64_t place = ranges.begin(x + 1);
-  int lo = 0, hi = a.b.n - 1;  // the sequence that the next range begins in
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.prefix[mid] <= place) lo = mid; else hi = mid - 1;
+  const int4 words = a.joins[x];
+  const Kv4Join& join = *reinterpret_cast<const Kv4Join*>(&words);
+  const int rows = join.rows_parts & 0xFFFF, parts = join.rows_parts >> 16;
+  if (parts < 2) return;
+  // a warp's rows together, so that their loads do not wait for one another
+  constexpr int kRows = 2 * kBlock / kStep;
+  float ref[kRows], total[kRows], o[kRows][kDims];
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    ref[k] = kNone, total[k] = 0.f;
+#pragma unroll
+    for (int d = 0; d < kDims; ++d) o[k][d] = 0.f;
   }
-  const Kv4Seq s = cut.seq(a, lo, false);
-  const int64_t p0 = a.prefix[lo], head_length = cut.before(a, s, s.tiles);
-  const int head = (int)kv4_div(place - p0, head_length), tile = cut.find(a, s, place - p0 - head * head_length);
-  int64_t first, last;
-  if (!cut.ends(a, s, head, tile, first, last)) return;
-  const int parts = ranges.owner(p0 + last) - x + 1;
-  if (ranges.owner(p0 + first) != x || parts < 2) return;
-  const int rows = min(cut.rows, (s.count - tile * cut.tokens) * a.group);
-  const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + head] : 1.f;
-  for (int col = row0; col < rows; col += kStep) {
-    const int row = tile * cut.rows + col;
-    const int64_t at = (int64_t)(s.begin + row / a.group) * a.q_heads + head * a.group + row % a.group;
-    float ref = kNone, total = 0.f, o[kDims] = {};
-    for (int p = 0; p < parts; ++p) {
-      // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
-      const float* part = a.parts + ((int64_t)(2 * (x + p) + (p == 0)) * cut.rows + col) * kv4_part_floats(D);
-      const float2 rs = *reinterpret_cast<const float2*>(part + D);
-      const float to = fmaxf(ref, rs.x), f = exp2_approx(ref - to), g = exp2_approx(rs.x - to);
-      ref = to;
-      total = total * f + rs.y * g;
+  for (int p = 0; p < parts; ++p) {
+    // the first part begins the item (slot 2 w + 1), the others continue it (slot 2 w)
+    const float* part = a.parts + ((int64_t)(2 * (x + p) + (p == 0)) * cut.rows + row0) * kv4_part_floats(D);
+    float2 rs[kRows];
+    float v[kRows][kDims];
 #pragma unroll
-      for (int d = 0; d < kDims; ++d) o[d] = o[d] * f + part[kDims * lane + d] * g;
+    for (int k = 0; k < kRows; ++k) {
+      const float* of = part + (row0 + k * kStep < rows ? k * kStep : 0) * kv4_part_floats(D);
+      rs[k] = row0 < rows ? *reinterpret_cast<const float2*>(of + D) : make_float2(kNone, 0.f);
+      if constexpr (kDims == 4) {
+        const float4 y = row0 < rows ? *reinterpret_cast<const float4*>(of + 4 * lane) : float4{};
+        v[k][0] = y.x, v[k][1] = y.y, v[k][2] = y.z, v[k][3] = y.w;
+      } else {
+        const float2 y = row0 < rows ? *reinterpret_cast<const float2*>(of + 2 * lane) : float2{};
+        v[k][0] = y.x, v[k][1] = y.y;
+      }
     }
-    const float inv = total == 0.f ? 0.f : gv / total;
 #pragma unroll
-    for (int d = 0; d < kDims; d += 2)
-      *reinterpret_cast<uint32_t*>(a.out + at * D + kDims * lane + d) = pack_out<BF16>(o[d] * inv, o[d + 1] * inv);
-    if (a.lse && lane == 0) a.lse[at] = total == 0.f ? -INFINITY : (ref + log2f(total)) * 0.6931471805599453f;
+    for (int k = 0; k < kRows; ++k) {
+      const float to = fmaxf(ref[k], rs[k].x), f = exp2_approx(ref[k] - to), g = exp2_approx(rs[k].x - to);
+      ref[k] = to;
+      total[k] = total[k] * f + rs[k].y * g;
+#pragma unroll
+      for (int d = 0; d < kDims; ++d) o[k][d] = o[k][d] * f + v[k][d] * g;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int col = row0 + k * kStep;
+    if (col >= rows) continue;
+    const int64_t at = join.first_row + cut.token_of(col) * (a.q_heads - a.group) + col;
+    const float inv = total[k] == 0.f ? 0.f : join.gv / total[k];
+    uint32_t* to = reinterpret_cast<uint32_t*>(a.out + at * D + kDims * lane);
+#pragma unroll
+    for (int d = 0; d < kDims; d += 2) to[d / 2] = pack_out<BF16>(o[k][d] * inv, o[k][d + 1] * inv);
+    if (a.lse && lane == 0) a.lse[at] = total[k] == 0.f ? -INFINITY : (ref[k] + log2f(total[k])) * 0.6931471805599453f;
   }
 }
 
@@ -1113,6 +1148,9 @@ bool kv4_many(const Kv4Batch& b, int group, int D) {
   return (int64_t)b.max_count * group > (D == 128 ? 32 : 48) && group <= 2 * kBlock;
 }
 
+size_t kv4_many_front_bytes(const Kv4Batch& b, int sms) {
+  return (((size_t)b.n + 1) * 8 + 15 & ~(size_t)15) + (size_t)sms * sizeof(int4);
+}
 size_t kv4_many_part_floats(int D, int sms) { return (size_t)2 * sms * 2 * kBlock * kv4_part_floats(D); }
 
 cudaError_t launch_kv4_many(const Kv4Attend& a, int dtype, int sms, cudaStream_t stream) {
