@@ -133,13 +133,19 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&v)[16
       SEMKV_I8(v, 8), "r"(at)
       : "memory");
 }
+__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,"
+      "%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::SEMKV_I8(v, 0),
+      SEMKV_I8(v, 8), SEMKV_I8(v, 16), SEMKV_I8(v, 24), "r"(at)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 constexpr int kWalkBytes = 384, kBarBytes = 32 * 8;
-constexpr int kStagePitch = 80, kStageBytes = 32 * kStagePitch;  // a softmax warp's stage of results
 
 template <int D>
 struct Layout {
@@ -149,8 +155,7 @@ struct Layout {
   static constexpr int v(int b) { return b * kTile; }
   static constexpr int k(int b) { return (2 + b) * kTile; }
   static constexpr int q(int t) { return (4 + t) * kTile; }
-  static constexpr int stage() { return 6 * kTile; }
-  static constexpr int prefix() { return stage() + 8 * kStageBytes; }
+  static constexpr int prefix() { return 6 * kTile; }
   static constexpr int undo() { return prefix() + (kThreads + 2) * 8; }
   static constexpr int other() { return undo() + 4 * kBlock * 4; }
   static constexpr int sums() { return other() + kBlock * 8; }
@@ -412,7 +417,7 @@ __device__ __forceinline__ void query_warps(const Kv4Attend& a, const Kv4ManyCut
 // ------------------------------------------------------------- softmax ------
 
 template <int D, bool BF16>
-__device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, const float* undo, float2* other, uint8_t* stage, Bars* bars, uint32_t tmem) {
+__device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyCut& cut, Walk& walk, const float* undo, float2* other, Bars* bars, uint32_t tmem) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = warp >> 2, r = (warp & 3) * 32 + lane;
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's tensor memory lanes
@@ -428,17 +433,21 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
     const int u0 = it.u0 + (split ? t : 0), u1 = it.u1, step = split ? 2 : 1;
     if (u0 >= u1) continue;
     const int rr = split ? r : t * kBlock + r;  // this thread's row of the tile
-    const bool there = rr < it.rows;
     const float gk = a.c.k_scale ? a.c.k_scale[a.layer * a.c.H + it.head] : 1.f;
     const float gv = a.c.v_scale ? a.c.v_scale[a.layer * a.c.H + it.head] : 1.f;
     const float scale = fabsf(a.scale_log2) * gk;
     float mul = 0.f;
-    int lo = 0, hi = 0x7FFFFFFF;  // (a row that is not there sees all: its zeros are nobody's)
-    if (there) {
-      hi = it.length - it.count + it.tile * cut.tokens + cut.token_of(rr);
-      lo = a.window && hi >= a.window ? hi - a.window + 1 : 0;
-    }
-    const int most_lo = __reduce_max_sync(~0u, lo), least_hi = __reduce_min_sync(~0u, hi);
+    // the positions that the row sees (a row that is not there sees all: its zeros are nobody's)
+    auto sight = [&](int& lo, int& hi) {
+      lo = 0, hi = 0x7FFFFFFF;
+      if (rr < it.rows) {
+        hi = it.length - it.count + it.tile * cut.tokens + cut.token_of(rr);
+        lo = a.window && hi >= a.window ? hi - a.window + 1 : 0;
+      }
+    };
+    int most_lo, least_hi;
+    sight(most_lo, least_hi);
+    most_lo = __reduce_max_sync(~0u, most_lo), least_hi = __reduce_min_sync(~0u, least_hi);
     float ref = kNone, sum = 0.f;
     bool ok = true;
     for (int u = u0; u < u1; u += step) {
@@ -490,54 +499,42 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
           asm("max.f32 %0, %0, %1, %2;" : "+f"(m[i >> 1 & 1]) : "f"(__uint_as_float(v[i])), "f"(__uint_as_float(v[i + 1])));
         return fmaxf(m[0], m[1]);
       };
-      if (open) {
-        uint32_t v[kUnit / 32][32];
-        float top = -INFINITY;
-        tmem_load(S, v[0]);
-#pragma unroll
-        for (int c = 0; c < kUnit / 32; ++c) {
-          tmem_wait(v[c]);
-          if (c + 1 < kUnit / 32) tmem_load(S + 32 * (c + 1), v[c + 1]);  // on its way behind this one's maximum
-          top = fmaxf(top, largest(v[c]));
-        }
-        settle(top * mul);
-        const uint64_t mul2 = pair(mul, mul), ref2 = pair(-ref, -ref);
-#pragma unroll
-        for (int c = 0; c < kUnit / 32; ++c) {
-          uint32_t w[16];
-          turn(v[c], mul2, ref2, w);
-          tmem_store16(S + 16 * c, w);  // in S's place
-        }
-      } else {
-        // a unit that some row sees a part of: in short loops, since what runs seldom has to be fetched first
-        // (with everything unrolled six ragged prompts took 268 us, so 236)
-        float top = -INFINITY;
-        uint32_t v[32];
-        auto hide = [&](int c) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const int p = pos + c + i;
-            if (p < lo || p > hi) v[i] = 0xFF800000u;
-          }
-        };
+      if (__builtin_expect(!open, 0)) {
+        // a unit that some row sees a part of: what is hidden becomes -infinity where it lies.  A warp's rows are a
+        // few tokens, so that of its groups of 32 positions one or two are hidden in part and need a look.
+        // (With a loop of its own for such units, which took 6600 cycles, six ragged prompts were 7 us of 232 slower.)
+        int lo, hi;
+        sight(lo, hi);
 #pragma unroll 1
         for (int c = 0; c < kUnit; c += 32) {
+          const int from = lo - pos - c, to = hi - pos - c;  // this row sees from .. to of the 32
+          if (__all_sync(~0u, from <= 0 && to >= 31)) continue;
+          uint32_t v[32];
           tmem_load(S + c, v);
           tmem_wait(v);
-          hide(c);
-          top = fmaxf(top, largest(v));
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (i < from || i > to) v[i] = 0xFF800000u;
+          tmem_store(S + c, v);
         }
-        settle(top * mul);
-        const uint64_t mul2 = pair(mul, mul), ref2 = pair(-ref, -ref);
-#pragma unroll 1
-        for (int c = 0; c < kUnit; c += 32) {
-          uint32_t w[16];
-          tmem_load(S + c, v);
-          tmem_wait(v);
-          hide(c);
-          turn(v, mul2, ref2, w);
-          tmem_store16(S + c / 2, w);
-        }
+        tmem_stored();
+      }
+      uint32_t v[kUnit / 32][32];
+      float top = -INFINITY;
+      tmem_load(S, v[0]);
+#pragma unroll
+      for (int c = 0; c < kUnit / 32; ++c) {
+        tmem_wait(v[c]);
+        if (c + 1 < kUnit / 32) tmem_load(S + 32 * (c + 1), v[c + 1]);  // on its way behind this one's maximum
+        top = fmaxf(top, largest(v[c]));
+      }
+      settle(top * mul);
+      const uint64_t mul2 = pair(mul, mul), ref2 = pair(-ref, -ref);
+#pragma unroll
+      for (int c = 0; c < kUnit / 32; ++c) {
+        uint32_t w[16];
+        turn(v[c], mul2, ref2, w);
+        tmem_store16(S + 16 * c, w);  // in S's place
       }
       {
         float x, y;
@@ -549,23 +546,12 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       __syncwarp();
       if (lane == 0) arrive(&bars->p_full[t]);
     }
-    // ---- while the last products run: where the rows go, or this range's part of them.  They go 64 bytes of
-    // each at a time through the warp's stage, so that a store writes eight rows' 64 bytes and not 32 rows'
-    // 16 (which took 6000 cycles an item).
+    // ---- while the last products run: where the row goes, or this range's part of it
     const bool done = it.u0 == it.first && it.u1 == it.last;
-    uint8_t* mine = stage + warp * kStageBytes;
-    uint4* put = reinterpret_cast<uint4*>(mine + lane * kStagePitch);
-    const uint4* get = reinterpret_cast<const uint4*>(mine + (lane >> 2) * kStagePitch + (lane & 3) * 16);
-    float* parts = a.parts + (int64_t)(2 * blockIdx.x + (it.u0 == it.first ? 1 : 0)) * cut.rows * kv4_part_floats(D);
-    const int64_t first_row = (int64_t)(it.begin + it.tile * cut.tokens) * a.q_heads + it.head * a.group;
-    uint8_t* to[4];  // row 8 i + lane / 4 of the warp's
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int x = rr - lane + 8 * i + (lane >> 2), j = cut.token_of(x);
-      to[i] = done ? reinterpret_cast<uint8_t*>(a.out + (first_row + j * a.q_heads + (x - j * a.group)) * D)
-                   : reinterpret_cast<uint8_t*>(parts + x * kv4_part_floats(D));
-      to[i] = x < it.rows ? to[i] + (lane & 3) * 16 : nullptr;
-    }
+    const int64_t at = (int64_t)(it.begin + it.tile * cut.tokens) * a.q_heads + it.head * a.group +
+                       cut.token_of(rr) * (a.q_heads - a.group) + rr;
+    float* part = a.parts + ((int64_t)(2 * blockIdx.x + (it.u0 == it.first ? 1 : 0)) * cut.rows + rr) * kv4_part_floats(D);
+    uint4* to = done ? reinterpret_cast<uint4*>(a.out + at * D) : reinterpret_cast<uint4*>(part);
     ok = ok && wait(&bars->o_full[t], o_phase, failed);
     o_phase ^= 1;
     if (!ok) return;
@@ -594,15 +580,6 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       sum = sum * f + o.y * g;
     }
     const float inv = sum == 0.f ? 0.f : gv / sum;
-    auto flush = [&](int piece) {  // the stage's rows to byte `piece` of theirs
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint4 w = get[i * (8 * kStagePitch / 16)];
-        if (to[i]) *reinterpret_cast<uint4*>(to[i] + piece) = w;
-      }
-      __syncwarp();
-    };
     // (a loop: code that runs once an item is fetched anew each time, and unrolled it was 4% of a prompt slower)
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
@@ -624,32 +601,26 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
           if (lane == 0) arrive(&bars->x_empty);
         }
       }
-      if (done) {
+      if (rr < it.rows && done) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t w[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x)
             w[x] = pack_out<BF16>(__uint_as_float(v[8 * i + 2 * x]) * inv, __uint_as_float(v[8 * i + 2 * x + 1]) * inv);
-          put[i] = make_uint4(w[0], w[1], w[2], w[3]);
+          to[4 * c + i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        flush(64 * c);
-      } else {
+      } else if (rr < it.rows) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            put[i] = make_uint4(v[16 * half + 4 * i], v[16 * half + 4 * i + 1], v[16 * half + 4 * i + 2], v[16 * half + 4 * i + 3]);
-          flush(128 * c + 64 * half);
-        }
+        for (int i = 0; i < 8; ++i) to[8 * c + i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
       }
+      __syncwarp();
     }
-    if (there) {
+    if (rr < it.rows) {
       if (done) {
-        if (a.lse)
-          a.lse[first_row + cut.token_of(rr) * (a.q_heads - a.group) + rr] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+        if (a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
       } else {
-        *reinterpret_cast<float2*>(parts + rr * kv4_part_floats(D) + D) = make_float2(ref, sum);
+        *reinterpret_cast<float2*>(part + D) = make_float2(ref, sum);
       }
     }
     fence_before();
@@ -956,7 +927,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
     // 176 + 176 + 88 + 72 = 4 * 128, the registers of the launch
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-      softmax_warps<D, BF16>(a, cut, walk, undo, reinterpret_cast<float2*>(smem + L::other()), smem + L::stage(), bars, tmem);
+      softmax_warps<D, BF16>(a, cut, walk, undo, reinterpret_cast<float2*>(smem + L::other()), bars, tmem);
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
       code_warps<D>(a, cut, walk, smem, bars);
