@@ -1,5 +1,7 @@
 // kv4_attend.cu — attention over the paged 4-bit cache for few query rows (single tokens,
-// drafted tokens), bound by reading the cache.
+// drafted tokens), bound by reading the cache and by turning it into operands: 16 sequences of 64K
+// with 8 KV heads in groups of 4 take 216 us, 82% of the copy rate, at 50% of the issue slots (336
+// instructions for a tile of 16 tokens) and 19% of the tensor pipe.
 //
 // For a tile of 16 tokens, on mma.sync m16n8k16 with fp16 operands and fp32 sums:
 //   S^T = K Q^T      M = 16 tokens, N = 8 query rows, K = head dim
