@@ -613,18 +613,15 @@ cudaError_t launch_few_rows(const Kv4Attend& a, int n_tiles, int ctas, cudaStrea
     case 1: return launch_few<D, 1, BF16>(a, ctas, stream);
     case 2: return launch_few<D, 2, BF16>(a, ctas, stream);
     case 3: return launch_few<D, 3, BF16>(a, ctas, stream);
-    case 4: return launch_few<D, 4, BF16>(a, ctas, stream);
-    default:
-      if constexpr (D == 64) return launch_few<64, 6, BF16>(a, ctas, stream);
-      return cudaErrorInvalidValue;
+    default: return launch_few<D, 4, BF16>(a, ctas, stream);
   }
 }
 
 // n tiles of 8 rows for the step's most rows: the fewest that hold them, up to what the registers hold
 // (O takes D / 4 of them for each)
-int few_tiles(const Kv4Batch& b, int group, int D) {
+int few_tiles(const Kv4Batch& b, int group) {
   const int64_t rows = (int64_t)b.max_count * group;
-  return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : rows <= 32 || D == 128 ? 4 : 6;
+  return rows <= 8 ? 1 : rows <= 16 ? 2 : rows <= 24 ? 3 : 4;
 }
 int few_ctas(int n_tiles, int sms) { return n_tiles == 1 ? 2 * sms : sms; }
 
@@ -635,14 +632,14 @@ static int few_items(const Kv4Batch& b, int group, int n_tiles) {
   return (int)(((int64_t)b.max_count * group + 8 * n_tiles - 1) / (8 * n_tiles));
 }
 static size_t front_bytes(const Kv4Cache& c, const Kv4Batch& b, int group, int sms) {
-  if (kv4_many(b, group, c.D)) return kv4_many_front_bytes(b, sms);
-  const size_t spans = (size_t)b.n * c.H * few_items(b, group, few_tiles(b, group, c.D));
+  if (kv4_many(b, group)) return kv4_many_front_bytes(b, sms);
+  const size_t spans = (size_t)b.n * c.H * few_items(b, group, few_tiles(b, group));
   return (spans * 8 + 15) & ~(size_t)15;
 }
 
 size_t kv4_attention_workspace(const Kv4Cache& c, const Kv4Batch& b, int q_heads, int sms) {
-  const int group = q_heads / c.H, n = few_tiles(b, group, c.D);
-  const size_t floats = kv4_many(b, group, c.D) ? kv4_many_part_floats(c.D, sms)
+  const int group = q_heads / c.H, n = few_tiles(b, group);
+  const size_t floats = kv4_many(b, group) ? kv4_many_part_floats(c.D, sms)
                                            : (size_t)2 * few_ctas(n, sms) * kWarps * 8 * n * kv4_part_floats(c.D);
   return floats * 4 + front_bytes(c, b, group, sms);
 }
@@ -666,8 +663,8 @@ cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer
   a.spans = static_cast<int2*>(ws);
   a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + front_bytes(c, b, a.group, sms));
   a.joins = reinterpret_cast<int4*>(a.parts) - sms;
-  if (kv4_many(b, a.group, c.D)) return launch_kv4_many(a, dtype, sms, stream);
-  const int n = few_tiles(b, a.group, c.D), ctas = few_ctas(n, sms);
+  if (kv4_many(b, a.group)) return launch_kv4_many(a, dtype, sms, stream);
+  const int n = few_tiles(b, a.group), ctas = few_ctas(n, sms);
   a.tiles = few_items(b, a.group, n);
   const bool bf = dtype == SEMKV_BF16;
   const cudaError_t e =

@@ -300,7 +300,7 @@ __device__ __forceinline__ float exp2_approx(float x) {
 }
 
 // The kernel for many rows (kv4_chunk.cu): whether a step takes it, its parts, its launch.
-bool kv4_many(const Kv4Batch& b, int group, int D);
+bool kv4_many(const Kv4Batch& b, int group);
 size_t kv4_many_part_floats(int D, int sms);
 size_t kv4_many_front_bytes(const Kv4Batch& b, int sms);  // prefix, then joins
 cudaError_t launch_kv4_many(const Kv4Attend& a, int dtype, int sms, cudaStream_t stream);

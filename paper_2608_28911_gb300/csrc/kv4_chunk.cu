@@ -1118,10 +1118,11 @@ cudaError_t launch_chunk(const Kv4Attend& a, const Kv4ManyCut& cut, int sms, cud
 
 }  // namespace
 
-bool kv4_many(const Kv4Batch& b, int group, int D) {
-  // one tile of the small kernel holds up to 32 rows, 48 at head dim 64; more would read the cache again.
-  // 8 sequences of 32K, head dim 128: 20 rows 117 us there and 190 here, 36 rows 261 and 190.
-  return (int64_t)b.max_count * group > (D == 128 ? 32 : 48) && group <= 2 * kBlock;
+bool kv4_many(const Kv4Batch& b, int group) {
+  // one tile of the small kernel holds up to 32 rows; more would read the cache again.  8 sequences of 32K, head
+  // dim 128: 20 rows 118 us there and 184 here, 36 rows 261 and 184.  (A tile of 48 rows, which head dim 64
+  // leaves registers for, was no faster than this kernel: 36 rows of 8 sequences of 4K 32 us, 30 here.)
+  return (int64_t)b.max_count * group > 32 && group <= 2 * kBlock;
 }
 
 size_t kv4_many_front_bytes(const Kv4Batch& b, int sms) {
