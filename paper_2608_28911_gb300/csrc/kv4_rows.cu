@@ -87,7 +87,8 @@ __device__ __forceinline__ bool quantize_block(const uint4 (&in)[2], float g, ui
       }
       c[i] = to_e2m1x8(y);
     }
-    codes = make_uint2(c[0], c[1]);
+    // (with scale 0 the quotients are zeros of either sign: the format's codes are 0)
+    codes = scale ? make_uint2(c[0], c[1]) : make_uint2(0, 0);
     return true;
   }
   // a NaN, an infinity, or values past the top of the grid: one value at a time
