@@ -158,7 +158,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
   const int row_a = token_at(g), tok_v = token_at(2 * t);  // K row of lane group g; V's first token
   const int64_t head_bytes = (int64_t)L::kTile << (a.c.page_shift - 4);
   const int64_t page_stride = head_bytes * a.c.H;
-  uint32_t phase = 0;  // parity of each stage's barrier, a bit each
+  uint32_t phase = 0;  // parity of each stage's barrier, a bit each; kFarBit: a reference of the item is far (kFar)
+  constexpr uint32_t kFarBit = 0x80000000u;  // (a variable of its own made the eight-row kernel spill)
   int stage = 0;       // of the next unit
 
   for (int64_t place = ranges.begin(worker); place < end;) {
@@ -269,6 +270,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
         for (int x = 0; x < 4; ++x) O[n][m][x] = 0.f;
 #pragma unroll
     for (int x = 0; x < 2 * NT; ++x) ref[x] = kNone, sum[x] = 0.f;
+    phase &= ~kFarBit;
     __syncwarp();  // Q's fragments are there
 
     // S^T += K Q^T of a tile
@@ -390,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
         const bool open = t0 >= most_lo && t0 + 16 * kTogether - 1 <= least_hi;  // every row sees all of it
         float E[kTogether][NT][4];
         float top = -INFINITY;
-        auto exponents = [&] {
+        auto exponents = [&](bool rounded) {
 #pragma unroll
           for (int h = 0; h < kTogether; ++h) {
             const int pos_a = t0 + 16 * h + row_a, pos_b = pos_a + 8;
@@ -398,8 +400,13 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
             for (int n = 0; n < NT; ++n) {
               const uint64_t m2 = pair(mul[2 * n], mul[2 * n + 1]), r2 = pair(-ref[2 * n], -ref[2 * n + 1]);
               float(&e)[4] = E[h][n];
-              unpair(pair_fma(pair(S[h][n][0], S[h][n][1]), m2, r2), e[0], e[1]);
-              unpair(pair_fma(pair(S[h][n][2], S[h][n][3]), m2, r2), e[2], e[3]);
+              if (rounded) {  // (scalar: of a packed product and a packed sum one fused operation was made)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) e[x] = __fsub_rn(__fmul_rn(S[h][n][x], mul[2 * n + (x & 1)]), ref[2 * n + (x & 1)]);
+              } else {
+                unpair(pair_fma(pair(S[h][n][0], S[h][n][1]), m2, r2), e[0], e[1]);
+                unpair(pair_fma(pair(S[h][n][2], S[h][n][3]), m2, r2), e[2], e[3]);
+              }
               if (!open) {
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -412,9 +419,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
             }
           }
         };
-        exponents();
-        if (__any_sync(~0u, top > kMost)) {
+        exponents(false);
+        if (__any_sync(~0u, top > kMost || (phase & kFarBit))) {
           // references move to 2^8 below their rows' largest, and the sums with them
+          bool far = false;
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -430,8 +438,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
               l = fmaxf(l, __shfl_xor_sync(~0u, l, 4));
               l = fmaxf(l, __shfl_xor_sync(~0u, l, 8));
               l = fmaxf(l, __shfl_xor_sync(~0u, l, 16));
-              if (l > ref[i] + kMost) {
-                const float to = l - kHead, f = exp2_approx(ref[i] - to);
+              if (l - ref[i] > kMost) {
+                const float to = reference_for(l), f = exp2_approx(ref[i] - to);
                 ref[i] = to;
                 sum[i] *= f;
 #pragma unroll
@@ -440,8 +448,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(K
                   O[n][m][2 + x] *= f;
                 }
               }
+              far = far || is_far(ref[i]);
             }
-          exponents();
+          far = __any_sync(~0u, far);
+          phase = far ? phase | kFarBit : phase & ~kFarBit;
+          exponents(far);
         }
 #pragma unroll
         for (int h = 0; h < kTogether; ++h) {

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from kv4_plain import Plain
-from test_gpu_kv4 import cu_of, make
+from test_gpu_kv4 import cu_of, make, rows_like
 
 pytestmark = pytest.mark.gpu
 
@@ -36,3 +36,52 @@ def test_blocks_without_a_scale_hold_zeros(dtype, D):
         bits = y.view(torch.int16)
         bits[5, :, :16] = 0
         assert not bits.any()
+
+
+@pytest.mark.parametrize("count", [2, 8, 25, 75])    # 8 rows, a tile of 32, halves of a block, two blocks
+@pytest.mark.parametrize("dtype,power", [("float16", 20), ("float16", 30), ("float16", 60),
+                                         ("bfloat16", 30), ("bfloat16", 90)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_logits_of_any_finite_size(count, dtype, power, sign):
+    """Logits of about +-2^power.  A row that sees one token returns it, equal logits share the weight, a logit that
+    is twice the others' takes all of it or none, whatever the size.
+
+    Every q and every K entry is one power of two or the same number, so equal logits are equal bit by bit and
+    their weights are one number w; w is rounded to fp16 (2^-11), the products' sums lose 17 addends' last places for
+    each 16 tokens.  lse goes through fewer than eight roundings of binary32."""
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    dt, D, H, G = getattr(torch, dtype), 128, 2, 4
+    lens, counts, special = [1, 100, 300], [1, count, count], 137
+    c = make(lens, H, D, 32, seed=4, scales=False)
+    rng = np.random.default_rng(1)
+    v = rows_like(rng, (sum(lens), H, D), torch.float16)
+    k = torch.ones_like(v)
+    k[1 + 100 + special] *= 2                     # the block's scale doubles, the codes are the same
+    semkv.semkv_kv4_write(c, semkv.KV4Batch(3, cu=cu_of(lens), total=sum(lens), max_count=300), 0, k, v)
+    plain = Plain(c)
+    e = 10 if dtype == "float16" else power - 4   # 128 dims times D^-0.5 are about 2^3.5
+    scale = 2.0 ** (power - 17) if dtype == "float16" else D ** -0.5
+    total = sum(counts)
+    q = torch.full((total, H * G, D), sign * 2.0 ** e, dtype=dt, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((total, H * G), 7.0, device="cuda")
+    b = semkv.KV4Batch(3, cu=cu_of(counts), total=total, max_count=max(counts))
+    semkv.semkv_kv4_attention(c, b, 0, q, out, scale, c.attention_workspace(b, H * G), lse=lse)
+    assert int(c.dev_error.item()) == 0
+    got, gl = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    u = torch.finfo(dt).eps / 2
+    row = 0
+    for s, m in enumerate(counts):
+        ks, vs = [plain.rows(0, s, kv, range(lens[s])) for kv in (0, 1)]
+        one = ks[0, 0].sum() * sign * 2.0 ** e * float(np.float32(scale))
+        for j in range(m):
+            seen = np.arange(lens[s] - m + j + 1)
+            if s == 2:
+                seen = seen[seen == special] if sign > 0 else seen[seen != special]
+            want, size = vs[seen].mean(0), np.abs(vs[seen]).mean(0)        # [H][D]
+            tol = u * np.abs(want) + (1 + u) * (2.0 ** -10 + 17 * 2.0 ** -23 * np.ceil(lens[s] / 16)) * size + 2.0 ** -25
+            off = np.abs(got[row + j].reshape(H, G, D) - want[:, None])
+            assert (off <= tol[:, None]).all(), (s, j, float(np.nanmax(off)))
+            l = (2 * one if s == 2 and sign > 0 else one) + np.log(len(seen))
+            assert (np.abs(gl[row + j] - l) <= abs(l) * 2.0 ** -21 + 2.0 ** -18).all(), (s, j, gl[row + j], l)
+        row += m
