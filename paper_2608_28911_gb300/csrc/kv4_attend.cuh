@@ -281,7 +281,7 @@ __device__ __forceinline__ float query_factor(float most, float& undo) {
   return e == 127 ? 0x1p-127f : __uint_as_float((uint32_t)(127 - e) << 23);
 }
 
-constexpr float kNone = -1e30f;  // reference exponent of a row without tokens
+constexpr float kNone = -0x1.fffffep127f;  // reference exponent of a row without tokens: below every finite logit
 constexpr float kHead = 8.f;     // a moved reference puts the largest weight at 2^8
 constexpr float kMost = 15.f;    // largest exponent of a weight
 // A logit past 2^22 has steps of a half and more in binary32.  The exponent as one fused product and sum would hold up
