@@ -369,7 +369,7 @@ def semkv_kv4_attention(cache: "KV4Cache", batch: "KV4Batch", layer: int, q: tor
     if lse is not None:
         _need(lse.dtype == torch.float32 and lse.shape == shape[:2], "lse is float32 [total][q_heads]")
         _here(lse)
-    _here(cache.pages, q, out, ws)
+    _here(cache.pages, batch.start, q, out, ws)  # (a batch's tensors are on one device)
     _check("semkv_kv4_attention",
            LIB.semkv_kv4_attention(cache.ref, batch.ref, layer, kind, q.data_ptr(), qs, heads,
                                    _ptr(out), _ptr(lse), softmax_scale, window, _ptr(ws), ws.nbytes,
@@ -586,6 +586,8 @@ class KV4Batch:
         self.cu, self.seqs = _list(cu, n + 1, "cu"), _list(seqs, n, "seqs")
         self.start = (torch.zeros(n, dtype=torch.int32, device=device) if start is None
                       else _list(start, n, "start"))
+        for t in (self.cu, self.seqs):
+            _need(t is None or t.get_device() == self.start.get_device(), "a batch lies on one device")
         self.total = n if total is None else total
         self.s = KV4BatchStruct(n=n, total=self.total, max_count=max_count,
                                 seqs=_ptr(self.seqs), cu=_ptr(self.cu), start=_ptr(self.start))
