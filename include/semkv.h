@@ -315,8 +315,9 @@ typedef struct {
   int32_t* table;       /* device [max_seqs][max_pages]: the page of each page_tokens
                            tokens.  Entries past a sequence's length mean nothing.   */
   int32_t* length;      /* device [max_seqs]: tokens that each sequence holds        */
-  int32_t* refs;        /* device [num_pages]: table entries in use that name the page;
-                           0 = free.  All zero, like length, in a new cache.         */
+  int32_t* refs;        /* device [num_pages], 16-byte aligned: table entries in use that
+                           name the page; 0 = free.  All zero, like length, in a new
+                           cache.                                                    */
   int32_t* dev_error;   /* device int32 error word (may be NULL)                     */
 } semkv_kv4_cache;
 

@@ -547,6 +547,8 @@ class KV4Cache:
         for t, shape in ((table, table.shape), (length, table.shape[:1]), (refs, (num_pages,))):
             _need(t.dtype == torch.int32 and t.is_contiguous() and t.shape == shape,
                   "table, length and refs are contiguous int32 tensors that fit each other")
+        _need(pages.data_ptr() % 16 == 0 and refs.data_ptr() % 16 == 0,
+              "pages and refs begin on a multiple of 16 bytes")
         for t in (k_scale, v_scale):
             _need(t is None or (t.dtype == torch.float32 and t.is_contiguous()
                                 and t.shape == (layers, kv_heads)),

@@ -53,3 +53,21 @@ def test_a_batch_lies_on_one_device(sk, monkeypatch):
         monkeypatch.setattr(sk, "_here", lambda *t: None)
         with pytest.raises(ValueError, match="one device"):
             sk.KV4Batch(2, start=Elsewhere(), **kw)
+
+
+def test_buffers_that_the_library_would_refuse_make_no_cache(sk):
+    """Table, length and refs carved out of one allocation: refs and pages begin on a multiple of 16 bytes."""
+    store = torch.zeros(2 * 3 + 2 + 4 + 4, dtype=torch.int32)
+    table, length = store[:6].view(2, 3), store[6:8]
+    size = 4 * 2 * 1 * 1152
+    room = torch.zeros(size + 32, dtype=torch.uint8)
+    pages = room[-room.data_ptr() % 16:][:size].view(1, 4, 2, 1, 1152)
+    at = -store.data_ptr() // 4 % 4 + 8             # the next multiple of 16 bytes
+    c = sk.KV4Cache.over(pages, table, length, store[at:at + 4], 64)
+    assert c.s.refs % 16 == 0
+    for refs in (store[at - 1:at + 3], store[at - 2:at + 2]):
+        with pytest.raises(ValueError, match="16 bytes"):
+            sk.KV4Cache.over(pages, table, length, refs, 64)
+    shifted = room[-room.data_ptr() % 16 + 4:][:size]
+    with pytest.raises(ValueError, match="16 bytes"):
+        sk.KV4Cache.over(shifted.view(1, 4, 2, 1, 1152), table, length, c.refs, 64)
