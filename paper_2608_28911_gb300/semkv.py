@@ -580,9 +580,10 @@ class KV4Cache:
 class KV4Batch:
     """The rows of one step over a KV4Cache (semkv_kv4_batch).  cu: int32 [n + 1], or None
     for one row to a sequence; seqs: int32 [n], or None for 0 .. n-1; total: rows of the
-    step's tensors; max_count: no sequence has more rows."""
+    step's tensors; max_count: no sequence has more rows (one that has is left out).  With
+    cu it is `total` unless named; the step's own largest count makes for faster kernels."""
 
-    def __init__(self, n: int, cu=None, seqs=None, start=None, total=None, max_count: int = 1,
+    def __init__(self, n: int, cu=None, seqs=None, start=None, total=None, max_count=None,
                  device="cuda"):
         _need(total is not None or cu is None, "total: the rows of the step's tensors")
         self.cu, self.seqs = _list(cu, n + 1, "cu"), _list(seqs, n, "seqs")
@@ -591,6 +592,8 @@ class KV4Batch:
         for t in (self.cu, self.seqs):
             _need(t is None or t.get_device() == self.start.get_device(), "a batch lies on one device")
         self.total = n if total is None else total
+        if max_count is None:
+            max_count = 1 if cu is None else self.total
         self.s = KV4BatchStruct(n=n, total=self.total, max_count=max_count,
                                 seqs=_ptr(self.seqs), cu=_ptr(self.cu), start=_ptr(self.start))
         self.ref = ctypes.byref(self.s)

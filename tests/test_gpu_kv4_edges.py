@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from kv4_plain import Plain
-from test_gpu_kv4 import cu_of, make, rows_like
+from test_gpu_kv4 import attend, cu_of, fill, make, rows_like
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +85,22 @@ def test_logits_of_any_finite_size(count, dtype, power, sign):
             l = (2 * one if s == 2 and sign > 0 else one) + np.log(len(seen))
             assert (np.abs(gl[row + j] - l) <= abs(l) * 2.0 ** -21 + 2.0 ** -18).all(), (s, j, gl[row + j], l)
         row += m
+
+
+def test_a_step_that_names_no_largest_count():
+    """Without max_count every sequence may have as many rows as the step: none is left out."""
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    c = make([60, 9, 30], 2, 64, 16, spare=9, more_pages=1)
+    plain = fill(c)
+    counts = [5, 0, 12]
+    b = semkv.KV4Batch(3, cu=cu_of(counts), total=17)
+    q = rows_like(np.random.default_rng(3), (17, 4, 64), torch.float16)
+    out = torch.full_like(q, 7.0)
+    semkv.semkv_kv4_attention(c, b, 0, q, out, 0.125, c.attention_workspace(b, 4))
+    assert int(c.dev_error.item()) == 0
+    want, _, _ = attend(c, plain, counts, 2, torch.float16, q=torch.cat([q, q[:3]]), scale=0.125)
+    assert (out - want[:17]).abs().max() < 0.01 and not (out == 7).any()
+    semkv.semkv_kv4_reserve(c, b, c.pages_workspace(3))
+    assert b.start.tolist() == [60, 9, 30] and c.length.tolist() == [65, 9, 42]
+    assert semkv.KV4Batch(5).s.max_count == 1      # one row to a sequence

@@ -71,3 +71,13 @@ def test_buffers_that_the_library_would_refuse_make_no_cache(sk):
     shifted = room[-room.data_ptr() % 16 + 4:][:size]
     with pytest.raises(ValueError, match="16 bytes"):
         sk.KV4Cache.over(shifted.view(1, 4, 2, 1, 1152), table, length, c.refs, 64)
+
+
+def test_the_largest_count_of_a_step_that_names_none(sk):
+    """As many rows as there are, so that no sequence is left out; one where each has one."""
+    cu = torch.zeros(4, dtype=torch.int32)
+    start = torch.zeros(3, dtype=torch.int32)
+    assert sk.KV4Batch(3, cu=cu, start=start, total=17).s.max_count == 17
+    assert sk.KV4Batch(3, cu=cu, start=start, total=17, max_count=9).s.max_count == 9
+    assert sk.KV4Batch(3, cu=cu, start=start, total=0).s.max_count == 0
+    assert sk.KV4Batch(3, start=start).s.max_count == 1
