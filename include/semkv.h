@@ -298,7 +298,19 @@ semkv_status semkv_decode_attention_noalloc(const semkv_quant_desc* desc,
  * destination in use, 3 an index outside its range (a page, a sequence, a row range) or
  * a sequence listed twice where it may not be, 4 a NaN or an infinity stored.  The first
  * one written stays.  What an entry does with a wrong index is given with each call; none
- * reads or writes outside the buffers it was given. */
+ * reads or writes outside the buffers it was given.
+ *
+ * Table, length and refs are these calls' to change.  A length lowered by hand leaves the
+ * pages behind its end counted although no table entry in use names them: they do not come
+ * back to the pool.
+ *
+ * Calls that may overlap on the GPU.  Reserve, fork, free and compact find free pages by
+ * the counts and change them without locks: on one cache they run one after the other (one
+ * stream, or events between them), else a page may be given away twice.  Write, read and
+ * attention may overlap with one another, and with those four where these take other
+ * sequences.  No call may overlap with one that changes the length, the table row or the
+ * stored rows of a sequence that it uses; the promise above holds for state that stands
+ * still while the call runs. */
 enum { SEMKV_F16 = 0, SEMKV_BF16 = 1 };
 enum { SEMKV_KV4_MAX_SEQS = 65535 };  /* sequences of one call */
 
@@ -326,7 +338,8 @@ typedef struct {
 typedef struct {
   int32_t n;             /* sequences that take part, 0..SEMKV_KV4_MAX_SEQS           */
   int32_t total;         /* rows of the tensors, 0..2^30; with 0 they may be NULL     */
-  int32_t max_count;     /* no sequence has more rows than this                       */
+  int32_t max_count;     /* no sequence has more rows than this (one that has is left
+                            out, 3); it chooses the kernel and sizes the workspace    */
   const int32_t* seqs;   /* device [n], or NULL for 0 .. n-1                          */
   const int32_t* cu;     /* device [n+1], ascending: rows cu[i] .. cu[i+1]-1 are the
                             i-th sequence's; rows from cu[n] on belong to nobody and are
@@ -379,7 +392,10 @@ semkv_status semkv_kv4_read(const semkv_kv4_cache* cache, const semkv_kv4_batch*
  * range (more than max_count rows among them) is left out, its rows untouched (3); a length
  * past the table counts as the table's end and a page index outside the pool as page 0 (3).
  * Accuracy: products are exact in binary32; the weights are rounded to fp16 before they meet V
- * (relative 2^-11 each), as the result is to its type.
+ * (relative 2^-11 each), as the result is to its type.  The sums are binary32, one chain over each
+ * worker's share of the positions: every 16 of them can add 17 * 2^-23 of sum_t p_t |V_t| (2^-11 of
+ * it for a share of 3800), every share that is joined 2^-20.  Logits are binary32 and may have any
+ * finite size; their own rounding then decides what the softmax sees.
  * ws: device workspace of semkv_kv4_attention_workspace_bytes bytes, 16-byte aligned; calls
  * that may overlap on the GPU need one each. */
 size_t semkv_kv4_attention_workspace_bytes(const semkv_kv4_cache* cache,

@@ -1,11 +1,12 @@
 // kv4_attend.cu — attention over the paged 4-bit cache for few query rows (single tokens,
 // drafted tokens), bound by reading the cache and by turning it into operands: 16 sequences of 64K
-// with 8 KV heads in groups of 4 take 216 us, 82% of the copy rate, at 50% of the issue slots (336
+// with 8 KV heads in groups of 4 take 215 us, 83% of the copy rate, at 52% of the issue slots (337
 // instructions for a tile of 16 tokens) and 19% of the tensor pipe.
 //
 // For a tile of 16 tokens, on mma.sync m16n8k16 with fp16 operands and fp32 sums:
 //   S^T = K Q^T      M = 16 tokens, N = 8 query rows, K = head dim
 //   P   = 2^(S - e)  e: the row's reference exponent, moved only when a weight would pass 2^15
+//                    (far logits: kFar)
 //   O^T += V^T P^T   M = head dim, N = 8 query rows, K = 16 tokens
 // The tokens and the head dim are the M side, so eight rows (a GQA group, a few drafted
 // tokens) fill N, and more rows are further N tiles of the same dequantized operands.  The order of

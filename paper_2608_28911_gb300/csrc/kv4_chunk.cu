@@ -25,7 +25,8 @@
 // (S_t's barrier, which follows it, tells) and the next waits for P_t.
 // Two blocks and a unit of 128 take 3050 cycles of an SM, of which the products are 2350 at the rate of the
 // peak and the operands' trips through shared memory 2050: 2048 tokens over 30K run at 1.49 PFLOP/s, 79% of a
-// large library product.  An item costs about 10000 cycles besides, mostly for its results and the unit on its diagonal.
+// large library product, from a captured graph (655 us), and at 1.45, 77%, as calls among others (670 us).  An item
+// costs about 10000 cycles besides, mostly for its results and the unit on its diagonal.
 // A tile of one block only (a few tokens of a large group, the end of a chunk) has both halves work on it:
 // they take its units in turn, and the first puts the two sums together, which halves its time.
 // Tensor memory: S_0, S_1, O_0, O_1, 128 columns each.
@@ -186,7 +187,8 @@ struct Item {
   int parts;                      // workers that share it, where it begins and does not end here; else 0
 };
 // What the join has to know of an item that a worker begins and does not end: its first row (of those of all
-// query heads), rows | parts << 16, V's scale.  Left here rather than looked for in the join, it takes 4 of 236 us off six ragged prompts.
+// query heads), rows | parts << 16, V's scale.  (With the join looking for it six ragged prompts took 236 us, not the 232
+// of that time.)
 struct Kv4Join {
   int64_t first_row;
   uint32_t rows_parts;
@@ -581,7 +583,8 @@ __device__ __forceinline__ void softmax_warps(const Kv4Attend& a, const Kv4ManyC
       if (__builtin_expect(!open, 0)) {
         // a unit that some row sees a part of: what is hidden becomes -infinity where it lies.  A warp's rows are a
         // few tokens, so that of its groups of 32 positions one or two are hidden in part and need a look.
-        // (With a loop of its own for such units, which took 6600 cycles, six ragged prompts were 7 us of 232 slower.)
+        // (With a loop of its own for such units, which took 6600 cycles, six ragged prompts took 239 us, not the 232 of
+        // that time.)
         int lo, hi;
         sight(lo, hi);
 #pragma unroll 1
@@ -1011,8 +1014,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_chunk_kernel(Kv4Attend a, Kv4
   if (W > 0 && (int)blockIdx.x < ranges.count) {
     Walk& walk = *reinterpret_cast<Walk*>(smem + L::walk());
     if (warp == kThreads / 32 - 1) walk.start(a, cut, prefix, ranges);
-    // 184 + 184 + 80 + 64 = 4 * 128, the registers of the launch.  2048 tokens over 30K take 653 us with these,
-    // 712 with 176, 176, 88, 72, 700 with 184, 184, 72, 72 and 710 with 192, 192, 72, 56.
+    // 184 + 184 + 80 + 64 = 4 * 128, the registers of the launch.  2048 tokens over 30K took 653 us with these,
+    // 712 with 176, 176, 88, 72, 700 with 184, 184, 72, 72 and 710 with 192, 192, 72, 56.  ptxas still spills a few
+    // registers (40 bytes stored with f16 rows, 24 with bf16).
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
       softmax_warps<D, BF16>(a, cut, walk, undo, reinterpret_cast<float2*>(smem + L::other()), bars, tmem);
@@ -1203,8 +1207,10 @@ cudaError_t launch_chunk(const Kv4Attend& a, const Kv4ManyCut& cut, int sms, cud
 
 bool kv4_many(const Kv4Batch& b, int group) {
   // one tile of the small kernel holds up to 32 rows; more would read the cache again.  8 sequences of 32K, head
-  // dim 128: 20 rows 118 us there and 184 here, 36 rows 261 and 184.  (A tile of 48 rows, which head dim 64
-  // leaves registers for, was no faster than this kernel: 36 rows of 8 sequences of 4K 32 us, 30 here.)
+  // dim 128: 20 and 24 rows 124 us there, 28 rows 145, 32 rows 149, here 194 each; one sequence of 32K: 40, 44 and 46
+  // us there, 50 here; head dim 64, 8 sequences: 87, 104 and 104 there, 153 here.  With a second tile, 36 rows of 8
+  // sequences took 261 us there and 184 here.  (A tile of 48 rows, which head dim 64 leaves registers for, was no
+  // faster than this kernel: 36 rows of 8 sequences of 4K 32 us, 30 here.)
   return (int64_t)b.max_count * group > 32 && group <= 2 * kBlock;
 }
 
