@@ -286,9 +286,9 @@ constexpr float kHead = 8.f;     // a moved reference puts the largest weight at
 constexpr float kMost = 15.f;    // largest exponent of a weight
 // A logit past 2^22 has steps of a half and more in binary32.  The exponent as one fused product and sum would hold up
 // to half a step of what the reference was rounded by, so that far out equal logits all had weight 0 or infinity; there
-// the product is rounded first and the reference is the largest itself.
+// the product is rounded first, and where kHead is no longer exact beside it the reference is the largest itself.
 constexpr float kFar = 0x1p22f;
-__device__ __forceinline__ float reference_for(float top) { return fabsf(top) > kFar ? top : top - kHead; }
+__device__ __forceinline__ float reference_for(float top) { return fabsf(top) > 0x1p26f ? top : top - kHead; }
 __device__ __forceinline__ bool is_far(float ref) { return fabsf(ref) > kFar && ref != kNone; }
 
 // Which positions a query row sees: [lo, hi]; hi < 0 for a row that is not there.
