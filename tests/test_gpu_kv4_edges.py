@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from kv4_plain import Plain
-from test_gpu_kv4 import attend, cu_of, fill, make, rows_like
+from test_gpu_kv4 import attend, cu_of, fill, make, rows_like, t32
 
 pytestmark = pytest.mark.gpu
 
@@ -104,3 +104,29 @@ def test_a_step_that_names_no_largest_count():
     semkv.semkv_kv4_reserve(c, b, c.pages_workspace(3))
     assert b.start.tolist() == [60, 9, 30] and c.length.tolist() == [65, 9, 42]
     assert semkv.KV4Batch(5).s.max_count == 1      # one row to a sequence
+
+
+def test_page_calls_over_many_sequences():
+    """More sequences than a plan has threads, forked, freed and pruned in one call each."""
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    rng = np.random.default_rng(2)
+    n, T = 1500, 70
+    lens = [int(x) for x in rng.integers(0, T, n)] + [4000]
+    c = make(lens, 1, 64, 16, spare=6000, extra_seqs=n, seed=3)
+    c.pages.copy_(torch.randint(0, 256, c.pages.shape, dtype=torch.uint8))
+    plain = Plain(c)
+    src, dst = rng.integers(0, n + 1, n), n + 1 + rng.permutation(n)
+    semkv.semkv_kv4_fork(c, t32(src), t32(dst))
+    plain.fork(src.tolist(), dst.tolist())
+    plain.same_state(c)
+    gone = rng.permutation(2 * n + 1)[:n]
+    semkv.semkv_kv4_free(c, t32(gone))
+    plain.free(gone.tolist())
+    plain.same_state(c)
+    seqs = rng.permutation(2 * n + 1)[:n + 200]
+    keep = (rng.random((len(seqs), T)) < 0.4).astype(np.uint8)
+    semkv.semkv_kv4_compact(c, t32(seqs), torch.tensor(keep, device="cuda"), c.pages_workspace(len(seqs), T))
+    assert plain.compact(seqs.tolist(), keep)
+    plain.same_state(c)
+    assert int(c.dev_error.item()) == 0
