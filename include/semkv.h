@@ -67,6 +67,7 @@ typedef enum {
 enum { SEMKV_BASE_AFFINE = 0, SEMKV_BASE_TQ = 1, SEMKV_BASE_AFFINE_HAD = 2,
        SEMKV_BASE_TQ_DENSE = 3 };
 enum { SEMKV_HEAD_DIM = 128, SEMKV_MAX_LEVELS = 8 };
+enum { SEMKV_F16 = 0, SEMKV_BF16 = 1, SEMKV_F32 = 2 };  /* types of tensors (F32: semkv_beam_select only) */
 
 /* Quantizer description (host struct; the pointers inside are device pointers).
  * base AFFINE: per-row asymmetric min/max quantizer with fp16 scale and offset
@@ -275,6 +276,42 @@ semkv_status semkv_decode_attention_noalloc(const semkv_quant_desc* desc,
                                             const uint16_t* q, float* out, float softmax_scale,
                                             void* stream);
 
+/* One step of beam search: the best continuations of each group's beams.  Row r = group * beams + b of
+ * the logits belongs to beam b of the group, which stands at scores[r] (the sum of its tokens' log
+ * probabilities).  Token t of that row is a candidate with
+ *   scores[r] + logits[r][t] - ln sum_u exp(logits[r][u])
+ * and the k best of the group's beams * vocab candidates, best first, go to parent (the row r), token
+ * and score.  The order is that of the exact scores as far as 40 bits tell them apart (see below);
+ * equal ones: the lower row first, then the lower token.  (-0 equals +0.)
+ *  - A logit of -infinity is no candidate (a banned token).  Neither is a NaN or +infinity, which count
+ *    as -infinity; they write 4 into the error word.
+ *  - A row whose score is -infinity has no candidates and is not read (the first step of a search: all
+ *    beams but one).  Nor has one whose score is a NaN or +infinity, which writes 4.
+ *  - done (may be NULL): device u8 [groups * beams].  A row with done != 0 is not read either; it has one
+ *    candidate, end_token at scores[r].
+ *  - Where there are fewer than k candidates the rest is parent -1, token -1, score -infinity.
+ * logits: device [groups * beams][vocab] of type `dtype` (SEMKV_F16, SEMKV_BF16 or SEMKV_F32), `stride`
+ * >= vocab elements from row to row, aligned to its type; scores: device f32 [groups * beams]; parent,
+ * token: device i32 [groups][k]; score: device f32 [groups][k].  beams, k: 1 .. 128; vocab: 1 .. 2^24;
+ * groups * beams: up to 2^20.  end_token: 0 .. vocab-1 where done is given, else not used.  dev_error:
+ * device i32 or NULL.
+ * Accuracy: sums of exponentials are binary32 with a known bound (some 2^-18 of the sum); where two
+ * candidates of different beams whose order matters lie within it, their rows are summed again to 2^-37,
+ * so that what comes out is the order by exact scores unless these agree to 2^-36.  Equal rows with equal
+ * scores agree in every bit.  score is rounded once to binary32 from a sum within the first bound.
+ * ws: device workspace of semkv_beam_select_workspace_bytes bytes, 16-byte aligned; calls that may
+ * overlap on the GPU need one each.  Nothing in it has to be kept or cleared.
+ * Errors: SEMKV_EINVAL, SEMKV_EALIGN, SEMKV_EUNSUPPORTED (dtype, more beams, k, vocab or rows than above),
+ * SEMKV_EWORKSPACE.  groups 0 is a no-op. */
+enum { SEMKV_BEAM_MAX = 128 };  /* beams of a group, and k */
+size_t semkv_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t vocab, int32_t dtype,
+                                         int32_t k);
+semkv_status semkv_beam_select(int32_t groups, int32_t beams, int32_t vocab, int32_t dtype,
+                               const void* logits, int64_t stride, const float* scores,
+                               const uint8_t* done, int32_t end_token, int32_t k, int32_t* parent,
+                               int32_t* token, float* score, int32_t* dev_error, void* ws,
+                               size_t ws_bytes, void* stream);
+
 /* ------------------------------------------------ a paged cache held in 4 bits ----
  * A cache of its own beside semkv_cache, for serving: sequences of different lengths,
  * pages that several sequences share, queries of one token or of many.  The paper has no
@@ -304,14 +341,13 @@ semkv_status semkv_decode_attention_noalloc(const semkv_quant_desc* desc,
  * pages behind its end counted although no table entry in use names them: they do not come
  * back to the pool.
  *
- * Calls that may overlap on the GPU.  Reserve, fork, free and compact find free pages by
+ * Calls that may overlap on the GPU.  Reserve, fork, free, reorder and compact go by
  * the counts and change them without locks: on one cache they run one after the other (one
  * stream, or events between them), else a page may be given away twice.  Write, read and
- * attention may overlap with one another, and with those four where these take other
+ * attention may overlap with one another, and with those five where these take other
  * sequences.  No call may overlap with one that changes the length, the table row or the
  * stored rows of a sequence that it uses; the promise above holds for state that stands
  * still while the call runs. */
-enum { SEMKV_F16 = 0, SEMKV_BF16 = 1 };
 enum { SEMKV_KV4_MAX_SEQS = 65535 };  /* sequences of one call */
 
 typedef struct {
@@ -379,6 +415,40 @@ semkv_status semkv_kv4_read(const semkv_kv4_cache* cache, const semkv_kv4_batch*
                             int32_t layer, int32_t dtype, void* k_out, void* v_out,
                             void* stream);
 
+/* semkv_kv4_write of rows whose position is still to be worked into them: keys are turned on their
+ * way into the pages, and the step's queries, where q_heads > 0, from q into q_out.  A pair (a, b) of
+ * the first rot_dim dims of a head becomes (a c - b s, b c + a s) with c and s the table's entries of the
+ * row's position, in binary32, each product, sum and difference rounded by itself; the other dims stay
+ * as they are.  A query is rounded once to `dtype`; K's blocks are quantized from the binary32 values.
+ * The pair's index j selects cosine j and sine j:
+ *   SEMKV_KV4_HALVES  dims j and j + rot_dim / 2
+ *   SEMKV_KV4_PAIRS   dims 2 j and 2 j + 1
+ * positions: device i32 [total], the position of each row, or NULL: where it goes in its sequence
+ * (start[i] + j).  They differ where a sequence was pruned.  A row whose position lies outside the table
+ * is left out (3), queries and values too, like a row without a place in the pages; nothing of a row
+ * that is left out is written.
+ * q, q_out: device [total][q_heads][head_dim] of type `dtype`, with q_stride and q_out_stride
+ * elements from row to row (as k's), 16-byte aligned; q_out may be q, with the same stride, and does not
+ * overlap it otherwise.  With q_heads 0 they are not used.
+ * Errors: SEMKV_EINVAL (rot_dim outside 1..head_dim among them), SEMKV_EALIGN, SEMKV_EUNSUPPORTED
+ * (rot_dim not a multiple of 16, an unknown layout). */
+enum { SEMKV_KV4_HALVES = 0, SEMKV_KV4_PAIRS = 1 };
+
+typedef struct {
+  int32_t rot_dim;       /* dims of each head that are turned: a multiple of 16, up to head_dim */
+  int32_t layout;        /* SEMKV_KV4_HALVES or SEMKV_KV4_PAIRS                         */
+  int32_t rows;          /* positions in the table                                      */
+  const float* cos_sin;  /* device [rows][rot_dim], 16-byte aligned: the position's rot_dim / 2
+                            cosines, then its sines                                      */
+} semkv_kv4_rotation;
+
+semkv_status semkv_kv4_write_rotated(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch,
+                                     int32_t layer, const semkv_kv4_rotation* rotation,
+                                     const int32_t* positions, int32_t dtype, const void* q,
+                                     int64_t q_stride, int32_t q_heads, void* q_out,
+                                     int64_t q_out_stride, const void* k, int64_t k_stride,
+                                     const void* v, int64_t v_stride, void* stream);
+
 /* Causal attention of a step's rows over one layer of their sequences.  With length L and m
  * rows, the sequence's j-th row stands at position p = L - m + j and sees the positions
  * max(0, p - window + 1) .. p (window 0: all up to p); a row at a negative position sees
@@ -417,6 +487,18 @@ semkv_status semkv_kv4_fork(const semkv_kv4_cache* cache, int32_t n, const int32
  * 0 .. n-1. */
 semkv_status semkv_kv4_free(const semkv_kv4_cache* cache, int32_t n, const int32_t* seqs,
                             void* stream);
+
+/* Sequences take one another's place, all at once: the i-th sequence of the list becomes a branch of
+ * what the parent[i]-th of the list was before the call (its length, and its pages, which both then
+ * share); parent[i] = i keeps it, parent[i] = -1 empties it.  Any map will do, a cycle among them, and a
+ * state that no entry takes up is gone: its pages' refs fall.  Table entries past a new length stay
+ * as they are.  An entry whose sequence was listed before or is out of range, or whose parent[i] is outside
+ * -1 .. n-1 or names an entry out of range, is left out: it changes nothing (3).  (One whose sequence was
+ * listed before still serves as a parent.)  seqs: device [n] or NULL for 0 .. n-1; parent: device [n], such
+ * as semkv_beam_select gives for the rows that go on.
+ * ws: device workspace of semkv_kv4_pages_workspace_bytes(cache, n, 0) bytes, 16-byte aligned. */
+semkv_status semkv_kv4_reorder(const semkv_kv4_cache* cache, int32_t n, const int32_t* seqs,
+                               const int32_t* parent, void* ws, size_t ws_bytes, void* stream);
 
 /* Prunes sequences to some of their tokens, in order, in every layer: of the i-th sequence the
  * tokens t < tokens with keep[i][t] != 0 stay, and all from `tokens` on (they have no flag).

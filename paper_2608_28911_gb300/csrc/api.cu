@@ -126,6 +126,37 @@ semkv_status semkv_rank_assign(const float* scores, int32_t batch, int32_t T, ui
   return from_cuda(launch_rank_assign(a, (cudaStream_t)stream));
 }
 
+namespace {
+semkv_status check_beam(int32_t groups, int32_t beams, int32_t vocab, int32_t dtype, int32_t k) {
+  if (groups < 0 || beams < 1 || vocab < 1 || k < 1) return SEMKV_EINVAL;
+  if (beams > SEMKV_BEAM_MAX || k > SEMKV_BEAM_MAX || vocab > 1 << 24) return SEMKV_EUNSUPPORTED;
+  if ((int64_t)groups * beams > 1 << 20) return SEMKV_EUNSUPPORTED;
+  return dtype == SEMKV_F16 || dtype == SEMKV_BF16 || dtype == SEMKV_F32 ? SEMKV_OK : SEMKV_EUNSUPPORTED;
+}
+}  // namespace
+
+size_t semkv_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t vocab, int32_t dtype, int32_t k) {
+  if (check_beam(groups, beams, vocab, dtype, k) != SEMKV_OK || groups == 0) return 0;
+  return beam_select_workspace(groups, beams, vocab, dtype, k);
+}
+
+semkv_status semkv_beam_select(int32_t groups, int32_t beams, int32_t vocab, int32_t dtype, const void* logits, int64_t stride,
+                               const float* scores, const uint8_t* done, int32_t end_token, int32_t k, int32_t* parent,
+                               int32_t* token, float* score, int32_t* dev_error, void* ws, size_t ws_bytes, void* stream) {
+  const TraceRange trace("semkv_beam_select");
+  const semkv_status s = check_beam(groups, beams, vocab, dtype, k);
+  if (s != SEMKV_OK) return s;
+  if (stride < vocab || (done && (end_token < 0 || end_token >= vocab))) return SEMKV_EINVAL;
+  if (groups == 0) return SEMKV_OK;
+  if (!logits || !scores || !parent || !token || !score) return SEMKV_EINVAL;
+  if (!aligned(logits, dtype == SEMKV_F32 ? 4 : 2) || !aligned(scores, 4) || !aligned(parent, 4) || !aligned(token, 4) ||
+      !aligned(score, 4) || !aligned(dev_error, 4))
+    return SEMKV_EALIGN;
+  if (!ws || !aligned(ws, 16) || ws_bytes < beam_select_workspace(groups, beams, vocab, dtype, k)) return SEMKV_EWORKSPACE;
+  const BeamArgs a{groups, beams, vocab, k, end_token, logits, stride, scores, done, parent, token, score, dev_error};
+  return from_cuda(launch_beam_select(a, dtype, ws, (cudaStream_t)stream));
+}
+
 semkv_status semkv_fake_quant(const semkv_quant_desc* desc, const uint16_t* k, const uint16_t* v,
                               int32_t batch, int32_t layers, int32_t kv_heads, int32_t T,
                               const uint8_t* is_high, uint16_t* k_out, uint16_t* v_out,

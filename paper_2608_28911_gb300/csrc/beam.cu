@@ -1,0 +1,713 @@
+// beam.cu — one step of beam search: the k best of a group's beams * vocab continuations.
+//
+// Two kernels.  The scan has CTAs over pieces of the rows: each reads its piece once, keeps sum exp(x - m) of
+// what it saw and the best logits, k of them and a few more.  The merge has a CTA for each group: the rows'
+// normalizers from the pieces' sums, then the k best of the pieces' candidates by score.
+//
+// A candidate is a key: a number whose order is the candidates', and all keys differ.  The k best
+// of many keys, spread over a CTA's threads, come in two steps: a key T such that k threads, or a few
+// more, have a largest key of T or above (found bit by bit, a barrier that counts for each), and then all keys from T
+// on, which those threads alone hold.  Nothing else is sorted; ties, constant rows and rows in ascending order take the
+// same way.
+//
+// A sum's terms are 2^(x log2 e - c) with a whole number c, so that sums of different c are brought together exactly.
+// They are binary32, with a bound on their error.  If that leaves open which of two rows' candidates
+// comes first, the merge sums the rows in question again, in pairs of binary32 numbers.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <float.h>
+
+#include "common.cuh"
+#include "kernels.h"
+
+namespace semkv {
+namespace {
+
+constexpr int kScanThreads = 256, kMergeThreads = 512;
+constexpr int kSlack = 16;       // keys that a threshold may let through beside the k best
+constexpr int kMergePer = 4;     // candidates that a thread of the merge looks at in one go
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.69314718055994530942;
+// Past this logits are too coarse for x log2 e in one rounding: rows with a largest logit beyond it are summed exactly.
+constexpr float kFar = 1048576.f;
+constexpr float kNone = -INFINITY;
+
+// ------------------------------------------------------------------ keys ------
+
+// A float as an unsigned number of the same order; -0 as +0.
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b ^ ((int32_t)b < 0 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t u) {
+  return __uint_as_float(u ^ ((int32_t)u < 0 ? 0x80000000u : 0xFFFFFFFFu));
+}
+// In a row: the logit, then the lower token.  0: none.
+struct RowKey {
+  uint64_t a;
+  static constexpr int kBits = 64;
+  __device__ __forceinline__ static RowKey none() { return {0}; }
+  __device__ __forceinline__ static RowKey of(float x, int token) {
+    return {(uint64_t)ordered(x) << 32 | (0xFFFFFFFFu - (uint32_t)token)};
+  }
+  __device__ __forceinline__ float logit() const { return unordered((uint32_t)(a >> 32)); }
+  __device__ __forceinline__ int token() const { return (int)(0xFFFFFFFFu - (uint32_t)a); }
+  __device__ __forceinline__ bool valid() const { return a != 0; }
+  __device__ __forceinline__ bool operator>=(const RowKey& o) const { return a >= o.a; }
+  __device__ __forceinline__ RowKey with(int bit) const { return {a | 1ull << bit}; }
+};
+// In a group: the score (a binary32 number and what it lacks), then the lower beam, the larger logit and the lower
+// token.  a = 0: none.
+struct GroupKey {
+  uint64_t a, b;
+  static constexpr int kBits = 128;
+  __device__ __forceinline__ static GroupKey none() { return {0, 0}; }
+  __device__ __forceinline__ static GroupKey of(float score, float rest, int beam, float x, int token) {
+    return {(uint64_t)ordered(score) << 32 | ordered(rest),
+            (uint64_t)(SEMKV_BEAM_MAX - 1 - beam) << 56 | (uint64_t)ordered(x) << 24 | (0xFFFFFFu - (uint32_t)token)};
+  }
+  __device__ __forceinline__ float score() const { return unordered((uint32_t)(a >> 32)); }
+  __device__ __forceinline__ float rest() const { return unordered((uint32_t)a); }
+  __device__ __forceinline__ int beam() const { return SEMKV_BEAM_MAX - 1 - (int)(b >> 56); }
+  __device__ __forceinline__ int token() const { return (int)(0xFFFFFFu - (uint32_t)(b & 0xFFFFFFu)); }
+  __device__ __forceinline__ bool valid() const { return a != 0; }
+  __device__ __forceinline__ bool operator>=(const GroupKey& o) const { return a > o.a || (a == o.a && b >= o.b); }
+  __device__ __forceinline__ GroupKey with(int bit) const {
+    return bit >= 64 ? GroupKey{a | 1ull << (bit - 64), b} : GroupKey{a, b | 1ull << bit};
+  }
+};
+
+// The best keys of a CTA so far, in shared memory: at least the k best of all that were offered.
+template <typename Key, int THREADS>
+struct Best {
+  Key* list;    // [cap]
+  Key* spare;   // [k + kSlack]
+  int* count;
+  int k, cap;
+  Key floor;    // k keys of this or more are in the list (or have been): a key below does not matter
+
+  // A T that k or a few more of the threads' keys reach, each thread bringing `per` of the n keys in `keys`.
+  // All keys differ, so that there is one; n is at least k.
+  __device__ __forceinline__ Key threshold_of(const Key* keys, int n) const {
+    Key t = Key::none();
+    for (int bit = Key::kBits - 1; bit >= 0; --bit) {
+      const Key up = t.with(bit);
+      int c = 0;
+      for (int j = 0; j < n; j += THREADS) c += __syncthreads_count(j + (int)threadIdx.x < n && keys[j + threadIdx.x] >= up);
+      if (c < k) continue;
+      t = up;
+      if (c <= k + kSlack) break;
+    }
+    return t;
+  }
+  // The same, a key from each thread; more than k + kSlack of them are valid.
+  __device__ __forceinline__ Key threshold_of(Key mine) const {
+    Key t = Key::none();
+    for (int bit = Key::kBits - 1; bit >= 0; --bit) {
+      const Key up = t.with(bit);
+      const int c = __syncthreads_count(mine >= up);
+      if (c < k) continue;
+      t = up;
+      if (c <= k + kSlack) break;
+    }
+    return t;
+  }
+  // For all threads at once, behind a barrier: the list is cut down to the k best and up to kSlack more.
+  __device__ __forceinline__ void cut(int n) {
+    const Key t = threshold_of(list, n);
+    __syncthreads();
+    if (threadIdx.x == 0) *count = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += THREADS)
+      if (list[i] >= t) spare[atomicAdd(count, 1)] = list[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < *count; i += THREADS) list[i] = spare[i];
+    __syncthreads();
+    floor = t;
+  }
+  __device__ __forceinline__ void put(const Key& x) { list[atomicAdd(count, 1)] = x; }
+};
+
+// Threads bring a few keys each; `top` is the largest of the thread's own and collect(bound) puts those from the bound on.
+template <typename Key, int THREADS, int PER, typename Collect>
+__device__ __forceinline__ void offer(Best<Key, THREADS>& best, const Key& top, Collect collect) {
+  // (a key equal to the floor is in the list already)
+  bool hot = top.valid() && top >= best.floor;
+  int n = __syncthreads_count(hot);
+  if (n == 0) return;
+  const int held = *best.count;
+  __syncthreads();
+  if ((n > best.k + kSlack || held + n * PER > best.cap) && held > best.k + kSlack) {
+    best.cut(held);
+    hot = top.valid() && top >= best.floor;
+    n = __syncthreads_count(hot);
+  }
+  if (n > best.k + kSlack) {
+    const Key t = best.threshold_of(hot ? top : Key::none());
+    if (t >= best.floor) best.floor = t;
+    hot = top.valid() && top >= best.floor;
+  }
+  if (hot) collect(best.floor);
+}
+
+// ------------------------------------------------------------------ rows ------
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 2^d for a whole number d <= 0 (or minus infinity)
+__device__ __forceinline__ float pow2(float d) {
+  return d < -126.f ? 0.f : __uint_as_float((uint32_t)((int)d + 127) << 23);
+}
+// The whole number that terms beside a largest logit m are scaled by: their sum is at least 1/2.
+__device__ __forceinline__ float scale_of(float m) { return ceilf(fminf(fmaxf(m, -kFar), kFar) * kLog2e); }
+// a + b = s + e exactly
+__device__ __forceinline__ void two_sum(float a, float b, float& s, float& e) {
+  s = __fadd_rn(a, b);
+  const float z = __fsub_rn(s, a);
+  e = __fadd_rn(__fsub_rn(a, __fsub_rn(s, z)), __fsub_rn(b, z));
+}
+
+// Eight 16-bit or four 32-bit logits as they lie in memory.
+template <int DTYPE>
+struct Vec {
+  static constexpr int kSize = DTYPE == SEMKV_F32 ? 4 : 2, kCount = 16 / kSize;
+  uint32_t w[4];
+
+  __device__ __forceinline__ static uint32_t none() {
+    return DTYPE == SEMKV_F32 ? 0xFF800000u : DTYPE == SEMKV_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
+  }
+  __device__ __forceinline__ void fill_none() { w[0] = w[1] = w[2] = w[3] = none(); }
+  __device__ __forceinline__ float at(int i) const {
+    if (DTYPE == SEMKV_F32) return __uint_as_float(w[i]);
+    if (DTYPE == SEMKV_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    return __half2float(__ushort_as_half((uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2])));
+  }
+  __device__ __forceinline__ void set(int i, uint32_t bits) {
+    if (DTYPE == SEMKV_F32) w[i] = bits;
+    else w[i / 2] = i & 1 ? (w[i / 2] & 0xFFFFu) | bits << 16 : (w[i / 2] & 0xFFFF0000u) | (bits & 0xFFFFu);
+  }
+  // the largest, a NaN if one is
+  __device__ __forceinline__ static uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    if (DTYPE == SEMKV_F32) asm("max.NaN.f32 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else if (DTYPE == SEMKV_BF16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  __device__ __forceinline__ float largest() const {
+    const uint32_t m = max2(max2(w[0], w[1]), max2(w[2], w[3]));
+    if (DTYPE == SEMKV_F32) return __uint_as_float(m);
+    Vec v;
+    v.w[0] = m;
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(v.at(0)), "f"(v.at(1)));
+    return d;
+  }
+  // NaN and +infinity become -infinity
+  __device__ __forceinline__ void clean() {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i)
+      if (!(at(i) < INFINITY)) set(i, none());
+  }
+};
+
+// Logits first .. first + count of a row, the others -infinity.  The vectors lie `lead` bytes behind a multiple of
+// 16; those inside the row are brought by whole aligned loads all the same, two for one of them (its neighbour's
+// other half is in the cache).  So a thread's logits, and the order of every sum, do not depend on where a row lies.
+template <int DTYPE>
+__device__ __forceinline__ Vec<DTYPE> load_vec(const char* row, int first, int vocab, int lead) {
+  using V = Vec<DTYPE>;
+  V v;
+  const char* at = row + (int64_t)first * V::kSize;
+  const int room = V::kCount + (lead ? V::kCount : 0);  // logits that the loads below may touch
+  if (lead == 0 && first + V::kCount <= vocab) {
+    const uint4 x = __ldcs(reinterpret_cast<const uint4*>(at));
+    v.w[0] = x.x, v.w[1] = x.y, v.w[2] = x.z, v.w[3] = x.w;
+  } else if (lead != 0 && first >= V::kCount && first + room <= vocab) {
+    const uint4 x = __ldg(reinterpret_cast<const uint4*>(at - lead)), y = __ldg(reinterpret_cast<const uint4*>(at - lead) + 1);
+    uint32_t t[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    if (lead & 8) {
+#pragma unroll
+      for (int i = 0; i < 6; ++i) t[i] = t[i + 2];
+    }
+    if (lead & 4) {
+#pragma unroll
+      for (int i = 0; i < 5; ++i) t[i] = t[i + 1];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v.w[i] = lead & 2 ? __funnelshift_r(t[i], t[i + 1], 16) : t[i];
+  } else {
+    v.fill_none();
+#pragma unroll
+    for (int i = 0; i < V::kCount; ++i)
+      if (first + i < vocab)
+        v.set(i, DTYPE == SEMKV_F32 ? reinterpret_cast<const uint32_t*>(at)[i] : (uint32_t)reinterpret_cast<const uint16_t*>(at)[i]);
+  }
+  return v;
+}
+
+// ------------------------------------------------------------------ scan ------
+
+// Where a call's pieces lie: `splits` pieces of `piece` logits to a row.
+struct Pieces {
+  int splits, piece;
+  float4* sums;  // [rows][splits] the largest logit, and the sum of 2^(x log2 e - scale_of(it)) as two numbers
+  RowKey* keys;  // [rows][splits][k + kSlack]
+};
+
+// A row that is read: neither done nor without a chance.
+__device__ __forceinline__ bool row_counts(const BeamArgs& a, int row) {
+  const float s = a.scores[row];
+  return (!a.done || !a.done[row]) && s > -INFINITY && s < INFINITY;
+}
+
+template <int DTYPE>
+__device__ __forceinline__ const char* row_at(const BeamArgs& a, int row) {
+  return static_cast<const char*>(a.logits) + (int64_t)row * a.stride * Vec<DTYPE>::kSize;
+}
+
+constexpr int kVecs = 4;  // vectors of a thread in one go
+
+__host__ __device__ constexpr int scan_cap(int k, int dtype) { return (k + kSlack) * (1 + kVecs * (dtype == SEMKV_F32 ? 4 : 8)); }
+__host__ __device__ constexpr int merge_cap(int k) { return (k + kSlack) * (1 + kMergePer); }
+
+template <int DTYPE>
+__global__ void __launch_bounds__(kScanThreads) beam_scan_kernel(BeamArgs a, Pieces p) {
+  using V = Vec<DTYPE>;
+  constexpr int kPer = kVecs * V::kCount, kTile = kScanThreads * kPer;
+  extern __shared__ __align__(16) unsigned char shared[];
+  __shared__ int count;
+  __shared__ float part[kScanThreads / 32];
+  __shared__ float part_low[kScanThreads / 32];
+  const int slots = a.k + kSlack;
+  Best<RowKey, kScanThreads> best;
+  best.list = reinterpret_cast<RowKey*>(shared);
+  best.spare = best.list + scan_cap(a.k, DTYPE);
+  best.count = &count;
+  best.k = a.k;
+  best.cap = scan_cap(a.k, DTYPE);
+  best.floor = RowKey::none();
+  if (threadIdx.x == 0) count = 0;
+  __syncthreads();
+  const int row = blockIdx.x / p.splits, split = blockIdx.x - row * p.splits;
+  pdl_wait();
+  pdl_trigger();
+  if (!row_counts(a, row)) return;
+  const char* at = row_at<DTYPE>(a, row);
+  const int lead = (int)((uintptr_t)at & 15);
+  const int begin = split * p.piece, end = min(a.vocab, begin + p.piece);
+  float m = kNone, c = -4 * kFar, sum = 0.f, low = 0.f;  // of this thread's logits
+  for (int t0 = begin; t0 < end; t0 += kTile) {
+    V v[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int first = t0 + (i * kScanThreads + (int)threadIdx.x) * V::kCount;
+      if (first < end) v[i] = load_vec<DTYPE>(at, first, a.vocab, lead);
+      else v[i].fill_none();
+    }
+    float big[kVecs], top = kNone;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      big[i] = v[i].largest();
+      if (!(big[i] < INFINITY)) {
+        v[i].clean();
+        big[i] = v[i].largest();
+        raise_error(a.err, kDevNonFinite);
+      }
+      top = fmaxf(top, big[i]);
+    }
+    if (top > kNone) {
+      if (top > m) {
+        m = top;
+        const float up = scale_of(m), by = pow2(c - up);  // (0 the first time)
+        sum *= by;
+        low *= by;
+        c = up;
+      }
+      float s[kVecs];
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        float e[V::kCount];
+#pragma unroll
+        for (int j = 0; j < V::kCount; ++j) e[j] = exp2_fast(__fmaf_rn(v[i].at(j), kLog2e, -c));
+#pragma unroll
+        for (int w = V::kCount / 2; w > 0; w /= 2)
+#pragma unroll
+          for (int j = 0; j < w; ++j) e[j] += e[j + w];
+        s[i] = e[0];
+      }
+      float err;
+      two_sum(sum, (s[0] + s[1]) + (s[2] + s[3]), sum, err);
+      low += err;
+    }
+    // the best logits
+    int where = 0;
+    if (top > kNone && ordered(top) >= (uint32_t)(best.floor.a >> 32)) {  // its lowest token
+#pragma unroll
+      for (int i = kVecs - 1; i >= 0; --i)
+#pragma unroll
+        for (int j = V::kCount - 1; j >= 0; --j)
+          if (v[i].at(j) == top) where = t0 + (i * kScanThreads + (int)threadIdx.x) * V::kCount + j;
+    }
+    offer<RowKey, kScanThreads, kPer>(best, top > kNone ? RowKey::of(top, where) : RowKey::none(), [&](const RowKey& from) {
+      const float least = from.valid() ? from.logit() : kNone;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i)
+        if (big[i] >= least)
+#pragma unroll
+          for (int j = 0; j < V::kCount; ++j) {
+            const float x = v[i].at(j);
+            const RowKey key = RowKey::of(x, t0 + (i * kScanThreads + (int)threadIdx.x) * V::kCount + j);
+            if (x > kNone && key >= from) best.put(key);
+          }
+    });
+  }
+  // the sum over the threads, a pair of numbers each
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float M = m;
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) M = fmaxf(M, __shfl_xor_sync(~0u, M, d));
+  if (lane == 0) part[warp] = M;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kScanThreads / 32; ++w) M = fmaxf(M, part[w]);
+  __syncthreads();
+  const float by = m > kNone ? pow2(c - scale_of(M)) : 0.f;
+  sum *= by;
+  low *= by;
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) {
+    float err;
+    const float other = __shfl_xor_sync(~0u, sum, d);
+    low += __shfl_xor_sync(~0u, low, d);
+    two_sum(sum, other, sum, err);
+    low += err;
+  }
+  if (lane == 0) {
+    part[warp] = sum;
+    part_low[warp] = low;
+  }
+  __syncthreads();
+  const int held = count;
+  if (threadIdx.x == 0) {
+    sum = part[0];
+    low = part_low[0];
+    for (int w = 1; w < kScanThreads / 32; ++w) {
+      float err;
+      two_sum(sum, part[w], sum, err);
+      low += part_low[w] + err;
+    }
+    p.sums[(int64_t)row * p.splits + split] = make_float4(M, sum, low, 0.f);
+  }
+  if (held > slots) {
+    __syncthreads();
+    best.cut(held);
+  }
+  const int left = held > slots ? count : held;
+  RowKey* out = p.keys + (int64_t)blockIdx.x * slots;
+  for (int i = threadIdx.x; i < slots; i += kScanThreads) out[i] = i < left ? best.list[i] : RowKey::none();
+}
+
+// ------------------------------------------------------- the exact sums ------
+
+// exp(d) for d = x - m <= 0 as a sum of three numbers, 2^-38 of it off: 2^n * 2^(j/32) * exp(t), with d log2 e taken in
+// two numbers and |t| <= ln 2 / 64, exp(t) - 1 by its series.
+__device__ __forceinline__ bool exp_parts(float x, float m, const float2* powers, float (&out)[3]) {
+  float d, dl;
+  two_sum(x, -m, d, dl);
+  if (!(d > -100.f)) return false;  // (below 2^-144 of the largest: past every bit that counts)
+  constexpr float kHigh = 1.4426950408889634f, kLow = (float)(1.4426950408889634074 - (double)kHigh);
+  const float p = __fmul_rn(d, kHigh);
+  const float e = __fmaf_rn(d, kHigh, -p) + __fmaf_rn(d, kLow, dl * kHigh);
+  const float n = rintf(p), f = p - n;
+  const float j = rintf(f * 32.f), r = __fmaf_rn(j, -1.f / 32, f);
+  constexpr float kBig = (float)kLn2, kSmall = (float)(kLn2 - (double)kBig);
+  const float t = __fmul_rn(r, kBig);
+  const float tl = __fmaf_rn(r, kBig, -t) + __fmaf_rn(r, kSmall, e * kBig);
+  const float q = t * t * __fmaf_rn(t, __fmaf_rn(t, __fmaf_rn(t, 1.f / 120, 1.f / 24), 1.f / 6), 0.5f);
+  // (exp(t + tl) - 1 = t + tl + t tl + q + ...)
+  const float rest = __fmaf_rn(t, tl, tl) + q;
+  const float2 w = powers[(int)j + 16];
+  const float a = __fmul_rn(w.x, t);
+  const float s = __uint_as_float((uint32_t)((int)n + 127) << 23);
+  out[0] = w.x * s;
+  out[1] = a * s;
+  out[2] = (__fmaf_rn(w.x, t, -a) + w.y + __fmaf_rn(w.y, t, w.x * rest)) * s;
+  return n >= -120.f;
+}
+
+// ln sum exp(x - most) of a row, by a whole CTA, to 2^-37, for its first warp.  `most` is the row's largest logit.
+template <int DTYPE>
+__device__ double exact_normalizer(const BeamArgs& a, int row, float most, const float2* powers, double* parts) {
+  using V = Vec<DTYPE>;
+  const char* at = row_at<DTYPE>(a, row);
+  const int lead = (int)((uintptr_t)at & 15);
+  float sum = 0.f, low = 0.f;
+  for (int first = threadIdx.x * V::kCount; first < a.vocab; first += kMergeThreads * V::kCount) {
+    V v = load_vec<DTYPE>(at, first, a.vocab, lead);
+#pragma unroll
+    for (int j = 0; j < V::kCount; ++j) {
+      const float x = v.at(j);
+      float e[3];
+      if (x > kNone && x < INFINITY && exp_parts(x, most, powers, e)) {
+        float err;
+        two_sum(sum, e[0], sum, err);
+        low += err;
+        two_sum(sum, e[1], sum, err);
+        low += err + e[2];
+      }
+    }
+  }
+  double total = (double)sum + (double)low;
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) total += __shfl_xor_sync(~0u, total, d);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = total;
+  __syncthreads();
+  if (threadIdx.x >= 32) return 0.0;
+  total = threadIdx.x < kMergeThreads / 32 ? parts[threadIdx.x] : 0.0;
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) total += __shfl_xor_sync(~0u, total, d);
+  return log(total);
+}
+
+// ----------------------------------------------------------------- merge ------
+
+// What a row's logits need to become scores: value + rest + (logit - most).
+struct Base {
+  float value, rest;
+  float most;   // the row's largest logit
+  float error;  // how far value + rest may be off
+  int kind;     // kNobody, kLogits, kDone
+};
+enum { kNobody, kLogits, kDone };
+
+__device__ __forceinline__ void set_value(Base& r, float score, float norm, float norm_low) {
+  two_sum(score, -norm, r.value, r.rest);
+  r.rest -= norm_low;
+}
+__device__ __forceinline__ GroupKey score_of(const Base& r, int beam, float x, int token) {
+  float d, dl, s, e;
+  two_sum(x, -r.most, d, dl);
+  two_sum(r.value, d, s, e);
+  if (!(s > kNone)) return GroupKey::of(-FLT_MAX, 0.f, beam, x, token);  // below all binary32 numbers
+  e += r.rest + dl;
+  const float score = __fadd_rn(s, e);
+  return GroupKey::of(score, __fadd_rn(__fsub_rn(s, score), e), beam, x, token);
+}
+
+template <int DTYPE>
+__global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, Pieces p) {
+  extern __shared__ __align__(16) unsigned char shared[];
+  __shared__ int count;
+  __shared__ double parts[kMergeThreads / 32];
+  __shared__ Base base[SEMKV_BEAM_MAX];
+  __shared__ uint32_t again[SEMKV_BEAM_MAX / 32];  // rows to be summed once more
+  __shared__ float2 powers[33];
+  __shared__ GroupKey out[SEMKV_BEAM_MAX];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = blockIdx.x, row0 = group * a.beams, slots = a.k + kSlack;
+  Best<GroupKey, kMergeThreads> best;
+  best.list = reinterpret_cast<GroupKey*>(shared);
+  best.spare = best.list + merge_cap(a.k);
+  best.count = &count;
+  best.k = a.k;
+  best.cap = merge_cap(a.k);
+  if (threadIdx.x < SEMKV_BEAM_MAX / 32) again[threadIdx.x] = 0;
+  pdl_wait();
+  pdl_trigger();
+  // a warp for each row: its pieces' sums together
+  for (int b = warp; b < a.beams; b += kMergeThreads / 32) {
+    const int row = row0 + b;
+    const float score = a.scores[row];
+    const bool is_done = a.done && a.done[row];
+    Base r{score, 0.f, 0.f, 0.f, kNobody};
+    if (score != score || score == INFINITY) {
+      if (lane == 0) raise_error(a.err, kDevNonFinite);
+    } else if (score > kNone && is_done) {
+      r.kind = kDone;
+    } else if (score > kNone) {
+      const float4* s = p.sums + (int64_t)row * p.splits;
+      float m = kNone;
+      for (int i = lane; i < p.splits; i += 32) m = fmaxf(m, s[i].x);
+#pragma unroll
+      for (int d = 16; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+      if (m > kNone) {
+        const float c = scale_of(m);
+        float sum = 0.f, low = 0.f, err;
+        for (int i = lane; i < p.splits; i += 32) {
+          const float4 x = s[i];
+          const float by = x.x > kNone ? pow2(scale_of(x.x) - c) : 0.f;
+          two_sum(sum, x.y * by, sum, err);
+          low += x.z * by + err;
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) {
+          const float other = __shfl_xor_sync(~0u, sum, d);
+          low += __shfl_xor_sync(~0u, low, d);
+          two_sum(sum, other, sum, err);
+          low += err;
+        }
+        r.most = m;
+        r.kind = kLogits;
+        // ln sum exp(x - m) = (c ln 2 - m) + ln(sum), the logarithm by the sum's exponent and a number from 3/4 to 3/2.
+        // What the terms' log2 e lacks is made up for with the weighted mean of the logits, m - u at the
+        // lowest with u = ln vocab - ln sum exp(x - m): m - u / 2 is taken, half the range is the error.
+        constexpr float kBig = (float)kLn2, kSmall = (float)(kLn2 - (double)kBig);
+        constexpr float kLack = (float)((double)kLog2e * kLn2 - 1.0);
+        const int e = ((int)(__float_as_uint(sum) - 0x3F400000u)) >> 23;
+        const float n = c + (float)e, h = __fmul_rn(n, kBig);
+        float norm, rest;
+        two_sum(h, -m, norm, rest);
+        rest += __fmaf_rn(n, kBig, -h) + n * kSmall + low / sum;
+        two_sum(norm, logf(ldexpf(sum, -e)), norm, err);
+        const float u = logf((float)a.vocab) - norm;
+        rest += err - kLack * (m - 0.5f * u);
+        set_value(r, score, norm, rest);
+        // In units of 2^-24: an exponent's argument is off by half a step, so 1 for each of |x - m| + ln 2, on the average
+        // over the terms u + ln 2; exponentials by 4; sums of eight and of four numbers by 5; the logarithm by 1.
+        r.error = (1.125f * fmaxf(u, 0.f) + 12.f) * 0x1p-24f;
+      }
+    }
+    if (lane == 0) base[b] = r;
+  }
+  if (threadIdx.x < 33) {
+    const double p = exp2(((int)threadIdx.x - 16) / 32.0);
+    powers[threadIdx.x] = make_float2((float)p, (float)(p - (double)(float)p));
+  }
+  __syncthreads();
+  auto sum_again = [&](int b) {
+    const double norm = exact_normalizer<DTYPE>(a, row0 + b, base[b].most, powers, parts);
+    if (threadIdx.x == 0) {
+      set_value(base[b], a.scores[row0 + b], (float)norm, (float)(norm - (double)(float)norm));
+      base[b].error = 0x1p-36f;
+    }
+    __syncthreads();
+  };
+  float worst = 0.f;
+  for (int b = 0; b < a.beams; ++b) {
+    if (base[b].kind == kLogits && fabsf(base[b].most) > kFar) sum_again(b);
+    worst = fmaxf(worst, base[b].error);
+  }
+  const int per_row = p.splits * slots, total = a.beams * per_row;
+  const RowKey* keys = p.keys + (int64_t)row0 * per_row;
+  auto candidate = [&](int e) {
+    const int b = e / per_row;
+    const Base& r = base[b];
+    if (r.kind == kNobody) return GroupKey::none();
+    if (r.kind == kDone) return e == b * per_row ? score_of(r, b, 0.f, a.end_token) : GroupKey::none();
+    const RowKey key = keys[e];
+    return key.valid() ? score_of(r, b, key.logit(), key.token()) : GroupKey::none();
+  };
+  int held = 0;
+  for (int round = 0;; ++round) {
+    best.floor = GroupKey::none();
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    for (int e0 = 0; e0 < total; e0 += kMergeThreads * kMergePer) {
+      GroupKey mine[kMergePer], top = GroupKey::none();
+#pragma unroll
+      for (int i = 0; i < kMergePer; ++i) {
+        const int e = e0 + i * kMergeThreads + threadIdx.x;
+        mine[i] = e < total ? candidate(e) : GroupKey::none();
+        if (mine[i] >= top) top = mine[i];
+      }
+      offer<GroupKey, kMergeThreads, kMergePer>(best, top, [&](const GroupKey& from) {
+#pragma unroll
+        for (int i = 0; i < kMergePer; ++i)
+          if (mine[i].valid() && mine[i] >= from) best.put(mine[i]);
+      });
+    }
+    __syncthreads();
+    held = count;
+    __syncthreads();
+    if (held > slots) {
+      best.cut(held);
+      held = count;
+    }
+    // the place of each among them
+    for (int i = threadIdx.x; i < held; i += kMergeThreads) {
+      const GroupKey x = best.list[i];
+      int place = -1;
+      for (int j = 0; j < held; ++j) place += best.list[j] >= x;
+      if (place < a.k) out[place] = x;
+    }
+    held = min(held, a.k);
+    __syncthreads();
+    if (round == 1) break;
+    // Is the order sure?  Neighbours of different rows, and whoever comes close to the last one.  (If two are as near as
+    // the worst rows' errors, so are all between them, and the rows of both have a neighbour of another row there.)
+    auto close = [&](const GroupKey& x, const GroupKey& y) {
+      const int b = x.beam(), c = y.beam();
+      if (b == c || fabsf((x.score() - y.score()) + (x.rest() - y.rest())) > 2.001f * worst) return false;
+      atomicOr(again + (b >> 5), 1u << (b & 31));
+      atomicOr(again + (c >> 5), 1u << (c & 31));
+      return base[b].kind == kLogits || base[c].kind == kLogits;
+    };
+    bool open = false;
+    for (int i = threadIdx.x; i + 1 < held; i += kMergeThreads) open |= close(out[i], out[i + 1]);
+    if (held == a.k) {
+      const GroupKey last = out[held - 1];
+      for (int e = threadIdx.x; e < total; e += kMergeThreads) {
+        const GroupKey x = candidate(e);
+        if (x.valid() && !(x >= last)) open |= close(x, last);
+      }
+    }
+    if (!__syncthreads_or(open)) break;
+    for (int b = 0; b < a.beams; ++b)
+      if (again[b >> 5] >> (b & 31) & 1 && base[b].kind == kLogits) sum_again(b);
+  }
+  for (int i = threadIdx.x; i < a.k; i += kMergeThreads) {
+    const int64_t at = (int64_t)group * a.k + i;
+    const bool is = i < held;
+    a.parent[at] = is ? row0 + out[i].beam() : -1;
+    a.token[at] = is ? out[i].token() : -1;
+    a.score[at] = is ? out[i].score() : kNone;
+  }
+}
+
+int vec_logits(int dtype) { return dtype == SEMKV_F32 ? 4 : 8; }
+
+// Rows are cut into pieces until there are a few CTAs for each SM, whole strides of a CTA each.  The cut depends on
+// the sizes alone, so that equal calls give equal bits.
+constexpr int kWantCtas = 152 * 8;
+Pieces cut_rows(int rows, int vocab, int dtype) {
+  const int unit = kScanThreads * vec_logits(dtype), units = (vocab + unit - 1) / unit;
+  int splits = (kWantCtas + rows - 1) / rows;
+  if (splits > units) splits = units;
+  Pieces p = {};
+  p.piece = (units + splits - 1) / splits * unit;
+  p.splits = (vocab + p.piece - 1) / p.piece;
+  return p;
+}
+
+template <int DTYPE>
+cudaError_t launch(const BeamArgs& a, const Pieces& p, cudaStream_t stream) {
+  const size_t scan = (scan_cap(a.k, DTYPE) + a.k + kSlack) * sizeof(RowKey);
+  const size_t merge = (merge_cap(a.k) + a.k + kSlack) * sizeof(GroupKey);
+  const cudaError_t e = launch_pdl(beam_scan_kernel<DTYPE>, dim3(a.groups * a.beams * p.splits), dim3(kScanThreads), scan, stream, a, p);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(beam_merge_kernel<DTYPE>, dim3(a.groups), dim3(kMergeThreads), merge, stream, a, p);
+}
+
+}  // namespace
+
+size_t beam_select_workspace(int groups, int beams, int vocab, int dtype, int k) {
+  const int rows = groups * beams;
+  const size_t pieces = (size_t)rows * cut_rows(rows, vocab, dtype).splits;
+  return pieces * sizeof(float4) + (pieces * (k + kSlack) * sizeof(RowKey) + 15) / 16 * 16;
+}
+
+cudaError_t launch_beam_select(const BeamArgs& a, int dtype, void* ws, cudaStream_t stream) {
+  const int rows = a.groups * a.beams;
+  Pieces p = cut_rows(rows, a.vocab, dtype);
+  p.sums = static_cast<float4*>(ws);
+  p.keys = reinterpret_cast<RowKey*>(p.sums + (size_t)rows * p.splits);
+  if (dtype == SEMKV_F32) return launch<SEMKV_F32>(a, p, stream);
+  return dtype == SEMKV_BF16 ? launch<SEMKV_BF16>(a, p, stream) : launch<SEMKV_F16>(a, p, stream);
+}
+
+}  // namespace semkv

@@ -53,6 +53,21 @@ struct RankArgs {
 size_t rank_workspace_words(int B, int T);
 cudaError_t launch_rank_assign(const RankArgs& a, cudaStream_t stream);
 
+// One step of beam search (semkv_beam_select).
+struct BeamArgs {
+  int groups, beams, vocab, k, end_token;
+  const void* logits;       // [groups * beams][vocab] (row stride in elements)
+  int64_t stride;
+  const float* scores;      // [groups * beams]
+  const uint8_t* done;      // [groups * beams] or null
+  int32_t* parent;          // [groups][k], as token and score
+  int32_t* token;
+  float* score;
+  int32_t* err;
+};
+size_t beam_select_workspace(int groups, int beams, int vocab, int dtype, int k);
+cudaError_t launch_beam_select(const BeamArgs& a, int dtype, void* ws, cudaStream_t stream);
+
 // Fake quantization: quantize + reconstruct every row to fp16 (Sec. 4.1 protocol).
 struct FakeArgs {
   int base, L_hi, L_lo;
@@ -137,6 +152,11 @@ struct Kv4Batch;
 cudaError_t launch_kv4_rows(const Kv4Cache& c, const Kv4Batch& b, bool write, int layer, int dtype,
                             void* k, int64_t k_stride, void* v, int64_t v_stride, int sms,
                             cudaStream_t stream);
+struct Kv4Rotation;
+struct Kv4Rows;
+cudaError_t launch_kv4_write_rotated(const Kv4Cache& c, const Kv4Batch& b, int layer, const Kv4Rotation& t,
+                                     int dtype, const Kv4Rows& q, const Kv4Rows& q_out, int q_heads,
+                                     const Kv4Rows& k, const Kv4Rows& v, int sms, cudaStream_t stream);
 size_t kv4_attention_workspace(const Kv4Cache& c, const Kv4Batch& b, int q_heads, int sms);
 cudaError_t launch_kv4_attention(const Kv4Cache& c, const Kv4Batch& b, int layer, int dtype,
                                  const void* q, int64_t q_stride, int q_heads, void* out, float* lse,
@@ -148,6 +168,8 @@ cudaError_t launch_kv4_reserve(const Kv4Cache& c, const Kv4Batch& b, void* ws, i
 cudaError_t launch_kv4_fork(const Kv4Cache& c, int n, const int32_t* src, const int32_t* dst,
                             cudaStream_t stream);
 cudaError_t launch_kv4_free(const Kv4Cache& c, int n, const int32_t* seqs, cudaStream_t stream);
+cudaError_t launch_kv4_reorder(const Kv4Cache& c, int n, const int32_t* seqs, const int32_t* parent,
+                               void* ws, cudaStream_t stream);
 cudaError_t launch_kv4_compact(const Kv4Cache& c, int n, const int32_t* seqs, const uint8_t* keep,
                                int tokens, void* ws, int sms, cudaStream_t stream);
 

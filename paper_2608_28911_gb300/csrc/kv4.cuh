@@ -35,6 +35,19 @@ struct Kv4Batch {
   int32_t* start;
 };
 
+struct Kv4Rotation {
+  int rot, rows;   // turned dims of a head; positions in the table
+  bool pairs;      // (2 j, 2 j + 1), else (j, j + rot / 2)
+  const float* cos_sin;
+  const int32_t* positions;  // of the step's rows, or null: a row's place in its sequence
+};
+
+// Rows of a step's tensor, `stride` elements apart.
+struct Kv4Rows {
+  void* p;
+  int64_t stride;
+};
+
 __host__ __device__ constexpr int kv4_tile_bytes(int D) { return 18 * D; }
 
 __device__ __forceinline__ int64_t kv4_record(const Kv4Cache& c, int layer, int page, int head) {

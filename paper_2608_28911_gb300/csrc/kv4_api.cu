@@ -63,6 +63,19 @@ semkv_status check_kv4_batch(const semkv_kv4_batch* b, bool start, Kv4Batch& to)
   return SEMKV_OK;
 }
 
+semkv_status check_rotation(const semkv_kv4_rotation* r, const int32_t* positions, int head_dim, Kv4Rotation& to) {
+  if (!r || r->rows < 1 || r->rot_dim < 1 || r->rot_dim > head_dim || !r->cos_sin) return SEMKV_EINVAL;
+  if (r->rot_dim % 16) return SEMKV_EUNSUPPORTED;
+  if (r->layout != SEMKV_KV4_HALVES && r->layout != SEMKV_KV4_PAIRS) return SEMKV_EUNSUPPORTED;
+  if (!aligned(r->cos_sin, 16) || !aligned(positions, 4)) return SEMKV_EALIGN;
+  to.rot = r->rot_dim;
+  to.rows = r->rows;
+  to.pairs = r->layout == SEMKV_KV4_PAIRS;
+  to.cos_sin = r->cos_sin;
+  to.positions = positions;
+  return SEMKV_OK;
+}
+
 semkv_status check_ws(const void* ws, size_t bytes, size_t want) {
   return !ws || !aligned(ws, 16) || bytes < want ? SEMKV_EWORKSPACE : SEMKV_OK;
 }
@@ -129,6 +142,40 @@ semkv_status semkv_kv4_read(const semkv_kv4_cache* cache, const semkv_kv4_batch*
   return rows(cache, batch, false, layer, dtype, k_out, row, v_out, row, stream);
 }
 
+semkv_status semkv_kv4_write_rotated(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch, int32_t layer,
+                                     const semkv_kv4_rotation* rotation, const int32_t* positions, int32_t dtype,
+                                     const void* q, int64_t q_stride, int32_t q_heads, void* q_out, int64_t q_out_stride,
+                                     const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* stream) {
+  const TraceRange trace("semkv_kv4_write_rotated");
+  Kv4Cache c;
+  Kv4Batch b;
+  Kv4Rotation t;
+  semkv_status s = check_kv4(cache, c);
+  if (s != SEMKV_OK) return s;
+  s = check_kv4_batch(batch, true, b);
+  if (s != SEMKV_OK) return s;
+  s = check_rotation(rotation, positions, c.D, t);
+  if (s != SEMKV_OK) return s;
+  if ((b.total > 0 && (!k || !v)) || layer < 0 || layer >= c.layers) return SEMKV_EINVAL;
+  if (dtype != SEMKV_F16 && dtype != SEMKV_BF16) return SEMKV_EUNSUPPORTED;
+  const int64_t row = (int64_t)c.H * c.D;
+  if (k_stride < row || v_stride < row) return SEMKV_EINVAL;
+  if (!aligned(k, 16) || !aligned(v, 16) || k_stride % 8 || v_stride % 8) return SEMKV_EALIGN;
+  if (q_heads < 0 || (q_heads > 0 && b.total > 0 && (!q || !q_out))) return SEMKV_EINVAL;
+  if ((int64_t)q_heads * c.D > 1 << 30) return SEMKV_EUNSUPPORTED;  // a row's elements are 32-bit inside the kernel
+  if (q_heads > 0) {
+    if (q_stride < (int64_t)q_heads * c.D || q_out_stride < (int64_t)q_heads * c.D) return SEMKV_EINVAL;
+    if (!aligned(q, 16) || !aligned(q_out, 16) || q_stride % 8 || q_out_stride % 8) return SEMKV_EALIGN;
+    if (q && q == q_out && q_stride != q_out_stride) return SEMKV_EINVAL;
+  }
+  if (b.n == 0 || b.total == 0) return SEMKV_OK;
+  const int sms = device_sm_count();
+  if (sms <= 0) return SEMKV_ECUDA;
+  const Kv4Rows qr{const_cast<void*>(q_heads ? q : nullptr), q_stride}, qo{q_out, q_out_stride},
+      kr{const_cast<void*>(k), k_stride}, vr{const_cast<void*>(v), v_stride};
+  return from_cuda(launch_kv4_write_rotated(c, b, layer, t, dtype, qr, qo, q_heads, kr, vr, sms, (cudaStream_t)stream));
+}
+
 size_t semkv_kv4_attention_workspace_bytes(const semkv_kv4_cache* cache, const semkv_kv4_batch* batch, int32_t q_heads) {
   Kv4Cache c;
   Kv4Batch b;
@@ -185,6 +232,22 @@ semkv_status semkv_kv4_free(const semkv_kv4_cache* cache, int32_t n, const int32
   s = check_list(n, seqs);
   if (s != SEMKV_OK || n == 0) return s;
   return from_cuda(launch_kv4_free(c, n, seqs, (cudaStream_t)stream));
+}
+
+semkv_status semkv_kv4_reorder(const semkv_kv4_cache* cache, int32_t n, const int32_t* seqs, const int32_t* parent, void* ws,
+                               size_t ws_bytes, void* stream) {
+  const TraceRange trace("semkv_kv4_reorder");
+  Kv4Cache c;
+  semkv_status s = check_kv4(cache, c);
+  if (s != SEMKV_OK) return s;
+  s = check_list(n, seqs);
+  if (s != SEMKV_OK) return s;
+  if (n > 0 && !parent) return SEMKV_EINVAL;
+  if (!aligned(parent, 4)) return SEMKV_EALIGN;
+  if (n == 0) return SEMKV_OK;
+  s = check_ws(ws, ws_bytes, kv4_pages_workspace(c, n, 0, true));
+  if (s != SEMKV_OK) return s;
+  return from_cuda(launch_kv4_reorder(c, n, seqs, parent, ws, (cudaStream_t)stream));
 }
 
 semkv_status semkv_kv4_compact(const semkv_kv4_cache* cache, int32_t n, const int32_t* seqs, const uint8_t* keep,

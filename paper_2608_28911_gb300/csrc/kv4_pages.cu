@@ -1,4 +1,4 @@
-// kv4_pages.cu — page operations of the paged 4-bit cache: reserve, fork, free, compact.
+// kv4_pages.cu — page operations of the paged 4-bit cache: reserve, fork, free, reorder, compact.
 //
 // The state is three arrays: each sequence's table and length, and each page's reference
 // count.  A page is free when its count is 0, so there is no free list to keep in step
@@ -353,6 +353,57 @@ __global__ void __launch_bounds__(128) kv4_free_kernel(Kv4Cache c, int n, const 
   }
 }
 
+// ------------------------------------------------------------- reorder ------
+
+// The list's tables and lengths as they are before the call: whoever becomes a branch of another reads that
+// one's state here, whatever becomes of it meanwhile.  held -1: an entry out of range or listed before.
+__global__ void __launch_bounds__(256) kv4_note_kernel(Kv4Cache c, const int32_t* seqs, PagesWs w) {
+  pdl_wait();
+  pdl_trigger();
+  const int i = blockIdx.x, s = seqs ? seqs[i] : i;
+  if (s < 0 || s >= c.max_seqs) {
+    if (threadIdx.x == 0) w.held[i] = w.kept[i] = -1;
+    return;
+  }
+  const int tokens = tokens_of(c, s), used = pages_for(c, tokens);
+  const int32_t* row = c.table + (int64_t)s * c.max_pages;
+  int32_t* old = w.old + (int64_t)i * c.max_pages;
+  for (int k = threadIdx.x; k < used; k += blockDim.x) old[k] = row[k];
+  int before = 0;
+  if (seqs)
+    for (int j = threadIdx.x; j < i; j += blockDim.x) before |= seqs[j] == s;
+  before = __syncthreads_or(before);
+  if (threadIdx.x == 0) {
+    w.held[i] = tokens;
+    w.kept[i] = before ? -1 : s;  // the sequence that this entry changes
+  }
+}
+
+__global__ void __launch_bounds__(256) kv4_reorder_kernel(Kv4Cache c, int n, const int32_t* parent, PagesWs w) {
+  pdl_wait();
+  pdl_trigger();
+  const int i = blockIdx.x, s = w.kept[i], p = parent[i];
+  const int tokens = p >= 0 && p < n ? w.held[p] : p == -1 ? 0 : -1;
+  if (s < 0 || tokens < 0) {
+    if (threadIdx.x == 0) raise_error(c.err, kDevIndex);
+    return;
+  }
+  if (p == i) return;
+  const int had = pages_for(c, w.held[i]), used = pages_for(c, tokens);
+  const int32_t* mine = w.old + (int64_t)i * c.max_pages;
+  const int32_t* theirs = w.old + (int64_t)(p < 0 ? 0 : p) * c.max_pages;
+  int32_t* row = c.table + (int64_t)s * c.max_pages;
+  for (int k = threadIdx.x; k < (had > used ? had : used); k += blockDim.x) {
+    const int a = k < had ? mine[k] : -1, z = k < used ? theirs[k] : -1;
+    if ((k < had && !page_ok(c, a)) || (k < used && !page_ok(c, z))) raise_error(c.err, kDevIndex);
+    if (k < had && k < used && a == z) continue;  // a page that both had
+    if (page_ok(c, a)) atomicSub(c.refs + a, 1);
+    if (k < used) row[k] = z;
+    if (page_ok(c, z)) atomicAdd(c.refs + z, 1);
+  }
+  if (threadIdx.x == 0) c.length[s] = tokens;
+}
+
 // ------------------------------------------------------------- compact ------
 
 // Positions of the flagged tokens of one sequence, in order, and its pages as they were: the kernels
@@ -546,6 +597,14 @@ cudaError_t launch_kv4_fork(const Kv4Cache& c, int n, const int32_t* src, const 
 
 cudaError_t launch_kv4_free(const Kv4Cache& c, int n, const int32_t* seqs, cudaStream_t stream) {
   return launch_pdl(kv4_free_kernel, dim3(n), dim3(128), 0, stream, c, n, seqs);
+}
+
+cudaError_t launch_kv4_reorder(const Kv4Cache& c, int n, const int32_t* seqs, const int32_t* parent, void* ws,
+                               cudaStream_t stream) {
+  const PagesWs w = carve(c, n, ws);
+  const cudaError_t e = launch_pdl(kv4_note_kernel, dim3(n), dim3(256), 0, stream, c, seqs, w);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kv4_reorder_kernel, dim3(n), dim3(256), 0, stream, c, n, parent, w);
 }
 
 cudaError_t launch_kv4_compact(const Kv4Cache& c, int n, const int32_t* seqs, const uint8_t* keep, int tokens, void* ws,

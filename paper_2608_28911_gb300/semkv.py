@@ -69,6 +69,11 @@ class KV4BatchStruct(ctypes.Structure):
                 ("seqs", ctypes.c_void_p), ("cu", ctypes.c_void_p), ("start", ctypes.c_void_p)]
 
 
+class KV4RotationStruct(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("cos_sin", ctypes.c_void_p)]
+
+
 def _load():
     path = _build.LIB
     if not os.path.exists(path):
@@ -124,13 +129,19 @@ def _load():
     L.semkv_kv4_reserve.argtypes = [p, p, p, sz, p]
     L.semkv_kv4_write.argtypes = [p, p, i32, i32, p, i64, p, i64, p]
     L.semkv_kv4_read.argtypes = [p, p, i32, i32, p, p, p]
+    L.semkv_kv4_write_rotated.argtypes = [p, p, i32, p, p, i32, p, i64, i32, p, i64, p, i64, p, i64, p]
     L.semkv_kv4_attention.argtypes = [p, p, i32, i32, p, i64, i32, p, p, ctypes.c_float, i32, p,
                                       sz, p]
     L.semkv_kv4_fork.argtypes = [p, i32, p, p, p]
     L.semkv_kv4_free.argtypes = [p, i32, p, p]
     L.semkv_kv4_compact.argtypes = [p, i32, p, p, i32, p, sz, p]
-    for f in (L.semkv_kv4_reserve, L.semkv_kv4_write, L.semkv_kv4_read, L.semkv_kv4_attention,
-              L.semkv_kv4_fork, L.semkv_kv4_free, L.semkv_kv4_compact):
+    L.semkv_kv4_reorder.argtypes = [p, i32, p, p, p, sz, p]
+    L.semkv_beam_select_workspace_bytes.argtypes = [i32] * 5
+    L.semkv_beam_select_workspace_bytes.restype = sz
+    L.semkv_beam_select.argtypes = [i32, i32, i32, i32, p, i64, p, p, i32, i32, p, p, p, p, p, sz, p]
+    for f in (L.semkv_kv4_reserve, L.semkv_kv4_write, L.semkv_kv4_write_rotated, L.semkv_kv4_read,
+              L.semkv_kv4_attention, L.semkv_kv4_fork, L.semkv_kv4_free, L.semkv_kv4_reorder,
+              L.semkv_kv4_compact, L.semkv_beam_select):
         f.restype = ctypes.c_int
     return L
 
@@ -143,7 +154,9 @@ EXPORTED = ["semkv_row_bytes", "semkv_record_bytes", "semkv_high_count_floor",
             "semkv_decode_attention_noalloc", "semkv_debug_wait_timeout", "semkv_status_string",
             "semkv_kv4_tile_bytes", "semkv_kv4_pages_workspace_bytes", "semkv_kv4_reserve",
             "semkv_kv4_write", "semkv_kv4_read", "semkv_kv4_attention_workspace_bytes",
-            "semkv_kv4_attention", "semkv_kv4_fork", "semkv_kv4_free", "semkv_kv4_compact"]
+            "semkv_kv4_attention", "semkv_kv4_fork", "semkv_kv4_free", "semkv_kv4_compact",
+            "semkv_kv4_write_rotated", "semkv_kv4_reorder", "semkv_beam_select_workspace_bytes",
+            "semkv_beam_select"]
 
 
 def _ptr(t):
@@ -344,6 +357,33 @@ def semkv_kv4_write(cache: "KV4Cache", batch: "KV4Batch", layer: int, k: torch.T
                                _stream(stream)))
 
 
+def semkv_kv4_write_rotated(cache: "KV4Cache", batch: "KV4Batch", layer: int, rotation: "KV4Rotation",
+                            k: torch.Tensor, v: torch.Tensor, q=None, q_out=None, positions=None,
+                            stream=None):
+    """semkv_kv4_write with keys turned by their positions on the way, and the step's queries
+    q [total][q_heads][head_dim] (any row stride) turned into q_out, which may be q.  positions:
+    int32 [total], or None for the rows' places in their sequences."""
+    total, heads, head_dim = batch.total, cache.kv_heads, cache.head_dim
+    kind = _type16(k, v, "k and v")
+    ks = _rows(k, "k", total, heads, head_dim)
+    vs = _rows(v, "v", total, heads, head_dim)
+    q_heads = qs = ostr = 0
+    qp = op = None
+    if q is not None or q_out is not None:
+        _need(q is not None and q_out is not None and q.dim() == 3 and q.dtype == q_out.dtype == k.dtype,
+              "q and q_out come together, [total][q_heads][head_dim] of k's type")
+        q_heads = q.shape[1]
+        qs, ostr = _rows(q, "q", total, q_heads, head_dim), _rows(q_out, "q_out", total, q_heads, head_dim)
+        qp, op = q.data_ptr(), q_out.data_ptr()
+        _here(q, q_out)
+    _list(positions, total, "positions")
+    _here(cache.pages, batch.start, rotation.cos_sin, k, v)
+    _check("semkv_kv4_write_rotated",
+           LIB.semkv_kv4_write_rotated(cache.ref, batch.ref, layer, rotation.ref, _ptr(positions), kind,
+                                       qp, qs, q_heads, op, ostr, k.data_ptr(), ks, v.data_ptr(), vs,
+                                       _stream(stream)))
+
+
 def semkv_kv4_read(cache: "KV4Cache", batch: "KV4Batch", layer: int, k_out: torch.Tensor,
                    v_out: torch.Tensor, stream=None):
     """The values of the batch's rows into k_out, v_out [total][kv_heads][head_dim]."""
@@ -393,6 +433,16 @@ def semkv_kv4_free(cache: "KV4Cache", seqs: torch.Tensor, stream=None):
            LIB.semkv_kv4_free(cache.ref, n, _list(seqs, n, "seqs").data_ptr(), _stream(stream)))
 
 
+def semkv_kv4_reorder(cache: "KV4Cache", seqs, parent: torch.Tensor, ws: torch.Tensor, stream=None):
+    """The i-th sequence of the list becomes a branch of what its parent[i]-th was before the call; -1
+    empties it.  seqs: int32, or None for 0 .. n-1.  ws: cache.pages_workspace(n, 0)."""
+    n = parent.numel()
+    _here(cache.pages, ws)
+    _check("semkv_kv4_reorder",
+           LIB.semkv_kv4_reorder(cache.ref, n, _ptr(_list(seqs, n, "seqs")),
+                                 _list(parent, n, "parent").data_ptr(), _ptr(ws), ws.nbytes, _stream(stream)))
+
+
 def semkv_kv4_compact(cache: "KV4Cache", seqs: torch.Tensor, keep: torch.Tensor, ws: torch.Tensor,
                       stream=None):
     """Prunes sequences to the tokens with keep[i][t] != 0 (and all from keep.shape[1] on)."""
@@ -403,6 +453,54 @@ def semkv_kv4_compact(cache: "KV4Cache", seqs: torch.Tensor, keep: torch.Tensor,
     _check("semkv_kv4_compact",
            LIB.semkv_kv4_compact(cache.ref, n, _list(seqs, n, "seqs").data_ptr(), _ptr(keep),
                                  keep.shape[1], _ptr(ws), ws.nbytes, _stream(stream)))
+
+
+# ------------------------------------------------------------ beam search ----
+
+_BEAM_TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+
+
+def semkv_beam_select_workspace_bytes(groups: int, beams: int, vocab: int, dtype: torch.dtype,
+                                      k: int) -> int:
+    _need(dtype in _BEAM_TYPES, "logits are float16, bfloat16 or float32")
+    return LIB.semkv_beam_select_workspace_bytes(groups, beams, vocab, _BEAM_TYPES[dtype], k)
+
+
+def beam_select_workspace(logits: torch.Tensor, scores: torch.Tensor, k: int):
+    """For semkv_beam_select of logits and scores of these shapes and this type."""
+    size = semkv_beam_select_workspace_bytes(*scores.shape, logits.shape[1], logits.dtype, k)
+    return torch.empty(size, dtype=torch.uint8, device=logits.device)
+
+
+def semkv_beam_select(logits: torch.Tensor, scores: torch.Tensor, parent: torch.Tensor,
+                      token: torch.Tensor, score: torch.Tensor, ws: torch.Tensor, done=None,
+                      end_token: int = 0, dev_error=None, stream=None):
+    """The k best continuations of each group's beams into parent, token (int32) and score (float32)
+    [groups][k].  logits [groups * beams][vocab] (any row stride), scores float32 [groups][beams],
+    done: uint8 or bool, one for each beam, or None."""
+    _need(scores.dim() == 2 and parent.dim() == 2, "scores is [groups][beams], parent [groups][k]")
+    (groups, beams), k = scores.shape, parent.shape[1]
+    kind = _BEAM_TYPES.get(logits.dtype)
+    _need(kind is not None and logits.dim() == 2 and logits.shape[0] == groups * beams
+          and (logits.shape[1] <= 1 or logits.stride(1) == 1),
+          "logits is float16, bfloat16 or float32 [groups * beams][vocab], a row's values side by side")
+    for t, dtype, shape in ((scores, torch.float32, scores.shape), (parent, torch.int32, (groups, k)),
+                            (token, torch.int32, (groups, k)), (score, torch.float32, (groups, k))):
+        _need(t.dtype == dtype and t.is_contiguous() and t.shape == shape,
+              "scores (float32), parent, token (int32) and score (float32) are contiguous and fit each other")
+    if done is not None:
+        _need(done.dtype in (torch.uint8, torch.bool) and done.is_contiguous() and done.numel() == groups * beams,
+              "done is contiguous uint8 or bool, one for each beam")
+        _here(done)
+    if dev_error is not None:
+        _here(_list(dev_error, 1, "dev_error"))
+    _here(logits, scores, parent, token, score, ws)
+    vocab = logits.shape[1]
+    _check("semkv_beam_select",
+           LIB.semkv_beam_select(groups, beams, vocab, kind, logits.data_ptr(),
+                                 logits.stride(0) if logits.shape[0] > 1 else vocab, _ptr(scores), _ptr(done),
+                                 end_token, k, _ptr(parent), _ptr(token), _ptr(score), _ptr(dev_error), _ptr(ws),
+                                 ws.nbytes, _stream(stream)))
 
 
 # ------------------------------------------------------- owning wrappers ------
@@ -596,4 +694,21 @@ class KV4Batch:
             max_count = 1 if cu is None else self.total
         self.s = KV4BatchStruct(n=n, total=self.total, max_count=max_count,
                                 seqs=_ptr(self.seqs), cu=_ptr(self.cu), start=_ptr(self.start))
+        self.ref = ctypes.byref(self.s)
+
+
+class KV4Rotation:
+    """A table of positions' cosines and sines, float32 [positions][rot_dim]: rot_dim / 2 cosines, then
+    the sines.  The first rot_dim dims of a head are turned, in pairs (j, j + rot_dim / 2) or, with
+    pairs, (2 j, 2 j + 1)."""
+
+    def __init__(self, cos_sin: torch.Tensor, pairs: bool = False):
+        _need(cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.is_contiguous()
+              and cos_sin.shape[0] > 0 and cos_sin.shape[1] > 0 and cos_sin.shape[1] % 16 == 0
+              and cos_sin.data_ptr() % 16 == 0,
+              "cos_sin is contiguous float32 [positions][rot_dim], rot_dim a multiple of 16, on a multiple "
+              "of 16 bytes")
+        self.cos_sin = cos_sin
+        self.s = KV4RotationStruct(rot_dim=cos_sin.shape[1], layout=1 if pairs else 0, rows=cos_sin.shape[0],
+                                   cos_sin=_ptr(cos_sin))
         self.ref = ctypes.byref(self.s)
