@@ -6,9 +6,9 @@
 //
 // A candidate is a key: a number whose order is the candidates', and all keys differ.  The k best
 // of many keys, spread over a CTA's threads, come in two steps: a key T such that k threads, or a few
-// more, have a largest key of T or above (found bit by bit, a barrier that counts for each), and then all keys from T
-// on, which those threads alone hold.  Nothing else is sorted; ties, constant rows and rows in ascending order take the
-// same way.
+// more, have a largest key of T or above (found bit by bit, a barrier that counts for each, from the first bit in which
+// the keys differ), and then all keys from T on, which those threads alone hold.  Nothing else is sorted; ties, constant
+// rows and rows in ascending order take the same way.
 //
 // A sum's terms are 2^(x log2 e - c) with a whole number c, so that sums of different c are brought together exactly.
 // They are binary32, with a bound on their error.  If that leaves open which of two rows' candidates
@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kScanThreads = 256, kMergeThreads = 512;
 constexpr int kSlack = 16;       // keys that a threshold may let through beside the k best
+constexpr int kRanked = 256;     // keys that the merge puts in order without cutting them down first
 constexpr int kMergePer = 4;     // candidates that a thread of the merge looks at in one go
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.69314718055994530942;
@@ -50,6 +51,8 @@ struct RowKey {
   __device__ __forceinline__ static RowKey of(float x, int token) {
     return {(uint64_t)ordered(x) << 32 | (0xFFFFFFFFu - (uint32_t)token)};
   }
+  __device__ __forceinline__ static RowKey of_word(uint32_t w) { return {(uint64_t)w << 32}; }
+  __device__ __forceinline__ uint32_t word() const { return (uint32_t)(a >> 32); }
   __device__ __forceinline__ float logit() const { return unordered((uint32_t)(a >> 32)); }
   __device__ __forceinline__ int token() const { return (int)(0xFFFFFFFFu - (uint32_t)a); }
   __device__ __forceinline__ bool valid() const { return a != 0; }
@@ -66,6 +69,8 @@ struct GroupKey {
     return {(uint64_t)ordered(score) << 32 | ordered(rest),
             (uint64_t)(SEMKV_BEAM_MAX - 1 - beam) << 56 | (uint64_t)ordered(x) << 24 | (0xFFFFFFu - (uint32_t)token)};
   }
+  __device__ __forceinline__ static GroupKey of_word(uint32_t w) { return {(uint64_t)w << 32, 0}; }
+  __device__ __forceinline__ uint32_t word() const { return (uint32_t)(a >> 32); }
   __device__ __forceinline__ float score() const { return unordered((uint32_t)(a >> 32)); }
   __device__ __forceinline__ float rest() const { return unordered((uint32_t)a); }
   __device__ __forceinline__ int beam() const { return SEMKV_BEAM_MAX - 1 - (int)(b >> 56); }
@@ -77,44 +82,68 @@ struct GroupKey {
   }
 };
 
+// In a row, the logit alone.
+struct WordKey {
+  uint32_t a;
+  static constexpr int kBits = 32;
+  __device__ __forceinline__ static WordKey of_word(uint32_t w) { return {w}; }
+  __device__ __forceinline__ uint32_t word() const { return a; }
+  __device__ __forceinline__ WordKey with(int bit) const { return {a | 1u << bit}; }
+};
+
+// The least and the largest of the CTA's words.
+struct Extent {
+  uint32_t least, most;
+};
+template <int THREADS>
+__device__ __forceinline__ Extent extent_of(Extent mine, Extent* shared) {
+  constexpr int kWarps = THREADS / 32;
+  const int lane = threadIdx.x & 31;
+  mine = {__reduce_min_sync(~0u, mine.least), __reduce_max_sync(~0u, mine.most)};
+  __syncthreads();  // what the call before left has been read
+  if (lane == 0) shared[threadIdx.x >> 5] = mine;
+  __syncthreads();
+  mine = shared[lane % kWarps];
+  return {__reduce_min_sync(~0u, mine.least), __reduce_max_sync(~0u, mine.most)};
+}
+
+// A key that k or a few more of the keys reach (k exactly, or all that are equal, where no key tells the others
+// apart).  count(x): how many reach x, for all threads; there are k or more.  e: of their words.
+template <typename Key, typename Count>
+__device__ __forceinline__ Key threshold(int k, Extent e, Count count) {
+  const int same = __clz(e.least ^ e.most);  // bits that all keys share
+  Key t = Key::of_word(same == 32 ? e.least : e.least & ~(0xFFFFFFFFu >> same));
+  for (int bit = Key::kBits - 1 - same; bit >= 0; --bit) {
+    const Key up = t.with(bit);
+    if (up.word() > e.most) continue;
+    const int c = count(up);
+    if (c < k) continue;
+    t = up;
+    if (c <= k + kSlack) break;
+  }
+  return t;
+}
+
 // The best keys of a CTA so far, in shared memory: at least the k best of all that were offered.
 template <typename Key, int THREADS>
 struct Best {
   Key* list;    // [cap]
   Key* spare;   // [k + kSlack]
-  int* count;
+  int* count;   // keys in the list
+  Extent* extents;
   int k, cap;
   Key floor;    // k keys of this or more are in the list (or have been): a key below does not matter
 
-  // A T that k or a few more of the threads' keys reach, each thread bringing `per` of the n keys in `keys`.
-  // All keys differ, so that there is one; n is at least k.
-  __device__ __forceinline__ Key threshold_of(const Key* keys, int n) const {
-    Key t = Key::none();
-    for (int bit = Key::kBits - 1; bit >= 0; --bit) {
-      const Key up = t.with(bit);
-      int c = 0;
-      for (int j = 0; j < n; j += THREADS) c += __syncthreads_count(j + (int)threadIdx.x < n && keys[j + threadIdx.x] >= up);
-      if (c < k) continue;
-      t = up;
-      if (c <= k + kSlack) break;
-    }
-    return t;
-  }
-  // The same, a key from each thread; more than k + kSlack of them are valid.
-  __device__ __forceinline__ Key threshold_of(Key mine) const {
-    Key t = Key::none();
-    for (int bit = Key::kBits - 1; bit >= 0; --bit) {
-      const Key up = t.with(bit);
-      const int c = __syncthreads_count(mine >= up);
-      if (c < k) continue;
-      t = up;
-      if (c <= k + kSlack) break;
-    }
-    return t;
-  }
-  // For all threads at once, behind a barrier: the list is cut down to the k best and up to kSlack more.
+  // For all threads at once, behind a barrier: the list's n keys are cut down to the k best and up to kSlack more.
   __device__ __forceinline__ void cut(int n) {
-    const Key t = threshold_of(list, n);
+    Extent e{0xFFFFFFFFu, 0u};
+    for (int i = threadIdx.x; i < n; i += THREADS) e = {min(e.least, list[i].word()), max(e.most, list[i].word())};
+    e = extent_of<THREADS>(e, extents);
+    const Key t = threshold<Key>(k, e, [&](const Key& up) {
+      int c = 0;
+      for (int i = 0; i < n; i += THREADS) c += __syncthreads_count(i + (int)threadIdx.x < n && list[i + threadIdx.x] >= up);
+      return c;
+    });
     __syncthreads();
     if (threadIdx.x == 0) *count = 0;
     __syncthreads();
@@ -125,30 +154,31 @@ struct Best {
     __syncthreads();
     floor = t;
   }
+  // Threads bring a few keys each; `top` is the largest of the thread's own and collect(bound) puts those from the
+  // bound on.  The list holds k + kSlack threads' keys beside its own k + kSlack.
+  template <int PER, typename Collect>
+  __device__ __forceinline__ void offer(const Key& top, Collect collect) {
+    // (a key equal to the floor is in the list already)
+    bool hot = top.valid() && top >= floor;
+    int n = __syncthreads_count(hot);
+    if (n == 0) return;
+    const int held = *count;
+    __syncthreads();
+    const bool full = held + n * PER > cap;
+    if (full && held > k + kSlack) {
+      cut(held);
+      hot = top.valid() && top >= floor;
+      n = __syncthreads_count(hot);
+    }
+    if (full && n > k + kSlack) {
+      const Extent e = extent_of<THREADS>(hot ? Extent{top.word(), top.word()} : Extent{0xFFFFFFFFu, 0u}, extents);
+      floor = threshold<Key>(k, e, [&](const Key& up) { return __syncthreads_count(hot && top >= up); });
+      hot = hot && top >= floor;
+    }
+    if (hot) collect(floor);
+  }
   __device__ __forceinline__ void put(const Key& x) { list[atomicAdd(count, 1)] = x; }
 };
-
-// Threads bring a few keys each; `top` is the largest of the thread's own and collect(bound) puts those from the bound on.
-template <typename Key, int THREADS, int PER, typename Collect>
-__device__ __forceinline__ void offer(Best<Key, THREADS>& best, const Key& top, Collect collect) {
-  // (a key equal to the floor is in the list already)
-  bool hot = top.valid() && top >= best.floor;
-  int n = __syncthreads_count(hot);
-  if (n == 0) return;
-  const int held = *best.count;
-  __syncthreads();
-  if ((n > best.k + kSlack || held + n * PER > best.cap) && held > best.k + kSlack) {
-    best.cut(held);
-    hot = top.valid() && top >= best.floor;
-    n = __syncthreads_count(hot);
-  }
-  if (n > best.k + kSlack) {
-    const Key t = best.threshold_of(hot ? top : Key::none());
-    if (t >= best.floor) best.floor = t;
-    hot = top.valid() && top >= best.floor;
-  }
-  if (hot) collect(best.floor);
-}
 
 // ------------------------------------------------------------------ rows ------
 
@@ -172,7 +202,7 @@ __device__ __forceinline__ void two_sum(float a, float b, float& s, float& e) {
 
 // Eight 16-bit or four 32-bit logits as they lie in memory.
 template <int DTYPE>
-struct Vec {
+struct alignas(16) Vec {
   static constexpr int kSize = DTYPE == SEMKV_F32 ? 4 : 2, kCount = 16 / kSize;
   uint32_t w[4];
 
@@ -184,6 +214,12 @@ struct Vec {
     if (DTYPE == SEMKV_F32) return __uint_as_float(w[i]);
     if (DTYPE == SEMKV_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     return __half2float(__ushort_as_half((uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2])));
+  }
+  // the i-th of a vector in shared memory
+  __device__ __forceinline__ float at_dynamic(int i) const {
+    if (DTYPE == SEMKV_F32) return __uint_as_float(w[i]);
+    const uint16_t h = reinterpret_cast<const uint16_t*>(w)[i];
+    return DTYPE == SEMKV_BF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
   }
   __device__ __forceinline__ void set(int i, uint32_t bits) {
     if (DTYPE == SEMKV_F32) w[i] = bits;
@@ -271,26 +307,33 @@ __device__ __forceinline__ const char* row_at(const BeamArgs& a, int row) {
 
 constexpr int kVecs = 4;  // vectors of a thread in one go
 
-__host__ __device__ constexpr int scan_cap(int k, int dtype) { return (k + kSlack) * (1 + kVecs * (dtype == SEMKV_F32 ? 4 : 8)); }
+// What the scan keeps in shared memory: the list, what a cut needs, and the vectors that hold a logit that may be
+// among the best, each with its first token.
+__host__ __device__ constexpr int scan_cap(int k) { return k + kSlack + kScanThreads; }
+constexpr int kPending = kScanThreads * kVecs;
+__host__ __device__ constexpr int scan_bytes(int k) { return kPending * 20 + (scan_cap(k) + k + kSlack) * (int)sizeof(RowKey); }
 __host__ __device__ constexpr int merge_cap(int k) { return (k + kSlack) * (1 + kMergePer); }
 
 template <int DTYPE>
-__global__ void __launch_bounds__(kScanThreads) beam_scan_kernel(BeamArgs a, Pieces p) {
+__global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, Pieces p) {
   using V = Vec<DTYPE>;
-  constexpr int kPer = kVecs * V::kCount, kTile = kScanThreads * kPer;
+  constexpr int kTile = kScanThreads * kVecs * V::kCount;
   extern __shared__ __align__(16) unsigned char shared[];
-  __shared__ int count;
-  __shared__ float part[kScanThreads / 32];
-  __shared__ float part_low[kScanThreads / 32];
-  const int slots = a.k + kSlack;
+  __shared__ int count, pending_count;
+  __shared__ Extent extents[kScanThreads / 32];
+  __shared__ float part[kScanThreads / 32], part_low[kScanThreads / 32];
+  const int slots = a.k + kSlack, tid = threadIdx.x;
+  V* pending = reinterpret_cast<V*>(shared);
+  int* pending_first = reinterpret_cast<int*>(pending + kPending);
   Best<RowKey, kScanThreads> best;
-  best.list = reinterpret_cast<RowKey*>(shared);
-  best.spare = best.list + scan_cap(a.k, DTYPE);
+  best.list = reinterpret_cast<RowKey*>(pending_first + kPending);
+  best.spare = best.list + scan_cap(a.k);
   best.count = &count;
+  best.extents = extents;
   best.k = a.k;
-  best.cap = scan_cap(a.k, DTYPE);
+  best.cap = scan_cap(a.k);
   best.floor = RowKey::none();
-  if (threadIdx.x == 0) count = 0;
+  if (tid == 0) count = pending_count = 0;
   __syncthreads();
   const int row = blockIdx.x / p.splits, split = blockIdx.x - row * p.splits;
   pdl_wait();
@@ -300,11 +343,34 @@ __global__ void __launch_bounds__(kScanThreads) beam_scan_kernel(BeamArgs a, Pie
   const int lead = (int)((uintptr_t)at & 15);
   const int begin = split * p.piece, end = min(a.vocab, begin + p.piece);
   float m = kNone, c = -4 * kFar, sum = 0.f, low = 0.f;  // of this thread's logits
+  float floor = kNone;  // k logits of this or more have been seen: the same or less does not matter any more
+  int waiting = 0;      // vectors that are pending, or more
+
+  // the pending vectors' logits into the list
+  auto flush = [&]() {
+    __syncthreads();
+    const int n = pending_count * V::kCount;
+    for (int e0 = 0; e0 < n; e0 += kScanThreads) {
+      const int e = e0 + tid, v = e / V::kCount, j = e % V::kCount;
+      RowKey key = RowKey::none();
+      if (e < n) {
+        const float x = pending[v].at_dynamic(j);
+        if (x > kNone && x >= floor) key = RowKey::of(x, pending_first[v] + j);
+      }
+      best.template offer<1>(key, [&](const RowKey&) { best.put(key); });
+    }
+    __syncthreads();
+    if (tid == 0) pending_count = 0;
+    if (best.floor.valid()) floor = fmaxf(floor, best.floor.logit());
+    waiting = 0;
+    __syncthreads();
+  };
+
   for (int t0 = begin; t0 < end; t0 += kTile) {
     V v[kVecs];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int first = t0 + (i * kScanThreads + (int)threadIdx.x) * V::kCount;
+      const int first = t0 + (i * kScanThreads + tid) * V::kCount;
       if (first < end) v[i] = load_vec<DTYPE>(at, first, a.vocab, lead);
       else v[i].fill_none();
     }
@@ -343,30 +409,34 @@ __global__ void __launch_bounds__(kScanThreads) beam_scan_kernel(BeamArgs a, Pie
       two_sum(sum, (s[0] + s[1]) + (s[2] + s[3]), sum, err);
       low += err;
     }
-    // the best logits
-    int where = 0;
-    if (top > kNone && ordered(top) >= (uint32_t)(best.floor.a >> 32)) {  // its lowest token
-#pragma unroll
-      for (int i = kVecs - 1; i >= 0; --i)
-#pragma unroll
-        for (int j = V::kCount - 1; j >= 0; --j)
-          if (v[i].at(j) == top) where = t0 + (i * kScanThreads + (int)threadIdx.x) * V::kCount + j;
+    // vectors with a logit above the floor wait for the list
+    bool hot = top > floor;
+    int n = __syncthreads_count(hot);
+    if (n == 0) continue;
+    float least = floor;
+    bool same = false;  // `least` itself counts
+    if (n > slots) {
+      const uint32_t word = ordered(top);
+      const Extent e = extent_of<kScanThreads>(hot ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
+      least = floor = unordered(threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(hot && word >= up.a); }).a);
+      same = true;
+      hot = hot && top >= least;
+      n = __syncthreads_count(hot);
     }
-    offer<RowKey, kScanThreads, kPer>(best, top > kNone ? RowKey::of(top, where) : RowKey::none(), [&](const RowKey& from) {
-      const float least = from.valid() ? from.logit() : kNone;
+    if (waiting + n * kVecs > kPending) flush();
+    waiting += n * kVecs;
+    if (hot)
 #pragma unroll
       for (int i = 0; i < kVecs; ++i)
-        if (big[i] >= least)
-#pragma unroll
-          for (int j = 0; j < V::kCount; ++j) {
-            const float x = v[i].at(j);
-            const RowKey key = RowKey::of(x, t0 + (i * kScanThreads + (int)threadIdx.x) * V::kCount + j);
-            if (x > kNone && key >= from) best.put(key);
-          }
-    });
+        if (big[i] > least || (same && big[i] == least)) {
+          const int w = atomicAdd(&pending_count, 1);
+          pending[w] = v[i];
+          pending_first[w] = t0 + (i * kScanThreads + tid) * V::kCount;
+        }
   }
+  flush();
   // the sum over the threads, a pair of numbers each
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = tid & 31, warp = tid >> 5;
   float M = m;
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) M = fmaxf(M, __shfl_xor_sync(~0u, M, d));
@@ -391,8 +461,7 @@ __global__ void __launch_bounds__(kScanThreads) beam_scan_kernel(BeamArgs a, Pie
     part_low[warp] = low;
   }
   __syncthreads();
-  const int held = count;
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     sum = part[0];
     low = part_low[0];
     for (int w = 1; w < kScanThreads / 32; ++w) {
@@ -402,16 +471,35 @@ __global__ void __launch_bounds__(kScanThreads) beam_scan_kernel(BeamArgs a, Pie
     }
     p.sums[(int64_t)row * p.splits + split] = make_float4(M, sum, low, 0.f);
   }
+  int held = count;
   if (held > slots) {
-    __syncthreads();
     best.cut(held);
+    held = count;
   }
-  const int left = held > slots ? count : held;
   RowKey* out = p.keys + (int64_t)blockIdx.x * slots;
-  for (int i = threadIdx.x; i < slots; i += kScanThreads) out[i] = i < left ? best.list[i] : RowKey::none();
+  for (int i = tid; i < slots; i += kScanThreads) out[i] = i < held ? best.list[i] : RowKey::none();
 }
 
 // ------------------------------------------------------- the exact sums ------
+
+// 2^(j/32) for j = -16 .. 16 as pairs of binary32 numbers, to 2^-48: products of the root in 64 bits.
+struct Powers {
+  float2 at[33];
+};
+constexpr Powers make_powers() {
+  Powers p{};
+  double up = 1.0, down = 1.0;
+  for (int j = 0; j <= 16; ++j) {
+    p.at[16 + j].x = (float)up;
+    p.at[16 + j].y = (float)(up - (double)(float)up);
+    p.at[16 - j].x = (float)down;
+    p.at[16 - j].y = (float)(down - (double)(float)down);
+    up *= 1.0218971486541166782;
+    down *= 0.97857206208770013451;
+  }
+  return p;
+}
+__constant__ const Powers kPowers = make_powers();
 
 // exp(d) for d = x - m <= 0 as a sum of three numbers, 2^-38 of it off: 2^n * 2^(j/32) * exp(t), with d log2 e taken in
 // two numbers and |t| <= ln 2 / 64, exp(t) - 1 by its series.
@@ -441,11 +529,13 @@ __device__ __forceinline__ bool exp_parts(float x, float m, const float2* powers
 
 // ln sum exp(x - most) of a row, by a whole CTA, to 2^-37, for its first warp.  `most` is the row's largest logit.
 template <int DTYPE>
-__device__ double exact_normalizer(const BeamArgs& a, int row, float most, const float2* powers, double* parts) {
+__device__ __noinline__ double exact_normalizer(const BeamArgs& a, int row, float most, float2* powers, double* parts) {
   using V = Vec<DTYPE>;
   const char* at = row_at<DTYPE>(a, row);
   const int lead = (int)((uintptr_t)at & 15);
   float sum = 0.f, low = 0.f;
+  if (threadIdx.x < 33) powers[threadIdx.x] = kPowers.at[threadIdx.x];
+  __syncthreads();
   for (int first = threadIdx.x * V::kCount; first < a.vocab; first += kMergeThreads * V::kCount) {
     V v = load_vec<DTYPE>(at, first, a.vocab, lead);
 #pragma unroll
@@ -504,6 +594,8 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   extern __shared__ __align__(16) unsigned char shared[];
   __shared__ int count;
   __shared__ double parts[kMergeThreads / 32];
+  __shared__ Extent extents[kMergeThreads / 32];
+  __shared__ int places[kRanked];
   __shared__ Base base[SEMKV_BEAM_MAX];
   __shared__ uint32_t again[SEMKV_BEAM_MAX / 32];  // rows to be summed once more
   __shared__ float2 powers[33];
@@ -514,11 +606,20 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   best.list = reinterpret_cast<GroupKey*>(shared);
   best.spare = best.list + merge_cap(a.k);
   best.count = &count;
+  best.extents = extents;
   best.k = a.k;
   best.cap = merge_cap(a.k);
   if (threadIdx.x < SEMKV_BEAM_MAX / 32) again[threadIdx.x] = 0;
   pdl_wait();
   pdl_trigger();
+  const int per_row = p.splits * slots, total = a.beams * per_row;
+  const RowKey* keys = p.keys + (int64_t)row0 * per_row;
+  RowKey ahead[kMergePer];  // the first of a thread's keys, on their way while the sums are brought together
+#pragma unroll
+  for (int i = 0; i < kMergePer; ++i) {
+    const int e = i * kMergeThreads + threadIdx.x;
+    ahead[i] = e < total ? keys[e] : RowKey::none();
+  }
   // a warp for each row: its pieces' sums together
   for (int b = warp; b < a.beams; b += kMergeThreads / 32) {
     const int row = row0 + b;
@@ -574,10 +675,6 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     }
     if (lane == 0) base[b] = r;
   }
-  if (threadIdx.x < 33) {
-    const double p = exp2(((int)threadIdx.x - 16) / 32.0);
-    powers[threadIdx.x] = make_float2((float)p, (float)(p - (double)(float)p));
-  }
   __syncthreads();
   auto sum_again = [&](int b) {
     const double norm = exact_normalizer<DTYPE>(a, row0 + b, base[b].most, powers, parts);
@@ -592,14 +689,11 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     if (base[b].kind == kLogits && fabsf(base[b].most) > kFar) sum_again(b);
     worst = fmaxf(worst, base[b].error);
   }
-  const int per_row = p.splits * slots, total = a.beams * per_row;
-  const RowKey* keys = p.keys + (int64_t)row0 * per_row;
-  auto candidate = [&](int e) {
+  auto candidate = [&](int e, const RowKey& key) {
     const int b = e / per_row;
     const Base& r = base[b];
     if (r.kind == kNobody) return GroupKey::none();
     if (r.kind == kDone) return e == b * per_row ? score_of(r, b, 0.f, a.end_token) : GroupKey::none();
-    const RowKey key = keys[e];
     return key.valid() ? score_of(r, b, key.logit(), key.token()) : GroupKey::none();
   };
   int held = 0;
@@ -612,10 +706,12 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
 #pragma unroll
       for (int i = 0; i < kMergePer; ++i) {
         const int e = e0 + i * kMergeThreads + threadIdx.x;
-        mine[i] = e < total ? candidate(e) : GroupKey::none();
+        RowKey key = ahead[i];
+        if (e0 > 0 && e < total) key = keys[e];
+        mine[i] = e < total ? candidate(e, key) : GroupKey::none();
         if (mine[i] >= top) top = mine[i];
       }
-      offer<GroupKey, kMergeThreads, kMergePer>(best, top, [&](const GroupKey& from) {
+      best.template offer<kMergePer>(top, [&](const GroupKey& from) {
 #pragma unroll
         for (int i = 0; i < kMergePer; ++i)
           if (mine[i].valid() && mine[i] >= from) best.put(mine[i]);
@@ -624,17 +720,24 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     __syncthreads();
     held = count;
     __syncthreads();
-    if (held > slots) {
+    if (held > kRanked) {
       best.cut(held);
       held = count;
     }
-    // the place of each among them
-    for (int i = threadIdx.x; i < held; i += kMergeThreads) {
-      const GroupKey x = best.list[i];
-      int place = -1;
-      for (int j = 0; j < held; ++j) place += best.list[j] >= x;
-      if (place < a.k) out[place] = x;
+    // the place of each among them, counted by several threads for each
+    const int parts_of = kMergeThreads / max(held, 1) > 0 ? kMergeThreads / max(held, 1) : 1;
+    for (int i = threadIdx.x; i < held; i += kMergeThreads) places[i] = -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < held * parts_of; i += kMergeThreads) {
+      const int which = i % held;
+      const GroupKey x = best.list[which];
+      int ahead_of = 0;
+      for (int j = i / held; j < held; j += parts_of) ahead_of += best.list[j] >= x;
+      atomicAdd(places + which, ahead_of);
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < held; i += kMergeThreads)
+      if (places[i] < a.k) out[places[i]] = best.list[i];
     held = min(held, a.k);
     __syncthreads();
     if (round == 1) break;
@@ -649,12 +752,16 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     };
     bool open = false;
     for (int i = threadIdx.x; i + 1 < held; i += kMergeThreads) open |= close(out[i], out[i + 1]);
+    // (candidates that are not in the list lie below the floor)
     if (held == a.k) {
       const GroupKey last = out[held - 1];
-      for (int e = threadIdx.x; e < total; e += kMergeThreads) {
-        const GroupKey x = candidate(e);
-        if (x.valid() && !(x >= last)) open |= close(x, last);
-      }
+      for (int i = threadIdx.x; i < count; i += kMergeThreads)
+        if (!(best.list[i] >= last)) open |= close(best.list[i], last);
+      if (best.floor.valid() && (last.score() - best.floor.score()) + last.rest() <= 2.001f * worst + 0x1p-22f * fabsf(last.score()))
+        for (int e = threadIdx.x; e < total; e += kMergeThreads) {
+          const GroupKey x = candidate(e, keys[e]);
+          if (x.valid() && !(x >= last)) open |= close(x, last);
+        }
     }
     if (!__syncthreads_or(open)) break;
     for (int b = 0; b < a.beams; ++b)
@@ -686,7 +793,7 @@ Pieces cut_rows(int rows, int vocab, int dtype) {
 
 template <int DTYPE>
 cudaError_t launch(const BeamArgs& a, const Pieces& p, cudaStream_t stream) {
-  const size_t scan = (scan_cap(a.k, DTYPE) + a.k + kSlack) * sizeof(RowKey);
+  const size_t scan = scan_bytes(a.k);
   const size_t merge = (merge_cap(a.k) + a.k + kSlack) * sizeof(GroupKey);
   const cudaError_t e = launch_pdl(beam_scan_kernel<DTYPE>, dim3(a.groups * a.beams * p.splits), dim3(kScanThreads), scan, stream, a, p);
   if (e != cudaSuccess) return e;
