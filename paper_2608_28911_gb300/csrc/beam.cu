@@ -233,11 +233,12 @@ struct alignas(16) Vec {
     else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
   }
-  __device__ __forceinline__ float largest() const {
-    const uint32_t m = max2(max2(w[0], w[1]), max2(w[2], w[3]));
-    if (DTYPE == SEMKV_F32) return __uint_as_float(m);
+  // the largest of each half of the words, and of both halves
+  __device__ __forceinline__ uint32_t largest2() const { return max2(max2(w[0], w[1]), max2(w[2], w[3])); }
+  __device__ __forceinline__ static float larger(uint32_t two) {
+    if (DTYPE == SEMKV_F32) return __uint_as_float(two);
     Vec v;
-    v.w[0] = m;
+    v.w[0] = two;
     float d;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(v.at(0)), "f"(v.at(1)));
     return d;
@@ -315,7 +316,7 @@ __host__ __device__ constexpr int scan_bytes(int k) { return kPending * 20 + (sc
 __host__ __device__ constexpr int merge_cap(int k) { return (k + kSlack) * (1 + kMergePer); }
 
 template <int DTYPE>
-__global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, Pieces p) {
+__global__ void __launch_bounds__(kScanThreads, 3) beam_scan_kernel(BeamArgs a, Pieces p) {
   using V = Vec<DTYPE>;
   constexpr int kTile = kScanThreads * kVecs * V::kCount;
   extern __shared__ __align__(16) unsigned char shared[];
@@ -366,24 +367,42 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
     __syncthreads();
   };
 
-  for (int t0 = begin; t0 < end; t0 += kTile) {
-    V v[kVecs];
+  auto load = [&](V (&v)[kVecs], int t0) {
+    if (lead == 0 && t0 + kTile <= end) {
+      const uint4* from = reinterpret_cast<const uint4*>(at + (int64_t)t0 * V::kSize) + tid;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        const uint4 x = __ldcs(from + i * kScanThreads);
+        v[i].w[0] = x.x, v[i].w[1] = x.y, v[i].w[2] = x.z, v[i].w[3] = x.w;
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       const int first = t0 + (i * kScanThreads + tid) * V::kCount;
       if (first < end) v[i] = load_vec<DTYPE>(at, first, a.vocab, lead);
       else v[i].fill_none();
     }
-    float big[kVecs], top = kNone;
+  };
+  V next[kVecs];  // the tile behind, on its way
+  load(next, begin);
+  for (int t0 = begin; t0 < end; t0 += kTile) {
+    V v[kVecs];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      big[i] = v[i].largest();
-      if (!(big[i] < INFINITY)) {
-        v[i].clean();
-        big[i] = v[i].largest();
-        raise_error(a.err, kDevNonFinite);
-      }
-      top = fmaxf(top, big[i]);
+    for (int i = 0; i < kVecs; ++i) v[i] = next[i];
+    if (t0 + kTile < end) load(next, t0 + kTile);
+    auto largest = [&]() {
+      uint32_t two = v[0].largest2();
+#pragma unroll
+      for (int i = 1; i < kVecs; ++i) two = V::max2(two, v[i].largest2());
+      return V::larger(two);
+    };
+    float top = largest();
+    if (!(top < INFINITY)) {
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) v[i].clean();
+      top = largest();
+      raise_error(a.err, kDevNonFinite);
     }
     if (top > kNone) {
       if (top > m) {
@@ -415,24 +434,36 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
     if (n == 0) continue;
     float least = floor;
     bool same = false;  // `least` itself counts
-    if (n > slots) {
-      const uint32_t word = ordered(top);
-      const Extent e = extent_of<kScanThreads>(hot ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
-      least = floor = unordered(threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(hot && word >= up.a); }).a);
-      same = true;
-      hot = hot && top >= least;
-      n = __syncthreads_count(hot);
+    if (2 * n > a.k) {  // more than a tile further on should have: the threads' largest so far tell of a higher floor
+      const bool in = m >= floor && m > kNone;
+      if (__syncthreads_count(in) > slots) {
+        const uint32_t word = ordered(m);
+        const Extent e = extent_of<kScanThreads>(in ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
+        least = floor = unordered(threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(in && word >= up.a); }).a);
+        same = true;
+        hot = top >= least && top > kNone;
+        n = __syncthreads_count(hot);
+      }
     }
     if (waiting + n * kVecs > kPending) flush();
     waiting += n * kVecs;
-    if (hot)
+    if (hot) {
+      bool keep[kVecs];
+      int kept = 0;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        const float big = V::larger(v[i].largest2());
+        keep[i] = big > least || (same && big == least);
+        kept += keep[i];
+      }
+      int w = atomicAdd(&pending_count, kept);
 #pragma unroll
       for (int i = 0; i < kVecs; ++i)
-        if (big[i] > least || (same && big[i] == least)) {
-          const int w = atomicAdd(&pending_count, 1);
+        if (keep[i]) {
           pending[w] = v[i];
-          pending_first[w] = t0 + (i * kScanThreads + tid) * V::kCount;
+          pending_first[w++] = t0 + (i * kScanThreads + tid) * V::kCount;
         }
+    }
   }
   flush();
   // the sum over the threads, a pair of numbers each
@@ -780,7 +811,7 @@ int vec_logits(int dtype) { return dtype == SEMKV_F32 ? 4 : 8; }
 
 // Rows are cut into pieces until there are a few CTAs for each SM, whole strides of a CTA each.  The cut depends on
 // the sizes alone, so that equal calls give equal bits.
-constexpr int kWantCtas = 152 * 8;
+constexpr int kWantCtas = 152 * 4;
 Pieces cut_rows(int rows, int vocab, int dtype) {
   const int unit = kScanThreads * vec_logits(dtype), units = (vocab + unit - 1) / unit;
   int splits = (kWantCtas + rows - 1) / rows;
