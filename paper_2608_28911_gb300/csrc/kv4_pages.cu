@@ -18,7 +18,8 @@ constexpr int kPlanThreads = 1024;
 constexpr int kMoveThreads = 256;
 
 // Workspace: [claim: max_seqs][offset: n + 1][kept: n][held: n][pairs: 2 n][counters: 4][list: num_pages]
-// and for compact [old: n * max_pages][source: n * tokens], 32-bit words.
+// and for compact and reorder [old: n * max_pages][source: n * tokens][trades: 6 n], 32-bit words.
+struct Trade;
 struct PagesWs {
   int32_t* claim;   // lowest list index that names the sequence
   int32_t* offset;  // first of the i-th sequence's new pages in the list; bit 31: copy its last page
@@ -27,18 +28,19 @@ struct PagesWs {
   int2* pairs;      // (reserve) pages to copy: from, to
   int32_t* counters;  // [0] pages to copy, [1] new pages (-1: refused)
   int32_t* list;    // new pages, ascending
-  int32_t* old;     // (compact) [n][max_pages] the sequences' pages before the call
+  int32_t* old;     // (compact, reorder) [n][max_pages] the sequences' pages before the call
   int32_t* source;  // (compact) [n][tokens] position of each flagged token that stays
+  Trade* trades;    // (reorder) [n]
 };
 
 __host__ __device__ inline int64_t pad4(int64_t words) { return (words + 3) & ~(int64_t)3; }
 
 int64_t ws_words(const Kv4Cache& c, int64_t n, int64_t tokens, bool compact) {
   return pad4(c.max_seqs) + pad4(n + 1) + 2 * pad4(n) + pad4(2 * n) + 4 + pad4(c.num_pages) +
-         (compact ? pad4(n * c.max_pages) + pad4(n * tokens) : 0);
+         (compact ? pad4(n * c.max_pages) + pad4(n * tokens) + pad4(6 * n) : 0);
 }
 
-PagesWs carve(const Kv4Cache& c, int n, void* ws) {
+PagesWs carve(const Kv4Cache& c, int n, int tokens, void* ws) {
   PagesWs w;
   int32_t* p = static_cast<int32_t*>(ws);
   w.claim = p;
@@ -58,6 +60,8 @@ PagesWs carve(const Kv4Cache& c, int n, void* ws) {
   w.old = p;
   p += pad4((int64_t)n * c.max_pages);
   w.source = p;
+  p += pad4((int64_t)n * tokens);
+  w.trades = reinterpret_cast<Trade*>(p);
   return w;
 }
 
@@ -355,53 +359,135 @@ __global__ void __launch_bounds__(128) kv4_free_kernel(Kv4Cache c, int n, const 
 
 // ------------------------------------------------------------- reorder ------
 
-// The list's tables and lengths as they are before the call: whoever becomes a branch of another reads that
-// one's state here, whatever becomes of it meanwhile.  held -1: an entry out of range or listed before.
-__global__ void __launch_bounds__(256) kv4_note_kernel(Kv4Cache c, const int32_t* seqs, PagesWs w) {
-  pdl_wait();
-  pdl_trigger();
-  const int i = blockIdx.x, s = seqs ? seqs[i] : i;
-  if (s < 0 || s >= c.max_seqs) {
-    if (threadIdx.x == 0) w.held[i] = w.kept[i] = -1;
-    return;
-  }
-  const int tokens = tokens_of(c, s), used = pages_for(c, tokens);
-  const int32_t* row = c.table + (int64_t)s * c.max_pages;
-  int32_t* old = w.old + (int64_t)i * c.max_pages;
-  for (int k = threadIdx.x; k < used; k += blockDim.x) old[k] = row[k];
-  int before = 0;
-  if (seqs)
-    for (int j = threadIdx.x; j < i; j += blockDim.x) before |= seqs[j] == s;
-  before = __syncthreads_or(before);
-  if (threadIdx.x == 0) {
-    w.held[i] = tokens;
-    w.kept[i] = before ? -1 : s;  // the sequence that this entry changes
-  }
+// Entry i of a list: the sequence that it changes, or -1 where it changes none, and what takes its place.
+struct Trade {
+  int seq, from;     // from: the parent's sequence, or -1
+  int had, used;     // pages
+  int tokens;
+  int moves;         // what stood there before the call may not stand there after it
+};
+
+// `before`: the sequence was listed before.  Raises the error of an entry that is left out.
+__device__ __forceinline__ Trade trade_of(const Kv4Cache& c, int n, const int32_t* seqs, const int32_t* parent, int i, bool before,
+                                          bool raise) {
+  const int s = seqs ? seqs[i] : i, p = parent[i];
+  const int from = p >= 0 && p < n ? (seqs ? seqs[p] : p) : -1;
+  const bool there = s >= 0 && s < c.max_seqs;
+  const bool fine = there && !before && (p == -1 || (from >= 0 && from < c.max_seqs));
+  if (!fine && raise) raise_error(c.err, kDevIndex);
+  Trade t{-1, -1, 0, 0, 0, 0};
+  if (there) t.had = pages_for(c, tokens_of(c, s));
+  t.moves = there && (before || p != i);
+  if (!fine || p == i) return t;
+  t.seq = s;
+  t.from = from;
+  t.tokens = p >= 0 ? tokens_of(c, from) : 0;
+  t.used = pages_for(c, t.tokens);
+  return t;
 }
 
-__global__ void __launch_bounds__(256) kv4_reorder_kernel(Kv4Cache c, int n, const int32_t* parent, PagesWs w) {
+// One column of a sequence's table: `mine` was there (-1: nothing), `theirs` comes.
+__device__ __forceinline__ void trade_page(const Kv4Cache& c, const Trade& t, int column, int mine, int theirs) {
+  const bool had = column < t.had, used = column < t.used;
+  if ((had && !page_ok(c, mine)) || (used && !page_ok(c, theirs))) raise_error(c.err, kDevIndex);
+  if (had && used && mine == theirs) return;  // a page that both had
+  if (had && page_ok(c, mine)) atomicSub(c.refs + mine, 1);
+  if (!used) return;
+  c.table[(int64_t)t.seq * c.max_pages + column] = theirs;
+  if (page_ok(c, theirs)) atomicAdd(c.refs + theirs, 1);
+}
+
+// Whoever becomes a branch of another takes its state before the call, whatever becomes of that one
+// meanwhile.  Lists whose tables fit into the registers of one cluster: all of it is read, then the CTAs
+// wait for one another, then all is written.
+constexpr int kTradeThreads = 1024, kTradeCtas = 8, kTradeHold = 8, kTradeEntries = 128;
+__host__ __device__ constexpr bool trades_fit(int n, int max_pages) {
+  return (n + kTradeCtas - 1) / kTradeCtas <= kTradeEntries &&
+         (int64_t)((n + kTradeCtas - 1) / kTradeCtas) * max_pages <= kTradeThreads * kTradeHold;
+}
+__global__ void __launch_bounds__(kTradeThreads) kv4_trade_kernel(Kv4Cache c, int n, const int32_t* seqs, const int32_t* parent) {
+  __shared__ Trade trades[kTradeEntries];
   pdl_wait();
   pdl_trigger();
-  const int i = blockIdx.x, s = w.kept[i], p = parent[i];
-  const int tokens = p >= 0 && p < n ? w.held[p] : p == -1 ? 0 : -1;
-  if (s < 0 || tokens < 0) {
-    if (threadIdx.x == 0) raise_error(c.err, kDevIndex);
-    return;
+  const int each = (n + gridDim.x - 1) / gridDim.x, first = blockIdx.x * each;
+  const int count = max(0, min(each, n - first));
+  for (int e = threadIdx.x >> 5; e < count; e += kTradeThreads / 32) {
+    const int i = first + e, lane = threadIdx.x & 31;
+    int before = 0;
+    if (seqs)
+      for (int j = lane; j < i; j += 32) before |= seqs[j] == seqs[i];
+    before = __any_sync(~0u, before);
+    const Trade t = trade_of(c, n, seqs, parent, i, before, lane == 0);
+    if (lane == 0) trades[e] = t;
   }
-  if (p == i) return;
-  const int had = pages_for(c, w.held[i]), used = pages_for(c, tokens);
-  const int32_t* mine = w.old + (int64_t)i * c.max_pages;
-  const int32_t* theirs = w.old + (int64_t)(p < 0 ? 0 : p) * c.max_pages;
-  int32_t* row = c.table + (int64_t)s * c.max_pages;
-  for (int k = threadIdx.x; k < (had > used ? had : used); k += blockDim.x) {
-    const int a = k < had ? mine[k] : -1, z = k < used ? theirs[k] : -1;
-    if ((k < had && !page_ok(c, a)) || (k < used && !page_ok(c, z))) raise_error(c.err, kDevIndex);
-    if (k < had && k < used && a == z) continue;  // a page that both had
-    if (page_ok(c, a)) atomicSub(c.refs + a, 1);
-    if (k < used) row[k] = z;
-    if (page_ok(c, z)) atomicAdd(c.refs + z, 1);
+  __syncthreads();
+  int mine[kTradeHold], theirs[kTradeHold];
+#pragma unroll
+  for (int j = 0; j < kTradeHold; ++j) {
+    const int at = j * kTradeThreads + threadIdx.x, e = at / c.max_pages, column = at - e * c.max_pages;
+    mine[j] = theirs[j] = -1;
+    if (e >= count || trades[e].seq < 0) continue;
+    if (column < trades[e].had) mine[j] = c.table[(int64_t)trades[e].seq * c.max_pages + column];
+    if (column < trades[e].used) theirs[j] = c.table[(int64_t)trades[e].from * c.max_pages + column];
   }
-  if (threadIdx.x == 0) c.length[s] = tokens;
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < kTradeHold; ++j) {
+    const int at = j * kTradeThreads + threadIdx.x, e = at / c.max_pages, column = at - e * c.max_pages;
+    if (e >= count || trades[e].seq < 0) continue;
+    trade_page(c, trades[e], column, mine[j], theirs[j]);
+  }
+  for (int e = threadIdx.x; e < count; e += kTradeThreads)
+    if (trades[e].seq >= 0) c.length[trades[e].seq] = trades[e].tokens;
+}
+
+// Longer lists take two kernels: the first notes the trades, and the tables that change as they were where somebody wants them.
+constexpr int kNoteThreads = 256;
+__global__ void __launch_bounds__(kNoteThreads) kv4_note_kernel(Kv4Cache c, int n, const int32_t* seqs, const int32_t* parent, PagesWs w) {
+  pdl_wait();
+  pdl_trigger();
+  const int i = blockIdx.x;
+  int before = 0, wanted = 0;
+  for (int j = threadIdx.x; j < n; j += blockDim.x) {
+    wanted |= j != i && parent[j] == i;
+    if (seqs) before |= j < i && seqs[j] == seqs[i];
+  }
+  before = __syncthreads_or(before);
+  wanted = __syncthreads_or(wanted);
+  const Trade t = trade_of(c, n, seqs, parent, i, before, threadIdx.x == 0);
+  if (threadIdx.x == 0) w.trades[i] = t;
+  if (!t.moves || !wanted) return;
+  const int32_t* row = c.table + (int64_t)(seqs ? seqs[i] : i) * c.max_pages;
+  int32_t* old = w.old + (int64_t)i * c.max_pages;
+#pragma unroll 8
+  for (int k = threadIdx.x; k < t.had; k += kNoteThreads) old[k] = row[k];
+}
+
+__global__ void __launch_bounds__(kNoteThreads) kv4_reorder_kernel(Kv4Cache c, const int32_t* parent, PagesWs w) {
+  pdl_wait();
+  pdl_trigger();
+  const int i = blockIdx.x;
+  const Trade t = w.trades[i];
+  if (t.seq < 0) return;
+  const int32_t* mine = c.table + (int64_t)t.seq * c.max_pages;
+  const int32_t* theirs = nullptr;
+  if (t.from >= 0) {
+    const int p = parent[i];
+    theirs = w.trades[p].moves ? w.old + (int64_t)p * c.max_pages : c.table + (int64_t)t.from * c.max_pages;
+  }
+  constexpr int kAhead = 8;  // of a thread's columns, all read before the first is dealt with
+  for (int k0 = threadIdx.x; k0 < max(t.had, t.used); k0 += kAhead * kNoteThreads) {
+    int a[kAhead], z[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int k = k0 + j * kNoteThreads;
+      a[j] = k < t.had ? mine[k] : -1;
+      z[j] = k < t.used ? theirs[k] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) trade_page(c, t, k0 + j * kNoteThreads, a[j], z[j]);
+  }
+  if (threadIdx.x == 0) c.length[t.seq] = t.tokens;
 }
 
 // ------------------------------------------------------------- compact ------
@@ -583,7 +669,7 @@ size_t kv4_pages_workspace(const Kv4Cache& c, int n, int tokens, bool compact) {
 }
 
 cudaError_t launch_kv4_reserve(const Kv4Cache& c, const Kv4Batch& b, void* ws, int sms, cudaStream_t stream) {
-  const PagesWs w = carve(c, b.n, ws);
+  const PagesWs w = carve(c, b.n, 0, ws);
   cudaError_t e = launch_pdl(kv4_reserve_kernel, dim3(1), dim3(kPlanThreads), 0, stream, c, b, w);
   if (e != cudaSuccess) return e;
   const int64_t bytes = (int64_t)c.H * (kv4_tile_bytes(c.D) << (c.page_shift - 4));
@@ -601,15 +687,30 @@ cudaError_t launch_kv4_free(const Kv4Cache& c, int n, const int32_t* seqs, cudaS
 
 cudaError_t launch_kv4_reorder(const Kv4Cache& c, int n, const int32_t* seqs, const int32_t* parent, void* ws,
                                cudaStream_t stream) {
-  const PagesWs w = carve(c, n, ws);
-  const cudaError_t e = launch_pdl(kv4_note_kernel, dim3(n), dim3(256), 0, stream, c, seqs, w);
+  if (trades_fit(n, c.max_pages)) {
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = n < kTradeCtas ? n : kTradeCtas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(attr[1].val.clusterDim.x);
+    cfg.blockDim = dim3(kTradeThreads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kv4_trade_kernel, c, n, seqs, parent);
+  }
+  const PagesWs w = carve(c, n, 0, ws);
+  const cudaError_t e = launch_pdl(kv4_note_kernel, dim3(n), dim3(kNoteThreads), 0, stream, c, n, seqs, parent, w);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kv4_reorder_kernel, dim3(n), dim3(256), 0, stream, c, n, parent, w);
+  return launch_pdl(kv4_reorder_kernel, dim3(n), dim3(kNoteThreads), 0, stream, c, parent, w);
 }
 
 cudaError_t launch_kv4_compact(const Kv4Cache& c, int n, const int32_t* seqs, const uint8_t* keep, int tokens, void* ws,
                                int sms, cudaStream_t stream) {
-  const PagesWs w = carve(c, n, ws);
+  const PagesWs w = carve(c, n, tokens, ws);
   cudaError_t e = launch_pdl(kv4_keep_kernel, dim3(n), dim3(kPlanThreads), 0, stream, c, seqs, keep, tokens, w);
   if (e != cudaSuccess) return e;
   e = launch_pdl(kv4_compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, c, n, seqs, tokens, w);
