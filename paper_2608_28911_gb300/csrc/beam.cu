@@ -215,12 +215,6 @@ struct alignas(16) Vec {
     if (DTYPE == SEMKV_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     return __half2float(__ushort_as_half((uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2])));
   }
-  // the i-th of a vector in shared memory
-  __device__ __forceinline__ float at_dynamic(int i) const {
-    if (DTYPE == SEMKV_F32) return __uint_as_float(w[i]);
-    const uint16_t h = reinterpret_cast<const uint16_t*>(w)[i];
-    return DTYPE == SEMKV_BF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
-  }
   __device__ __forceinline__ void set(int i, uint32_t bits) {
     if (DTYPE == SEMKV_F32) w[i] = bits;
     else w[i / 2] = i & 1 ? (w[i / 2] & 0xFFFFu) | bits << 16 : (w[i / 2] & 0xFFFF0000u) | (bits & 0xFFFFu);
@@ -308,33 +302,33 @@ __device__ __forceinline__ const char* row_at(const BeamArgs& a, int row) {
 
 constexpr int kVecs = 4;  // vectors of a thread in one go
 
-// What the scan keeps in shared memory: the list, what a cut needs, and the vectors that hold a logit that may be
-// among the best, each with its first token.
-__host__ __device__ constexpr int scan_cap(int k) { return k + kSlack + kScanThreads; }
-constexpr int kPending = kScanThreads * kVecs;
-__host__ __device__ constexpr int scan_bytes(int k) { return kPending * 20 + (scan_cap(k) + k + kSlack) * (int)sizeof(RowKey); }
+// What the scan keeps in shared memory: places of a row to look at once more, the list, and what a cut needs.
+__host__ __device__ constexpr int scan_cap(int k, int dtype) { return (k + kSlack) * (1 + (dtype == SEMKV_F32 ? 4 : 8)); }
+constexpr int kPlaces = 4 * kScanThreads;
+__host__ __device__ constexpr int scan_bytes(int k, int dtype) {
+  return kPlaces * (int)sizeof(int) + (scan_cap(k, dtype) + k + kSlack) * (int)sizeof(RowKey);
+}
 __host__ __device__ constexpr int merge_cap(int k) { return (k + kSlack) * (1 + kMergePer); }
 
 template <int DTYPE>
-__global__ void __launch_bounds__(kScanThreads, 3) beam_scan_kernel(BeamArgs a, Pieces p) {
+__global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, Pieces p) {
   using V = Vec<DTYPE>;
   constexpr int kTile = kScanThreads * kVecs * V::kCount;
   extern __shared__ __align__(16) unsigned char shared[];
-  __shared__ int count, pending_count;
+  __shared__ int count, place_count;
   __shared__ Extent extents[kScanThreads / 32];
   __shared__ float part[kScanThreads / 32], part_low[kScanThreads / 32];
   const int slots = a.k + kSlack, tid = threadIdx.x;
-  V* pending = reinterpret_cast<V*>(shared);
-  int* pending_first = reinterpret_cast<int*>(pending + kPending);
+  int* places = reinterpret_cast<int*>(shared);  // the first token of a thread's vectors
   Best<RowKey, kScanThreads> best;
-  best.list = reinterpret_cast<RowKey*>(pending_first + kPending);
-  best.spare = best.list + scan_cap(a.k);
+  best.list = reinterpret_cast<RowKey*>(places + kPlaces);
+  best.spare = best.list + scan_cap(a.k, DTYPE);
   best.count = &count;
   best.extents = extents;
   best.k = a.k;
-  best.cap = scan_cap(a.k);
+  best.cap = scan_cap(a.k, DTYPE);
   best.floor = RowKey::none();
-  if (tid == 0) count = pending_count = 0;
+  if (tid == 0) count = place_count = 0;
   __syncthreads();
   const int row = blockIdx.x / p.splits, split = blockIdx.x - row * p.splits;
   pdl_wait();
@@ -345,25 +339,66 @@ __global__ void __launch_bounds__(kScanThreads, 3) beam_scan_kernel(BeamArgs a, 
   const int begin = split * p.piece, end = min(a.vocab, begin + p.piece);
   float m = kNone, c = -4 * kFar, sum = 0.f, low = 0.f;  // of this thread's logits
   float floor = kNone;  // k logits of this or more have been seen: the same or less does not matter any more
-  int waiting = 0;      // vectors that are pending, or more
+  uint32_t seen = 0;    // tiles (of the last 32) in which this thread saw a logit above the floor
 
-  // the pending vectors' logits into the list
-  auto flush = [&]() {
+  // The threads' largest so far tell of a higher floor, if enough of them reach the present one.
+  auto raise = [&]() {
+    const bool in = m >= floor && m > kNone;
+    if (__syncthreads_count(in) <= slots) return false;
+    const uint32_t word = ordered(m);
+    const Extent e = extent_of<kScanThreads>(in ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
+    floor = unordered(threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(in && word >= up.a); }).a);
+    return true;
+  };
+  // What was seen goes into the list.  Few logits are left above the floor by now: they are read again, from the
+  // caches, rather than put aside when they were met, which took as long as all else together.
+  auto settle = [&](int t0) {
+    raise();
+    const uint32_t mine = m >= floor && m > kNone ? seen : 0u;
+    int w = mine ? atomicAdd(&place_count, __popc(mine)) : 0;
     __syncthreads();
-    const int n = pending_count * V::kCount;
-    for (int e0 = 0; e0 < n; e0 += kScanThreads) {
-      const int e = e0 + tid, v = e / V::kCount, j = e % V::kCount;
-      RowKey key = RowKey::none();
-      if (e < n) {
-        const float x = pending[v].at_dynamic(j);
-        if (x > kNone && x >= floor) key = RowKey::of(x, pending_first[v] + j);
+    const int passes = place_count > kPlaces ? 8 : 1;  // more than there is room for: four tiles at a time
+    for (int pass = 0; pass < passes; ++pass) {
+      uint32_t bits = mine;
+      if (passes > 1) {
+        bits &= 15u << (4 * pass);
+        __syncthreads();
+        if (tid == 0) place_count = 0;
+        __syncthreads();
+        w = bits ? atomicAdd(&place_count, __popc(bits)) : 0;
       }
-      best.template offer<1>(key, [&](const RowKey&) { best.put(key); });
+      for (; bits; bits &= bits - 1) places[w++] = t0 + (__ffs(bits) - 1) * kTile + tid * V::kCount;
+      __syncthreads();
+      const int n = place_count * kVecs;
+      for (int e0 = 0; e0 < n; e0 += kScanThreads) {
+        const int e = e0 + tid, first = e < n ? places[e / kVecs] + e % kVecs * (kScanThreads * V::kCount) : end;
+        V x;
+        RowKey top = RowKey::none();
+        if (first < end) {
+          x = load_vec<DTYPE>(at, first, a.vocab, lead);
+          if (!(V::larger(x.largest2()) < INFINITY)) x.clean();
+          const float big = V::larger(x.largest2());
+          if (big >= floor && big > kNone) {
+            int where = 0;
+#pragma unroll
+            for (int j = V::kCount - 1; j >= 0; --j)
+              if (x.at(j) == big) where = j;
+            top = RowKey::of(big, first + where);
+          }
+        }
+        best.template offer<V::kCount>(top, [&](const RowKey& from) {
+#pragma unroll
+          for (int j = 0; j < V::kCount; ++j) {
+            const RowKey key = RowKey::of(x.at(j), first + j);
+            if (x.at(j) > kNone && x.at(j) >= floor && key >= from) best.put(key);
+          }
+        });
+      }
     }
     __syncthreads();
-    if (tid == 0) pending_count = 0;
+    if (tid == 0) place_count = 0;
     if (best.floor.valid()) floor = fmaxf(floor, best.floor.logit());
-    waiting = 0;
+    seen = 0;
     __syncthreads();
   };
 
@@ -384,13 +419,10 @@ __global__ void __launch_bounds__(kScanThreads, 3) beam_scan_kernel(BeamArgs a, 
       else v[i].fill_none();
     }
   };
-  V next[kVecs];  // the tile behind, on its way
-  load(next, begin);
+  V v[kVecs];
+  load(v, begin);
+  int tile = 0;
   for (int t0 = begin; t0 < end; t0 += kTile) {
-    V v[kVecs];
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) v[i] = next[i];
-    if (t0 + kTile < end) load(next, t0 + kTile);
     auto largest = [&]() {
       uint32_t two = v[0].largest2();
 #pragma unroll
@@ -405,8 +437,8 @@ __global__ void __launch_bounds__(kScanThreads, 3) beam_scan_kernel(BeamArgs a, 
       raise_error(a.err, kDevNonFinite);
     }
     if (top > kNone) {
-      if (top > m) {
-        m = top;
+      m = fmaxf(m, top);
+      if (__fmaf_rn(m, kLog2e, -c) > 2.f) {
         const float up = scale_of(m), by = pow2(c - up);  // (0 the first time)
         sum *= by;
         low *= by;
@@ -428,44 +460,16 @@ __global__ void __launch_bounds__(kScanThreads, 3) beam_scan_kernel(BeamArgs a, 
       two_sum(sum, (s[0] + s[1]) + (s[2] + s[3]), sum, err);
       low += err;
     }
-    // vectors with a logit above the floor wait for the list
+    if (t0 + kTile < end) load(v, t0 + kTile);
     bool hot = top > floor;
-    int n = __syncthreads_count(hot);
-    if (n == 0) continue;
-    float least = floor;
-    bool same = false;  // `least` itself counts
-    if (2 * n > a.k) {  // more than a tile further on should have: the threads' largest so far tell of a higher floor
-      const bool in = m >= floor && m > kNone;
-      if (__syncthreads_count(in) > slots) {
-        const uint32_t word = ordered(m);
-        const Extent e = extent_of<kScanThreads>(in ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
-        least = floor = unordered(threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(in && word >= up.a); }).a);
-        same = true;
-        hot = top >= least && top > kNone;
-        n = __syncthreads_count(hot);
-      }
-    }
-    if (waiting + n * kVecs > kPending) flush();
-    waiting += n * kVecs;
-    if (hot) {
-      bool keep[kVecs];
-      int kept = 0;
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        const float big = V::larger(v[i].largest2());
-        keep[i] = big > least || (same && big == least);
-        kept += keep[i];
-      }
-      int w = atomicAdd(&pending_count, kept);
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i)
-        if (keep[i]) {
-          pending[w] = v[i];
-          pending_first[w++] = t0 + (i * kScanThreads + tid) * V::kCount;
-        }
+    const int n = __syncthreads_count(hot);
+    if (2 * n > a.k && raise()) hot = top >= floor && top > kNone;  // (more than a tile further on should have)
+    seen |= (uint32_t)hot << tile;
+    if (++tile == 32 || t0 + kTile >= end) {
+      settle(t0 - (tile - 1) * kTile);
+      tile = 0;
     }
   }
-  flush();
   // the sum over the threads, a pair of numbers each
   const int lane = tid & 31, warp = tid >> 5;
   float M = m;
@@ -699,9 +703,9 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
         const float u = logf((float)a.vocab) - norm;
         rest += err - kLack * (m - 0.5f * u);
         set_value(r, score, norm, rest);
-        // In units of 2^-24: an exponent's argument is off by half a step, so 1 for each of |x - m| + ln 2, on the average
-        // over the terms u + ln 2; exponentials by 4; sums of eight and of four numbers by 5; the logarithm by 1.
-        r.error = (1.125f * fmaxf(u, 0.f) + 12.f) * 0x1p-24f;
+        // In units of 2^-24: an exponent's argument is off by half a step, so 1 for each of |x - m| + 3 ln 2, on the average
+        // over the terms u + 3 ln 2; exponentials by 4; sums of eight and of four numbers by 5; the logarithm by 1.
+        r.error = (1.125f * fmaxf(u, 0.f) + 13.f) * 0x1p-24f;
       }
     }
     if (lane == 0) base[b] = r;
@@ -824,7 +828,7 @@ Pieces cut_rows(int rows, int vocab, int dtype) {
 
 template <int DTYPE>
 cudaError_t launch(const BeamArgs& a, const Pieces& p, cudaStream_t stream) {
-  const size_t scan = scan_bytes(a.k);
+  const size_t scan = scan_bytes(a.k, DTYPE);
   const size_t merge = (merge_cap(a.k) + a.k + kSlack) * sizeof(GroupKey);
   const cudaError_t e = launch_pdl(beam_scan_kernel<DTYPE>, dim3(a.groups * a.beams * p.splits), dim3(kScanThreads), scan, stream, a, p);
   if (e != cudaSuccess) return e;
