@@ -1,14 +1,14 @@
 // beam.cu — one step of beam search: the k best of a group's beams * vocab continuations.
 //
-// Two kernels.  The scan has CTAs over pieces of the rows: each reads its piece once, keeps sum exp(x - m) of
-// what it saw and the best logits, k of them and a few more.  The merge has a CTA for each group: the rows'
-// normalizers from the pieces' sums, then the k best of the pieces' candidates by score.
+// Two kernels.  The scan streams the rows once.  Each thread keeps sum exp(x - m) of its logits, the largest of
+// them, and in which of its tiles it saw one above a floor, a logit that k of the piece are known to reach.  The merge has a
+// CTA for each group: the rows' normalizers from the sums; then a score that k of the scan's threads reach with
+// their largest logits; and of those threads alone, k or a few more, the marked tiles once more, logit by logit.
+// So what the scan writes of a piece of up to 262144 logits is 2 KB, whatever k is, and it sorts nothing.
 //
-// A candidate is a key: a number whose order is the candidates', and all keys differ.  The k best
-// of many keys, spread over a CTA's threads, come in two steps: a key T such that k threads, or a few
-// more, have a largest key of T or above (found bit by bit, a barrier that counts for each, from the first bit in which
-// the keys differ), and then all keys from T on, which those threads alone hold.  Nothing else is sorted; ties, constant
-// rows and rows in ascending order take the same way.
+// A candidate is a key: a number whose order is the candidates', and all keys differ.  A key T that k or a few more of
+// the threads' largest keys reach is found bit by bit, a barrier that counts for each, from the first bit in which the keys
+// differ.
 //
 // A sum's terms are 2^(x log2 e - c) with a whole number c, so that sums of different c are brought together exactly.
 // They are binary32, with a bound on their error.  If that leaves open which of two rows' candidates
@@ -23,10 +23,9 @@
 namespace semkv {
 namespace {
 
-constexpr int kScanThreads = 256, kMergeThreads = 512;
+constexpr int kScanThreads = 256, kMergeThreads = 1024;
 constexpr int kSlack = 16;       // keys that a threshold may let through beside the k best
-constexpr int kRanked = 256;     // keys that the merge puts in order without cutting them down first
-constexpr int kMergePer = 4;     // candidates that a thread of the merge looks at in one go
+constexpr int kRanked = 512;     // keys that the merge puts in order without cutting them down first
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.69314718055994530942;
 // Past this logits are too coarse for x log2 e in one rounding: rows with a largest logit beyond it are summed exactly.
@@ -43,22 +42,6 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 __device__ __forceinline__ float unordered(uint32_t u) {
   return __uint_as_float(u ^ ((int32_t)u < 0 ? 0x80000000u : 0xFFFFFFFFu));
 }
-// In a row: the logit, then the lower token.  0: none.
-struct RowKey {
-  uint64_t a;
-  static constexpr int kBits = 64;
-  __device__ __forceinline__ static RowKey none() { return {0}; }
-  __device__ __forceinline__ static RowKey of(float x, int token) {
-    return {(uint64_t)ordered(x) << 32 | (0xFFFFFFFFu - (uint32_t)token)};
-  }
-  __device__ __forceinline__ static RowKey of_word(uint32_t w) { return {(uint64_t)w << 32}; }
-  __device__ __forceinline__ uint32_t word() const { return (uint32_t)(a >> 32); }
-  __device__ __forceinline__ float logit() const { return unordered((uint32_t)(a >> 32)); }
-  __device__ __forceinline__ int token() const { return (int)(0xFFFFFFFFu - (uint32_t)a); }
-  __device__ __forceinline__ bool valid() const { return a != 0; }
-  __device__ __forceinline__ bool operator>=(const RowKey& o) const { return a >= o.a; }
-  __device__ __forceinline__ RowKey with(int bit) const { return {a | 1ull << bit}; }
-};
 // In a group: the score (a binary32 number and what it lacks), then the lower beam, the larger logit and the lower
 // token.  a = 0: none.
 struct GroupKey {
@@ -74,6 +57,7 @@ struct GroupKey {
   __device__ __forceinline__ float score() const { return unordered((uint32_t)(a >> 32)); }
   __device__ __forceinline__ float rest() const { return unordered((uint32_t)a); }
   __device__ __forceinline__ int beam() const { return SEMKV_BEAM_MAX - 1 - (int)(b >> 56); }
+  __device__ __forceinline__ float logit() const { return unordered((uint32_t)(b >> 24)); }
   __device__ __forceinline__ int token() const { return (int)(0xFFFFFFu - (uint32_t)(b & 0xFFFFFFu)); }
   __device__ __forceinline__ bool valid() const { return a != 0; }
   __device__ __forceinline__ bool operator>=(const GroupKey& o) const { return a > o.a || (a == o.a && b >= o.b); }
@@ -82,7 +66,7 @@ struct GroupKey {
   }
 };
 
-// In a row, the logit alone.
+// A number alone.
 struct WordKey {
   uint32_t a;
   static constexpr int kBits = 32;
@@ -245,6 +229,12 @@ struct alignas(16) Vec {
   }
 };
 
+template <int DTYPE>
+__device__ __forceinline__ float logit_at(const char* row, int token) {
+  if (DTYPE == SEMKV_F32) return reinterpret_cast<const float*>(row)[token];
+  const uint16_t h = reinterpret_cast<const uint16_t*>(row)[token];
+  return DTYPE == SEMKV_BF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
+}
 // Logits first .. first + count of a row, the others -infinity.  The vectors lie `lead` bytes behind a multiple of
 // 16; those inside the row are brought by whole aligned loads all the same, two for one of them (its neighbour's
 // other half is in the cache).  So a thread's logits, and the order of every sum, do not depend on where a row lies.
@@ -282,11 +272,30 @@ __device__ __forceinline__ Vec<DTYPE> load_vec(const char* row, int first, int v
 
 // ------------------------------------------------------------------ scan ------
 
-// Where a call's pieces lie: `splits` pieces of `piece` logits to a row.
+constexpr int kScanWarps = kScanThreads / 32, kVecs = 4;  // kVecs: vectors of a thread in one tile
+// How a call's rows are cut.  Each is `units` units of a vector for each of a CTA's threads; a CTA has `share`
+// units, of one row behind the other, up to 32 tiles, so a row lies in up to `splits` pieces.
 struct Pieces {
-  int splits, piece;
-  float4* sums;  // [rows][splits] the largest logit, and the sum of 2^(x log2 e - scale_of(it)) as two numbers
-  RowKey* keys;  // [rows][splits][k + kSlack]
+  int units, share, splits;
+  uint32_t per_split;  // 2^32 / splits, rounded up: a product's upper half is the quotient (0: splits is 1)
+  // [rows][splits][warps] the largest logit, the sum of 2^(x log2 e - scale_of(it)) as two numbers, and the floor
+  float4* sums;
+  // [rows][splits][threads] ordered(the largest logit) of the threads that reach the floor, in no order, then zeros
+  uint32_t* words;
+  uint2* marks;  // beside those that reach it: the tiles to look at, and the thread
+  // how many of its pieces row `row` has, and where the one numbered `split` ends
+  __device__ __forceinline__ int pieces_of(int row) const {
+    const int64_t first = (int64_t)row * units;
+    return (int)((first + units - 1) / share - first / share) + 1;
+  }
+  __device__ __forceinline__ int end_unit(int row, int split) const {
+    const int64_t first = (int64_t)row * units;
+    return (int)min((int64_t)units, (first / share + split + 1) * share - first);
+  }
+  __device__ __forceinline__ int begin_unit(int row, int split) const {
+    const int64_t first = (int64_t)row * units;
+    return (int)max((int64_t)0, (first / share + split) * share - first);
+  }
 };
 
 // A row that is read: neither done nor without a chance.
@@ -300,143 +309,84 @@ __device__ __forceinline__ const char* row_at(const BeamArgs& a, int row) {
   return static_cast<const char*>(a.logits) + (int64_t)row * a.stride * Vec<DTYPE>::kSize;
 }
 
-constexpr int kVecs = 4;  // vectors of a thread in one go
-
-// What the scan keeps in shared memory: places of a row to look at once more, the list, and what a cut needs.
-__host__ __device__ constexpr int scan_cap(int k, int dtype) { return (k + kSlack) * (1 + (dtype == SEMKV_F32 ? 4 : 8)); }
-constexpr int kPlaces = 4 * kScanThreads;
-__host__ __device__ constexpr int scan_bytes(int k, int dtype) {
-  return kPlaces * (int)sizeof(int) + (scan_cap(k, dtype) + k + kSlack) * (int)sizeof(RowKey);
+// A thread's vectors of a tile, the first of them from logit `first` on; behind the piece's end -infinity.
+template <int DTYPE>
+__device__ __forceinline__ void load_vecs(Vec<DTYPE> (&v)[kVecs], const char* row, int lead, int first, int end, int vocab) {
+  using V = Vec<DTYPE>;
+  constexpr int kUnit = kScanThreads * V::kCount;
+  if (lead == 0 && first + (kVecs - 1) * kUnit + V::kCount <= end) {
+    const uint4* from = reinterpret_cast<const uint4*>(row + (int64_t)first * V::kSize);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const uint4 x = __ldcs(from + i * kScanThreads);
+      v[i].w[0] = x.x, v[i].w[1] = x.y, v[i].w[2] = x.z, v[i].w[3] = x.w;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    if (first + i * kUnit < end) v[i] = load_vec<DTYPE>(row, first + i * kUnit, vocab, lead);
+    else v[i].fill_none();
+  }
 }
-__host__ __device__ constexpr int merge_cap(int k) { return (k + kSlack) * (1 + kMergePer); }
 
 template <int DTYPE>
 __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, Pieces p) {
   using V = Vec<DTYPE>;
-  constexpr int kTile = kScanThreads * kVecs * V::kCount;
-  extern __shared__ __align__(16) unsigned char shared[];
-  __shared__ int count, place_count;
-  __shared__ Extent extents[kScanThreads / 32];
-  __shared__ float part[kScanThreads / 32], part_low[kScanThreads / 32];
-  const int slots = a.k + kSlack, tid = threadIdx.x;
-  int* places = reinterpret_cast<int*>(shared);  // the first token of a thread's vectors
-  Best<RowKey, kScanThreads> best;
-  best.list = reinterpret_cast<RowKey*>(places + kPlaces);
-  best.spare = best.list + scan_cap(a.k, DTYPE);
-  best.count = &count;
-  best.extents = extents;
-  best.k = a.k;
-  best.cap = scan_cap(a.k, DTYPE);
-  best.floor = RowKey::none();
-  if (tid == 0) count = place_count = 0;
-  __syncthreads();
-  const int row = blockIdx.x / p.splits, split = blockIdx.x - row * p.splits;
+  constexpr int kUnit = kScanThreads * V::kCount, kTile = kVecs * kUnit;
+  __shared__ uint32_t warp_words[2][kScanWarps];
+  __shared__ int reaching[2], others[2];  // (of this piece, and the one behind it)
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_trigger();
-  if (!row_counts(a, row)) return;
-  const char* at = row_at<DTYPE>(a, row);
-  const int lead = (int)((uintptr_t)at & 15);
-  const int begin = split * p.piece, end = min(a.vocab, begin + p.piece);
-  float m = kNone, c = -4 * kFar, sum = 0.f, low = 0.f;  // of this thread's logits
-  float floor = kNone;  // k logits of this or more have been seen: the same or less does not matter any more
-  uint32_t seen = 0;    // tiles (of the last 32) in which this thread saw a logit above the floor
-
-  // The threads' largest so far tell of a higher floor, if enough of them reach the present one.
-  auto raise = [&]() {
-    const bool in = m >= floor && m > kNone;
-    if (__syncthreads_count(in) <= slots) return false;
-    const uint32_t word = ordered(m);
-    const Extent e = extent_of<kScanThreads>(in ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
-    floor = unordered(threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(in && word >= up.a); }).a);
-    return true;
-  };
-  // What was seen goes into the list.  Few logits are left above the floor by now: they are read again, from the
-  // caches, rather than put aside when they were met, which took as long as all else together.
-  auto settle = [&](int t0) {
-    raise();
-    const uint32_t mine = m >= floor && m > kNone ? seen : 0u;
-    int w = mine ? atomicAdd(&place_count, __popc(mine)) : 0;
-    __syncthreads();
-    const int passes = place_count > kPlaces ? 8 : 1;  // more than there is room for: four tiles at a time
-    for (int pass = 0; pass < passes; ++pass) {
-      uint32_t bits = mine;
-      if (passes > 1) {
-        bits &= 15u << (4 * pass);
-        __syncthreads();
-        if (tid == 0) place_count = 0;
-        __syncthreads();
-        w = bits ? atomicAdd(&place_count, __popc(bits)) : 0;
+  int64_t unit = (int64_t)blockIdx.x * p.share;
+  const int64_t past = min((int64_t)a.groups * a.beams * p.units, unit + p.share);
+  int raised = 0, turn = 0;
+  if (tid < 2) reaching[tid] = others[tid] = 0;
+  while (unit < past) {
+    const int row = (int)(unit / p.units), split = (int)(blockIdx.x - (int64_t)row * p.units / p.share);
+    const int begin = p.begin_unit(row, split) * kUnit, end_unit = p.end_unit(row, split), end = min(a.vocab, end_unit * kUnit);
+    unit = (int64_t)row * p.units + end_unit;
+    if (!row_counts(a, row)) continue;
+    const char* at = row_at<DTYPE>(a, row);
+    const int lead = (int)((uintptr_t)at & 15);
+    // of this thread's logits; k logits of `floor` or more have been seen: the same or less does not matter any more
+    float m = kNone, c = -4 * kFar, sum = 0.f, low = 0.f, floor = kNone;
+    uint32_t seen = 0;
+    int tile = 0;
+    // The threads' largest so far tell of a floor: every warp's so-manieth, the lowest of which k threads reach.
+    auto raise = [&]() {
+      const int want = (a.k + kScanWarps - 1) / kScanWarps;
+      uint32_t mine = m > kNone ? ordered(m) : 0u, word;
+      for (int have = 0;;) {
+        word = __reduce_max_sync(~0u, mine);
+        have += __popc(__ballot_sync(~0u, mine == word));
+        if (have >= want || word == 0) break;
+        if (mine == word) mine = 0;
       }
-      for (; bits; bits &= bits - 1) places[w++] = t0 + (__ffs(bits) - 1) * kTile + tid * V::kCount;
+      uint32_t* words = warp_words[raised++ & 1];
+      if (lane == 0) words[warp] = word;
       __syncthreads();
-      const int n = place_count * kVecs;
-      for (int e0 = 0; e0 < n; e0 += kScanThreads) {
-        const int e = e0 + tid, first = e < n ? places[e / kVecs] + e % kVecs * (kScanThreads * V::kCount) : end;
-        V x;
-        RowKey top = RowKey::none();
-        if (first < end) {
-          x = load_vec<DTYPE>(at, first, a.vocab, lead);
-          if (!(V::larger(x.largest2()) < INFINITY)) x.clean();
-          const float big = V::larger(x.largest2());
-          if (big >= floor && big > kNone) {
-            int where = 0;
-#pragma unroll
-            for (int j = V::kCount - 1; j >= 0; --j)
-              if (x.at(j) == big) where = j;
-            top = RowKey::of(big, first + where);
-          }
-        }
-        best.template offer<V::kCount>(top, [&](const RowKey& from) {
-#pragma unroll
-          for (int j = 0; j < V::kCount; ++j) {
-            const RowKey key = RowKey::of(x.at(j), first + j);
-            if (x.at(j) > kNone && x.at(j) >= floor && key >= from) best.put(key);
-          }
-        });
-      }
-    }
-    __syncthreads();
-    if (tid == 0) place_count = 0;
-    if (best.floor.valid()) floor = fmaxf(floor, best.floor.logit());
-    seen = 0;
-    __syncthreads();
-  };
-
-  auto load = [&](V (&v)[kVecs], int t0) {
-    if (lead == 0 && t0 + kTile <= end) {
-      const uint4* from = reinterpret_cast<const uint4*>(at + (int64_t)t0 * V::kSize) + tid;
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        const uint4 x = __ldcs(from + i * kScanThreads);
-        v[i].w[0] = x.x, v[i].w[1] = x.y, v[i].w[2] = x.z, v[i].w[3] = x.w;
-      }
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int first = t0 + (i * kScanThreads + tid) * V::kCount;
-      if (first < end) v[i] = load_vec<DTYPE>(at, first, a.vocab, lead);
-      else v[i].fill_none();
-    }
-  };
-  V v[kVecs];
-  load(v, begin);
-  int tile = 0;
-  for (int t0 = begin; t0 < end; t0 += kTile) {
-    auto largest = [&]() {
-      uint32_t two = v[0].largest2();
-#pragma unroll
-      for (int i = 1; i < kVecs; ++i) two = V::max2(two, v[i].largest2());
-      return V::larger(two);
+      // (the counts of the piece before, which all have left behind: the one behind this begins with them)
+      if (tid == 0) reaching[~turn & 1] = others[~turn & 1] = 0;
+      word = __reduce_min_sync(~0u, words[lane % kScanWarps]);
+      if (word) floor = fmaxf(floor, unordered(word));
     };
-    float top = largest();
-    if (!(top < INFINITY)) {
+    // One tile, whose vectors make room for those two tiles on.
+    auto step = [&](V (&v)[kVecs], int t0) {
+      auto largest = [&]() {
+        uint32_t two = v[0].largest2();
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i) v[i].clean();
-      top = largest();
-      raise_error(a.err, kDevNonFinite);
-    }
-    if (top > kNone) {
+        for (int i = 1; i < kVecs; ++i) two = V::max2(two, v[i].largest2());
+        return V::larger(two);
+      };
+      float top = largest();
+      if (!(top < INFINITY)) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) v[i].clean();
+        top = largest();
+        raise_error(a.err, kDevNonFinite);
+      }
       m = fmaxf(m, top);
       if (__fmaf_rn(m, kLog2e, -c) > 2.f) {
         const float up = scale_of(m), by = pow2(c - up);  // (0 the first time)
@@ -459,60 +409,53 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
       float err;
       two_sum(sum, (s[0] + s[1]) + (s[2] + s[3]), sum, err);
       low += err;
+      if (t0 + 2 * kTile < end) load_vecs<DTYPE>(v, at, lead, t0 + 2 * kTile + tid * V::kCount, end, a.vocab);
+      seen |= (uint32_t)(top > floor) << tile++;
+    };
+    V v0[kVecs], v1[kVecs];
+    load_vecs<DTYPE>(v0, at, lead, begin + tid * V::kCount, end, a.vocab);
+    if (begin + kTile < end) load_vecs<DTYPE>(v1, at, lead, begin + kTile + tid * V::kCount, end, a.vocab);
+    for (int t0 = begin; t0 < end; t0 += 2 * kTile) {
+      step(v0, t0);
+      if (t0 + kTile < end) step(v1, t0 + kTile);
+      if (t0 + 2 * kTile >= end || (tile & (tile - 1)) != 0) continue;
+      raise();  // (behind the second tile, the fourth, the eighth ...: a tile further on has less and less above it)
     }
-    if (t0 + kTile < end) load(v, t0 + kTile);
-    bool hot = top > floor;
-    const int n = __syncthreads_count(hot);
-    if (2 * n > a.k && raise()) hot = top >= floor && top > kNone;  // (more than a tile further on should have)
-    seen |= (uint32_t)hot << tile;
-    if (++tile == 32 || t0 + kTile >= end) {
-      settle(t0 - (tile - 1) * kTile);
-      tile = 0;
+    const int64_t piece = (int64_t)row * p.splits + split;
+    raise();
+    {
+      const bool in = m >= floor && m > kNone;
+      const uint32_t ins = __ballot_sync(~0u, in);
+      int at_in = 0, at_out = 0;
+      if (lane == 0) {
+        at_in = atomicAdd(reaching + (turn & 1), __popc(ins));
+        at_out = atomicAdd(others + (turn & 1), 32 - __popc(ins));
+      }
+      at_in = __shfl_sync(~0u, at_in, 0);
+      at_out = __shfl_sync(~0u, at_out, 0);
+      const int64_t to = piece * kScanThreads + (in ? at_in + __popc(ins & ((1u << lane) - 1))
+                                                    : kScanThreads - 1 - at_out - __popc(~ins & ((1u << lane) - 1)));
+      p.words[to] = in ? ordered(m) : 0u;
+      if (in) p.marks[to] = make_uint2(seen, tid);
+      ++turn;
     }
-  }
-  // the sum over the threads, a pair of numbers each
-  const int lane = tid & 31, warp = tid >> 5;
-  float M = m;
+    // the warp's sum, a pair of numbers
+    float most = m;
 #pragma unroll
-  for (int d = 16; d > 0; d /= 2) M = fmaxf(M, __shfl_xor_sync(~0u, M, d));
-  if (lane == 0) part[warp] = M;
-  __syncthreads();
+    for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+    const float by = m > kNone ? pow2(c - scale_of(most)) : 0.f;
+    sum *= by;
+    low *= by;
 #pragma unroll
-  for (int w = 0; w < kScanThreads / 32; ++w) M = fmaxf(M, part[w]);
-  __syncthreads();
-  const float by = m > kNone ? pow2(c - scale_of(M)) : 0.f;
-  sum *= by;
-  low *= by;
-#pragma unroll
-  for (int d = 16; d > 0; d /= 2) {
-    float err;
-    const float other = __shfl_xor_sync(~0u, sum, d);
-    low += __shfl_xor_sync(~0u, low, d);
-    two_sum(sum, other, sum, err);
-    low += err;
-  }
-  if (lane == 0) {
-    part[warp] = sum;
-    part_low[warp] = low;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    sum = part[0];
-    low = part_low[0];
-    for (int w = 1; w < kScanThreads / 32; ++w) {
+    for (int d = 16; d > 0; d /= 2) {
       float err;
-      two_sum(sum, part[w], sum, err);
-      low += part_low[w] + err;
+      const float other = __shfl_xor_sync(~0u, sum, d);
+      low += __shfl_xor_sync(~0u, low, d);
+      two_sum(sum, other, sum, err);
+      low += err;
     }
-    p.sums[(int64_t)row * p.splits + split] = make_float4(M, sum, low, 0.f);
+    if (lane == 0) p.sums[piece * kScanWarps + warp] = make_float4(most, sum, low, floor);
   }
-  int held = count;
-  if (held > slots) {
-    best.cut(held);
-    held = count;
-  }
-  RowKey* out = p.keys + (int64_t)blockIdx.x * slots;
-  for (int i = tid; i < slots; i += kScanThreads) out[i] = i < held ? best.list[i] : RowKey::none();
 }
 
 // ------------------------------------------------------- the exact sums ------
@@ -606,7 +549,9 @@ struct Base {
   float value, rest;
   float most;   // the row's largest logit
   float error;  // how far value + rest may be off
+  float cut;    // no score below this (value + (logit - most), rounded) is among the k best
   int kind;     // kNobody, kLogits, kDone
+  int pieces;
 };
 enum { kNobody, kLogits, kDone };
 
@@ -624,57 +569,76 @@ __device__ __forceinline__ GroupKey score_of(const Base& r, int beam, float x, i
   return GroupKey::of(score, __fadd_rn(__fsub_rn(s, score), e), beam, x, token);
 }
 
+constexpr int kPlaces = 1024;
+// The list holds what offer() asks of it: k + kSlack threads' keys, a vector each, beside its own k + kSlack.
+__host__ __device__ constexpr int merge_cap(int k, int dtype) {
+  return (k + kSlack) * (dtype == SEMKV_F32 ? 5 : 9) > 2 * kRanked ? (k + kSlack) * (dtype == SEMKV_F32 ? 5 : 9) : 2 * kRanked;
+}
+__host__ __device__ constexpr int merge_bytes(int k, int dtype) {
+  return (merge_cap(k, dtype) + k + kSlack) * (int)sizeof(GroupKey) + kPlaces * (int)sizeof(int2);
+}
+
 template <int DTYPE>
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, Pieces p) {
+  using V = Vec<DTYPE>;
+  constexpr int kUnit = kScanThreads * V::kCount, kTile = kVecs * kUnit, kBatch = 8;
   extern __shared__ __align__(16) unsigned char shared[];
-  __shared__ int count;
+  __shared__ int count, place_count;
   __shared__ double parts[kMergeThreads / 32];
   __shared__ Extent extents[kMergeThreads / 32];
-  __shared__ int places[kRanked];
+  __shared__ int order[kRanked];
   __shared__ Base base[SEMKV_BEAM_MAX];
   __shared__ uint32_t again[SEMKV_BEAM_MAX / 32];  // rows to be summed once more
   __shared__ float2 powers[33];
   __shared__ GroupKey out[SEMKV_BEAM_MAX];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int group = blockIdx.x, row0 = group * a.beams, slots = a.k + kSlack;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int group = blockIdx.x, row0 = group * a.beams;
   Best<GroupKey, kMergeThreads> best;
   best.list = reinterpret_cast<GroupKey*>(shared);
-  best.spare = best.list + merge_cap(a.k);
+  best.spare = best.list + merge_cap(a.k, DTYPE);
   best.count = &count;
   best.extents = extents;
   best.k = a.k;
-  best.cap = merge_cap(a.k);
-  if (threadIdx.x < SEMKV_BEAM_MAX / 32) again[threadIdx.x] = 0;
+  best.cap = merge_cap(a.k, DTYPE);
+  int2* places = reinterpret_cast<int2*>(best.spare + a.k + kSlack);  // beam and split, the first token of a thread's vectors
+  if (tid < SEMKV_BEAM_MAX / 32) again[tid] = 0;
+  if (tid == 0) count = place_count = 0;
   pdl_wait();
   pdl_trigger();
-  const int per_row = p.splits * slots, total = a.beams * per_row;
-  const RowKey* keys = p.keys + (int64_t)row0 * per_row;
-  RowKey ahead[kMergePer];  // the first of a thread's keys, on their way while the sums are brought together
+  // The scan's threads, one behind the other: of each batch this thread has every kMergeThreads-th.
+  const int marked = a.beams * p.splits * kScanThreads;
+  const uint32_t* words = p.words + (int64_t)row0 * p.splits * kScanThreads;
+  const uint2* marks = p.marks + (int64_t)row0 * p.splits * kScanThreads;
+  uint32_t word[kBatch];  // (the first are on their way while the sums are brought together)
+  auto load_words = [&](int i0) {
 #pragma unroll
-  for (int i = 0; i < kMergePer; ++i) {
-    const int e = i * kMergeThreads + threadIdx.x;
-    ahead[i] = e < total ? keys[e] : RowKey::none();
-  }
-  // a warp for each row: its pieces' sums together
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = i0 + j * kMergeThreads + tid;
+      word[j] = i < marked ? words[i] : 0u;
+    }
+  };
+  load_words(0);
+  // a warp for each row: its warps' sums together
   for (int b = warp; b < a.beams; b += kMergeThreads / 32) {
     const int row = row0 + b;
     const float score = a.scores[row];
     const bool is_done = a.done && a.done[row];
-    Base r{score, 0.f, 0.f, 0.f, kNobody};
+    Base r{score, 0.f, 0.f, 0.f, kNone, kNobody, p.pieces_of(row)};
     if (score != score || score == INFINITY) {
       if (lane == 0) raise_error(a.err, kDevNonFinite);
     } else if (score > kNone && is_done) {
       r.kind = kDone;
     } else if (score > kNone) {
-      const float4* s = p.sums + (int64_t)row * p.splits;
+      const float4* s = p.sums + (int64_t)row * p.splits * kScanWarps;
+      const int sums = r.pieces * kScanWarps;
       float m = kNone;
-      for (int i = lane; i < p.splits; i += 32) m = fmaxf(m, s[i].x);
+      for (int i = lane; i < sums; i += 32) m = fmaxf(m, s[i].x);
 #pragma unroll
       for (int d = 16; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
       if (m > kNone) {
         const float c = scale_of(m);
         float sum = 0.f, low = 0.f, err;
-        for (int i = lane; i < p.splits; i += 32) {
+        for (int i = lane; i < sums; i += 32) {
           const float4 x = s[i];
           const float by = x.x > kNone ? pow2(scale_of(x.x) - c) : 0.f;
           two_sum(sum, x.y * by, sum, err);
@@ -713,7 +677,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   __syncthreads();
   auto sum_again = [&](int b) {
     const double norm = exact_normalizer<DTYPE>(a, row0 + b, base[b].most, powers, parts);
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
       set_value(base[b], a.scores[row0 + b], (float)norm, (float)(norm - (double)(float)norm));
       base[b].error = 0x1p-36f;
     }
@@ -724,58 +688,153 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     if (base[b].kind == kLogits && fabsf(base[b].most) > kFar) sum_again(b);
     worst = fmaxf(worst, base[b].error);
   }
-  auto candidate = [&](int e, const RowKey& key) {
-    const int b = e / per_row;
+  // The score of the largest logit that a word tells of, rounded; -infinity: none.  (A warp's are of one piece.)
+  auto beam_of = [&](int i) { return p.per_split ? (int)__umulhi((uint32_t)i / kScanThreads, p.per_split) : i / kScanThreads; };
+  auto score_at = [&](int i, uint32_t word) {
+    if (!__any_sync(~0u, word) || i >= marked) return kNone;
+    const int b = beam_of(i);
     const Base& r = base[b];
-    if (r.kind == kNobody) return GroupKey::none();
-    if (r.kind == kDone) return e == b * per_row ? score_of(r, b, 0.f, a.end_token) : GroupKey::none();
-    return key.valid() ? score_of(r, b, key.logit(), key.token()) : GroupKey::none();
+    if (r.kind != kLogits || i / kScanThreads - b * p.splits >= r.pieces || !word) return kNone;
+    return r.value + (unordered(word) - r.most);
   };
-  int held = 0;
-  for (int round = 0;; ++round) {
-    best.floor = GroupKey::none();
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
-    for (int e0 = 0; e0 < total; e0 += kMergeThreads * kMergePer) {
-      GroupKey mine[kMergePer], top = GroupKey::none();
+  // A score that k of them reach, and how far below it a candidate may stay and be among the k best all the same.
+  float top = tid < a.beams && base[tid].kind == kDone ? base[tid].value : kNone;
+  for (int i0 = 0; i0 < marked; i0 += kBatch * kMergeThreads) {
+    if (i0 > 0) load_words(i0);
 #pragma unroll
-      for (int i = 0; i < kMergePer; ++i) {
-        const int e = e0 + i * kMergeThreads + threadIdx.x;
-        RowKey key = ahead[i];
-        if (e0 > 0 && e < total) key = keys[e];
-        mine[i] = e < total ? candidate(e, key) : GroupKey::none();
-        if (mine[i] >= top) top = mine[i];
+    for (int j = 0; j < kBatch; ++j) top = fmaxf(top, score_at(i0 + j * kMergeThreads + tid, word[j]));
+  }
+  float reach = kNone;
+  {
+    const bool in = top > kNone;
+    const uint32_t word = ordered(top);
+    const int n = __syncthreads_count(in);
+    if (n >= a.k) {
+      const Extent e = extent_of<kMergeThreads>(in ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
+      reach = unordered(n <= a.k + kSlack ? e.least
+                                          : threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(in && word >= up.a); }).a);
+    }
+  }
+  // (2^-20 of the numbers that were added is far more than their roundings)
+  for (int b = tid; b < a.beams; b += kMergeThreads)
+    base[b].cut = reach > kNone ? reach - 2.1f * worst - 0x1p-20f * (fabsf(base[b].value) + fabsf(reach)) : kNone;
+  __syncthreads();
+  // the marked tiles of those that come near it
+  if (tid < a.beams && base[tid].kind == kDone && base[tid].value >= base[tid].cut) best.put(score_of(base[tid], tid, 0.f, a.end_token));
+  for (int i0 = 0; i0 < marked; i0 += kBatch * kMergeThreads) {
+    if (marked > kBatch * kMergeThreads) load_words(i0);
+    uint32_t near = 0;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = i0 + j * kMergeThreads + tid;
+      const float s = score_at(i, word[j]);
+      near |= (uint32_t)(s > kNone && s >= base[i < marked ? beam_of(i) : 0].cut) << j;
+    }
+    for (; near; near &= near - 1) {
+      const int i = i0 + (__ffs(near) - 1) * kMergeThreads + tid, b = beam_of(i), split = i / kScanThreads - b * p.splits;
+      const uint2 mark = marks[i];
+      uint32_t bits = mark.x;
+      int w = atomicAdd(&place_count, __popc(bits));
+      const int first = p.begin_unit(row0 + b, split) * kUnit + (int)mark.y * V::kCount;
+      for (; bits && w < kPlaces; bits &= bits - 1) places[w++] = make_int2(i / kScanThreads, first + (__ffs(bits) - 1) * kTile);
+    }
+  }
+  __syncthreads();
+  const bool many_places = place_count > kPlaces;
+  if (!many_places) {
+    for (int i = tid; i < place_count; i += kMergeThreads) {
+      const int2 at = places[i];
+      const int b = beam_of(at.x * kScanThreads), row = row0 + b;
+      const Base& r = base[b];
+      const char* from = row_at<DTYPE>(a, row);
+      const float floor = p.sums[((int64_t)row0 * p.splits + at.x) * kScanWarps].w;
+      V v[kVecs];
+      load_vecs<DTYPE>(v, from, (int)((uintptr_t)from & 15), at.y, min(a.vocab, p.end_unit(row, at.x - b * p.splits) * kUnit), a.vocab);
+      uint32_t hits = 0;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int j = 0; j < V::kCount; ++j) {
+          const float x = v[i].at(j);
+          hits |= (uint32_t)(x > kNone && x < INFINITY && x >= floor && r.value + (x - r.most) >= r.cut) << (i * V::kCount + j);
+        }
+      int w = hits ? atomicAdd(&count, __popc(hits)) : 0;
+      for (; hits && w < best.cap; hits &= hits - 1) {
+        const int n = __ffs(hits) - 1, token = at.y + n / V::kCount * kUnit + n % V::kCount;
+        best.list[w++] = score_of(r, b, logit_at<DTYPE>(from, token), token);
       }
-      best.template offer<kMergePer>(top, [&](const GroupKey& from) {
+    }
+  }
+  __syncthreads();
+  bool exact = many_places || count > kRanked;
+  if (exact) {
+    // Ties of very many.  All rows are summed again, so that a key says which is better, and the k best
+    // are kept while the marked tiles go by.
+    for (int b = 0; b < a.beams; ++b)
+      if (base[b].kind == kLogits) sum_again(b);
+    if (tid == 0) count = 0;
+    best.floor = GroupKey::none();
+    __syncthreads();
+    for (int i0 = 0; i0 < marked; i0 += kMergeThreads) {
+      const int i = i0 + tid, b = i < marked ? beam_of(i) : 0, split = i < marked ? i / kScanThreads - b * p.splits : 0;
+      const float s = score_at(i, i < marked ? words[i] : 0u);
+      uint2 mark = make_uint2(0u, 0u);
+      if (s > kNone && s >= base[b].cut) mark = marks[i];
+      uint32_t bits = mark.x;
+      if (i0 == 0) {
+        const GroupKey end_key = tid < a.beams && base[tid].kind == kDone ? score_of(base[tid], tid, 0.f, a.end_token) : GroupKey::none();
+        best.template offer<1>(end_key, [&](const GroupKey&) { best.put(end_key); });
+      }
+      const int row = row0 + b;
+      const char* from = row_at<DTYPE>(a, row);
+      const int lead = (int)((uintptr_t)from & 15), end = min(a.vocab, p.end_unit(row, split) * kUnit);
+      const int first0 = p.begin_unit(row, split) * kUnit + (int)mark.y * V::kCount;
+      for (; __syncthreads_or(bits != 0); bits &= bits - 1)
+        for (int j = 0; j < kVecs; ++j) {
+          const int first = bits ? first0 + (__ffs(bits) - 1) * kTile + j * kUnit : end;
+          V v;
+          v.fill_none();
+          if (first < end) v = load_vec<DTYPE>(from, first, a.vocab, lead);
+          v.clean();
+          GroupKey most = GroupKey::none();
 #pragma unroll
-        for (int i = 0; i < kMergePer; ++i)
-          if (mine[i].valid() && mine[i] >= from) best.put(mine[i]);
-      });
+          for (int e = 0; e < V::kCount; ++e)
+            if (v.at(e) > kNone) {
+              const GroupKey key = score_of(base[b], b, v.at(e), first + e);
+              if (key >= most) most = key;
+            }
+          best.template offer<V::kCount>(most, [&](const GroupKey& least) {
+#pragma unroll
+            for (int e = 0; e < V::kCount; ++e)
+              if (v.at(e) > kNone) {
+                const GroupKey key = score_of(base[b], b, v.at(e), first + e);
+                if (key >= least) best.put(key);
+              }
+          });
+        }
     }
     __syncthreads();
-    held = count;
-    __syncthreads();
-    if (held > kRanked) {
-      best.cut(held);
-      held = count;
-    }
+    if (count > kRanked) best.cut(count);
+  }
+  int held;
+  for (;;) {
     // the place of each among them, counted by several threads for each
-    const int parts_of = kMergeThreads / max(held, 1) > 0 ? kMergeThreads / max(held, 1) : 1;
-    for (int i = threadIdx.x; i < held; i += kMergeThreads) places[i] = -1;
+    const int all = count, times = max(kMergeThreads / max(all, 1), 1);
+    for (int i = tid; i < all; i += kMergeThreads) order[i] = -1;
     __syncthreads();
-    for (int i = threadIdx.x; i < held * parts_of; i += kMergeThreads) {
-      const int which = i % held;
+    for (int i = tid; i < all * times; i += kMergeThreads) {
+      const int which = i % all;
       const GroupKey x = best.list[which];
-      int ahead_of = 0;
-      for (int j = i / held; j < held; j += parts_of) ahead_of += best.list[j] >= x;
-      atomicAdd(places + which, ahead_of);
+      int before = 0;
+      for (int j = i / all; j < all; j += times) before += best.list[j] >= x;
+      atomicAdd(order + which, before);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < held; i += kMergeThreads)
-      if (places[i] < a.k) out[places[i]] = best.list[i];
-    held = min(held, a.k);
+    for (int i = tid; i < all; i += kMergeThreads)
+      if (order[i] < a.k) out[order[i]] = best.list[i];
+    held = min(all, a.k);
     __syncthreads();
-    if (round == 1) break;
+    if (exact) break;
     // Is the order sure?  Neighbours of different rows, and whoever comes close to the last one.  (If two are as near as
     // the worst rows' errors, so are all between them, and the rows of both have a neighbour of another row there.)
     auto close = [&](const GroupKey& x, const GroupKey& y) {
@@ -786,23 +845,21 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
       return base[b].kind == kLogits || base[c].kind == kLogits;
     };
     bool open = false;
-    for (int i = threadIdx.x; i + 1 < held; i += kMergeThreads) open |= close(out[i], out[i + 1]);
-    // (candidates that are not in the list lie below the floor)
-    if (held == a.k) {
-      const GroupKey last = out[held - 1];
-      for (int i = threadIdx.x; i < count; i += kMergeThreads)
-        if (!(best.list[i] >= last)) open |= close(best.list[i], last);
-      if (best.floor.valid() && (last.score() - best.floor.score()) + last.rest() <= 2.001f * worst + 0x1p-22f * fabsf(last.score()))
-        for (int e = threadIdx.x; e < total; e += kMergeThreads) {
-          const GroupKey x = candidate(e, keys[e]);
-          if (x.valid() && !(x >= last)) open |= close(x, last);
-        }
-    }
+    for (int i = tid; i + 1 < held; i += kMergeThreads) open |= close(out[i], out[i + 1]);
+    if (held == a.k)
+      for (int i = tid; i < all; i += kMergeThreads)
+        if (order[i] >= a.k) open |= close(best.list[i], out[a.k - 1]);
     if (!__syncthreads_or(open)) break;
     for (int b = 0; b < a.beams; ++b)
       if (again[b >> 5] >> (b & 31) & 1 && base[b].kind == kLogits) sum_again(b);
+    for (int i = tid; i < all; i += kMergeThreads) {
+      const GroupKey x = best.list[i];
+      best.list[i] = score_of(base[x.beam()], x.beam(), x.logit(), x.token());
+    }
+    __syncthreads();
+    exact = true;
   }
-  for (int i = threadIdx.x; i < a.k; i += kMergeThreads) {
+  for (int i = tid; i < a.k; i += kMergeThreads) {
     const int64_t at = (int64_t)group * a.k + i;
     const bool is = i < held;
     a.parent[at] = is ? row0 + out[i].beam() : -1;
@@ -813,41 +870,45 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
 
 int vec_logits(int dtype) { return dtype == SEMKV_F32 ? 4 : 8; }
 
-// Rows are cut into pieces until there are a few CTAs for each SM, whole strides of a CTA each.  The cut depends on
-// the sizes alone, so that equal calls give equal bits.
-constexpr int kWantCtas = 152 * 4;
+// One CTA to each of the places that the SMs have for them, if there is a unit for each; whole tiles, if that is
+// more than one, and no more than a mark can tell apart.  The cut depends on the sizes alone, so that equal calls give equal
+// bits.
+constexpr int kWantCtas = 152 * 4, kMarkTiles = 32;
 Pieces cut_rows(int rows, int vocab, int dtype) {
-  const int unit = kScanThreads * vec_logits(dtype), units = (vocab + unit - 1) / unit;
-  int splits = (kWantCtas + rows - 1) / rows;
-  if (splits > units) splits = units;
+  const int unit = kScanThreads * vec_logits(dtype);
   Pieces p = {};
-  p.piece = (units + splits - 1) / splits * unit;
-  p.splits = (vocab + p.piece - 1) / p.piece;
+  p.units = (vocab + unit - 1) / unit;
+  int64_t share = ((int64_t)rows * p.units + kWantCtas - 1) / kWantCtas;
+  if (share > 1 || p.units >= kVecs) share = (share + kVecs - 1) / kVecs * kVecs;
+  if (share > kVecs * kMarkTiles) share = kVecs * kMarkTiles;
+  p.share = (int)share;
+  p.splits = p.units % p.share == 0 ? p.units / p.share : (p.units + p.share - 2) / p.share + 1;
+  p.per_split = p.splits > 1 ? 0xFFFFFFFFu / (uint32_t)p.splits + 1 : 0u;
   return p;
 }
 
 template <int DTYPE>
 cudaError_t launch(const BeamArgs& a, const Pieces& p, cudaStream_t stream) {
-  const size_t scan = scan_bytes(a.k, DTYPE);
-  const size_t merge = (merge_cap(a.k) + a.k + kSlack) * sizeof(GroupKey);
-  const cudaError_t e = launch_pdl(beam_scan_kernel<DTYPE>, dim3(a.groups * a.beams * p.splits), dim3(kScanThreads), scan, stream, a, p);
+  const unsigned ctas = (unsigned)(((int64_t)a.groups * a.beams * p.units + p.share - 1) / p.share);
+  const cudaError_t e = launch_pdl(beam_scan_kernel<DTYPE>, dim3(ctas), dim3(kScanThreads), 0, stream, a, p);
   if (e != cudaSuccess) return e;
-  return launch_pdl(beam_merge_kernel<DTYPE>, dim3(a.groups), dim3(kMergeThreads), merge, stream, a, p);
+  return launch_pdl(beam_merge_kernel<DTYPE>, dim3(a.groups), dim3(kMergeThreads), merge_bytes(a.k, DTYPE), stream, a, p);
 }
 
 }  // namespace
 
 size_t beam_select_workspace(int groups, int beams, int vocab, int dtype, int k) {
+  (void)k;
   const int rows = groups * beams;
-  const size_t pieces = (size_t)rows * cut_rows(rows, vocab, dtype).splits;
-  return pieces * sizeof(float4) + (pieces * (k + kSlack) * sizeof(RowKey) + 15) / 16 * 16;
+  return (size_t)rows * cut_rows(rows, vocab, dtype).splits * (kScanWarps * sizeof(float4) + kScanThreads * (sizeof(uint2) + sizeof(uint32_t)));
 }
 
 cudaError_t launch_beam_select(const BeamArgs& a, int dtype, void* ws, cudaStream_t stream) {
   const int rows = a.groups * a.beams;
   Pieces p = cut_rows(rows, a.vocab, dtype);
   p.sums = static_cast<float4*>(ws);
-  p.keys = reinterpret_cast<RowKey*>(p.sums + (size_t)rows * p.splits);
+  p.marks = reinterpret_cast<uint2*>(p.sums + (size_t)rows * p.splits * kScanWarps);
+  p.words = reinterpret_cast<uint32_t*>(p.marks + (size_t)rows * p.splits * kScanThreads);
   if (dtype == SEMKV_F32) return launch<SEMKV_F32>(a, p, stream);
   return dtype == SEMKV_BF16 ? launch<SEMKV_BF16>(a, p, stream) : launch<SEMKV_F16>(a, p, stream);
 }
