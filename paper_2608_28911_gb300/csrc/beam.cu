@@ -16,6 +16,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <float.h>
+#include <math.h>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -283,19 +284,15 @@ struct Pieces {
   // [rows][splits][threads] ordered(the largest logit) of the threads that reach the floor, in no order, then zeros
   uint32_t* words;
   uint2* marks;  // beside those that reach it: the tiles to look at, and the thread
-  // how many of its pieces row `row` has, and where the one numbered `split` ends
-  __device__ __forceinline__ int pieces_of(int row) const {
-    const int64_t first = (int64_t)row * units;
-    return (int)((first + units - 1) / share - first / share) + 1;
+  float ln_vocab;
+  // Shares begin anywhere in a row: `offset` units before it is where the share that holds its first unit begins.
+  __device__ __forceinline__ int offset_of(int row) const {
+    const uint32_t n = share;
+    return (int)((uint32_t)row % n * ((uint32_t)units % n) % n);
   }
-  __device__ __forceinline__ int end_unit(int row, int split) const {
-    const int64_t first = (int64_t)row * units;
-    return (int)min((int64_t)units, (first / share + split + 1) * share - first);
-  }
-  __device__ __forceinline__ int begin_unit(int row, int split) const {
-    const int64_t first = (int64_t)row * units;
-    return (int)max((int64_t)0, (first / share + split) * share - first);
-  }
+  __device__ __forceinline__ int pieces_of(int offset) const { return (offset + units - 1) / share + 1; }
+  __device__ __forceinline__ int begin_unit(int offset, int split) const { return max(0, split * share - offset); }
+  __device__ __forceinline__ int end_unit(int offset, int split) const { return min(units, (split + 1) * share - offset); }
 };
 
 // A row that is read: neither done nor without a chance.
@@ -341,12 +338,12 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
   pdl_trigger();
   int64_t unit = (int64_t)blockIdx.x * p.share;
   const int64_t past = min((int64_t)a.groups * a.beams * p.units, unit + p.share);
-  int raised = 0, turn = 0;
+  int row = (int)(unit / p.units), first_unit = (int)(unit - (int64_t)row * p.units), raised = 0, turn = 0;
   if (tid < 2) reaching[tid] = others[tid] = 0;
-  while (unit < past) {
-    const int row = (int)(unit / p.units), split = (int)(blockIdx.x - (int64_t)row * p.units / p.share);
-    const int begin = p.begin_unit(row, split) * kUnit, end_unit = p.end_unit(row, split), end = min(a.vocab, end_unit * kUnit);
-    unit = (int64_t)row * p.units + end_unit;
+  for (; unit < past; ++row, first_unit = 0) {
+    const int offset = p.offset_of(row), split = (first_unit + offset) / p.share, end_unit = p.end_unit(offset, split);
+    const int begin = first_unit * kUnit, end = min(a.vocab, end_unit * kUnit);
+    unit += end_unit - first_unit;
     if (!row_counts(a, row)) continue;
     const char* at = row_at<DTYPE>(a, row);
     const int lead = (int)((uintptr_t)at & 15);
@@ -551,7 +548,7 @@ struct Base {
   float error;  // how far value + rest may be off
   float cut;    // no score below this (value + (logit - most), rounded) is among the k best
   int kind;     // kNobody, kLogits, kDone
-  int pieces;
+  int pieces, offset;
 };
 enum { kNobody, kLogits, kDone };
 
@@ -586,7 +583,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   __shared__ int count, place_count;
   __shared__ double parts[kMergeThreads / 32];
   __shared__ Extent extents[kMergeThreads / 32];
-  __shared__ int order[kRanked];
+  __shared__ uint32_t worst_error, lowest_cut;  // (as ordered numbers)
   __shared__ Base base[SEMKV_BEAM_MAX];
   __shared__ uint32_t again[SEMKV_BEAM_MAX / 32];  // rows to be summed once more
   __shared__ float2 powers[33];
@@ -602,7 +599,8 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   best.cap = merge_cap(a.k, DTYPE);
   int2* places = reinterpret_cast<int2*>(best.spare + a.k + kSlack);  // beam and split, the first token of a thread's vectors
   if (tid < SEMKV_BEAM_MAX / 32) again[tid] = 0;
-  if (tid == 0) count = place_count = 0;
+  if (tid == 0) count = place_count = 0, worst_error = 0u, lowest_cut = 0xFFFFFFFFu;
+  __syncthreads();
   pdl_wait();
   pdl_trigger();
   // The scan's threads, one behind the other: of each batch this thread has every kMergeThreads-th.
@@ -621,25 +619,26 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   // a warp for each row: its warps' sums together
   for (int b = warp; b < a.beams; b += kMergeThreads / 32) {
     const int row = row0 + b;
+    const float4* s = p.sums + (int64_t)row * p.splits * kScanWarps;
+    const int offset = p.offset_of(row), pieces = p.pieces_of(offset), sums = pieces * kScanWarps;
+    const float4 mine = lane < sums ? s[lane] : make_float4(kNone, 0.f, 0.f, 0.f);
     const float score = a.scores[row];
     const bool is_done = a.done && a.done[row];
-    Base r{score, 0.f, 0.f, 0.f, kNone, kNobody, p.pieces_of(row)};
+    Base r{score, 0.f, 0.f, 0.f, kNone, kNobody, pieces, offset};
     if (score != score || score == INFINITY) {
       if (lane == 0) raise_error(a.err, kDevNonFinite);
     } else if (score > kNone && is_done) {
       r.kind = kDone;
     } else if (score > kNone) {
-      const float4* s = p.sums + (int64_t)row * p.splits * kScanWarps;
-      const int sums = r.pieces * kScanWarps;
-      float m = kNone;
-      for (int i = lane; i < sums; i += 32) m = fmaxf(m, s[i].x);
+      float m = mine.x;
+      for (int i = lane + 32; i < sums; i += 32) m = fmaxf(m, s[i].x);
 #pragma unroll
       for (int d = 16; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
       if (m > kNone) {
         const float c = scale_of(m);
         float sum = 0.f, low = 0.f, err;
         for (int i = lane; i < sums; i += 32) {
-          const float4 x = s[i];
+          const float4 x = i == lane ? mine : s[i];
           const float by = x.x > kNone ? pow2(scale_of(x.x) - c) : 0.f;
           two_sum(sum, x.y * by, sum, err);
           low += x.z * by + err;
@@ -662,19 +661,24 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
         const float n = c + (float)e, h = __fmul_rn(n, kBig);
         float norm, rest;
         two_sum(h, -m, norm, rest);
-        rest += __fmaf_rn(n, kBig, -h) + n * kSmall + low / sum;
-        two_sum(norm, logf(ldexpf(sum, -e)), norm, err);
-        const float u = logf((float)a.vocab) - norm;
+        rest += __fmaf_rn(n, kBig, -h) + n * kSmall + __fdividef(low, sum);
+        two_sum(norm, logf(__uint_as_float(__float_as_uint(sum) - ((uint32_t)e << 23))), norm, err);
+        const float u = p.ln_vocab - norm;
         rest += err - kLack * (m - 0.5f * u);
         set_value(r, score, norm, rest);
         // In units of 2^-24: an exponent's argument is off by half a step, so 1 for each of |x - m| + 3 ln 2, on the average
         // over the terms u + 3 ln 2; exponentials by 4; sums of eight and of four numbers by 5; the logarithm by 1.
-        r.error = (1.125f * fmaxf(u, 0.f) + 13.f) * 0x1p-24f;
+        r.error = fabsf(m) > kFar ? 0.f : (1.125f * fmaxf(u, 0.f) + 13.f) * 0x1p-24f;
       }
     }
-    if (lane == 0) base[b] = r;
+    if (lane == 0) {
+      base[b] = r;
+      atomicMax(&worst_error, ordered(r.error));
+      if (r.kind == kLogits && fabsf(r.most) > kFar) atomicOr(again + (b >> 5), 1u << (b & 31));
+    }
   }
   __syncthreads();
+  const float worst = unordered(worst_error);
   auto sum_again = [&](int b) {
     const double norm = exact_normalizer<DTYPE>(a, row0 + b, base[b].most, powers, parts);
     if (tid == 0) {
@@ -683,11 +687,14 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     }
     __syncthreads();
   };
-  float worst = 0.f;
-  for (int b = 0; b < a.beams; ++b) {
-    if (base[b].kind == kLogits && fabsf(base[b].most) > kFar) sum_again(b);
-    worst = fmaxf(worst, base[b].error);
-  }
+  auto sum_marked = [&]() {
+    for (int w = 0; w < SEMKV_BEAM_MAX / 32; ++w)
+      for (uint32_t bits = again[w]; bits; bits &= bits - 1) {
+        const int b = 32 * w + __ffs(bits) - 1;
+        if (base[b].kind == kLogits) sum_again(b);
+      }
+  };
+  sum_marked();  // (logits past what the scan's sums are made for)
   // The score of the largest logit that a word tells of, rounded; -infinity: none.  (A warp's are of one piece.)
   auto beam_of = [&](int i) { return p.per_split ? (int)__umulhi((uint32_t)i / kScanThreads, p.per_split) : i / kScanThreads; };
   auto score_at = [&](int i, uint32_t word) {
@@ -698,16 +705,23 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     return r.value + (unordered(word) - r.most);
   };
   // A score that k of them reach, and how far below it a candidate may stay and be among the k best all the same.
-  float top = tid < a.beams && base[tid].kind == kDone ? base[tid].value : kNone;
+  float top = kNone, second = kNone;  // of this thread's
+  int top_at = 0;
   for (int i0 = 0; i0 < marked; i0 += kBatch * kMergeThreads) {
     if (i0 > 0) load_words(i0);
 #pragma unroll
-    for (int j = 0; j < kBatch; ++j) top = fmaxf(top, score_at(i0 + j * kMergeThreads + tid, word[j]));
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = i0 + j * kMergeThreads + tid;
+      const float s = score_at(i, word[j]);
+      second = fmaxf(second, fminf(s, top));
+      if (s > top) top = s, top_at = i;
+    }
   }
+  const float own = tid < a.beams && base[tid].kind == kDone ? base[tid].value : kNone;  // a beam that is done
   float reach = kNone;
   {
-    const bool in = top > kNone;
-    const uint32_t word = ordered(top);
+    const bool in = fmaxf(top, own) > kNone;
+    const uint32_t word = ordered(fmaxf(top, own));
     const int n = __syncthreads_count(in);
     if (n >= a.k) {
       const Extent e = extent_of<kMergeThreads>(in ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
@@ -715,29 +729,35 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
                                           : threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(in && word >= up.a); }).a);
     }
   }
-  // (2^-20 of the numbers that were added is far more than their roundings)
-  for (int b = tid; b < a.beams; b += kMergeThreads)
-    base[b].cut = reach > kNone ? reach - 2.1f * worst - 0x1p-20f * (fabsf(base[b].value) + fabsf(reach)) : kNone;
+  // (2^-20 of the numbers that were added is far more than their roundings; a beam's scores are its value at most)
+  if (tid < a.beams) {
+    const float value = base[tid].value;
+    const float cut = reach > kNone ? reach - 2.1f * worst - 0x1p-20f * (fabsf(value) + fabsf(reach)) : kNone;
+    base[tid].cut = cut;
+    if (base[tid].kind != kNobody && value >= cut) atomicMin(&lowest_cut, ordered(cut));
+    if (own > kNone && own >= cut) best.put(score_of(base[tid], tid, 0.f, a.end_token));
+  }
   __syncthreads();
   // the marked tiles of those that come near it
-  if (tid < a.beams && base[tid].kind == kDone && base[tid].value >= base[tid].cut) best.put(score_of(base[tid], tid, 0.f, a.end_token));
-  for (int i0 = 0; i0 < marked; i0 += kBatch * kMergeThreads) {
-    if (marked > kBatch * kMergeThreads) load_words(i0);
-    uint32_t near = 0;
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      const int i = i0 + j * kMergeThreads + tid;
-      const float s = score_at(i, word[j]);
-      near |= (uint32_t)(s > kNone && s >= base[i < marked ? beam_of(i) : 0].cut) << j;
+  auto look_at = [&](int i) {
+    const int b = beam_of(i), split = i / kScanThreads - b * p.splits;
+    const uint2 mark = marks[i];
+    int w = atomicAdd(&place_count, __popc(mark.x));
+    const int first = p.begin_unit(base[b].offset, split) * kUnit + (int)mark.y * V::kCount;
+    for (uint32_t bits = mark.x; bits && w < kPlaces; bits &= bits - 1)
+      places[w++] = make_int2(i / kScanThreads, first + (__ffs(bits) - 1) * kTile);
+  };
+  const float lowest = unordered(lowest_cut);
+  if (second > kNone && second >= lowest) {
+    for (int i = tid; i < marked; i += kMergeThreads) {
+      const uint32_t x = words[i];
+      const int b = beam_of(i);
+      if (x && base[b].kind == kLogits && i / kScanThreads - b * p.splits < base[b].pieces &&
+          base[b].value + (unordered(x) - base[b].most) >= base[b].cut)
+        look_at(i);
     }
-    for (; near; near &= near - 1) {
-      const int i = i0 + (__ffs(near) - 1) * kMergeThreads + tid, b = beam_of(i), split = i / kScanThreads - b * p.splits;
-      const uint2 mark = marks[i];
-      uint32_t bits = mark.x;
-      int w = atomicAdd(&place_count, __popc(bits));
-      const int first = p.begin_unit(row0 + b, split) * kUnit + (int)mark.y * V::kCount;
-      for (; bits && w < kPlaces; bits &= bits - 1) places[w++] = make_int2(i / kScanThreads, first + (__ffs(bits) - 1) * kTile);
-    }
+  } else if (top > kNone && top >= lowest && top >= base[beam_of(top_at)].cut) {
+    look_at(top_at);
   }
   __syncthreads();
   const bool many_places = place_count > kPlaces;
@@ -749,7 +769,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
       const char* from = row_at<DTYPE>(a, row);
       const float floor = p.sums[((int64_t)row0 * p.splits + at.x) * kScanWarps].w;
       V v[kVecs];
-      load_vecs<DTYPE>(v, from, (int)((uintptr_t)from & 15), at.y, min(a.vocab, p.end_unit(row, at.x - b * p.splits) * kUnit), a.vocab);
+      load_vecs<DTYPE>(v, from, (int)((uintptr_t)from & 15), at.y, min(a.vocab, p.end_unit(r.offset, at.x - b * p.splits) * kUnit), a.vocab);
       uint32_t hits = 0;
 #pragma unroll
       for (int i = 0; i < kVecs; ++i)
@@ -787,8 +807,8 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
       }
       const int row = row0 + b;
       const char* from = row_at<DTYPE>(a, row);
-      const int lead = (int)((uintptr_t)from & 15), end = min(a.vocab, p.end_unit(row, split) * kUnit);
-      const int first0 = p.begin_unit(row, split) * kUnit + (int)mark.y * V::kCount;
+      const int lead = (int)((uintptr_t)from & 15), end = min(a.vocab, p.end_unit(base[b].offset, split) * kUnit);
+      const int first0 = p.begin_unit(base[b].offset, split) * kUnit + (int)mark.y * V::kCount;
       for (; __syncthreads_or(bits != 0); bits &= bits - 1)
         for (int j = 0; j < kVecs; ++j) {
           const int first = bits ? first0 + (__ffs(bits) - 1) * kTile + j * kUnit : end;
@@ -816,22 +836,21 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     __syncthreads();
     if (count > kRanked) best.cut(count);
   }
+  // A warp for each key: its place among them.
+  auto place_of_key = [&](int i, int all) {
+    const GroupKey x = best.list[i];
+    int before = 0;
+    for (int j = lane; j < all; j += 32) before += best.list[j] >= x;
+    return (int)__reduce_add_sync(~0u, before) - 1;
+  };
   int held;
   for (;;) {
-    // the place of each among them, counted by several threads for each
-    const int all = count, times = max(kMergeThreads / max(all, 1), 1);
-    for (int i = tid; i < all; i += kMergeThreads) order[i] = -1;
-    __syncthreads();
-    for (int i = tid; i < all * times; i += kMergeThreads) {
-      const int which = i % all;
-      const GroupKey x = best.list[which];
-      int before = 0;
-      for (int j = i / all; j < all; j += times) before += best.list[j] >= x;
-      atomicAdd(order + which, before);
+    const int all = count;
+    for (int i = warp; i < all; i += kMergeThreads / 32) {
+      const int place = place_of_key(i, all);
+      if (place < a.k && lane == 0) out[place] = best.list[i];
+      if (lane == 0) places[i].x = place;  // (the places are done with; there are as many at least)
     }
-    __syncthreads();
-    for (int i = tid; i < all; i += kMergeThreads)
-      if (order[i] < a.k) out[order[i]] = best.list[i];
     held = min(all, a.k);
     __syncthreads();
     if (exact) break;
@@ -848,10 +867,9 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     for (int i = tid; i + 1 < held; i += kMergeThreads) open |= close(out[i], out[i + 1]);
     if (held == a.k)
       for (int i = tid; i < all; i += kMergeThreads)
-        if (order[i] >= a.k) open |= close(best.list[i], out[a.k - 1]);
+        if (places[i].x >= a.k) open |= close(best.list[i], out[a.k - 1]);
     if (!__syncthreads_or(open)) break;
-    for (int b = 0; b < a.beams; ++b)
-      if (again[b >> 5] >> (b & 31) & 1 && base[b].kind == kLogits) sum_again(b);
+    sum_marked();
     for (int i = tid; i < all; i += kMergeThreads) {
       const GroupKey x = best.list[i];
       best.list[i] = score_of(base[x.beam()], x.beam(), x.logit(), x.token());
@@ -883,6 +901,7 @@ Pieces cut_rows(int rows, int vocab, int dtype) {
   if (share > kVecs * kMarkTiles) share = kVecs * kMarkTiles;
   p.share = (int)share;
   p.splits = p.units % p.share == 0 ? p.units / p.share : (p.units + p.share - 2) / p.share + 1;
+  p.ln_vocab = logf((float)vocab);
   p.per_split = p.splits > 1 ? 0xFFFFFFFFu / (uint32_t)p.splits + 1 : 0u;
   return p;
 }
