@@ -185,6 +185,15 @@ __device__ __forceinline__ void two_sum(float a, float b, float& s, float& e) {
   e = __fadd_rn(__fsub_rn(a, __fsub_rn(s, z)), __fsub_rn(b, z));
 }
 
+// sum + low with the lane's whose number differs in bit d
+__device__ __forceinline__ void add_pair(float& sum, float& low, int d) {
+  float err;
+  const float other = __shfl_xor_sync(~0u, sum, d);
+  low += __shfl_xor_sync(~0u, low, d);
+  two_sum(sum, other, sum, err);
+  low += err;
+}
+
 // Eight 16-bit or four 32-bit logits as they lie in memory.
 template <int DTYPE>
 struct alignas(16) Vec {
@@ -199,6 +208,13 @@ struct alignas(16) Vec {
     if (DTYPE == SEMKV_F32) return __uint_as_float(w[i]);
     if (DTYPE == SEMKV_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     return __half2float(__ushort_as_half((uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2])));
+  }
+  __device__ __forceinline__ static float pick(const uint32_t (&x)[4], int i) {
+    const int of = DTYPE == SEMKV_F32 ? i : i / 2;
+    const uint32_t two = of & 2 ? (of & 1 ? x[3] : x[2]) : (of & 1 ? x[1] : x[0]);
+    if (DTYPE == SEMKV_F32) return __uint_as_float(two);
+    const uint32_t half = i & 1 ? two >> 16 : two & 0xFFFFu;
+    return DTYPE == SEMKV_BF16 ? __uint_as_float(half << 16) : __half2float(__ushort_as_half((uint16_t)half));
   }
   __device__ __forceinline__ void set(int i, uint32_t bits) {
     if (DTYPE == SEMKV_F32) w[i] = bits;
@@ -230,12 +246,6 @@ struct alignas(16) Vec {
   }
 };
 
-template <int DTYPE>
-__device__ __forceinline__ float logit_at(const char* row, int token) {
-  if (DTYPE == SEMKV_F32) return reinterpret_cast<const float*>(row)[token];
-  const uint16_t h = reinterpret_cast<const uint16_t*>(row)[token];
-  return DTYPE == SEMKV_BF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
-}
 // Logits first .. first + count of a row, the others -infinity.  The vectors lie `lead` bytes behind a multiple of
 // 16; those inside the row are brought by whole aligned loads all the same, two for one of them (its neighbour's
 // other half is in the cache).  So a thread's logits, and the order of every sum, do not depend on where a row lies.
@@ -279,7 +289,7 @@ constexpr int kScanWarps = kScanThreads / 32, kVecs = 4;  // kVecs: vectors of a
 struct Pieces {
   int units, share, splits;
   uint32_t per_split;  // 2^32 / splits, rounded up: a product's upper half is the quotient (0: splits is 1)
-  // [rows][splits][warps] the largest logit, the sum of 2^(x log2 e - scale_of(it)) as two numbers, and the floor
+  // [rows][splits] the largest logit, the sum of 2^(x log2 e - scale_of(it)) as two numbers, and the floor
   float4* sums;
   // [rows][splits][threads] ordered(the largest logit) of the threads that reach the floor, in no order, then zeros
   uint32_t* words;
@@ -332,6 +342,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
   using V = Vec<DTYPE>;
   constexpr int kUnit = kScanThreads * V::kCount, kTile = kVecs * kUnit;
   __shared__ uint32_t warp_words[2][kScanWarps];
+  __shared__ float4 warp_sums[2][kScanWarps];
   __shared__ int reaching[2], others[2];  // (of this piece, and the one behind it)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
@@ -419,6 +430,16 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
       raise();  // (behind the second tile, the fourth, the eighth ...: a tile further on has less and less above it)
     }
     const int64_t piece = (int64_t)row * p.splits + split;
+    // the warp's sum, a pair of numbers
+    float most = m;
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+    const float by = m > kNone ? pow2(c - scale_of(most)) : 0.f;
+    sum *= by;
+    low *= by;
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) add_pair(sum, low, d);
+    if (lane == 0) warp_sums[turn & 1][warp] = make_float4(most, sum, low, 0.f);
     raise();
     {
       const bool in = m >= floor && m > kNone;
@@ -434,24 +455,21 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
                                                     : kScanThreads - 1 - at_out - __popc(~ins & ((1u << lane) - 1)));
       p.words[to] = in ? ordered(m) : 0u;
       if (in) p.marks[to] = make_uint2(seen, tid);
-      ++turn;
     }
-    // the warp's sum, a pair of numbers
-    float most = m;
+    if (warp == 0) {
+      // the warps' sums together
+      float all = lane < kScanWarps ? warp_sums[turn & 1][lane].x : kNone;
+      const float4 x = lane < kScanWarps ? warp_sums[turn & 1][lane] : make_float4(kNone, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
-    const float by = m > kNone ? pow2(c - scale_of(most)) : 0.f;
-    sum *= by;
-    low *= by;
+      for (int d = kScanWarps / 2; d > 0; d /= 2) all = fmaxf(all, __shfl_xor_sync(~0u, all, d));
+      const float by = x.x > kNone ? pow2(scale_of(x.x) - scale_of(all)) : 0.f;
+      sum = x.y * by;
+      low = x.z * by;
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) {
-      float err;
-      const float other = __shfl_xor_sync(~0u, sum, d);
-      low += __shfl_xor_sync(~0u, low, d);
-      two_sum(sum, other, sum, err);
-      low += err;
+      for (int d = kScanWarps / 2; d > 0; d /= 2) add_pair(sum, low, d);
+      if (lane == 0) p.sums[piece] = make_float4(all, sum, low, floor);
     }
-    if (lane == 0) p.sums[piece * kScanWarps + warp] = make_float4(most, sum, low, floor);
+    ++turn;
   }
 }
 
@@ -566,13 +584,13 @@ __device__ __forceinline__ GroupKey score_of(const Base& r, int beam, float x, i
   return GroupKey::of(score, __fadd_rn(__fsub_rn(s, score), e), beam, x, token);
 }
 
-constexpr int kPlaces = 1024;
+constexpr int kPlaces = 1024, kTable = 1024;
 // The list holds what offer() asks of it: k + kSlack threads' keys, a vector each, beside its own k + kSlack.
 __host__ __device__ constexpr int merge_cap(int k, int dtype) {
   return (k + kSlack) * (dtype == SEMKV_F32 ? 5 : 9) > 2 * kRanked ? (k + kSlack) * (dtype == SEMKV_F32 ? 5 : 9) : 2 * kRanked;
 }
 __host__ __device__ constexpr int merge_bytes(int k, int dtype) {
-  return (merge_cap(k, dtype) + k + kSlack) * (int)sizeof(GroupKey) + kPlaces * (int)sizeof(int2);
+  return (merge_cap(k, dtype) + k + kSlack) * (int)sizeof(GroupKey) + (kPlaces + kTable) * (int)sizeof(int2);
 }
 
 template <int DTYPE>
@@ -598,30 +616,34 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   best.k = a.k;
   best.cap = merge_cap(a.k, DTYPE);
   int2* places = reinterpret_cast<int2*>(best.spare + a.k + kSlack);  // beam and split, the first token of a thread's vectors
+  float2* table = reinterpret_cast<float2*>(places + kPlaces);  // of pieces: what makes their logits scores
   if (tid < SEMKV_BEAM_MAX / 32) again[tid] = 0;
   if (tid == 0) count = place_count = 0, worst_error = 0u, lowest_cut = 0xFFFFFFFFu;
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  // The scan's threads, one behind the other: of each batch this thread has every kMergeThreads-th.
-  const int marked = a.beams * p.splits * kScanThreads;
+  // The scan's threads, 32 at a time: a warp has every so-manieth set of them, of each piece the first few sets (2^log_sets),
+  // which are more than a piece of random logits needs, and where the last of these is full the others.
+  constexpr int kWarps = kMergeThreads / 32;
+  const int pieces = a.beams * p.splits, log_sets = a.k <= 16 ? 1 : a.k <= 48 ? 2 : 3, last_set = (1 << log_sets) - 1;
   const uint32_t* words = p.words + (int64_t)row0 * p.splits * kScanThreads;
   const uint2* marks = p.marks + (int64_t)row0 * p.splits * kScanThreads;
   uint32_t word[kBatch];  // (the first are on their way while the sums are brought together)
-  auto load_words = [&](int i0) {
+  auto word_of = [&](int set) { return (set >> log_sets) * kScanThreads + (set & last_set) * 32 + lane; };
+  auto load_words = [&](int set0, int sets) {
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      const int i = i0 + j * kMergeThreads + tid;
-      word[j] = i < marked ? words[i] : 0u;
+      const int set = set0 + j * kWarps + warp;
+      word[j] = set < sets ? words[word_of(set)] : 0u;
     }
   };
-  load_words(0);
+  load_words(0, min(pieces, kTable) << log_sets);
   // a warp for each row: its warps' sums together
   for (int b = warp; b < a.beams; b += kMergeThreads / 32) {
     const int row = row0 + b;
-    const float4* s = p.sums + (int64_t)row * p.splits * kScanWarps;
-    const int offset = p.offset_of(row), pieces = p.pieces_of(offset), sums = pieces * kScanWarps;
-    const float4 mine = lane < sums ? s[lane] : make_float4(kNone, 0.f, 0.f, 0.f);
+    const float4* s = p.sums + (int64_t)row * p.splits;
+    const int offset = p.offset_of(row), pieces = p.pieces_of(offset);
+    const float4 mine = lane < pieces ? s[lane] : make_float4(kNone, 0.f, 0.f, 0.f);
     const float score = a.scores[row];
     const bool is_done = a.done && a.done[row];
     Base r{score, 0.f, 0.f, 0.f, kNone, kNobody, pieces, offset};
@@ -631,25 +653,20 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
       r.kind = kDone;
     } else if (score > kNone) {
       float m = mine.x;
-      for (int i = lane + 32; i < sums; i += 32) m = fmaxf(m, s[i].x);
+      for (int i = lane + 32; i < pieces; i += 32) m = fmaxf(m, s[i].x);
 #pragma unroll
       for (int d = 16; d > 0; d /= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
       if (m > kNone) {
         const float c = scale_of(m);
         float sum = 0.f, low = 0.f, err;
-        for (int i = lane; i < sums; i += 32) {
+        for (int i = lane; i < pieces; i += 32) {
           const float4 x = i == lane ? mine : s[i];
           const float by = x.x > kNone ? pow2(scale_of(x.x) - c) : 0.f;
           two_sum(sum, x.y * by, sum, err);
           low += x.z * by + err;
         }
 #pragma unroll
-        for (int d = 16; d > 0; d /= 2) {
-          const float other = __shfl_xor_sync(~0u, sum, d);
-          low += __shfl_xor_sync(~0u, low, d);
-          two_sum(sum, other, sum, err);
-          low += err;
-        }
+        for (int d = 16; d > 0; d /= 2) add_pair(sum, low, d);
         r.most = m;
         r.kind = kLogits;
         // ln sum exp(x - m) = (c ln 2 - m) + ln(sum), the logarithm by the sum's exponent and a number from 3/4 to 3/2.
@@ -695,27 +712,50 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
       }
   };
   sum_marked();  // (logits past what the scan's sums are made for)
-  // The score of the largest logit that a word tells of, rounded; -infinity: none.  (A warp's are of one piece.)
+  // Scores of the largest logits that the words tell of, rounded, -infinity for none: what(i, score) for all of this
+  // thread's.  more(word): there are more in the piece (the same for a whole warp if the scores are to be).
   auto beam_of = [&](int i) { return p.per_split ? (int)__umulhi((uint32_t)i / kScanThreads, p.per_split) : i / kScanThreads; };
-  auto score_at = [&](int i, uint32_t word) {
-    if (!__any_sync(~0u, word) || i >= marked) return kNone;
-    const int b = beam_of(i);
-    const Base& r = base[b];
-    if (r.kind != kLogits || i / kScanThreads - b * p.splits >= r.pieces || !word) return kNone;
-    return r.value + (unordered(word) - r.most);
+  auto fill_table = [&](int q0) {
+    __syncthreads();
+    for (int q = q0 + tid; q < min(pieces, q0 + kTable); q += kMergeThreads) {
+      const int b = beam_of(q * kScanThreads);
+      const bool is = base[b].kind == kLogits && q - b * p.splits < base[b].pieces;
+      table[q - q0] = is ? make_float2(base[b].value, base[b].most) : make_float2(kNone, 0.f);
+    }
+    __syncthreads();
+  };
+  auto over_table = [&](int q0, auto what, auto more) {
+    const int first = q0 << log_sets, sets = min(pieces, q0 + kTable) << log_sets;
+    for (int set0 = first; set0 < sets; set0 += kBatch * kWarps) {
+      if (set0 > 0 || sets > kBatch * kWarps) load_words(set0, sets);
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int set = set0 + j * kWarps + warp;
+        if (set >= sets) break;
+        const float2 t = table[(set >> log_sets) - q0];
+        if (t.x == kNone) continue;  // (nothing was written)
+        int i = word_of(set);
+        what(i, word[j] ? t.x + (unordered(word[j]) - t.y) : kNone);
+        if ((set & last_set) == last_set && more(word[j]))
+          for (int s = last_set + 1; s < kScanThreads / 32; ++s) {
+            const uint32_t x = words[i += 32];
+            what(i, x ? t.x + (unordered(x) - t.y) : kNone);
+          }
+      }
+    }
   };
   // A score that k of them reach, and how far below it a candidate may stay and be among the k best all the same.
   float top = kNone, second = kNone;  // of this thread's
   int top_at = 0;
-  for (int i0 = 0; i0 < marked; i0 += kBatch * kMergeThreads) {
-    if (i0 > 0) load_words(i0);
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      const int i = i0 + j * kMergeThreads + tid;
-      const float s = score_at(i, word[j]);
-      second = fmaxf(second, fminf(s, top));
-      if (s > top) top = s, top_at = i;
-    }
+  for (int q0 = 0; q0 < pieces; q0 += kTable) {
+    fill_table(q0);
+    over_table(
+        q0,
+        [&](int i, float s) {
+          second = fmaxf(second, fminf(s, top));
+          if (s > top) top = s, top_at = i;
+        },
+        [&](uint32_t x) { return __any_sync(~0u, lane == 31 && x != 0); });
   }
   const float own = tid < a.beams && base[tid].kind == kDone ? base[tid].value : kNone;  // a beam that is done
   float reach = kNone;
@@ -748,14 +788,15 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
       places[w++] = make_int2(i / kScanThreads, first + (__ffs(bits) - 1) * kTile);
   };
   const float lowest = unordered(lowest_cut);
-  if (second > kNone && second >= lowest) {
-    for (int i = tid; i < marked; i += kMergeThreads) {
-      const uint32_t x = words[i];
-      const int b = beam_of(i);
-      if (x && base[b].kind == kLogits && i / kScanThreads - b * p.splits < base[b].pieces &&
-          base[b].value + (unordered(x) - base[b].most) >= base[b].cut)
-        look_at(i);
+  if (pieces > kTable) {
+    for (int q0 = 0; q0 < pieces; q0 += kTable) {
+      fill_table(q0);
+      over_table(
+          q0, [&](int i, float s) { if (s > kNone && s >= base[beam_of(i)].cut) look_at(i); }, [&](uint32_t) { return true; });
     }
+  } else if (second > kNone && second >= lowest) {
+    over_table(
+        0, [&](int i, float s) { if (s > kNone && s >= base[beam_of(i)].cut) look_at(i); }, [&](uint32_t) { return true; });
   } else if (top > kNone && top >= lowest && top >= base[beam_of(top_at)].cut) {
     look_at(top_at);
   }
@@ -767,7 +808,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
       const int b = beam_of(at.x * kScanThreads), row = row0 + b;
       const Base& r = base[b];
       const char* from = row_at<DTYPE>(a, row);
-      const float floor = p.sums[((int64_t)row0 * p.splits + at.x) * kScanWarps].w;
+      const float floor = p.sums[(int64_t)row0 * p.splits + at.x].w;
       V v[kVecs];
       load_vecs<DTYPE>(v, from, (int)((uintptr_t)from & 15), at.y, min(a.vocab, p.end_unit(r.offset, at.x - b * p.splits) * kUnit), a.vocab);
       uint32_t hits = 0;
@@ -779,9 +820,12 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
           hits |= (uint32_t)(x > kNone && x < INFINITY && x >= floor && r.value + (x - r.most) >= r.cut) << (i * V::kCount + j);
         }
       int w = hits ? atomicAdd(&count, __popc(hits)) : 0;
-      for (; hits && w < best.cap; hits &= hits - 1) {
-        const int n = __ffs(hits) - 1, token = at.y + n / V::kCount * kUnit + n % V::kCount;
-        best.list[w++] = score_of(r, b, logit_at<DTYPE>(from, token), token);
+      for (; hits && w < best.cap; hits &= hits - 1) {  // (one or two)
+        const int n = __ffs(hits) - 1, i = n / V::kCount;
+        uint32_t x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = i & 2 ? (i & 1 ? v[3].w[e] : v[2].w[e]) : (i & 1 ? v[1].w[e] : v[0].w[e]);
+        best.list[w++] = score_of(r, b, V::pick(x, n % V::kCount), at.y + i * kUnit + n % V::kCount);
       }
     }
   }
@@ -795,11 +839,12 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     if (tid == 0) count = 0;
     best.floor = GroupKey::none();
     __syncthreads();
+    const int marked = pieces * kScanThreads;
     for (int i0 = 0; i0 < marked; i0 += kMergeThreads) {
       const int i = i0 + tid, b = i < marked ? beam_of(i) : 0, split = i < marked ? i / kScanThreads - b * p.splits : 0;
-      const float s = score_at(i, i < marked ? words[i] : 0u);
-      uint2 mark = make_uint2(0u, 0u);
-      if (s > kNone && s >= base[b].cut) mark = marks[i];
+      const uint32_t x = i < marked && base[b].kind == kLogits && split < base[b].pieces ? words[i] : 0u;
+      const float s = x ? base[b].value + (unordered(x) - base[b].most) : kNone;
+      const uint2 mark = s > kNone && s >= base[b].cut ? marks[i] : make_uint2(0u, 0u);
       uint32_t bits = mark.x;
       if (i0 == 0) {
         const GroupKey end_key = tid < a.beams && base[tid].kind == kDone ? score_of(base[tid], tid, 0.f, a.end_token) : GroupKey::none();
@@ -919,14 +964,14 @@ cudaError_t launch(const BeamArgs& a, const Pieces& p, cudaStream_t stream) {
 size_t beam_select_workspace(int groups, int beams, int vocab, int dtype, int k) {
   (void)k;
   const int rows = groups * beams;
-  return (size_t)rows * cut_rows(rows, vocab, dtype).splits * (kScanWarps * sizeof(float4) + kScanThreads * (sizeof(uint2) + sizeof(uint32_t)));
+  return (size_t)rows * cut_rows(rows, vocab, dtype).splits * (sizeof(float4) + kScanThreads * (sizeof(uint2) + sizeof(uint32_t)));
 }
 
 cudaError_t launch_beam_select(const BeamArgs& a, int dtype, void* ws, cudaStream_t stream) {
   const int rows = a.groups * a.beams;
   Pieces p = cut_rows(rows, a.vocab, dtype);
   p.sums = static_cast<float4*>(ws);
-  p.marks = reinterpret_cast<uint2*>(p.sums + (size_t)rows * p.splits * kScanWarps);
+  p.marks = reinterpret_cast<uint2*>(p.sums + (size_t)rows * p.splits);
   p.words = reinterpret_cast<uint32_t*>(p.marks + (size_t)rows * p.splits * kScanThreads);
   if (dtype == SEMKV_F32) return launch<SEMKV_F32>(a, p, stream);
   return dtype == SEMKV_BF16 ? launch<SEMKV_BF16>(a, p, stream) : launch<SEMKV_F16>(a, p, stream);
