@@ -295,10 +295,11 @@ semkv_status semkv_decode_attention_noalloc(const semkv_quant_desc* desc,
  * token: device i32 [groups][k]; score: device f32 [groups][k].  beams, k: 1 .. 128; vocab: 1 .. 2^24;
  * groups * beams: up to 2^20.  end_token: 0 .. vocab-1 where done is given, else not used.  dev_error:
  * device i32 or NULL.
- * Accuracy: sums of exponentials are binary32 with a known bound (some 2^-18 of the sum); where two
+ * Accuracy: sums of exponentials are binary32 with a known bound (2^-19 of the sum at most); where two
  * candidates of different beams whose order matters lie within it, their rows are summed again to 2^-37,
  * so that what comes out is the order by exact scores unless these agree to 2^-36.  Equal rows with equal
- * scores agree in every bit.  score is rounded once to binary32 from a sum within the first bound.
+ * scores agree in every bit.  score is rounded once to binary32 from a sum within the first bound.  The results
+ * do not depend on where the rows lie or on the GPU's number of SMs, and are the same every time.
  * ws: device workspace of semkv_beam_select_workspace_bytes bytes, 16-byte aligned; calls that may
  * overlap on the GPU need one each.  Nothing in it has to be kept or cleared.
  * Errors: SEMKV_EINVAL, SEMKV_EALIGN, SEMKV_EUNSUPPORTED (dtype, more beams, k, vocab or rows than above),

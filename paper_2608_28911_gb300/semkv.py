@@ -375,9 +375,11 @@ def semkv_kv4_write_rotated(cache: "KV4Cache", batch: "KV4Batch", layer: int, ro
         q_heads = q.shape[1]
         qs, ostr = _rows(q, "q", total, q_heads, head_dim), _rows(q_out, "q_out", total, q_heads, head_dim)
         qp, op = q.data_ptr(), q_out.data_ptr()
-        _here(q, q_out)
-    _list(positions, total, "positions")
-    _here(cache.pages, batch.start, rotation.cos_sin, k, v)
+        _here(cache.pages, batch.start, rotation.cos_sin, k, v, q, q_out)
+    else:
+        _here(cache.pages, batch.start, rotation.cos_sin, k, v)
+    if positions is not None:
+        _list(positions, total, "positions")
     _check("semkv_kv4_write_rotated",
            LIB.semkv_kv4_write_rotated(cache.ref, batch.ref, layer, rotation.ref, _ptr(positions), kind,
                                        qp, qs, q_heads, op, ostr, k.data_ptr(), ks, v.data_ptr(), vs,

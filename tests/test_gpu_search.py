@@ -128,10 +128,11 @@ def test_rotated_rows_without_a_place_are_left_out():
 # -------------------------------------------------------------- beam selection ------
 
 def score_bound(vocab, want):
-    """A normalizer's error as the kernel counts it (at most 1.125 ln vocab + 12 units of 2^-24), and half a
-    step of the score's own rounding."""
+    """A normalizer's error as the kernel counts it, in units of 2^-24: exponents' arguments are off by half a step, 1
+    for each of |x - m| + 3 ln 2 and 1.125 with what log2 e lacks, at most ln vocab on the average; the exponentials
+    by 4, sums of eight and of four numbers by 5, the logarithm by 1; and half a step of the score's own rounding."""
     with np.errstate(invalid="ignore"):
-        return (1.125 * np.log(vocab) + 12.5) * 2.0 ** -24 + 2.0 ** -24 * np.abs(want)
+        return (1.125 * np.log(vocab) + 13.5) * 2.0 ** -24 + 2.0 ** -24 * np.abs(want)
 
 
 def check_select(logits, scores, k, done=None, end=0, error=0, again=True):
