@@ -246,44 +246,45 @@ struct alignas(16) Vec {
   }
 };
 
+// The 16 bytes that begin `lead` bytes into x and y.
+template <int DTYPE>
+__device__ __forceinline__ Vec<DTYPE> join_vec(const uint4& x, const uint4& y, int lead) {
+  const uint32_t t[7] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z};
+  uint32_t a[5], b[5];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) a[i] = lead & 8 ? t[i + 2] : t[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = lead & 4 ? a[i + 1] : a[i];
+  b[4] = lead & 4 ? (lead & 8 ? y.w : y.y) : a[4];
+  Vec<DTYPE> v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v.w[i] = DTYPE == SEMKV_F32 ? b[i] : __funnelshift_r(b[i], b[i + 1], 8 * (lead & 2));
+  return v;
+}
 // Logits first .. first + count of a row, the others -infinity.  The vectors lie `lead` bytes behind a multiple of
 // 16; those inside the row are brought by whole aligned loads all the same, two for one of them (its neighbour's
 // other half is in the cache).  So a thread's logits, and the order of every sum, do not depend on where a row lies.
 template <int DTYPE>
 __device__ __forceinline__ Vec<DTYPE> load_vec(const char* row, int first, int vocab, int lead) {
   using V = Vec<DTYPE>;
-  V v;
   const char* at = row + (int64_t)first * V::kSize;
   const int room = V::kCount + (lead ? V::kCount : 0);  // logits that the loads below may touch
-  if (lead == 0 && first + V::kCount <= vocab) {
-    const uint4 x = __ldcs(reinterpret_cast<const uint4*>(at));
-    v.w[0] = x.x, v.w[1] = x.y, v.w[2] = x.z, v.w[3] = x.w;
-  } else if (lead != 0 && first >= V::kCount && first + room <= vocab) {
-    const uint4 x = __ldg(reinterpret_cast<const uint4*>(at - lead)), y = __ldg(reinterpret_cast<const uint4*>(at - lead) + 1);
-    uint32_t t[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-    if (lead & 8) {
-#pragma unroll
-      for (int i = 0; i < 6; ++i) t[i] = t[i + 2];
-    }
-    if (lead & 4) {
-#pragma unroll
-      for (int i = 0; i < 5; ++i) t[i] = t[i + 1];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v.w[i] = lead & 2 ? __funnelshift_r(t[i], t[i + 1], 16) : t[i];
-  } else {
-    v.fill_none();
-#pragma unroll
-    for (int i = 0; i < V::kCount; ++i)
-      if (first + i < vocab)
-        v.set(i, DTYPE == SEMKV_F32 ? reinterpret_cast<const uint32_t*>(at)[i] : (uint32_t)reinterpret_cast<const uint16_t*>(at)[i]);
+  V v;
+  if (first + room <= vocab && (lead == 0 || first >= V::kCount)) {
+    const uint4* from = reinterpret_cast<const uint4*>(at - lead);
+    return join_vec<DTYPE>(__ldg(from), lead ? __ldg(from + 1) : make_uint4(0, 0, 0, 0), lead);
   }
+  v.fill_none();
+#pragma unroll
+  for (int i = 0; i < V::kCount; ++i)
+    if (first + i < vocab)
+      v.set(i, DTYPE == SEMKV_F32 ? reinterpret_cast<const uint32_t*>(at)[i] : (uint32_t)reinterpret_cast<const uint16_t*>(at)[i]);
   return v;
 }
 
 // ------------------------------------------------------------------ scan ------
 
-constexpr int kScanWarps = kScanThreads / 32, kVecs = 4;  // kVecs: vectors of a thread in one tile
+constexpr int kScanWarps = kScanThreads / 32, kVecs = 4, kMarkTiles = 32;  // vectors of a thread in a tile, tiles of a piece
 // How a call's rows are cut.  Each is `units` units of a vector for each of a CTA's threads; a CTA has `share`
 // units, of one row behind the other, up to 32 tiles, so a row lies in up to `splits` pieces.
 struct Pieces {
@@ -328,6 +329,15 @@ __device__ __forceinline__ void load_vecs(Vec<DTYPE> (&v)[kVecs], const char* ro
       const uint4 x = __ldcs(from + i * kScanThreads);
       v[i].w[0] = x.x, v[i].w[1] = x.y, v[i].w[2] = x.z, v[i].w[3] = x.w;
     }
+    return;
+  }
+  if (lead != 0 && first >= V::kCount && first + (kVecs - 1) * kUnit + 2 * V::kCount <= end) {
+    const uint4* from = reinterpret_cast<const uint4*>(row + (int64_t)first * V::kSize - lead);
+    uint4 x[kVecs], y[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) x[i] = __ldg(from + i * kScanThreads), y[i] = __ldg(from + i * kScanThreads + 1);
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) v[i] = join_vec<DTYPE>(x[i], y[i], lead);
     return;
   }
 #pragma unroll
@@ -584,24 +594,27 @@ __device__ __forceinline__ GroupKey score_of(const Base& r, int beam, float x, i
   return GroupKey::of(score, __fadd_rn(__fsub_rn(s, score), e), beam, x, token);
 }
 
-constexpr int kPlaces = 1024, kTable = 1024;
+constexpr int kPlaces = 2048, kTable = 1024, kFew = 32, kBatch = 4;
+__host__ __device__ constexpr int log_sets_of(int k) { return k <= 16 ? 1 : k <= 48 ? 2 : 3; }
 // The list holds what offer() asks of it: k + kSlack threads' keys, a vector each, beside its own k + kSlack.
 __host__ __device__ constexpr int merge_cap(int k, int dtype) {
   return (k + kSlack) * (dtype == SEMKV_F32 ? 5 : 9) > 2 * kRanked ? (k + kSlack) * (dtype == SEMKV_F32 ? 5 : 9) : 2 * kRanked;
 }
 __host__ __device__ constexpr int merge_bytes(int k, int dtype) {
-  return (merge_cap(k, dtype) + k + kSlack) * (int)sizeof(GroupKey) + (kPlaces + kTable) * (int)sizeof(int2);
+  return (merge_cap(k, dtype) + k + kSlack) * (int)sizeof(GroupKey) + kPlaces * (int)sizeof(int2) + kTable * (int)sizeof(float3);
 }
 
-template <int DTYPE>
+// MANY: a group has many pieces, more than there are places for in two steps of its warps, so that it pays to tell
+// first which of them matter.
+template <int DTYPE, bool MANY>
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, Pieces p) {
   using V = Vec<DTYPE>;
-  constexpr int kUnit = kScanThreads * V::kCount, kTile = kVecs * kUnit, kBatch = 8;
+  constexpr int kUnit = kScanThreads * V::kCount, kTile = kVecs * kUnit;
   extern __shared__ __align__(16) unsigned char shared[];
-  __shared__ int count, place_count;
+  __shared__ int count, place_count, live;
   __shared__ double parts[kMergeThreads / 32];
   __shared__ Extent extents[kMergeThreads / 32];
-  __shared__ uint32_t worst_error, lowest_cut;  // (as ordered numbers)
+  __shared__ uint32_t worst_error, lowest_cut, best_floor;  // (as ordered numbers)
   __shared__ Base base[SEMKV_BEAM_MAX];
   __shared__ uint32_t again[SEMKV_BEAM_MAX / 32];  // rows to be summed once more
   __shared__ float2 powers[33];
@@ -616,28 +629,32 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   best.k = a.k;
   best.cap = merge_cap(a.k, DTYPE);
   int2* places = reinterpret_cast<int2*>(best.spare + a.k + kSlack);  // beam and split, the first token of a thread's vectors
-  float2* table = reinterpret_cast<float2*>(places + kPlaces);  // of pieces: what makes their logits scores
+  float3* table = reinterpret_cast<float3*>(places + kPlaces);  // of pieces: which, and what makes their logits scores
   if (tid < SEMKV_BEAM_MAX / 32) again[tid] = 0;
-  if (tid == 0) count = place_count = 0, worst_error = 0u, lowest_cut = 0xFFFFFFFFu;
+  if (tid == 0) count = place_count = 0, worst_error = best_floor = 0u, lowest_cut = 0xFFFFFFFFu;
   __syncthreads();
   pdl_wait();
   pdl_trigger();
+  const int pieces = a.beams * p.splits;
+  const float4* sums = p.sums + (int64_t)row0 * p.splits;
+  const uint32_t* words = p.words + (int64_t)row0 * p.splits * kScanThreads;
+  const uint2* marks = p.marks + (int64_t)row0 * p.splits * kScanThreads;
   // The scan's threads, 32 at a time: a warp has every so-manieth set of them, of each piece the first few sets (2^log_sets),
   // which are more than a piece of random logits needs, and where the last of these is full the others.
   constexpr int kWarps = kMergeThreads / 32;
-  const int pieces = a.beams * p.splits, log_sets = a.k <= 16 ? 1 : a.k <= 48 ? 2 : 3, last_set = (1 << log_sets) - 1;
-  const uint32_t* words = p.words + (int64_t)row0 * p.splits * kScanThreads;
-  const uint2* marks = p.marks + (int64_t)row0 * p.splits * kScanThreads;
-  uint32_t word[kBatch];  // (the first are on their way while the sums are brought together)
-  auto word_of = [&](int set) { return (set >> log_sets) * kScanThreads + (set & last_set) * 32 + lane; };
-  auto load_words = [&](int set0, int sets) {
+  const int log_sets = log_sets_of(a.k), last_set = (1 << log_sets) - 1;
+  // (the first are on their way while the sums are brought together: the pieces' largest, or the words themselves)
+  float4 first_sums;
+  uint32_t first_words[kBatch];
+  if constexpr (MANY) {
+    first_sums = tid < pieces ? sums[tid] : make_float4(kNone, 0.f, 0.f, kNone);
+  } else {
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      const int set = set0 + j * kWarps + warp;
-      word[j] = set < sets ? words[word_of(set)] : 0u;
+      const int set = j * kWarps + warp;
+      first_words[j] = set < pieces << log_sets ? words[(set >> log_sets) * kScanThreads + (set & last_set) * 32 + lane] : 0u;
     }
-  };
-  load_words(0, min(pieces, kTable) << log_sets);
+  }
   // a warp for each row: its warps' sums together
   for (int b = warp; b < a.beams; b += kMergeThreads / 32) {
     const int row = row0 + b;
@@ -712,103 +729,167 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
       }
   };
   sum_marked();  // (logits past what the scan's sums are made for)
-  // Scores of the largest logits that the words tell of, rounded, -infinity for none: what(i, score) for all of this
-  // thread's.  more(word): there are more in the piece (the same for a whole warp if the scores are to be).
   auto beam_of = [&](int i) { return p.per_split ? (int)__umulhi((uint32_t)i / kScanThreads, p.per_split) : i / kScanThreads; };
-  auto fill_table = [&](int q0) {
-    __syncthreads();
-    for (int q = q0 + tid; q < min(pieces, q0 + kTable); q += kMergeThreads) {
+  // what(q, beam, the piece's largest logit, its floor) for this thread's pieces of those from q0 on that were read
+  auto over_pieces = [&](int q0, int q1, auto what) {
+    for (int q = q0 + tid; q < q1; q += kMergeThreads) {
       const int b = beam_of(q * kScanThreads);
-      const bool is = base[b].kind == kLogits && q - b * p.splits < base[b].pieces;
-      table[q - q0] = is ? make_float2(base[b].value, base[b].most) : make_float2(kNone, 0.f);
+      if (base[b].kind != kLogits || q - b * p.splits >= base[b].pieces) continue;  // (nothing was written)
+      const float4 x = q == tid ? first_sums : sums[q];
+      what(q, b, x.x, x.w);
     }
+  };
+  // A score below a beam's cut is surely none of the k best if k reach `reach`.  (2^-20 of the numbers that were added is
+  // far more than their roundings.)
+  auto cut_of = [&](float value, float reach) {
+    return reach > kNone ? reach - 2.1f * worst - 0x1p-20f * (fabsf(value) + fabsf(reach)) : kNone;
+  };
+  float known = kNone;
+  if constexpr (MANY) {
+    // k reach each piece's floor: the best of these tells which pieces matter
+    over_pieces(0, pieces, [&](int, int b, float, float floor) {
+      if (floor > kNone) atomicMax(&best_floor, ordered(base[b].value + (floor - base[b].most)));
+    });
+    __syncthreads();
+    known = best_floor ? unordered(best_floor) : kNone;
+  }
+  // The pieces from q0 on whose best reaches cut(its beam's value), as many as there is room for.
+  auto fill_table = [&](int q0, auto cut) {
+    __syncthreads();
+    if (tid == 0) live = 0;
+    __syncthreads();
+    over_pieces(q0, min(pieces, q0 + kTable), [&](int q, int b, float most, float) {
+      const Base& r = base[b];
+      if (r.value + (most - r.most) >= cut(r.value)) table[atomicAdd(&live, 1)] = make_float3(__int_as_float(q), r.value, r.most);
+    });
     __syncthreads();
   };
-  auto over_table = [&](int q0, auto what, auto more) {
-    const int first = q0 << log_sets, sets = min(pieces, q0 + kTable) << log_sets;
-    for (int set0 = first; set0 < sets; set0 += kBatch * kWarps) {
-      if (set0 > 0 || sets > kBatch * kWarps) load_words(set0, sets);
+  // Scores of the largest logits that the words tell of, rounded, -infinity for none: what(i, score) for all of this
+  // thread's in the table.  more(word): there are more in the piece (the same for a whole warp).
+  auto over_table = [&](auto what, auto more) {
+    const int sets = live << log_sets;
+    for (int set0 = warp; set0 < sets; set0 += kBatch * kWarps) {
+      uint32_t word[kBatch];
+      float3 t[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const int set = set0 + j * kWarps + warp;
+        const int set = set0 + j * kWarps;
+        if (set < sets) {
+          t[j] = table[set >> log_sets];
+          if (!MANY && set0 == warp) word[j] = first_words[j];
+          else word[j] = words[__float_as_int(t[j].x) * kScanThreads + (set & last_set) * 32 + lane];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int set = set0 + j * kWarps;
         if (set >= sets) break;
-        const float2 t = table[(set >> log_sets) - q0];
-        if (t.x == kNone) continue;  // (nothing was written)
-        int i = word_of(set);
-        what(i, word[j] ? t.x + (unordered(word[j]) - t.y) : kNone);
+        if (!MANY && t[j].y == kNone) continue;  // (nothing was written)
+        int i = __float_as_int(t[j].x) * kScanThreads + (set & last_set) * 32 + lane;
+        what(i, word[j] ? t[j].y + (unordered(word[j]) - t[j].z) : kNone);
         if ((set & last_set) == last_set && more(word[j]))
           for (int s = last_set + 1; s < kScanThreads / 32; ++s) {
             const uint32_t x = words[i += 32];
-            what(i, x ? t.x + (unordered(x) - t.y) : kNone);
+            what(i, x ? t[j].y + (unordered(x) - t[j].z) : kNone);
           }
       }
     }
   };
-  // A score that k of them reach, and how far below it a candidate may stay and be among the k best all the same.
+  // A score that k threads reach with theirs (-infinity: fewer have one), from the largest of each thread's.
+  auto reached = [&](float mine) {
+    const bool in = mine > kNone;
+    const uint32_t word = ordered(mine);
+    const int n = __syncthreads_count(in);
+    if (n < a.k) return kNone;
+    const Extent e = extent_of<kMergeThreads>(in ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
+    if (n <= a.k + kSlack) return unordered(e.least);
+    return unordered(threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(in && word >= up.a); }).a);
+  };
+  const auto more = [&](uint32_t x) { return __any_sync(~0u, lane == 31 && x != 0); };
+  const auto by_known = [&](float value) { return cut_of(value, known); };
+  if constexpr (MANY) {
+    fill_table(0, by_known);
+    if (pieces > kTable || live > 2 * kFew) {
+      // very many pieces: first a score from the best of them alone
+      float most = kNone;
+      over_pieces(0, min(pieces, kTable), [&](int, int b, float x, float) { most = base[b].value + (x - base[b].most); });
+      const bool in = most > kNone;
+      const uint32_t word = ordered(most);
+      float least = kNone;
+      if (__syncthreads_count(in) > kFew + kSlack) {
+        const Extent e = extent_of<kMergeThreads>(in ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
+        least = unordered(threshold<WordKey>(kFew, e, [&](const WordKey& up) { return __syncthreads_count(in && word >= up.a); }).a);
+      }
+      fill_table(0, [&](float) { return least; });
+      most = kNone;
+      over_table([&](int, float s) { most = fmaxf(most, s); }, more);
+      known = fmaxf(known, reached(most));
+      fill_table(0, by_known);
+    }
+  } else {
+    for (int q = tid; q < pieces; q += kMergeThreads) {
+      const int b = beam_of(q * kScanThreads);
+      const bool is = base[b].kind == kLogits && q - b * p.splits < base[b].pieces;
+      table[q] = make_float3(__int_as_float(q), is ? base[b].value : kNone, base[b].most);
+    }
+    if (tid == 0) live = pieces;
+    __syncthreads();
+  }
+  // A score that k of all reach, and how far below it a candidate may stay and be among the k best all the same.
   float top = kNone, second = kNone;  // of this thread's
   int top_at = 0;
-  for (int q0 = 0; q0 < pieces; q0 += kTable) {
-    fill_table(q0);
+  for (int q0 = 0;;) {
     over_table(
-        q0,
         [&](int i, float s) {
           second = fmaxf(second, fminf(s, top));
           if (s > top) top = s, top_at = i;
         },
-        [&](uint32_t x) { return __any_sync(~0u, lane == 31 && x != 0); });
+        more);
+    if (!MANY || (q0 += kTable) >= pieces) break;
+    fill_table(q0, by_known);
   }
   const float own = tid < a.beams && base[tid].kind == kDone ? base[tid].value : kNone;  // a beam that is done
-  float reach = kNone;
-  {
-    const bool in = fmaxf(top, own) > kNone;
-    const uint32_t word = ordered(fmaxf(top, own));
-    const int n = __syncthreads_count(in);
-    if (n >= a.k) {
-      const Extent e = extent_of<kMergeThreads>(in ? Extent{word, word} : Extent{0xFFFFFFFFu, 0u}, extents);
-      reach = unordered(n <= a.k + kSlack ? e.least
-                                          : threshold<WordKey>(a.k, e, [&](const WordKey& up) { return __syncthreads_count(in && word >= up.a); }).a);
-    }
-  }
-  // (2^-20 of the numbers that were added is far more than their roundings; a beam's scores are its value at most)
+  const float reach = fmaxf(known, reached(fmaxf(top, own)));
+  // (a beam's scores are its value at most)
   if (tid < a.beams) {
     const float value = base[tid].value;
-    const float cut = reach > kNone ? reach - 2.1f * worst - 0x1p-20f * (fabsf(value) + fabsf(reach)) : kNone;
+    const float cut = cut_of(value, reach);
     base[tid].cut = cut;
     if (base[tid].kind != kNobody && value >= cut) atomicMin(&lowest_cut, ordered(cut));
     if (own > kNone && own >= cut) best.put(score_of(base[tid], tid, 0.f, a.end_token));
   }
   __syncthreads();
   // the marked tiles of those that come near it
-  auto look_at = [&](int i) {
+  auto look_at = [&](int i, uint32_t tiles) {
     const int b = beam_of(i), split = i / kScanThreads - b * p.splits;
     const uint2 mark = marks[i];
-    int w = atomicAdd(&place_count, __popc(mark.x));
+    tiles &= mark.x;
+    int w = atomicAdd(&place_count, __popc(tiles));
     const int first = p.begin_unit(base[b].offset, split) * kUnit + (int)mark.y * V::kCount;
-    for (uint32_t bits = mark.x; bits && w < kPlaces; bits &= bits - 1)
+    for (uint32_t bits = tiles; bits && w < kPlaces; bits &= bits - 1)
       places[w++] = make_int2(i / kScanThreads, first + (__ffs(bits) - 1) * kTile);
   };
   const float lowest = unordered(lowest_cut);
-  if (pieces > kTable) {
-    for (int q0 = 0; q0 < pieces; q0 += kTable) {
-      fill_table(q0);
-      over_table(
-          q0, [&](int i, float s) { if (s > kNone && s >= base[beam_of(i)].cut) look_at(i); }, [&](uint32_t) { return true; });
+  auto look = [&](uint32_t tiles) {
+    const auto near = [&](int i, float s) { if (s > kNone && s >= base[beam_of(i)].cut) look_at(i, tiles); };
+    if (MANY && pieces > kTable) {
+      for (int q0 = 0; q0 < pieces; q0 += kTable) {
+        fill_table(q0, by_known);
+        over_table(near, more);
+      }
+    } else if (second > kNone && second >= lowest) {
+      over_table(near, [&](uint32_t) { return true; });
+    } else if (top > kNone && top >= lowest) {
+      near(top_at, top);
     }
-  } else if (second > kNone && second >= lowest) {
-    over_table(
-        0, [&](int i, float s) { if (s > kNone && s >= base[beam_of(i)].cut) look_at(i); }, [&](uint32_t) { return true; });
-  } else if (top > kNone && top >= lowest && top >= base[beam_of(top_at)].cut) {
-    look_at(top_at);
-  }
-  __syncthreads();
-  const bool many_places = place_count > kPlaces;
-  if (!many_places) {
+  };
+  auto take = [&]() {
     for (int i = tid; i < place_count; i += kMergeThreads) {
       const int2 at = places[i];
       const int b = beam_of(at.x * kScanThreads), row = row0 + b;
       const Base& r = base[b];
       const char* from = row_at<DTYPE>(a, row);
-      const float floor = p.sums[(int64_t)row0 * p.splits + at.x].w;
+      const float floor = sums[at.x].w;
       V v[kVecs];
       load_vecs<DTYPE>(v, from, (int)((uintptr_t)from & 15), at.y, min(a.vocab, p.end_unit(r.offset, at.x - b * p.splits) * kUnit), a.vocab);
       uint32_t hits = 0;
@@ -828,14 +909,26 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
         best.list[w++] = score_of(r, b, V::pick(x, n % V::kCount), at.y + i * kUnit + n % V::kCount);
       }
     }
+  };
+  // (all marked tiles, or, where there is no room for that many places, four tiles of each piece at a time)
+  bool many = false;
+  for (int part = -1; part < kMarkTiles / 4; ++part) {
+    look(part < 0 ? ~0u : 15u << (4 * part));
+    __syncthreads();
+    many = place_count > kPlaces;
+    if (!many) take();
+    if (many != (part < 0)) break;  // all is done, or will not be
+    __syncthreads();
+    if (tid == 0) place_count = 0;
+    __syncthreads();
   }
   __syncthreads();
-  bool exact = many_places || count > kRanked;
+  bool exact = many || count > kRanked;
   if (exact) {
     // Ties of very many.  All rows are summed again, so that a key says which is better, and the k best
     // are kept while the marked tiles go by.
     for (int b = 0; b < a.beams; ++b)
-      if (base[b].kind == kLogits) sum_again(b);
+      if (base[b].kind == kLogits && base[b].value >= base[b].cut) sum_again(b);
     if (tid == 0) count = 0;
     best.floor = GroupKey::none();
     __syncthreads();
@@ -936,7 +1029,7 @@ int vec_logits(int dtype) { return dtype == SEMKV_F32 ? 4 : 8; }
 // One CTA to each of the places that the SMs have for them, if there is a unit for each; whole tiles, if that is
 // more than one, and no more than a mark can tell apart.  The cut depends on the sizes alone, so that equal calls give equal
 // bits.
-constexpr int kWantCtas = 152 * 4, kMarkTiles = 32;
+constexpr int kWantCtas = 152 * 4;
 Pieces cut_rows(int rows, int vocab, int dtype) {
   const int unit = kScanThreads * vec_logits(dtype);
   Pieces p = {};
@@ -954,9 +1047,17 @@ Pieces cut_rows(int rows, int vocab, int dtype) {
 template <int DTYPE>
 cudaError_t launch(const BeamArgs& a, const Pieces& p, cudaStream_t stream) {
   const unsigned ctas = (unsigned)(((int64_t)a.groups * a.beams * p.units + p.share - 1) / p.share);
-  const cudaError_t e = launch_pdl(beam_scan_kernel<DTYPE>, dim3(ctas), dim3(kScanThreads), 0, stream, a, p);
+  static bool ready[kAttrDevices] = {};
+  cudaError_t e = once_per_device(ready, [] {
+    const int bytes = merge_bytes(SEMKV_BEAM_MAX, DTYPE);
+    const cudaError_t e = cudaFuncSetAttribute(beam_merge_kernel<DTYPE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e == cudaSuccess ? cudaFuncSetAttribute(beam_merge_kernel<DTYPE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : e;
+  });
   if (e != cudaSuccess) return e;
-  return launch_pdl(beam_merge_kernel<DTYPE>, dim3(a.groups), dim3(kMergeThreads), merge_bytes(a.k, DTYPE), stream, a, p);
+  e = launch_pdl(beam_scan_kernel<DTYPE>, dim3(ctas), dim3(kScanThreads), 0, stream, a, p);
+  if (e != cudaSuccess) return e;
+  const auto merge = (a.beams * p.splits) << log_sets_of(a.k) > 2 * kBatch * (kMergeThreads / 32) ? beam_merge_kernel<DTYPE, true> : beam_merge_kernel<DTYPE, false>;
+  return launch_pdl(merge, dim3(a.groups), dim3(kMergeThreads), merge_bytes(a.k, DTYPE), stream, a, p);
 }
 
 }  // namespace

@@ -203,6 +203,21 @@ def test_rows_in_any_order_of_their_values(dtype):
             check_select(x, np.arange(len(rows))[None] * -0.2371, k)
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("groups,beams,vocab,k", [(1, 8, 1100000, 128), (1, 64, 100003, 128), (2, 128, 30000, 16)])
+def test_long_rows_in_any_order_of_their_values(dtype, groups, beams, vocab, k):
+    """Many pieces with many tiles each, whose logits rise all along, fall, or repeat."""
+    import torch
+    dt = getattr(torch, dtype)
+    rng = np.random.default_rng(vocab)
+    x = torch.empty((groups * beams, vocab), dtype=dt, device="cuda")
+    ramp = torch.linspace(-9, 9, vocab, device="cuda")
+    for r in range(len(x)):
+        x[r] = [ramp, -ramp, ramp.round(), torch.tensor(rng.standard_normal(vocab), device="cuda")][r % 4].to(dt)
+    check_select(x, rng.uniform(-3, -2, (groups, beams)), k, again=False)
+    check_select(x, np.where(np.arange(groups * beams).reshape(groups, beams) % 5 == 3, -1.0, -1e9), k, again=False)
+
+
 def test_equal_rows_and_equal_scores():
     """Beams that are alike: the lower one first, and wherever a row lies its sum is the same."""
     import torch
