@@ -380,13 +380,13 @@ MAPS = [([0, 1, 2, 3, 4], [0, 1, 2, 3, 4], 0), ([0, 1, 2, 3, 4], [1, 2, 3, 4, 0]
         ([1, 9, 3, -1], [2, 0, 1, 2], 3), ([1, 3, 2], [1, 3, -2], 3), (None, [1, 0, 7, 2, -1, 6, 5, 0], 3), ([], [], 0)]
 
 
-@pytest.mark.parametrize("P", [16, 128])
+@pytest.mark.parametrize("P,wide", [(16, 0), (128, 0), (16, 9000), (32, 8190)])
 @pytest.mark.parametrize("seqs,parent,error", MAPS)
-def test_sequences_trade_places(P, seqs, parent, error):
-    """Cycles, copies, emptied ones, a list in its own order, and entries that are left out."""
-    import torch
+def test_sequences_trade_places(P, wide, seqs, parent, error):
+    """Cycles, copies, emptied ones, a list in its own order, and entries that are left out; tables that one kernel
+    holds in its registers, and wider ones, which take two."""
     from paper_2608_28911_gb300 import semkv
-    c = make([0, 1, 40, 300, 129], 1, 64, P, extra_seqs=2, spare=12, seed=P)
+    c = make([0, 1, 40, 300, 129], 1, 64, P, extra_seqs=2, spare=12, seed=P, more_pages=wide)
     plain = fill(c)
     call_reorder(c, seqs, parent)
     reorder(plain, seqs, parent)
@@ -405,11 +405,12 @@ def test_sequences_trade_places(P, seqs, parent, error):
             plain.same_state(c)
 
 
-def test_a_search_over_many_sequences():
+@pytest.mark.parametrize("wide", [0, 300])
+def test_a_search_over_many_sequences(wide):
     """300 branches of 20 prompts, several steps of random maps, one of them with a list entry twice."""
     rng = np.random.default_rng(4)
     lens = [int(x) for x in rng.integers(0, 200, 20)] + [0] * 280
-    c = make(lens, 1, 64, 16, spare=0, seed=2)
+    c = make(lens, 1, 64, 16, spare=0, seed=2, more_pages=wide)
     plain = fill(c)
     for step in range(6):
         n = int(rng.integers(1, 301))
@@ -423,10 +424,11 @@ def test_a_search_over_many_sequences():
     assert (plain.refs >= 0).all() and plain.refs.sum() == sum(plain.used(t) for t in plain.length)
 
 
-def test_reorders_in_a_graph():
+@pytest.mark.parametrize("wide", [0, 9000])
+def test_reorders_in_a_graph(wide):
     import torch
     from paper_2608_28911_gb300 import semkv
-    c = make([33, 70, 5, 100], 1, 64, 32, seed=1)
+    c = make([33, 70, 5, 100], 1, 64, 32, seed=1, more_pages=wide)
     plain = fill(c)
     seqs, parent, ws = t32([0, 1, 2, 3]), t32([0, 1, 2, 3]), c.pages_workspace(4, 0)
     torch.cuda.synchronize()
