@@ -491,50 +491,47 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
 
 // ------------------------------------------------------- the exact sums ------
 
-// 2^(j/32) for j = -16 .. 16 as pairs of binary32 numbers, to 2^-48: products of the root in 64 bits.
+// 2^(j/32) for j = 0 .. 31 as pairs of binary32 numbers, to 2^-48: products of the root in 64 bits.
 struct Powers {
-  float2 at[33];
+  float2 at[32];
 };
 constexpr Powers make_powers() {
   Powers p{};
-  double up = 1.0, down = 1.0;
-  for (int j = 0; j <= 16; ++j) {
-    p.at[16 + j].x = (float)up;
-    p.at[16 + j].y = (float)(up - (double)(float)up);
-    p.at[16 - j].x = (float)down;
-    p.at[16 - j].y = (float)(down - (double)(float)down);
-    up *= 1.0218971486541166782;
-    down *= 0.97857206208770013451;
+  double x = 1.0;
+  for (int j = 0; j < 32; ++j) {
+    p.at[j].x = (float)x;
+    p.at[j].y = (float)(x - (double)(float)x);
+    x *= 1.0218971486541166782;
   }
   return p;
 }
 __constant__ const Powers kPowers = make_powers();
 
-// exp(d) for d = x - m <= 0 as a sum of three numbers, 2^-38 of it off: 2^n * 2^(j/32) * exp(t), with d log2 e taken in
-// two numbers and |t| <= ln 2 / 64, exp(t) - 1 by its series.
-__device__ __forceinline__ bool exp_parts(float x, float m, const float2* powers, float (&out)[3]) {
-  float d, dl;
-  two_sum(x, -m, d, dl);
-  if (!(d > -100.f)) return false;  // (below 2^-144 of the largest: past every bit that counts)
-  constexpr float kHigh = 1.4426950408889634f, kLow = (float)(1.4426950408889634074 - (double)kHigh);
-  const float p = __fmul_rn(d, kHigh);
-  const float e = __fmaf_rn(d, kHigh, -p) + __fmaf_rn(d, kLow, dl * kHigh);
-  const float n = rintf(p), f = p - n;
-  const float j = rintf(f * 32.f), r = __fmaf_rn(j, -1.f / 32, f);
+// sum + low grows by exp(x + xl) / 2^down, 2^-38 of it off, for |x| up to 1100 and an |xl| far below it: 2^(j/32) * exp(t) with
+// x log2 e in two numbers, a whole j, |t| <= ln 2 / 64, and exp(t) - 1 by its series (the fifth power is 2^-39).
+__device__ __forceinline__ void add_exp(float x, float xl, int down, const float2* powers, float& sum, float& low) {
+  constexpr float kLow = (float)(1.4426950408889634074 - (double)kLog2e), kWhole = 12582912.f;  // 1.5 * 2^23: the last bit is 1
   constexpr float kBig = (float)kLn2, kSmall = (float)(kLn2 - (double)kBig);
+  const float p = __fmul_rn(x, kLog2e);
+  const float e = __fmaf_rn(x, kLow, __fmaf_rn(xl, kLog2e, __fmaf_rn(x, kLog2e, -p)));
+  const float z = __fmaf_rn(p, 32.f, kWhole), r = __fmaf_rn(__fsub_rn(z, kWhole), -1.f / 32, p);
+  const int j = __float_as_int(z) - __float_as_int(kWhole);
   const float t = __fmul_rn(r, kBig);
-  const float tl = __fmaf_rn(r, kBig, -t) + __fmaf_rn(r, kSmall, e * kBig);
-  const float q = t * t * __fmaf_rn(t, __fmaf_rn(t, __fmaf_rn(t, 1.f / 120, 1.f / 24), 1.f / 6), 0.5f);
-  // (exp(t + tl) - 1 = t + tl + t tl + q + ...)
-  const float rest = __fmaf_rn(t, tl, tl) + q;
-  const float2 w = powers[(int)j + 16];
+  const float tl = __fmaf_rn(e, kBig, __fmaf_rn(r, kSmall, __fmaf_rn(r, kBig, -t)));
+  // exp(t + tl) - 1 = t + q
+  const float q = __fmaf_rn(__fmul_rn(t, t), __fmaf_rn(t, __fmaf_rn(t, 1.f / 24, 1.f / 6), 0.5f), __fmaf_rn(t, tl, tl));
+  const float2 w = powers[j & 31];
   const float a = __fmul_rn(w.x, t);
-  const float s = __uint_as_float((uint32_t)((int)n + 127) << 23);
-  out[0] = w.x * s;
-  out[1] = a * s;
-  out[2] = (__fmaf_rn(w.x, t, -a) + w.y + __fmaf_rn(w.y, t, w.x * rest)) * s;
-  return n >= -120.f;
+  const float b = __fmaf_rn(w.y, t, __fmaf_rn(w.x, q, w.y)) + __fmaf_rn(w.x, t, -a);
+  const float s = __int_as_float(((j >> 5) - down + 127) << 23);
+  const float high = __fadd_rn(w.x, a), rest = __fadd_rn(__fsub_rn(w.x, high), a) + b;
+  float err;
+  two_sum(sum, high * s, sum, err);
+  low += __fmaf_rn(rest, s, err);
 }
+
+// Logits up to this need not have the largest taken off for their sums: 2^down does as well.
+constexpr float kNear = 1024.f;
 
 // ln sum exp(x - most) of a row, by a whole CTA, to 2^-37, for its first warp.  `most` is the row's largest logit.
 template <int DTYPE>
@@ -542,21 +539,24 @@ __device__ __noinline__ double exact_normalizer(const BeamArgs& a, int row, floa
   using V = Vec<DTYPE>;
   const char* at = row_at<DTYPE>(a, row);
   const int lead = (int)((uintptr_t)at & 15);
+  const bool near = fabsf(most) <= kNear;
+  const int down = near ? (int)scale_of(most) : 0;
   float sum = 0.f, low = 0.f;
-  if (threadIdx.x < 33) powers[threadIdx.x] = kPowers.at[threadIdx.x];
+  if (threadIdx.x < 32) powers[threadIdx.x] = kPowers.at[threadIdx.x];
   __syncthreads();
   for (int first = threadIdx.x * V::kCount; first < a.vocab; first += kMergeThreads * V::kCount) {
-    V v = load_vec<DTYPE>(at, first, a.vocab, lead);
+    const V v = load_vec<DTYPE>(at, first, a.vocab, lead);
+    // (what lies 64 below the largest is less than 2^-92 of it: past every bit that counts.  A NaN is left out here, too.)
+    if (near) {
 #pragma unroll
-    for (int j = 0; j < V::kCount; ++j) {
-      const float x = v.at(j);
-      float e[3];
-      if (x > kNone && x < INFINITY && exp_parts(x, most, powers, e)) {
-        float err;
-        two_sum(sum, e[0], sum, err);
-        low += err;
-        two_sum(sum, e[1], sum, err);
-        low += err + e[2];
+      for (int j = 0; j < V::kCount; ++j)
+        if (v.at(j) <= most && v.at(j) > most - 64.f) add_exp(v.at(j), 0.f, down, powers, sum, low);
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < V::kCount; ++j) {
+        float d, dl;
+        two_sum(V::pick(v.w, j), -most, d, dl);
+        if (d <= 0.f && d > -64.f) add_exp(d, dl, 0, powers, sum, low);
       }
     }
   }
@@ -570,7 +570,7 @@ __device__ __noinline__ double exact_normalizer(const BeamArgs& a, int row, floa
   total = threadIdx.x < kMergeThreads / 32 ? parts[threadIdx.x] : 0.0;
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) total += __shfl_xor_sync(~0u, total, d);
-  return log(total);
+  return log(total) + (near ? (double)down * kLn2 - (double)most : 0.0);
 }
 
 // ----------------------------------------------------------------- merge ------
@@ -623,7 +623,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   __shared__ uint32_t worst_error, lowest_cut, best_floor;  // (as ordered numbers)
   __shared__ Base base[SEMKV_BEAM_MAX];
   __shared__ uint32_t again[SEMKV_BEAM_MAX / 32];  // rows to be summed once more
-  __shared__ float2 powers[33];
+  __shared__ float2 powers[32];
   __shared__ GroupKey out[SEMKV_BEAM_MAX];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group = blockIdx.x, row0 = group * a.beams;
