@@ -308,10 +308,15 @@ def _here(*tensors):
             raise ValueError("tensors have to be on the current CUDA device")
 
 
+def _ints(t, n, what):
+    if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what} is a contiguous int32 tensor of {n}")
+    return t.data_ptr()
+
+
 def _list(t, n, what):
     if t is not None:
-        _need(t.dtype == torch.int32 and t.is_contiguous() and t.shape == (n,),
-              f"{what} is a contiguous int32 tensor of {n}")
+        _ints(t, n, what)
         _here(t)
     return t
 
@@ -378,10 +383,12 @@ def semkv_kv4_write_rotated(cache: "KV4Cache", batch: "KV4Batch", layer: int, ro
         _here(cache.pages, batch.start, rotation.cos_sin, k, v, q, q_out)
     else:
         _here(cache.pages, batch.start, rotation.cos_sin, k, v)
+    where = None
     if positions is not None:
-        _list(positions, total, "positions")
+        where = _ints(positions, total, "positions")
+        _here(positions)
     _check("semkv_kv4_write_rotated",
-           LIB.semkv_kv4_write_rotated(cache.ref, batch.ref, layer, rotation.ref, _ptr(positions), kind,
+           LIB.semkv_kv4_write_rotated(cache.ref, batch.ref, layer, rotation.ref, where, kind,
                                        qp, qs, q_heads, op, ostr, k.data_ptr(), ks, v.data_ptr(), vs,
                                        _stream(stream)))
 
@@ -439,10 +446,15 @@ def semkv_kv4_reorder(cache: "KV4Cache", seqs, parent: torch.Tensor, ws: torch.T
     """The i-th sequence of the list becomes a branch of what its parent[i]-th was before the call; -1
     empties it.  seqs: int32, or None for 0 .. n-1.  ws: cache.pages_workspace(n, 0)."""
     n = parent.numel()
-    _here(cache.pages, ws)
+    at = _ints(parent, n, "parent")
+    if seqs is None:
+        of = None
+        _here(cache.pages, parent, ws)
+    else:
+        of = _ints(seqs, n, "seqs")
+        _here(cache.pages, parent, ws, seqs)
     _check("semkv_kv4_reorder",
-           LIB.semkv_kv4_reorder(cache.ref, n, _ptr(_list(seqs, n, "seqs")),
-                                 _list(parent, n, "parent").data_ptr(), _ptr(ws), ws.nbytes, _stream(stream)))
+           LIB.semkv_kv4_reorder(cache.ref, n, of, at, _ptr(ws), ws.nbytes, _stream(stream)))
 
 
 def semkv_kv4_compact(cache: "KV4Cache", seqs: torch.Tensor, keep: torch.Tensor, ws: torch.Tensor,
@@ -480,16 +492,18 @@ def semkv_beam_select(logits: torch.Tensor, scores: torch.Tensor, parent: torch.
     """The k best continuations of each group's beams into parent, token (int32) and score (float32)
     [groups][k].  logits [groups * beams][vocab] (any row stride), scores float32 [groups][beams],
     done: uint8 or bool, one for each beam, or None."""
-    _need(scores.dim() == 2 and parent.dim() == 2, "scores is [groups][beams], parent [groups][k]")
-    (groups, beams), k = scores.shape, parent.shape[1]
+    _need(scores.dim() == 2 and parent.dim() == 2 and logits.dim() == 2,
+          "scores is [groups][beams], parent [groups][k], logits [groups * beams][vocab]")
+    (groups, beams), k, (rows, vocab), steps = scores.shape, parent.shape[1], logits.shape, logits.stride()
     kind = _BEAM_TYPES.get(logits.dtype)
-    _need(kind is not None and logits.dim() == 2 and logits.shape[0] == groups * beams
-          and (logits.shape[1] <= 1 or logits.stride(1) == 1),
+    _need(kind is not None and rows == groups * beams and (vocab <= 1 or steps[1] == 1),
           "logits is float16, bfloat16 or float32 [groups * beams][vocab], a row's values side by side")
-    for t, dtype, shape in ((scores, torch.float32, scores.shape), (parent, torch.int32, (groups, k)),
-                            (token, torch.int32, (groups, k)), (score, torch.float32, (groups, k))):
-        _need(t.dtype == dtype and t.is_contiguous() and t.shape == shape,
-              "scores (float32), parent, token (int32) and score (float32) are contiguous and fit each other")
+    shape = (groups, k)
+    _need(scores.dtype == score.dtype == torch.float32 and parent.dtype == token.dtype == torch.int32
+          and parent.shape == shape and token.shape == shape and score.shape == shape
+          and scores.is_contiguous() and parent.is_contiguous() and token.is_contiguous()
+          and score.is_contiguous(),
+          "scores (float32), parent, token (int32) and score (float32) are contiguous and fit each other")
     if done is not None:
         _need(done.dtype in (torch.uint8, torch.bool) and done.is_contiguous() and done.numel() == groups * beams,
               "done is contiguous uint8 or bool, one for each beam")
@@ -497,11 +511,10 @@ def semkv_beam_select(logits: torch.Tensor, scores: torch.Tensor, parent: torch.
     if dev_error is not None:
         _here(_list(dev_error, 1, "dev_error"))
     _here(logits, scores, parent, token, score, ws)
-    vocab = logits.shape[1]
     _check("semkv_beam_select",
-           LIB.semkv_beam_select(groups, beams, vocab, kind, logits.data_ptr(),
-                                 logits.stride(0) if logits.shape[0] > 1 else vocab, _ptr(scores), _ptr(done),
-                                 end_token, k, _ptr(parent), _ptr(token), _ptr(score), _ptr(dev_error), _ptr(ws),
+           LIB.semkv_beam_select(groups, beams, vocab, kind, logits.data_ptr(), steps[0] if rows > 1 else vocab,
+                                 scores.data_ptr(), None if done is None else done.data_ptr(), end_token, k,
+                                 parent.data_ptr(), token.data_ptr(), score.data_ptr(), _ptr(dev_error), _ptr(ws),
                                  ws.nbytes, _stream(stream)))
 
 
