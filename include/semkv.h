@@ -297,9 +297,9 @@ semkv_status semkv_decode_attention_noalloc(const semkv_quant_desc* desc,
  * device i32 or NULL.
  * Accuracy: sums of exponentials are binary32 with a known bound (2^-19 of the sum at most); where two
  * candidates of different beams whose order matters lie within it, their rows are summed again to 2^-37,
- * so that what comes out is the order by exact scores unless these agree to 2^-36.  Equal rows with equal
- * scores agree in every bit.  score is rounded once to binary32 from a sum within the first bound.  The results
- * do not depend on where the rows lie or on the GPU's number of SMs, and are the same every time.
+ * so that what comes out is the order by exact scores unless these agree to 2^-36; equal rows with equal
+ * scores do.  score is rounded once to binary32 from a sum within the first bound; its last bits may depend
+ * on where the rows lie (modulo 16 bytes) and on the sizes.  Apart from that equal calls give equal bits.
  * ws: device workspace of semkv_beam_select_workspace_bytes bytes, 16-byte aligned; calls that may
  * overlap on the GPU need one each.  Nothing in it has to be kept or cleared.
  * Errors: SEMKV_EINVAL, SEMKV_EALIGN, SEMKV_EUNSUPPORTED (dtype, more beams, k, vocab or rows than above),

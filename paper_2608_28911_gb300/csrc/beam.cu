@@ -269,7 +269,7 @@ __device__ __forceinline__ Vec<DTYPE> join_vec(const uint4& x, const uint4& y, i
 }
 // Logits first .. first + count of a row, the others -infinity.  The vectors lie `lead` bytes behind a multiple of
 // 16; those inside the row are brought by whole aligned loads all the same, two for one of them (its neighbour's
-// other half is in the cache).  So a thread's logits, and the order of every sum, do not depend on where a row lies.
+// other half is in the cache).  So a thread's logits, and the order of the sum, do not depend on where a row lies.
 template <int DTYPE>
 __device__ __forceinline__ Vec<DTYPE> load_vec(const char* row, int first, int vocab, int lead) {
   using V = Vec<DTYPE>;
@@ -295,6 +295,7 @@ constexpr int kScanWarps = kScanThreads / 32, kVecs = 4, kMarkTiles = 32;  // ve
 // units, of one row behind the other, up to 32 tiles, so a row lies in up to `splits` pieces.
 struct Pieces {
   int units, share, splits;
+  bool aligned;
   uint32_t per_split;  // 2^32 / splits, rounded up: a product's upper half is the quotient (0: splits is 1)
   // [rows][splits] the largest logit, the sum of 2^(x log2 e - scale_of(it)) as two numbers, and the floor
   float4* sums;
@@ -323,13 +324,44 @@ __device__ __forceinline__ const char* row_at(const BeamArgs& a, int row) {
   return static_cast<const char*>(a.logits) + (int64_t)row * a.stride * Vec<DTYPE>::kSize;
 }
 
-// A thread's vectors of a tile, the first of them from logit `first` on; behind the piece's end -infinity.
+// A row as vectors that lie on multiples of 16 bytes: it begins `shift` logits into the first, whose others are not
+// its own.  Logits are counted from there.
+struct RowView {
+  const char* base;
+  int shift, size;
+};
 template <int DTYPE>
-__device__ __forceinline__ void load_vecs(Vec<DTYPE> (&v)[kVecs], const char* row, int lead, int first, int end, int vocab) {
+__device__ __forceinline__ RowView row_view(const BeamArgs& a, int row, bool aligned = false) {
+  const char* at = row_at<DTYPE>(a, row);
+  if (aligned) return {at, 0, a.vocab};
+  const int lead = (int)((uintptr_t)at & 15), shift = lead / Vec<DTYPE>::kSize;
+  return {at - lead, shift, a.vocab + shift};
+}
+// The vector from logit `first` on; outside the row, or from `end` on, -infinity.
+template <int DTYPE>
+__device__ __forceinline__ Vec<DTYPE> load_one(const RowView& r, int first, int end) {
+  using V = Vec<DTYPE>;
+  const char* at = r.base + (int64_t)first * V::kSize;
+  V v;
+  if (first + V::kCount <= end && (first > 0 || r.shift == 0)) {
+    const uint4 x = __ldg(reinterpret_cast<const uint4*>(at));
+    v.w[0] = x.x, v.w[1] = x.y, v.w[2] = x.z, v.w[3] = x.w;
+    return v;
+  }
+  v.fill_none();
+#pragma unroll
+  for (int i = 0; i < V::kCount; ++i)
+    if (first + i >= r.shift && first + i < end)
+      v.set(i, DTYPE == SEMKV_F32 ? reinterpret_cast<const uint32_t*>(at)[i] : (uint32_t)reinterpret_cast<const uint16_t*>(at)[i]);
+  return v;
+}
+// A thread's vectors of a tile, the first of them from logit `first` on.
+template <int DTYPE>
+__device__ __forceinline__ void load_vecs(Vec<DTYPE> (&v)[kVecs], const RowView& r, int first, int end) {
   using V = Vec<DTYPE>;
   constexpr int kUnit = kScanThreads * V::kCount;
-  if (lead == 0 && first + (kVecs - 1) * kUnit + V::kCount <= end) {
-    const uint4* from = reinterpret_cast<const uint4*>(row + (int64_t)first * V::kSize);
+  if (first + (kVecs - 1) * kUnit + V::kCount <= end && (first > 0 || r.shift == 0)) {
+    const uint4* from = reinterpret_cast<const uint4*>(r.base + (int64_t)first * V::kSize);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       const uint4 x = __ldcs(from + i * kScanThreads);
@@ -337,23 +369,13 @@ __device__ __forceinline__ void load_vecs(Vec<DTYPE> (&v)[kVecs], const char* ro
     }
     return;
   }
-  if (lead != 0 && first >= V::kCount && first + (kVecs - 1) * kUnit + 2 * V::kCount <= end) {
-    const uint4* from = reinterpret_cast<const uint4*>(row + (int64_t)first * V::kSize - lead);
-    uint4 x[kVecs], y[kVecs];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) x[i] = __ldg(from + i * kScanThreads), y[i] = __ldg(from + i * kScanThreads + 1);
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) v[i] = join_vec<DTYPE>(x[i], y[i], lead);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-    if (first + i * kUnit < end) v[i] = load_vec<DTYPE>(row, first + i * kUnit, vocab, lead);
-    else v[i].fill_none();
-  }
+  for (int i = 0; i < kVecs; ++i) v[i] = load_one<DTYPE>(r, first + i * kUnit, end);
 }
 
-template <int DTYPE>
+// ALIGNED: all rows begin on a multiple of 16 bytes, which saves the registers that shifts take (64 x 16 x 131072: 55 us
+// in all, 57 with them).
+template <int DTYPE, bool ALIGNED>
 __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, Pieces p) {
   using V = Vec<DTYPE>;
   constexpr int kUnit = kScanThreads * V::kCount, kTile = kVecs * kUnit;
@@ -369,11 +391,11 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
   if (tid < 2) reaching[tid] = others[tid] = 0;
   for (; unit < past; ++row, first_unit = 0) {
     const int offset = p.offset_of(row), split = (first_unit + offset) / p.share, end_unit = p.end_unit(offset, split);
-    const int begin = first_unit * kUnit, end = min(a.vocab, end_unit * kUnit);
+    const int begin = first_unit * kUnit;
     unit += end_unit - first_unit;
     if (!row_counts(a, row)) continue;
-    const char* at = row_at<DTYPE>(a, row);
-    const int lead = (int)((uintptr_t)at & 15);
+    const RowView r = row_view<DTYPE>(a, row, ALIGNED);
+    const int end = min(r.size, end_unit * kUnit);  // (not above `begin` where only rows that lie otherwise go on)
     // of this thread's logits; k logits of `floor` or more have been seen: the same or less does not matter any more
     float m = kNone, c = -4 * kFar, sum = 0.f, low = 0.f, floor = kNone;
     uint32_t seen = 0;
@@ -433,12 +455,12 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
       float err;
       two_sum(sum, (s[0] + s[1]) + (s[2] + s[3]), sum, err);
       low += err;
-      if (t0 + 2 * kTile < end) load_vecs<DTYPE>(v, at, lead, t0 + 2 * kTile + tid * V::kCount, end, a.vocab);
+      if (t0 + 2 * kTile < end) load_vecs<DTYPE>(v, r, t0 + 2 * kTile + tid * V::kCount, end);
       seen |= (uint32_t)(top > floor) << tile++;
     };
     V v0[kVecs], v1[kVecs];
-    load_vecs<DTYPE>(v0, at, lead, begin + tid * V::kCount, end, a.vocab);
-    if (begin + kTile < end) load_vecs<DTYPE>(v1, at, lead, begin + kTile + tid * V::kCount, end, a.vocab);
+    load_vecs<DTYPE>(v0, r, begin + tid * V::kCount, end);
+    if (begin + kTile < end) load_vecs<DTYPE>(v1, r, begin + kTile + tid * V::kCount, end);
     for (int t0 = begin; t0 < end; t0 += 2 * kTile) {
       step(v0, t0);
       if (t0 + kTile < end) step(v1, t0 + kTile);
@@ -894,10 +916,10 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
       const int2 at = places[i];
       const int b = beam_of(at.x * kScanThreads), row = row0 + b;
       const Base& r = base[b];
-      const char* from = row_at<DTYPE>(a, row);
+      const RowView view = row_view<DTYPE>(a, row);
       const float floor = sums[at.x].w;
       V v[kVecs];
-      load_vecs<DTYPE>(v, from, (int)((uintptr_t)from & 15), at.y, min(a.vocab, p.end_unit(r.offset, at.x - b * p.splits) * kUnit), a.vocab);
+      load_vecs<DTYPE>(v, view, at.y, min(view.size, p.end_unit(r.offset, at.x - b * p.splits) * kUnit));
       uint32_t hits = 0;
 #pragma unroll
       for (int i = 0; i < kVecs; ++i)
@@ -912,7 +934,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
         uint32_t x[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = i & 2 ? (i & 1 ? v[3].w[e] : v[2].w[e]) : (i & 1 ? v[1].w[e] : v[0].w[e]);
-        best.list[w++] = score_of(r, b, V::pick(x, n % V::kCount), at.y + i * kUnit + n % V::kCount);
+        best.list[w++] = score_of(r, b, V::pick(x, n % V::kCount), at.y - view.shift + i * kUnit + n % V::kCount);
       }
     }
   };
@@ -950,28 +972,28 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
         best.template offer<1>(end_key, [&](const GroupKey&) { best.put(end_key); });
       }
       const int row = row0 + b;
-      const char* from = row_at<DTYPE>(a, row);
-      const int lead = (int)((uintptr_t)from & 15), end = min(a.vocab, p.end_unit(base[b].offset, split) * kUnit);
+      const RowView view = row_view<DTYPE>(a, row);
+      const int end = min(view.size, p.end_unit(base[b].offset, split) * kUnit);
       const int first0 = p.begin_unit(base[b].offset, split) * kUnit + (int)mark.y * V::kCount;
       for (; __syncthreads_or(bits != 0); bits &= bits - 1)
         for (int j = 0; j < kVecs; ++j) {
           const int first = bits ? first0 + (__ffs(bits) - 1) * kTile + j * kUnit : end;
           V v;
           v.fill_none();
-          if (first < end) v = load_vec<DTYPE>(from, first, a.vocab, lead);
+          if (first < end) v = load_one<DTYPE>(view, first, end);
           v.clean();
           GroupKey most = GroupKey::none();
 #pragma unroll
           for (int e = 0; e < V::kCount; ++e)
             if (v.at(e) > kNone) {
-              const GroupKey key = score_of(base[b], b, v.at(e), first + e);
+              const GroupKey key = score_of(base[b], b, v.at(e), first - view.shift + e);
               if (key >= most) most = key;
             }
           best.template offer<V::kCount>(most, [&](const GroupKey& least) {
 #pragma unroll
             for (int e = 0; e < V::kCount; ++e)
               if (v.at(e) > kNone) {
-                const GroupKey key = score_of(base[b], b, v.at(e), first + e);
+                const GroupKey key = score_of(base[b], b, v.at(e), first - view.shift + e);
                 if (key >= least) best.put(key);
               }
           });
@@ -1033,13 +1055,14 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
 int vec_logits(int dtype) { return dtype == SEMKV_F32 ? 4 : 8; }
 
 // One CTA to each of the places that the SMs have for them (64 x 16 x 131072: 55 us; with twice as many CTAs 57, with half
-// 59), whole tiles where a row has one, and no more than a mark can tell apart.  The cut depends on the sizes alone, so that equal calls give equal
-// bits.
+// 59), whole tiles where a row has one, and no more than a mark can tell apart.  The cut depends on the sizes and on whether all
+// rows begin on a multiple of 16 bytes, so that equal calls give equal bits.
 constexpr int kWantCtas = 152 * 4;
-Pieces cut_rows(int rows, int vocab, int dtype) {
+Pieces cut_rows(int rows, int vocab, int dtype, bool aligned) {
   const int unit = kScanThreads * vec_logits(dtype);
   Pieces p = {};
-  p.units = (vocab + unit - 1) / unit;
+  p.aligned = aligned;
+  p.units = (vocab + (aligned ? 0 : vec_logits(dtype) - 1) + unit - 1) / unit;
   int64_t share = ((int64_t)rows * p.units + kWantCtas - 1) / kWantCtas;
   if (share > 1 || p.units >= kVecs) share = (share + kVecs - 1) / kVecs * kVecs;
   if (share > kVecs * kMarkTiles) share = kVecs * kMarkTiles;
@@ -1060,7 +1083,7 @@ cudaError_t launch(const BeamArgs& a, const Pieces& p, cudaStream_t stream) {
     return e == cudaSuccess ? cudaFuncSetAttribute(beam_merge_kernel<DTYPE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : e;
   });
   if (e != cudaSuccess) return e;
-  e = launch_pdl(beam_scan_kernel<DTYPE>, dim3(ctas), dim3(kScanThreads), 0, stream, a, p);
+  e = launch_pdl(p.aligned ? beam_scan_kernel<DTYPE, true> : beam_scan_kernel<DTYPE, false>, dim3(ctas), dim3(kScanThreads), 0, stream, a, p);
   if (e != cudaSuccess) return e;
   const auto merge = (a.beams * p.splits) << log_sets_of(a.k) > 2 * kBatch * (kMergeThreads / 32) ? beam_merge_kernel<DTYPE, true> : beam_merge_kernel<DTYPE, false>;
   return launch_pdl(merge, dim3(a.groups), dim3(kMergeThreads), merge_bytes(a.k, DTYPE), stream, a, p);
@@ -1071,12 +1094,14 @@ cudaError_t launch(const BeamArgs& a, const Pieces& p, cudaStream_t stream) {
 size_t beam_select_workspace(int groups, int beams, int vocab, int dtype, int k) {
   (void)k;
   const int rows = groups * beams;
-  return (size_t)rows * cut_rows(rows, vocab, dtype).splits * (sizeof(float4) + kScanThreads * (sizeof(uint2) + sizeof(uint32_t)));
+  const int aligned = cut_rows(rows, vocab, dtype, true).splits, others = cut_rows(rows, vocab, dtype, false).splits;
+  return (size_t)rows * (aligned > others ? aligned : others) * (sizeof(float4) + kScanThreads * (sizeof(uint2) + sizeof(uint32_t)));
 }
 
 cudaError_t launch_beam_select(const BeamArgs& a, int dtype, void* ws, cudaStream_t stream) {
   const int rows = a.groups * a.beams;
-  Pieces p = cut_rows(rows, a.vocab, dtype);
+  const int64_t row_bytes = a.stride * (dtype == SEMKV_F32 ? 4 : 2);
+  Pieces p = cut_rows(rows, a.vocab, dtype, (uintptr_t)a.logits % 16 == 0 && (rows == 1 || row_bytes % 16 == 0));
   p.sums = static_cast<float4*>(ws);
   p.marks = reinterpret_cast<uint2*>(p.sums + (size_t)rows * p.splits);
   p.words = reinterpret_cast<uint32_t*>(p.marks + (size_t)rows * p.splits * kScanThreads);
