@@ -7,8 +7,8 @@
 // So the scan sorts nothing and writes little, whatever k is; a piece has up to 262144 logits (131072 of 32 bits).
 //
 // Bound by memory where the rows are many: 64 x 16 rows of 131072 bf16 logits, k 32, take 55 us, the scan 47 of them
-// (5.7 TB/s; reading alone takes 40), 84 us with rows that do not begin on a multiple of 16 bytes.  Few
-// rows are bound by the latency of two kernels: 4 rows of 32768, k 8, 11 us, 25 of 50003 in f32 15 us.  What took longer:
+// (5.7 TB/s; reading alone takes 40), with rows of 131071, which do not begin on multiples of 16 bytes, 62 us.  Few
+// rows are bound by the latency of two kernels: 4 rows of 32768, k 8, 11 us, 25 of 50003 in f32 13 us.  What took longer:
 // lists of the best kept by the CTA as it streams (171 us for the scan), candidates put aside where they are met (93),
 // tiles brought by bulk copies (102), a warp that settles what the others stream (72).
 //
@@ -1055,7 +1055,8 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
 int vec_logits(int dtype) { return dtype == SEMKV_F32 ? 4 : 8; }
 
 // One CTA to each of the places that the SMs have for them (64 x 16 x 131072: 55 us; with twice as many CTAs 57, with half
-// 59), whole tiles where a row has one, and no more than a mark can tell apart.  The cut depends on the sizes and on whether all
+// 59), whole tiles where a row has one, rows of less than two tiles whole (16 x 8 x 10000: 12 us, cut anywhere 15), and no
+// more than a mark can tell apart.  The cut depends on the sizes and on whether all
 // rows begin on a multiple of 16 bytes, so that equal calls give equal bits.
 constexpr int kWantCtas = 152 * 4;
 Pieces cut_rows(int rows, int vocab, int dtype, bool aligned) {
@@ -1064,7 +1065,8 @@ Pieces cut_rows(int rows, int vocab, int dtype, bool aligned) {
   p.aligned = aligned;
   p.units = (vocab + (aligned ? 0 : vec_logits(dtype) - 1) + unit - 1) / unit;
   int64_t share = ((int64_t)rows * p.units + kWantCtas - 1) / kWantCtas;
-  if (share > 1 || p.units >= kVecs) share = (share + kVecs - 1) / kVecs * kVecs;
+  if (p.units >= kVecs) share = (share + kVecs - 1) / kVecs * kVecs;
+  if (share < p.units && p.units < 2 * kVecs) share = p.units;
   if (share > kVecs * kMarkTiles) share = kVecs * kMarkTiles;
   p.share = (int)share;
   p.splits = p.units % p.share == 0 ? p.units / p.share : (p.units + p.share - 2) / p.share + 1;
