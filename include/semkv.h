@@ -294,7 +294,7 @@ semkv_status semkv_decode_attention_noalloc(const semkv_quant_desc* desc,
  * >= vocab elements from row to row, aligned to its type; scores: device f32 [groups * beams]; parent,
  * token: device i32 [groups][k]; score: device f32 [groups][k].  beams, k: 1 .. 128; vocab: 1 .. 2^24;
  * groups * beams: up to 2^20.  end_token: 0 .. vocab-1 where done is given, else not used.  dev_error:
- * device i32 or NULL.
+ * device i32 or NULL.  With k = beams, score may be scores: the new ones take the old ones' place.
  * Accuracy: sums of exponentials are binary32 with a known bound (2^-19 of the sum at most); where two
  * candidates of different beams whose order matters lie within it, their rows are summed again to 2^-37,
  * so that what comes out is the order by exact scores unless these agree to 2^-36; equal rows with equal

@@ -125,6 +125,43 @@ def test_rotated_rows_without_a_place_are_left_out():
         assert torch.equal(c.pages, before) and (out == 7).all() and int(c.dev_error.item()) == 3
 
 
+def test_rotated_rows_in_graphs_and_on_streams():
+    """A step's reserve and append, captured and replayed on new rows, against eager calls on a stream."""
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    rng = np.random.default_rng(6)
+    rot = semkv.KV4Rotation(torch.tensor(table_of(64, 64), device="cuda"))
+    caches = [make([5, 31, 0], 2, 64, 32, spare=6, seed=4, more_pages=1) for _ in range(2)]
+    for c in caches:
+        c.pages.zero_()
+    steps = [semkv.KV4Batch(3) for _ in caches]
+    rows = [[rows_like(rng, (3, h, 64), torch.bfloat16) for h in (2, 2, 6)] for _ in range(4)]
+    k, v, q = [x.clone() for x in rows[0]]
+    outs = [torch.empty_like(q) for _ in caches]
+    spaces = [c.pages_workspace(3) for c in caches]
+
+    def step(i, k, v, q, **kw):
+        semkv.semkv_kv4_reserve(caches[i], steps[i], spaces[i], **kw)
+        semkv.semkv_kv4_write_rotated(caches[i], steps[i], 0, rot, k, v, q, outs[i], **kw)
+
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(0, k, v, q)
+    stream = torch.cuda.Stream()
+    for new in rows:
+        for to, x in zip((k, v, q), new):
+            to.copy_(x)
+        g.replay()
+        torch.cuda.synchronize()
+        step(1, *new, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1]) and torch.equal(caches[0].pages, caches[1].pages)
+        assert torch.equal(caches[0].length, caches[1].length)
+    assert int(caches[0].dev_error.item()) == int(caches[1].dev_error.item()) == 0
+    assert caches[0].length.tolist() == [9, 35, 4]
+
+
 # -------------------------------------------------------------- beam selection ------
 
 def score_bound(vocab, want):
@@ -364,6 +401,21 @@ def test_selections_in_graphs_and_on_streams():
     torch.cuda.synchronize()
     for o, w in zip(got, want):
         assert all(torch.equal(a, b) for a, b in zip(o, w))
+
+
+@pytest.mark.parametrize("groups,beams", [(1, 4), (70, 5)])
+def test_scores_in_place(groups, beams):
+    """As many places as beams: the new scores may take the old ones' place."""
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    rng = np.random.default_rng(groups)
+    x = logits_like(rng, groups * beams, 9001, torch.float16, 7)
+    scores = torch.tensor(rng.uniform(-8, -2, (groups, beams)).astype(np.float32), device="cuda")
+    want = check_select(x, scores.cpu().numpy(), beams)
+    parent, token = [torch.empty((groups, beams), dtype=torch.int32, device="cuda") for _ in range(2)]
+    semkv.semkv_beam_select(x, scores, parent, token, scores, semkv.beam_select_workspace(x, scores, beams))
+    for a, b in zip((parent, token, scores), want):
+        assert np.array_equal(a.cpu().numpy(), b)
 
 
 # --------------------------------------------------------------------- reorder ------
