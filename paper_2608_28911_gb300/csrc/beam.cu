@@ -608,9 +608,12 @@ struct Base {
 };
 enum { kNobody, kLogits, kDone };
 
+// (value is the sum's rounding, so that what goes by it alone is off by no more than that: norm_low grows with a row's
+// largest logit, 0.07 at a million)
 __device__ __forceinline__ void set_value(Base& r, float score, float norm, float norm_low) {
-  two_sum(score, -norm, r.value, r.rest);
-  r.rest -= norm_low;
+  float value, rest;
+  two_sum(score, -norm, value, rest);
+  two_sum(value, rest - norm_low, r.value, r.rest);
 }
 __device__ __forceinline__ GroupKey score_of(const Base& r, int beam, float x, int token) {
   float d, dl, s, e;
