@@ -645,7 +645,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   __shared__ int count, place_count, live;
   __shared__ double parts[kMergeThreads / 32];
   __shared__ Extent extents[kMergeThreads / 32];
-  __shared__ uint32_t worst_error, lowest_cut, best_floor;  // (as ordered numbers)
+  __shared__ uint32_t worst_error, top_score, lowest_cut, best_floor;  // (as ordered numbers)
   __shared__ Base base[SEMKV_BEAM_MAX];
   __shared__ uint32_t again[SEMKV_BEAM_MAX / 32];  // rows to be summed once more
   __shared__ float2 powers[32];
@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   int2* places = reinterpret_cast<int2*>(best.spare + a.k + kSlack);  // beam and split, the first token of a thread's vectors
   float3* table = reinterpret_cast<float3*>(places + kPlaces);  // of pieces: which, and what makes their logits scores
   if (tid < SEMKV_BEAM_MAX / 32) again[tid] = 0;
-  if (tid == 0) count = place_count = 0, worst_error = best_floor = 0u, lowest_cut = 0xFFFFFFFFu;
+  if (tid == 0) count = place_count = 0, worst_error = best_floor = 0u, top_score = ordered(0.f), lowest_cut = 0xFFFFFFFFu;
   __syncthreads();
   pdl_wait();
   pdl_trigger();
@@ -739,6 +739,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     if (lane == 0) {
       base[b] = r;
       atomicMax(&worst_error, ordered(r.error));
+      if (r.kind == kLogits) atomicMax(&top_score, ordered(score));  // (no value is above its beam's score)
       if (r.kind == kLogits && fabsf(r.most) > kFar) atomicOr(again + (b >> 5), 1u << (b & 31));
     }
   }
@@ -771,9 +772,11 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     }
   };
   // A score below a beam's cut is surely none of the k best if k reach `reach`.  (2^-20 of the numbers that were added is
-  // far more than their roundings.)
+  // far more than their roundings.  Those of a score that reaches it, some beam's value v and a logit that takes
+  // something off, are |v| and up to |v| + |score|: not more than the score itself unless v is above 0.)
+  const float slack = 2.1f * worst + 0x1p-20f * unordered(top_score);
   auto cut_of = [&](float value, float reach) {
-    return reach > kNone ? reach - 2.1f * worst - 0x1p-20f * (fabsf(value) + fabsf(reach)) : kNone;
+    return reach > kNone ? reach - slack - 0x1p-20f * (fabsf(value) + fabsf(reach)) : kNone;
   };
   float known = kNone;
   if constexpr (MANY) {

@@ -3,14 +3,14 @@ their own sizes.  Every index is that of the definition."""
 import numpy as np
 import pytest
 
-from test_gpu_search import check_select, score_bound
+from test_gpu_search import check_select
 
 pytestmark = pytest.mark.gpu
 
 
 # ----------------------------------------------------------- what is looked at ------
 
-def ties_beside_one(dt, far, beams, ties, where, positive=False):
+def ties_beside_one(dt, far, beams, ties, where):
     """Groups of two beams that are read, at where[0] and where[1]: one has a single candidate, the other `ties` of the same
     logit, in threads of their own and more of them than a threshold lets through beside k.  Either's logit is
     `far`, the other's 0, and the scores are a little apart, either way."""
@@ -50,3 +50,25 @@ def test_two_far_logits_by_hand():
         x[1, torch.arange(20) * 8] = 0
         parent, token, _ = check_select(x, np.array([[-5, score]]), 1)
         assert (parent[0, 0], token[0, 0]) == (first, 0)
+
+
+@pytest.mark.parametrize("k,beams", [(3, 2), (18, 2), (18, 128)])
+def test_scores_above_zero_that_logits_bring_back(k, beams):
+    """Twenty candidates (forty) of a beam at a large score come out near 0, as the one of a beam that stands there does."""
+    import torch
+    ties, rows, scores = 20 if k == 3 else 40, [], []
+    for big in (1e3, 1e5, 1e6, 3e7):
+        # beside the first two the ties weigh nothing: the row's norm is ln(1 + exp(-1/2))
+        base = np.float64(np.float32(big)) - np.log1p(np.exp(-0.5))
+        for logit in np.float32(-big) + np.spacing(np.float32(big)) * np.arange(-2, 4):
+            tie = base + np.float64(logit)
+            for gap in (0.3, -0.3, 0.05, -0.05, 0.01, -0.01):
+                x = torch.full((beams, 1024), -float("inf"))
+                x[0, 1], x[0, 1021] = 0, -0.5
+                x[0, torch.arange(ties) * 8 + 32] = float(logit)
+                x[1, 7] = 3
+                s = np.full(beams, -np.inf, np.float32)
+                s[0], s[1] = big, tie + gap * np.spacing(np.float32(big))
+                assert abs(tie - np.float64(s[1])) > 2.0 ** -20 * abs(tie)
+                rows.append(x), scores.append(s)
+    check_select(torch.cat(rows).cuda(), np.stack(scores), k, again=False)
