@@ -513,76 +513,78 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(BeamArgs a, 
 
 // ------------------------------------------------------- the exact sums ------
 
-// 2^(j/32) for j = 0 .. 31 as pairs of binary32 numbers, to 2^-48: products of the root in 64 bits.
+// 2^(j/256) for j = 0 .. 255 as pairs of binary32 numbers, to 2^-44: products of the root in 64 bits.
+constexpr int kPowerCount = 256;
 struct Powers {
-  float2 at[32];
+  float2 at[kPowerCount];
 };
 constexpr Powers make_powers() {
   Powers p{};
   double x = 1.0;
-  for (int j = 0; j < 32; ++j) {
+  for (int j = 0; j < kPowerCount; ++j) {
     p.at[j].x = (float)x;
     p.at[j].y = (float)(x - (double)(float)x);
-    x *= 1.0218971486541166782;
+    x *= 1.0027112750502024854;
   }
   return p;
 }
 __constant__ const Powers kPowers = make_powers();
 
-// sum + low grows by exp(x + xl) / 2^down, 2^-38 of it off, for |x| up to 1100 and an |xl| far below it: 2^(j/32) * exp(t) with
-// x log2 e in two numbers, a whole j, |t| <= ln 2 / 64, and exp(t) - 1 by its series (the fifth power is 2^-39).
-__device__ __forceinline__ void add_exp(float x, float xl, int down, const float2* powers, float& sum, float& low) {
+// sum + low grows by exp(x + xl) for -64 < x <= 0 and an |xl| of half a step of x at most: 2^(j/256) * exp(t) with x log2 e
+// in two numbers, a whole j, |t| <= ln 2 / 512, and exp(t) - 1 = t + t^2 / 2 + t^3 / 6.  2^-40 of it off: the fourth power is
+// 2^-42.6, t^2 / 2 below 2^-20, so that its roundings are 2^-44 each, and what x log2 e and t lack is carried along.
+// (Restated on the CPU, the worst of 2 million arguments is 2^-40.7 off, of those above -30 2^-41.2.)
+__device__ __forceinline__ void add_exp(float x, float xl, const float2* powers, float& sum, float& low) {
   constexpr float kLow = (float)(1.4426950408889634074 - (double)kLog2e), kWhole = 12582912.f;  // 1.5 * 2^23: the last bit is 1
   constexpr float kBig = (float)kLn2, kSmall = (float)(kLn2 - (double)kBig);
   const float p = __fmul_rn(x, kLog2e);
-  const float e = __fmaf_rn(x, kLow, __fmaf_rn(xl, kLog2e, __fmaf_rn(x, kLog2e, -p)));
-  const float z = __fmaf_rn(p, 32.f, kWhole), r = __fmaf_rn(__fsub_rn(z, kWhole), -1.f / 32, p);
+  float e = __fmaf_rn(x, kLow, __fmaf_rn(xl, kLog2e, __fmaf_rn(x, kLog2e, -p)));
+  const float z = __fmaf_rn(p, (float)kPowerCount, kWhole), r0 = __fmaf_rn(__fsub_rn(z, kWhole), -1.f / kPowerCount, p);
   const int j = __float_as_int(z) - __float_as_int(kWhole);
+  const float r = __fadd_rn(r0, e);
+  e = __fadd_rn(__fsub_rn(r0, r), e);
   const float t = __fmul_rn(r, kBig);
   const float tl = __fmaf_rn(e, kBig, __fmaf_rn(r, kSmall, __fmaf_rn(r, kBig, -t)));
-  // exp(t + tl) - 1 = t + q
-  const float q = __fmaf_rn(__fmul_rn(t, t), __fmaf_rn(t, __fmaf_rn(t, 1.f / 24, 1.f / 6), 0.5f), __fmaf_rn(t, tl, tl));
-  const float2 w = powers[j & 31];
-  const float a = __fmul_rn(w.x, t);
-  const float b = __fmaf_rn(w.y, t, __fmaf_rn(w.x, q, w.y)) + __fmaf_rn(w.x, t, -a);
-  const float s = __int_as_float(((j >> 5) - down + 127) << 23);
-  const float high = __fadd_rn(w.x, a), rest = __fadd_rn(__fsub_rn(w.x, high), a) + b;
+  // exp(t + tl) - 1 = h + hl
+  const float q = __fmaf_rn(__fmul_rn(t, t), __fmaf_rn(t, 1.f / 6, 0.5f), tl);
+  const float h = __fadd_rn(t, q), hl = __fadd_rn(__fsub_rn(t, h), q);
+  const float2 w = powers[j & (kPowerCount - 1)];
+  const float a = __fmul_rn(w.x, h);
+  const float b = __fmaf_rn(w.x, hl, __fmaf_rn(w.y, h, __fadd_rn(__fmaf_rn(w.x, h, -a), w.y)));
+  const float s = __int_as_float(((j >> 8) + 127) << 23);
+  const float high = __fadd_rn(w.x, a), rest = __fadd_rn(__fadd_rn(__fsub_rn(w.x, high), a), b);
   float err;
-  two_sum(sum, high * s, sum, err);
+  two_sum(sum, __fmul_rn(high, s), sum, err);
   low += __fmaf_rn(rest, s, err);
 }
 
-// Logits up to this need not have the largest taken off for their sums: 2^down does as well.
-constexpr float kNear = 1024.f;
-
-// ln sum exp(x - most) of a row, by a whole CTA, to 2^-37, for its first warp.  `most` is the row's largest logit.
+// ln sum exp(x - most) of a row, by a whole CTA, to 2^-38, for its first warp.  `most` is the row's largest logit.
 template <int DTYPE>
 __device__ __noinline__ double exact_normalizer(const BeamArgs& a, int row, float most, float2* powers, double* parts) {
   using V = Vec<DTYPE>;
   const char* at = row_at<DTYPE>(a, row);
   const int lead = (int)((uintptr_t)at & 15);
-  const bool near = fabsf(most) <= kNear;
-  const int down = near ? (int)scale_of(most) : 0;
-  float sum = 0.f, low = 0.f;
-  if (threadIdx.x < 32) powers[threadIdx.x] = kPowers.at[threadIdx.x];
+  double total = 0.0;
+  if (threadIdx.x < kPowerCount) powers[threadIdx.x] = kPowers.at[threadIdx.x];
   __syncthreads();
-  for (int first = threadIdx.x * V::kCount; first < a.vocab; first += kMergeThreads * V::kCount) {
-    const V v = load_vec<DTYPE>(at, first, a.vocab, lead);
-    // (what lies 64 below the largest is less than 2^-92 of it: past every bit that counts.  A NaN is left out here, too.)
-    if (near) {
-#pragma unroll
-      for (int j = 0; j < V::kCount; ++j)
-        if (v.at(j) <= most && v.at(j) > most - 64.f) add_exp(v.at(j), 0.f, down, powers, sum, low);
-    } else {
+  // 32 logits at a time in two numbers: `low` is off by 2^-25 of itself with each, and up to 32 steps of 2^-25 of the sum,
+  // so 2^-40 of it at most.  (All of a row's in one pair, equal logits' errors add up: 2^21 of them were 2^-34 off.)
+  constexpr int kBlock = 32 / V::kCount, kStep = kMergeThreads * V::kCount;
+  for (int begin = threadIdx.x * V::kCount; begin < a.vocab; begin += kBlock * kStep) {
+    float sum = 0.f, low = 0.f;
 #pragma unroll 1
+    for (int i = 0, first = begin; i < kBlock && first < a.vocab; ++i, first += kStep) {
+      const V v = load_vec<DTYPE>(at, first, a.vocab, lead);
+      // (what lies 64 below the largest is less than 2^-92 of it: past every bit that counts.  A NaN is left out here, too.)
+#pragma unroll
       for (int j = 0; j < V::kCount; ++j) {
         float d, dl;
-        two_sum(V::pick(v.w, j), -most, d, dl);
-        if (d <= 0.f && d > -64.f) add_exp(d, dl, 0, powers, sum, low);
+        two_sum(v.at(j), -most, d, dl);
+        if (d <= 0.f && d > -64.f) add_exp(d, dl, powers, sum, low);
       }
     }
+    total += (double)sum + (double)low;
   }
-  double total = (double)sum + (double)low;
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) total += __shfl_xor_sync(~0u, total, d);
   __syncthreads();
@@ -592,7 +594,7 @@ __device__ __noinline__ double exact_normalizer(const BeamArgs& a, int row, floa
   total = threadIdx.x < kMergeThreads / 32 ? parts[threadIdx.x] : 0.0;
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) total += __shfl_xor_sync(~0u, total, d);
-  return log(total) + (near ? (double)down * kLn2 - (double)most : 0.0);
+  return log(total);
 }
 
 // ----------------------------------------------------------------- merge ------
@@ -648,7 +650,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   __shared__ uint32_t worst_error, top_score, lowest_cut, best_floor;  // (as ordered numbers)
   __shared__ Base base[SEMKV_BEAM_MAX];
   __shared__ uint32_t again[SEMKV_BEAM_MAX / 32];  // rows to be summed once more
-  __shared__ float2 powers[32];
+  __shared__ float2 powers[kPowerCount];
   __shared__ GroupKey out[SEMKV_BEAM_MAX];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group = blockIdx.x, row0 = group * a.beams;

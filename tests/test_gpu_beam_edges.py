@@ -72,3 +72,55 @@ def test_scores_above_zero_that_logits_bring_back(k, beams):
                 assert abs(tie - np.float64(s[1])) > 2.0 ** -20 * abs(tie)
                 rows.append(x), scores.append(s)
     check_select(torch.cat(rows).cuda(), np.stack(scores), k, again=False)
+
+
+# ------------------------------------------------------ what is summed again ------
+
+def peaked(rng, m, groups):
+    """Pairs of rows of a logit near m and one or two more 18 to 24 below it, whose normalizers are 2^-34 to 2^-28 apart."""
+    rows = []
+    while len(rows) < 2 * groups:
+        first = m + rng.uniform(-1, 1, 2).astype(np.float32).astype(np.float64)
+        low = rng.uniform(18, 24, 2)
+        x = np.full((2, 3), -np.inf)
+        x[:, 0] = np.float32(first)
+        x[:, 1] = np.float32(x[:, 0] - low[0] - rng.choice([0, 0, 1]) * rng.uniform(-1, 1, 2) * 2.0 ** -rng.integers(0, 8))
+        if rng.random() < 0.5:
+            x[:, 2] = np.float32(x[:, 0] - low[1])
+        norms = np.log1p(np.exp(x[:, 1:] - x[:, :1]).sum(1))
+        if 2.0 ** -34 <= abs(norms[0] - norms[1]) <= 2.0 ** -28:
+            rows += list(x)
+    return np.array(rows)
+
+
+@pytest.mark.parametrize("m", [0, 20, -60, 1000, -1000, 5000, 4e5])
+@pytest.mark.parametrize("k", [1, 2])
+def test_normalizers_that_all_but_agree(m, k):
+    import torch
+    rng = np.random.default_rng(abs(int(m)) + k)
+    x = torch.full((600, 1024), -float("inf"), device="cuda")
+    x[:, torch.tensor([17, 400, 1000], device="cuda")] = torch.tensor(peaked(rng, m, 300), dtype=torch.float32, device="cuda")
+    check_select(x, np.zeros((300, 2)), k, again=False)
+
+
+@pytest.mark.parametrize("vocab", [30001, 1 << 21])
+@pytest.mark.parametrize("gap", [2.0 ** -34, -2.0 ** -34, 2.0 ** -31, -2.0 ** -31, 2.0 ** -28, -2.0 ** -28])
+def test_long_sums_that_all_but_agree(vocab, gap):
+    """Rows of one repeated logit each, where roundings add up; the second has two logits that bring it within `gap` of the first."""
+    import torch
+    n = vocab - 3
+    low = 20 - np.log(n)                                    # the repeated ones together weigh what the largest does
+    a = np.array([20.0] + [np.float32(low + 0.3)])
+    b = np.array([20.0] + [np.float32(low + 0.171)])
+    total = lambda x, extra=(): 1 + n * np.exp(x[1] - 20) + sum(np.exp(z - 20) for z in extra)
+    want = total(a) * np.exp(gap)                           # the second's sum
+    z1 = np.float64(np.float32(20 + np.log(want - total(b)) - 1e-4))
+    z2 = np.float64(np.float32(20 + np.log(want - total(b, [z1]))))
+    assert abs(np.log(total(b, [z1, z2]) / total(a)) / gap - 1) < 0.2
+    x = torch.empty((2, vocab), device="cuda")
+    x[0], x[1] = float(a[1]), float(b[1])
+    x[0, 77], x[0, -2:] = 20, -float("inf")
+    x[1, 9], x[1, -2], x[1, 5] = 20, z1, z2
+    for k in (1, 2):
+        parent, _, _ = check_select(x, np.zeros((1, 2)), k, again=False)
+        assert parent[0, 0] == (0 if gap > 0 else 1)
