@@ -289,6 +289,8 @@ semkv_status semkv_decode_attention_noalloc(const semkv_quant_desc* desc,
  *    beams but one).  Nor has one whose score is a NaN or +infinity, which writes 4.
  *  - done (may be NULL): device u8 [groups * beams].  A row with done != 0 is not read either; it has one
  *    candidate, end_token at scores[r].
+ *  - A score below binary32's range is given as its lowest number.  Such candidates come behind all others, the
+ *    lower row first, then the larger logit, then the lower token.
  *  - Where there are fewer than k candidates the rest is parent -1, token -1, score -infinity.
  * logits: device [groups * beams][vocab] of type `dtype` (SEMKV_F16, SEMKV_BF16 or SEMKV_F32), `stride`
  * >= vocab elements from row to row, aligned to its type; scores: device f32 [groups * beams]; parent,

@@ -604,7 +604,7 @@ struct Base {
   float value, rest;
   float most;   // the row's largest logit
   float error;  // how far value + rest may be off
-  float cut;    // no score below this (value + (logit - most), rounded) is among the k best
+  float cut;    // no score below this (as rough() gives it) is among the k best
   int kind;     // kNobody, kLogits, kDone
   int pieces, offset;
 };
@@ -617,13 +617,16 @@ __device__ __forceinline__ void set_value(Base& r, float score, float norm, floa
   two_sum(score, -norm, value, rest);
   two_sum(value, rest - norm_low, r.value, r.rest);
 }
+// A logit's score by rounded numbers.  What lies below binary32's range counts as its lowest number: -infinity is for what
+// is no candidate.
+__device__ __forceinline__ float rough(float value, float most, float x) { return fmaxf(value + (x - most), -FLT_MAX); }
 __device__ __forceinline__ GroupKey score_of(const Base& r, int beam, float x, int token) {
   float d, dl, s, e;
   two_sum(x, -r.most, d, dl);
   two_sum(r.value, d, s, e);
-  if (!(s > kNone)) return GroupKey::of(-FLT_MAX, 0.f, beam, x, token);  // below all binary32 numbers
   e += r.rest + dl;
   const float score = __fadd_rn(s, e);
+  if (!(score > kNone)) return GroupKey::of(-FLT_MAX, -FLT_MAX, beam, x, token);  // (behind those that are in the range)
   return GroupKey::of(score, __fadd_rn(__fsub_rn(s, score), e), beam, x, token);
 }
 
@@ -784,7 +787,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
   if constexpr (MANY) {
     // k reach each piece's floor: the best of these tells which pieces matter
     over_pieces(0, pieces, [&](int, int b, float, float floor) {
-      if (floor > kNone) atomicMax(&best_floor, ordered(base[b].value + (floor - base[b].most)));
+      if (floor > kNone) atomicMax(&best_floor, ordered(rough(base[b].value, base[b].most, floor)));
     });
     __syncthreads();
     known = best_floor ? unordered(best_floor) : kNone;
@@ -796,7 +799,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     __syncthreads();
     over_pieces(q0, min(pieces, q0 + kTable), [&](int q, int b, float most, float) {
       const Base& r = base[b];
-      if (r.value + (most - r.most) >= cut(r.value)) table[atomicAdd(&live, 1)] = make_float3(__int_as_float(q), r.value, r.most);
+      if (rough(r.value, r.most, most) >= cut(r.value)) table[atomicAdd(&live, 1)] = make_float3(__int_as_float(q), r.value, r.most);
     });
     __syncthreads();
   };
@@ -822,11 +825,11 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
         if (set >= sets) break;
         if (!MANY && t[j].y == kNone) continue;  // (nothing was written)
         int i = __float_as_int(t[j].x) * kScanThreads + (set & last_set) * 32 + lane;
-        what(i, word[j] ? t[j].y + (unordered(word[j]) - t[j].z) : kNone);
+        what(i, word[j] ? rough(t[j].y, t[j].z, unordered(word[j])) : kNone);
         if ((set & last_set) == last_set && more(word[j]))
           for (int s = last_set + 1; s < kScanThreads / 32; ++s) {
             const uint32_t x = words[i += 32];
-            what(i, x ? t[j].y + (unordered(x) - t[j].z) : kNone);
+            what(i, x ? rough(t[j].y, t[j].z, unordered(x)) : kNone);
           }
       }
     }
@@ -848,7 +851,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     if (pieces > kTable || live > 2 * kFew) {
       // very many pieces: first a score from the best of them alone
       float most = kNone;
-      over_pieces(0, min(pieces, kTable), [&](int, int b, float x, float) { most = base[b].value + (x - base[b].most); });
+      over_pieces(0, min(pieces, kTable), [&](int, int b, float x, float) { most = rough(base[b].value, base[b].most, x); });
       const bool in = most > kNone;
       const uint32_t word = ordered(most);
       float least = kNone;
@@ -934,7 +937,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
 #pragma unroll
         for (int j = 0; j < V::kCount; ++j) {
           const float x = v[i].at(j);
-          hits |= (uint32_t)(x > kNone && x < INFINITY && x >= floor && r.value + (x - r.most) >= r.cut) << (i * V::kCount + j);
+          hits |= (uint32_t)(x > kNone && x < INFINITY && x >= floor && rough(r.value, r.most, x) >= r.cut) << (i * V::kCount + j);
         }
       int w = hits ? atomicAdd(&count, __popc(hits)) : 0;
       for (; hits && w < best.cap; hits &= hits - 1) {  // (one or two)
@@ -972,7 +975,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(BeamArgs a, P
     for (int i0 = 0; i0 < marked; i0 += kMergeThreads) {
       const int i = i0 + tid, b = i < marked ? beam_of(i) : 0, split = i < marked ? i / kScanThreads - b * p.splits : 0;
       const uint32_t x = i < marked && base[b].kind == kLogits && split < base[b].pieces ? words[i] : 0u;
-      const float s = x ? base[b].value + (unordered(x) - base[b].most) : kNone;
+      const float s = x ? rough(base[b].value, base[b].most, unordered(x)) : kNone;
       const uint2 mark = s > kNone && s >= base[b].cut ? marks[i] : make_uint2(0u, 0u);
       uint32_t bits = mark.x;
       if (i0 == 0) {

@@ -124,3 +124,67 @@ def test_long_sums_that_all_but_agree(vocab, gap):
     for k in (1, 2):
         parent, _, _ = check_select(x, np.zeros((1, 2)), k, again=False)
         assert parent[0, 0] == (0 if gap > 0 else 1)
+
+
+# ------------------------------------------------- past the range of binary32 ------
+
+LOWEST = float(np.finfo(np.float32).min)
+
+
+def run(x, scores, k, done=None, end=0):
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    sc = torch.tensor(np.asarray(scores, np.float32), device="cuda")
+    out = [torch.full((sc.shape[0], k), 77, dtype=t, device="cuda") for t in (torch.int32, torch.int32, torch.float32)]
+    d = None if done is None else torch.tensor(done, dtype=torch.uint8, device="cuda")
+    semkv.semkv_beam_select(x, sc, *out, semkv.beam_select_workspace(x, sc, k), done=d, end_token=end)
+    return [t.cpu().numpy() for t in out]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("at", [1, 50, 700, 4000, 8999])
+@pytest.mark.parametrize("beams", [1, 128])
+def test_scores_below_the_lowest_number(dtype, at, beams):
+    """A finite logit is a candidate however far it lies below the largest, in whichever thread's vectors."""
+    import torch
+    dt = getattr(torch, dtype)
+    x = torch.full((beams, 9000), -float("inf"), dtype=dt, device="cuda")
+    b = beams - 1
+    x[b, 0], x[b, at] = 3e38, -3e38
+    s = np.full((1, beams), -np.inf)
+    s[0, b] = -1
+    parent, token, score = run(x, s, 3)
+    assert parent.tolist() == [[b, b, -1]] and token.tolist() == [[0, at, -1]]
+    assert score[0].tolist() == [-1.0, LOWEST, -np.inf]
+
+
+def test_scores_below_the_lowest_number_of_two_beams():
+    """Whatever they would be: the lower row first, then the larger logit, then the lower token."""
+    import torch
+    x = torch.full((2, 5000), -float("inf"), device="cuda")
+    x[0, 9], x[0, 4000], x[0, 4001], x[0, 20] = 3.2e38, -3.1e38, -3e38, -3.1e38
+    x[1, 8], x[1, 7], x[1, 3000] = 1.0, -3.1e38, -3.4e38
+    parent, token, score = run(x, [[-2, -3.1e38]], 8)
+    want = [(0, 9), (1, 8), (0, 4001), (0, 20), (0, 4000), (1, 7), (1, 3000), (-1, -1)]
+    assert list(zip(parent[0].tolist(), token[0].tolist())) == want
+    assert score[0].tolist() == [-2.0, np.float32(-3.1e38)] + [LOWEST] * 5 + [-np.inf]
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("vocab", [700, 40001])
+def test_a_beam_at_the_lowest_score(dtype, vocab):
+    """Tokens masked by the type's lowest number.  What lies below binary32's range comes behind all that does not."""
+    import torch
+    dt = getattr(torch, dtype)
+    x = torch.full((3, vocab), torch.finfo(dt).min, dtype=dt, device="cuda")
+    x[0, 77], x[2, 5], x[2, 600] = 3, 1, 2
+    for k in (2, 20, 128):
+        parent, token, score = run(x, [[LOWEST, -np.inf, -np.inf]], k)
+        assert (parent == 0).all() and (score == LOWEST).all()
+        assert token[0].tolist() == [77] + [t for t in range(128) if t != 77][:k - 1]
+        parent, token, score = run(x, [[LOWEST, -np.inf, -2.0]], k)
+        # the masked ones of the third row are near that type's lowest number; in binary32 a little below the first row's best
+        want = [(2, 600), (2, 5)] + ([(0, 77)] if dtype == "float32" else []) + [(2, t) for t in range(140) if t != 5]
+        assert list(zip(parent[0].tolist(), token[0].tolist())) == want[:k]
+    parent, token, score = run(x, [[LOWEST, -2.0, LOWEST]], 4, done=[0, 0, 1], end=9)
+    assert (parent[0] == 1).all() and token[0].tolist() == [0, 1, 2, 3]
