@@ -1,9 +1,9 @@
 """Selections where little decides: scores that lie within a rounding of one another, whatever their rows' logits and
-their own sizes.  Every index is that of the definition."""
+their own sizes, and calls that are cut into long or very many pieces.  Every index is that of the definition."""
 import numpy as np
 import pytest
 
-from test_gpu_search import check_select
+from test_gpu_search import check_select, score_bound
 
 pytestmark = pytest.mark.gpu
 
@@ -188,3 +188,123 @@ def test_a_beam_at_the_lowest_score(dtype, vocab):
         assert list(zip(parent[0].tolist(), token[0].tolist())) == want[:k]
     parent, token, score = run(x, [[LOWEST, -2.0, LOWEST]], 4, done=[0, 0, 1], end=9)
     assert (parent[0] == 1).all() and token[0].tolist() == [0, 1, 2, 3]
+
+
+# ------------------------------------------------------ long and many pieces ------
+
+def cut(rows, vocab, dtype, aligned):
+    """Units of a row, units of a CTA's share, pieces of a row: the rule that rows are cut by."""
+    per = 4 if dtype == "float32" else 8
+    unit = 256 * per
+    units = -(-(vocab + (0 if aligned else per - 1)) // unit)
+    share = -(-rows * units // 608)
+    if units >= 4:
+        share = -(-share // 4) * 4
+    if share < units < 8:
+        share = units
+    share = min(share, 128)
+    return units, share, units // share if units % share == 0 else (units + share - 2) // share + 1
+
+
+def is_cut_so(groups, beams, vocab, dtype, aligned, pieces):
+    """By the rule, and by the size of the library's workspace: 3088 bytes for each piece, however rows lie."""
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    rows = groups * beams
+    size = semkv.semkv_beam_select_workspace_bytes(groups, beams, vocab, getattr(torch, dtype), 128)
+    most = max(cut(rows, vocab, dtype, a)[2] for a in (True, False))
+    return cut(rows, vocab, dtype, aligned) == pieces and size == rows * most * (16 + 256 * 12)
+
+
+def best_of_rows(x):
+    """Each row's 128 best tokens with their log probabilities in 64 bits, by a stable sort on the GPU."""
+    import torch
+    tokens, values = [], []
+    for row in x:
+        best, at = row.float().sort(descending=True, stable=True)
+        norm = (row.double() - best[0]).exp_().sum().log()
+        tokens.append(at[:128]), values.append((best[:128].double() - best[0]) - norm)
+    return torch.stack(tokens).cpu(), torch.stack(values).cpu()
+
+
+def check_by(best, x, scores, k, done=None, end=0):
+    """A selection against best = best_of_rows(x)."""
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    groups, beams = scores.shape
+    sc = torch.tensor(np.asarray(scores, np.float32), device="cuda")
+    d = None if done is None else torch.tensor(np.asarray(done, np.uint8), device="cuda")
+    ws = semkv.beam_select_workspace(x, sc, k)
+    ws.fill_(255)
+    out = [torch.full((groups, k), 77, dtype=t, device="cuda") for t in (torch.int32, torch.int32, torch.float32)]
+    semkv.semkv_beam_select(x, sc, *out, ws, done=d, end_token=end)
+    parent, token, score = [t.cpu() for t in out]
+    sc = sc.double().cpu().view(-1)
+    for g in range(groups):
+        rows, tokens, values = [], [], []
+        for r in range(g * beams, (g + 1) * beams):
+            if sc[r] == -np.inf:
+                continue
+            over = done is not None and done[r]
+            values.append(sc[r:r + 1] if over else best[1][r] + sc[r])
+            tokens.append(torch.tensor([end]) if over else best[0][r])
+            rows.append(torch.full((len(tokens[-1]),), r))
+        rows, tokens, values = torch.cat(rows), torch.cat(tokens), torch.cat(values)
+        order = values.sort(descending=True, stable=True)[1][:k]
+        n = len(order)
+        wrong = (parent[g, :n] != rows[order]) | (token[g, :n] != tokens[order])
+        assert not wrong.any(), (g, k, wrong.nonzero()[:3].tolist())
+        assert ((score[g, :n].double() - values[order]).abs() <= torch.tensor(score_bound(x.shape[1], values[order].numpy()))).all()
+        assert (parent[g, n:] == -1).all()
+
+
+def fill_rows(x, kinds, seed):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    vocab = x.shape[1]
+    ramp = torch.linspace(-9, 9, vocab, device="cuda")
+    for r in range(len(x)):
+        kind = kinds[r % len(kinds)]
+        x[r] = {"random": lambda: torch.randn(vocab, generator=gen, device="cuda") * 3, "rising": lambda: ramp, "falling": lambda: -ramp,
+                "equal": lambda: torch.full_like(ramp, 1.25), "steps": lambda: (4 * ramp).round() / 4}[kind]().to(x.dtype)
+
+
+KINDS = [["random"], ["rising"], ["falling"], ["equal"], ["steps"], ["random", "rising", "equal", "falling", "steps"]]
+
+
+@pytest.mark.parametrize("dtype,groups,beams,vocab,pad,pieces", [
+    ("bfloat16", 64, 16, 131072, 0, (64, 108, 2)), ("bfloat16", 64, 16, 131071, 0, (65, 112, 2)), ("float16", 5, 16, (1 << 21) - 3, 1, (1025, 128, 9)),
+    ("float32", 3, 16, (1 << 21) + 8, 3, (2049, 128, 17)), ("bfloat16", 65, 20, 24576, 0, (12, 28, 2)), ("float32", 65, 20, 12291, 2, (13, 28, 2))])
+def test_shares_of_many_tiles(dtype, groups, beams, vocab, pad, pieces):
+    """Up to 32 tiles of four units each, shares that end anywhere in a row and hold several."""
+    import torch
+    assert is_cut_so(groups, beams, vocab, dtype, (vocab + pad) * (4 if dtype == "float32" else 2) % 16 == 0, pieces)
+    x = torch.empty((groups * beams, vocab + pad), dtype=getattr(torch, dtype), device="cuda")[:, :vocab]
+    rng = np.random.default_rng(vocab)
+    for i, kinds in enumerate(KINDS):
+        fill_rows(x, kinds, i)
+        best = best_of_rows(x)
+        for k in (1, 32, 128):
+            check_by(best, x, rng.uniform(-3, -2, (groups, beams)), k)
+
+
+def test_more_pieces_than_a_table_holds():
+    """The best beams among the last, rows of every kind, done ones, and beams of which all or few have a chance."""
+    import torch
+    beams, vocab = 128, 1100000
+    splits = 10
+    assert is_cut_so(1, beams, vocab, "float32", True, (1075, 128, splits)) and beams * splits > 1024
+    last = 1024 // splits + 2                     # all pieces from this beam on lie past the first table
+    x = torch.empty((beams, vocab), device="cuda")
+    rng = np.random.default_rng(3)
+    done = np.zeros(beams, int)
+    done[[5, 60, last + 3]] = 1
+    for i, kinds in enumerate(KINDS):
+        fill_rows(x, kinds, i)
+        best = best_of_rows(x)
+        for k in (1, 17, 128):
+            near = rng.uniform(-3, -2, (1, beams))
+            check_by(best, x, near, k)
+            check_by(best, x, near - 20.0 * (np.arange(beams) < last), k)
+            check_by(best, x, np.where(np.arange(beams) == last + 5, near, -np.inf), k, done, 99)
+            check_by(best, x, near - 20.0 * (np.arange(beams) != last + 1), k, done, 99)
