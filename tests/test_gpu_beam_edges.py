@@ -308,3 +308,68 @@ def test_more_pieces_than_a_table_holds():
             check_by(best, x, near - 20.0 * (np.arange(beams) < last), k)
             check_by(best, x, np.where(np.arange(beams) == last + 5, near, -np.inf), k, done, 99)
             check_by(best, x, near - 20.0 * (np.arange(beams) != last + 1), k, done, 99)
+
+
+# ------------------------------------------------------------ behind the ends ------
+
+class Fence:
+    """Tensors with known bytes before and behind them."""
+
+    def __init__(self):
+        self.held = []
+
+    def bytes(self, n):
+        import torch
+        store = torch.full((512 + n + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+        self.held.append((store, n))
+        return store[512:512 + n]
+
+    def like(self, shape, dtype):
+        import torch
+        return self.bytes(int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()).view(dtype).view(shape)
+
+    def whole(self):
+        return all(bool((s[:512] == 0xA5).all()) and bool((s[512 + n:] == 0xA5).all()) for s, n in self.held)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16", "float32"])
+@pytest.mark.parametrize("groups,beams,vocab,k", [(1, 1, 1, 1), (1, 4, 32768, 8), (5, 5, 50003, 10), (3, 7, 2049, 128), (1, 128, 9000, 128),
+                                                  (700, 2, 5000, 5), (1, 64, 100003, 33), (64, 16, 4099, 16)])
+def test_selections_stay_within_their_tensors(dtype, groups, beams, vocab, k):
+    import torch
+    from paper_2608_28911_gb300 import semkv
+    dt = getattr(torch, dtype)
+    rng = np.random.default_rng(vocab)
+    gen = torch.Generator(device="cuda").manual_seed(k)
+    for lead, pad in ((0, -vocab % 8), (0, 1 - vocab % 2), (3, 2 - vocab % 2)):
+        store = torch.randn(lead + groups * beams * (vocab + pad), generator=gen, device="cuda").to(dt)
+        x = store[lead:].view(groups * beams, vocab + pad)[:, :vocab]
+        scores = torch.tensor(rng.uniform(-3, -2, (groups, beams)).astype(np.float32), device="cuda")
+        plain = [torch.empty((groups, k), dtype=t, device="cuda") for t in (torch.int32, torch.int32, torch.float32)]
+        semkv.semkv_beam_select(x, scores, *plain, semkv.beam_select_workspace(x, scores, k))
+        f = Fence()
+        out = [f.like((groups, k), t) for t in (torch.int32, torch.int32, torch.float32)]
+        ws = f.bytes(semkv.semkv_beam_select_workspace_bytes(groups, beams, vocab, dt, k))
+        semkv.semkv_beam_select(x, scores, *out, ws)
+        assert all(torch.equal(a, b) for a, b in zip(out, plain))
+        assert f.whole()
+
+
+@pytest.mark.parametrize("wide", [0, 300, 9000])
+def test_reorders_stay_within_their_tensors(wide):
+    import torch
+    from search_plain import reorder
+    from test_gpu_kv4 import fill, make, t32
+    from paper_2608_28911_gb300 import semkv
+    rng = np.random.default_rng(4)
+    lens = [int(v) for v in rng.integers(0, 200, 60)]
+    c = make(lens, 1, 64, 16, spare=0, seed=2, more_pages=wide)
+    plain = fill(c)
+    for n in (60, 17, 1):
+        f = Fence()
+        ws = f.bytes(c.pages_workspace(n, 0).numel())
+        seqs, parent = rng.permutation(60)[:n], rng.integers(-1, n, n)
+        semkv.semkv_kv4_reorder(c, t32(seqs), t32(parent), ws)
+        reorder(plain, seqs, parent)
+        plain.same_state(c)
+        assert f.whole()
