@@ -7,7 +7,7 @@
 // So the scan sorts nothing and writes little, whatever k is; a piece has up to 262144 logits (131072 of 32 bits).
 //
 // Bound by memory where the rows are many: 64 x 16 rows of 131072 bf16 logits, k 32, take 55 us, the scan 47 of them
-// (5.7 TB/s; reading alone takes 40), with rows of 131071, which do not begin on multiples of 16 bytes, 62 us.  Few
+// (5.7 TB/s; reading alone takes 40), with rows of 131071, which do not begin on multiples of 16 bytes, 62 us, in f32 87.  Few
 // rows are bound by the latency of two kernels: 4 rows of 32768, k 8, 11 us, 25 of 50003 in f32 13 us.  What took longer:
 // lists of the best kept by the CTA as it streams (171 us for the scan), candidates put aside where they are met (93),
 // tiles brought by bulk copies (102), a warp that settles what the others stream (72).
@@ -18,7 +18,8 @@
 //
 // A sum's terms are 2^(x log2 e - c) with a whole number c, so that sums of different c are brought together exactly.
 // They are binary32, with a bound on their error.  If that leaves open which of two rows' candidates
-// comes first, the merge sums the rows in question again, in pairs of binary32 numbers.
+// comes first, the merge sums the rows in question again, in pairs of binary32 numbers: 44 us for a row of 131072, one after
+// the other (16 beams that are alike 0.7 ms; rows of equal logits, which are looked at key by key as well, 1.7 ms).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <float.h>

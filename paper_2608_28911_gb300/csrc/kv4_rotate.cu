@@ -7,6 +7,8 @@
 // binary32 values.  Memory-bound: a row of 32 query and 8 KV heads of 128 dims moves 23 KB, 61K rows take 224 us,
 // 6.2 TB/s (with their read back 278 us, 97% of the copy rate).  CTAs are for queries or for keys and values: together in
 // one they took 87 registers and 302 us; with 4 CTAs on an SM 278, with 3 318, with 2 373 (the read back among them).
+// Neighbouring pairs take the same (61K rows 230 us without the read back, halves 232; 20K rows 91 both); halves of an odd
+// number of pieces, whose keys read their mates as well, have 2 CTAs on an SM and take 298 us (20K rows 111, 2.5K 25 against 21).
 #include "kernels.h"
 #include "kv4_rows.cuh"
 
